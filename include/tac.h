@@ -355,6 +355,166 @@ typedef struct tac_stack_grads {
 int tac_stack_backward(const tac_stack_layer_t* layers, const tac_stack_grads_t* grads, const tac_backward_desc_t* bwd,
                        int32_t n_layers, const void* input, const float* grad_out_last, void* stream);
 
+/* ---- Dense operators over a stack's features ------------------------------------------------------------------------------
+ *
+ * What reads the spikes of a stack over time and answers: a residual block of a root-mean-square norm, dense products and leaky
+ * integrators whose leak is learned.  Matrices and sequences here are float32 (TAC_FP32) or bfloat16 (TAC_BF16), named by `dtype`;
+ * sums, statistics and states are float32.  Strides are in elements, the last axis is contiguous.  The entry points keep the
+ * conventions above: nothing is allocated or synchronised, arguments are checked before anything is launched, all can be recorded
+ * into a HIP graph.  Device pointers need the alignment of their elements (codes 16 bytes, scales and workspaces as stated);
+ * rows that start at multiples of 16 bytes are read faster.
+ *
+ * 8-bit matrices.  A matrix [rows][cols] in 8 bits is two buffers:
+ *   codes   uint8 [rows][128 ceil(cols / 128)], 16-byte aligned: OCP e4m3; pad bytes are zero on input and written as zero
+ *   scales  uint8 [rows][4 ceil(cols / 512)], 4-byte aligned: byte j of a row is 127 + e, and 2^e multiplies the codes of columns
+ *           128 j .. 128 j + 127; pad bytes are written as zero and read by nobody
+ * e is the smallest from -127 on for which the block's largest magnitude is at most 448 * 2^e, so a code is its value's nearest (even)
+ * e4m3 number in units of 2^e, rounded once.  Infinities and NaN become NaN codes; their block's scale is that of its finite values. */
+#define TAC_SCALE_BLOCK 128
+size_t tac_code_bytes(int64_t rows, int64_t cols);      /* 0 if a dimension is <= 0 */
+size_t tac_scale_bytes(int64_t rows, int64_t cols);
+
+/* Which values share a scale: 128 consecutive columns of one row, or a tile of 128 rows x 128 columns (its byte then stands once in
+ * each of its rows).  A matrix in tiles and its transpose hold the same values, which weights want: the forward product reads the one, the
+ * input gradient the other. */
+enum { TAC_BLOCK_ROW = 0, TAC_BLOCK_TILE = 1 };
+/* Source of tac_quantize beside TAC_FP32 and TAC_BF16: an 8-bit matrix (a kept activation).  Its values change only where a code
+ * falls below 2^-6 of its new block's 2^e: scales are powers of two. */
+enum { TAC_SCALED = 2 };
+typedef struct tac_quantize_desc {
+  int64_t rows, cols;        /* of the source */
+  int64_t src_stride;        /* elements from row to row; ignored for TAC_SCALED */
+  int32_t dtype;             /* TAC_FP32 / TAC_BF16 / TAC_SCALED */
+  int32_t block;             /* TAC_BLOCK_ROW / TAC_BLOCK_TILE */
+} tac_quantize_desc_t;
+
+/* A matrix to 8 bits: as it stands (blocks along its rows) and / or transposed, as a matrix [cols][rows] (blocks along the source's
+ * columns), in one pass over the source.
+ *   src         DEVICE, read-only: float32 / bfloat16 [rows] x src_stride, or codes
+ *   src_scales  DEVICE, read-only, the source's scales (TAC_SCALED), else ignored
+ *   codes, scales                  DEVICE, written, of [rows][cols], or both NULL
+ *   codes_t, scales_t              DEVICE, written, of [cols][rows], or both NULL (not all four)
+ * Errors: TAC_ERR_NULL, TAC_ERR_BAD_SHAPE (a dimension < 1, src_stride < cols, 2^24 or more tiles of 128 x 128), TAC_ERR_BAD_PARAM, TAC_ERR_ALIGN, TAC_ERR_HIP. */
+int tac_quantize(const tac_quantize_desc_t* desc, const void* src, const uint8_t* src_scales, uint8_t* codes, uint8_t* scales,
+                 uint8_t* codes_t, uint8_t* scales_t, void* stream);
+
+/* The values an 8-bit matrix stands for, exactly (every e4m3 number times 2^e is a bfloat16 number but where it is below the normal range).
+ *   dst  DEVICE, written, `dtype` [rows] x dst_stride */
+int tac_dequantize(int64_t rows, int64_t cols, const uint8_t* codes, const uint8_t* scales, int32_t dtype, void* dst,
+                   int64_t dst_stride, void* stream);
+
+/* Residual addition and root-mean-square norm of rows of `cols` values:
+ *   s = x + residual,  h = s in `dtype`,  rstd = 1 / sqrt(mean(s^2) + eps),  y = s rstd gain  (of the sum before it is rounded)
+ * with y in `dtype` and / or as an 8-bit matrix, each rounded once from the float32 value. */
+typedef struct tac_norm_desc {
+  int64_t rows;
+  int64_t x_stride, residual_stride, h_stride, y_stride;   /* elements from row to row, >= cols (those of absent tensors are ignored) */
+  int32_t cols;              /* 1 .. TAC_NORM_MAX_COLS */
+  int32_t dtype;             /* TAC_FP32 / TAC_BF16 */
+  float eps;                 /* > 0 */
+} tac_norm_desc_t;
+#define TAC_NORM_MAX_COLS 32768
+/*   x         DEVICE, read-only
+ *   residual  DEVICE, read-only, or NULL: s = x
+ *   gain      DEVICE, read-only, float32 [cols], or NULL: ones
+ *   h         DEVICE, written, or NULL; may be x or residual (with that tensor's stride): each row is read before it is written
+ *   y         DEVICE, written, or NULL
+ *   codes, scales  DEVICE, written, y as an 8-bit matrix [rows][cols], or both NULL
+ *   rstd      DEVICE, written, float32 [rows], or NULL
+ * At least one output.  The squares are summed in float32: rows of magnitudes beyond 2^63 overflow (rstd = 0).
+ * Errors: TAC_ERR_NULL, TAC_ERR_BAD_SHAPE, TAC_ERR_UNSUPPORTED (more than TAC_NORM_MAX_COLS columns), TAC_ERR_BAD_PARAM, TAC_ERR_ALIGN, TAC_ERR_HIP. */
+int tac_residual_norm(const tac_norm_desc_t* desc, const void* x, const void* residual, const float* gain, void* h, void* y,
+                      uint8_t* codes, uint8_t* scales, float* rstd, void* stream);
+
+/* Its backward pass.  With n = h rstd and w = gain grad_y:
+ *   grad_x = rstd (w - n mean(w n)) + grad_h,  grad_gain = sum over rows of grad_y n
+ * grad_x is the gradient of x and of the residual alike.  The rounding to 8 bits is differentiated as if it were not there.
+ *   h          DEVICE, read-only, h_stride: the stream as the forward pass stored it (x itself without a residual)
+ *   rstd       DEVICE, read-only, from the forward pass
+ *   grad_y     DEVICE, read-only, y_stride
+ *   grad_h     DEVICE, read-only, residual_stride: the gradient that reaches h past the norm, or NULL
+ *   grad_x     DEVICE, written, x_stride; may be grad_y or grad_h (with that tensor's stride)
+ *   grad_gain  DEVICE, written, float32 [cols], or NULL
+ *   workspace  DEVICE, scratch, tac_residual_norm_workspace_bytes(desc) bytes, 16-byte aligned; may be NULL where grad_gain is
+ * Rows are summed in an order that depends on the sizes alone: the same bits from call to call. */
+size_t tac_residual_norm_workspace_bytes(const tac_norm_desc_t* desc);
+int tac_residual_norm_backward(const tac_norm_desc_t* desc, const void* h, const float* gain, const float* rstd, const void* grad_y,
+                               const void* grad_h, void* grad_x, float* grad_gain, void* workspace, void* stream);
+
+/* Product of two 8-bit matrices, y[m][n] = bias[n] + sum_k a[m][k] b[n][k]: both have the summed axis as their columns, as
+ * tac_residual_norm and tac_quantize write them.  The products of a dense layer y = x W^T with W [N][K]:
+ *   output           a = x,                b = W           (M rows of x)
+ *   input gradient   a = grad_y,           b = W transposed (tac_quantize of W in tiles writes both)
+ *   weight gradient  a = grad_y transposed, b = x transposed: both with blocks along the rows of x; x from the 8-bit matrix that the
+ *                    output's product read (tac_quantize from TAC_SCALED)
+ * Codes are multiplied on the matrix cores with the blocks' powers of two, sums are float32, y is rounded once.  With a bfloat16 y the
+ * instruction for 8-bit operands adds eight products of neighbouring columns at a time and drops what is below 2^-13 of the largest of
+ * them (a relative error of a few 1e-5 in a sum, a hundredth of y's rounding); with a float32 y the codes are multiplied as bfloat16
+ * numbers, whose sums are float32 throughout (values below 2^-126 may count as zero), at half the rate.  A NaN among the codes of a row
+ * makes what is summed over it NaN. */
+typedef struct tac_product_desc {
+  int64_t M, N, K;
+  int64_t y_stride;          /* elements from row to row, >= N */
+  int32_t dtype;             /* of y: TAC_FP32 / TAC_BF16 */
+} tac_product_desc_t;
+/*   a_codes, a_scales  DEVICE, read-only, 8-bit matrix [M][K]
+ *   b_codes, b_scales  DEVICE, read-only, 8-bit matrix [N][K]
+ *   bias       DEVICE, read-only, float32 [N], or NULL
+ *   y          DEVICE, written
+ *   workspace  DEVICE, scratch, tac_scaled_product_workspace_bytes(desc) bytes, 16-byte aligned; NULL where those are 0
+ * The same bits from call to call.
+ * Errors: TAC_ERR_NULL, TAC_ERR_BAD_SHAPE (also M, N or K beyond 2^31 - 1), TAC_ERR_BAD_PARAM, TAC_ERR_ALIGN, TAC_ERR_HIP. */
+size_t tac_scaled_product_workspace_bytes(const tac_product_desc_t* desc);
+int tac_scaled_product(const tac_product_desc_t* desc, const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes,
+                       const uint8_t* b_scales, const float* bias, void* y, void* workspace, void* stream);
+
+/* Gated linear recurrence: leaky integrators without threshold whose leak is an input.  For every sequence b and channel d
+ *   a_t = 1 / (1 + exp(-gate_t)),   h_t = a_t h_{t-1} + (1 - a_t) value_t,   out_t = h_t in `dtype`
+ * (the membrane of Eq. 1 with a leak of its own at each step, and no reset).  Sequences may have different lengths: out is zero from a
+ * sequence's length on, what stands behind it is read into no result, and its last state is that of its last step (h0 where the
+ * length is 0). */
+#define TAC_SCAN_CHUNK 32
+typedef struct tac_scan_desc {
+  int64_t T;                     /* steps of the tensors */
+  int32_t B, D;                  /* sequences, channels */
+  int64_t in_stride_t, in_stride_b;      /* gate and value: elements from step to step and from sequence to sequence, >= D where more than one */
+  int64_t out_stride_t, out_stride_b;    /* out, grad_out */
+  int64_t grad_stride_t, grad_stride_b;  /* grad_gate, grad_value (backward only) */
+  int32_t dtype;                 /* TAC_FP32 / TAC_BF16 */
+} tac_scan_desc_t;
+/*   gate, value  DEVICE, read-only (halves of one product's rows, for instance)
+ *   lengths      DEVICE, read-only, int32 [B], taken as 0 .. T where outside; NULL: all T
+ *   h0           DEVICE, read-only, float32 [B][D], or NULL: zeros
+ *   out          DEVICE, written
+ *   h_last       DEVICE, written, float32 [B][D], or NULL; may be h0
+ *   states       DEVICE, written, float32 [ceil(T / TAC_SCAN_CHUNK)][B][D]: the state before every chunk of steps, all that the backward pass
+ *                keeps of the forward's states; or NULL
+ *   workspace    DEVICE, scratch, tac_gated_scan_workspace_bytes(desc) bytes, 16-byte aligned; NULL where those are 0 (the same for both calls)
+ * Errors: TAC_ERR_NULL, TAC_ERR_BAD_SHAPE, TAC_ERR_BAD_PARAM, TAC_ERR_ALIGN, TAC_ERR_HIP. */
+size_t tac_gated_scan_workspace_bytes(const tac_scan_desc_t* desc);
+int tac_gated_scan(const tac_scan_desc_t* desc, const void* gate, const void* value, const int32_t* lengths, const float* h0,
+                   void* out, float* h_last, float* states, void* workspace, void* stream);
+
+/* Its backward pass: with c_t = grad_out_t + a_{t+1} c_{t+1} (behind the last step: grad_h_last)
+ *   grad_value_t = (1 - a_t) c_t,   grad_gate_t = c_t (h_{t-1} - value_t) a_t (1 - a_t),   grad_h0 = a_1 c_1
+ * The states h_{t-1} are formed again from those that the forward pass kept.  Gradients are zero from a sequence's length on.
+ *   states       DEVICE, read-only, as tac_gated_scan wrote them
+ *   grad_h_last  DEVICE, read-only, float32 [B][D], or NULL: zeros
+ *   grad_gate, grad_value  DEVICE, written
+ *   grad_h0      DEVICE, written, float32 [B][D], or NULL; may be grad_h_last */
+int tac_gated_scan_backward(const tac_scan_desc_t* desc, const void* gate, const void* value, const int32_t* lengths,
+                            const float* states, const void* grad_out, const float* grad_h_last, void* grad_gate, void* grad_value,
+                            float* grad_h0, void* workspace, void* stream);
+
+/* One step of B running sequences whose states stand in a pool:  pool[slots[b]] <- a pool[slots[b]] + (1 - a) value[b].
+ *   desc   B, D, dtype, in_stride_b, out_stride_b count; T must be 1
+ *   pool   DEVICE, updated, float32 [n_slots][D]
+ *   slots  DEVICE, read-only, int32 [B], each slot at most once; a slot outside 0 .. n_slots - 1 stands for no sequence: its row of out is
+ *          zero and no state changes.  NULL: sequence b has slot b (n_slots >= B)
+ *   out    DEVICE, written */
+int tac_gated_step(const tac_scan_desc_t* desc, const void* gate, const void* value, float* pool, int64_t n_slots,
+                   const int32_t* slots, void* out, void* stream);
+
 /* Dense 0/1 bytes <-> packed words, `rows` rows of W pixels each (rows = T*B*C*H).
  *   dense01  DEVICE uint8 [rows][W]; any non-zero byte packs as 1
  *   packed   DEVICE uint32 [rows][ceil(W/32)]

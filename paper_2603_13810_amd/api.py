@@ -27,7 +27,9 @@ MODE_NAMES = {TAC_PER_STEP: "per_step", TAC_COLLAPSE: "TAC", TAC_PRESERVE: "TAC_
 EXPORTS = ("tac_out_shape", "tac_packed_bytes", "tac_select_kernel", "tac_prepared_weight_bytes",
            "tac_prepare_weights", "tac_conv_lif", "tac_aggregate_tiles", "tac_aggregate_sums", "tac_mfma_probe_workgroups", "tac_mfma_probe", "tac_pack_spikes", "tac_unpack_spikes", "tac_fold_batchnorm",
            "tac_stack_check", "tac_stack_forward", "tac_conv_lif_backward", "tac_conv_lif_backward_static", "tac_stack_backward", "tac_get_counters", "tac_reset_counters", "tac_status_string",
-           "tac_last_error")
+           "tac_last_error", "tac_code_bytes", "tac_scale_bytes", "tac_quantize", "tac_dequantize", "tac_residual_norm",
+           "tac_residual_norm_workspace_bytes", "tac_residual_norm_backward", "tac_scaled_product", "tac_scaled_product_workspace_bytes",
+           "tac_gated_scan", "tac_gated_scan_workspace_bytes", "tac_gated_scan_backward", "tac_gated_step")
 
 
 class tac_layer_desc_t(ctypes.Structure):
@@ -100,6 +102,18 @@ def lib() -> ctypes.CDLL:
         L.tac_status_string.restype = ctypes.c_char_p
         L.tac_last_error.argtypes = []
         L.tac_last_error.restype = ctypes.c_char_p
+        i64 = ctypes.c_int64
+        for name, args, result in (
+                ("tac_code_bytes", [i64, i64], ctypes.c_size_t), ("tac_scale_bytes", [i64, i64], ctypes.c_size_t),
+                ("tac_quantize", [vp] * 8, ctypes.c_int), ("tac_dequantize", [i64, i64, vp, vp, ctypes.c_int32, vp, i64, vp], ctypes.c_int),
+                ("tac_residual_norm", [vp] * 10, ctypes.c_int), ("tac_residual_norm_workspace_bytes", [vp], ctypes.c_size_t),
+                ("tac_residual_norm_backward", [vp] * 10, ctypes.c_int),
+                ("tac_scaled_product", [vp] * 9, ctypes.c_int), ("tac_scaled_product_workspace_bytes", [vp], ctypes.c_size_t),
+                ("tac_gated_scan", [vp] * 10, ctypes.c_int), ("tac_gated_scan_workspace_bytes", [vp], ctypes.c_size_t),
+                ("tac_gated_scan_backward", [vp] * 12, ctypes.c_int),
+                ("tac_gated_step", [vp, vp, vp, vp, i64, vp, vp, vp], ctypes.c_int)):
+            getattr(L, name).argtypes = args
+            getattr(L, name).restype = result
         _lib = L
     return _lib
 
@@ -492,3 +506,279 @@ def tac_get_counters() -> Tuple[int, int]:
 
 def tac_reset_counters() -> None:
     _check(lib().tac_reset_counters())
+
+
+# ---- dense operators over a stack's features (see include/tac.h) ---------------------------------
+# An 8-bit matrix is a pair (codes, scales) of uint8 tensors, [rows, 128 ceil(cols / 128)] and [rows, 4 ceil(cols / 512)].
+
+TAC_SCALED = 2
+TAC_BLOCK_ROW, TAC_BLOCK_TILE = 0, 1
+TAC_SCALE_BLOCK, TAC_SCAN_CHUNK, TAC_NORM_MAX_COLS = 128, 32, 32768
+
+
+class tac_quantize_desc_t(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("src_stride", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("block", ctypes.c_int32)]
+
+
+class tac_norm_desc_t(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("x_stride", ctypes.c_int64), ("residual_stride", ctypes.c_int64),
+                ("h_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64), ("cols", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class tac_product_desc_t(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int64), ("N", ctypes.c_int64), ("K", ctypes.c_int64), ("y_stride", ctypes.c_int64),
+                ("dtype", ctypes.c_int32)]
+
+
+class tac_scan_desc_t(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("B", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("in_stride_t", ctypes.c_int64), ("in_stride_b", ctypes.c_int64),
+                ("out_stride_t", ctypes.c_int64), ("out_stride_b", ctypes.c_int64),
+                ("grad_stride_t", ctypes.c_int64), ("grad_stride_b", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
+def _float_type(t, name) -> int:
+    import torch
+    if t.dtype == torch.bfloat16:
+        return TAC_BF16
+    if t.dtype == torch.float32:
+        return TAC_FP32
+    raise ValueError("%s must be float32 or bfloat16" % name)
+
+
+def _view_ptr(t, like, name, shape=None):
+    """Address of a device tensor whose last axis is contiguous (any strides before it), of `like`'s type and `shape`."""
+    if t is None:
+        return None
+    if not t.is_cuda or (t.stride(-1) != 1 and t.shape[-1] > 1):
+        raise ValueError("%s must be a device tensor with a contiguous last axis" % name)
+    if t.dtype != like.dtype:
+        raise ValueError("%s must have dtype %s" % (name, like.dtype))
+    if shape is not None and t.shape != shape:
+        raise ValueError("%s must be %s" % (name, list(shape)))
+    return t.data_ptr()
+
+
+def _row_stride(t):
+    """Elements from row to row; a matrix of one row has none that matters."""
+    return 0 if t is None else t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _shaped(t, dtype, name, *shape):
+    if t is None:
+        return None
+    if tuple(t.shape) != shape:
+        raise ValueError("%s must be %s" % (name, list(shape)))
+    return _dev_ptr(t, dtype, name)
+
+
+def _matrix(rows, cols, device):
+    """A new 8-bit matrix."""
+    import torch
+    return (torch.empty((rows, -(-cols // 128) * 128), dtype=torch.uint8, device=device),
+            torch.empty((rows, -(-cols // 512) * 4), dtype=torch.uint8, device=device))
+
+
+def _matrix_ptrs(m, rows, cols, name):
+    import torch
+    if m is None:
+        return None, None
+    return (_shaped(m[0], torch.uint8, name + " codes", rows, -(-cols // 128) * 128),
+            _shaped(m[1], torch.uint8, name + " scales", rows, -(-cols // 512) * 4))
+
+
+def _workspace(nbytes, device, stream):
+    """Scratch for one call.  It is torch's again when the call has been enqueued, so a stream of the caller's own is told to torch's allocator."""
+    import torch
+    if not nbytes:
+        return None
+    w = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    if stream is not None and int(stream) != torch.cuda.current_stream(device).cuda_stream:
+        w.record_stream(torch.cuda.ExternalStream(int(stream), device=device))
+    return w
+
+
+def tac_code_bytes(rows, cols) -> int:
+    return int(lib().tac_code_bytes(rows, cols))
+
+
+def tac_scale_bytes(rows, cols) -> int:
+    return int(lib().tac_scale_bytes(rows, cols))
+
+
+def tac_quantize(src, *, cols=None, tiles=False, rows=True, columns=False, stream=None):
+    """A matrix to 8 bits.  src: float32 / bfloat16 [R, C] with a contiguous last axis, or an 8-bit matrix (codes, scales) of `cols`
+    columns.  tiles: one scale per 128 x 128 instead of per row and 128 columns.  Returns dict(rows, columns) of 8-bit matrices:
+    `rows` is src itself, `columns` its transpose [C, R] (None where not asked for)."""
+    scaled = isinstance(src, (tuple, list))
+    t = src[0] if scaled else src
+    if t.dim() != 2 or (scaled and cols is None):
+        raise ValueError("src must be a matrix, and an 8-bit one needs its number of columns")
+    R, C = t.shape[0], int(cols) if scaled else t.shape[1]
+    if scaled:
+        at, at_scales = _matrix_ptrs(src, R, C, "src")
+    else:
+        at, at_scales = _view_ptr(t, t, "src"), None
+    desc = tac_quantize_desc_t(R, C, 0 if scaled else _row_stride(t), TAC_SCALED if scaled else _float_type(t, "src"),
+                               TAC_BLOCK_TILE if tiles else TAC_BLOCK_ROW)
+    straight = _matrix(R, C, t.device) if rows else None
+    turned = _matrix(C, R, t.device) if columns else None
+    to = (None, None) if straight is None else (straight[0].data_ptr(), straight[1].data_ptr())
+    to_t = (None, None) if turned is None else (turned[0].data_ptr(), turned[1].data_ptr())
+    _check(lib().tac_quantize(ctypes.addressof(desc), at, at_scales, to[0], to[1], to_t[0], to_t[1], _stream(stream)))
+    return dict(rows=straight, columns=turned)
+
+
+def tac_dequantize(matrix, cols, *, dtype=None, out=None, stream=None):
+    """The values of an 8-bit matrix (codes, scales) of `cols` columns, float32 (or `dtype`, or into `out`)."""
+    import torch
+    R = matrix[0].shape[0]
+    if out is None:
+        out = torch.empty((R, cols), dtype=dtype or torch.float32, device=matrix[0].device)
+    codes, scales = _matrix_ptrs(matrix, R, cols, "matrix")
+    _check(lib().tac_dequantize(R, cols, codes, scales, _float_type(out, "out"), _view_ptr(out, out, "out", (R, cols)),
+                                _row_stride(out), _stream(stream)))
+    return out
+
+
+def tac_residual_norm(x, residual=None, gain=None, *, eps, h=None, y=None, want_h=None, want_y=True, want_scaled=False,
+                      want_rstd=False, stream=None):
+    """y = rms_norm(x + residual) gain over rows.  x: float32 / bfloat16 [R, C] with a contiguous last axis; gain: float32 [C].
+    want_h: the sum x + residual (as it is where there is a residual).  Returns dict(h, y, scaled, rstd), `scaled` an 8-bit matrix of y;
+    what is not asked for is None.  h and y may be given (h may be x or residual)."""
+    import torch
+    if x.dim() != 2:
+        raise ValueError("x must be a matrix")
+    R, C = x.shape
+    if h is None and (residual is not None if want_h is None else want_h):
+        h = torch.empty((R, C), dtype=x.dtype, device=x.device)
+    if y is None and want_y:
+        y = torch.empty((R, C), dtype=x.dtype, device=x.device)
+    scaled = _matrix(R, C, x.device) if want_scaled else None
+    rstd = torch.empty((R,), dtype=torch.float32, device=x.device) if want_rstd else None
+    desc = tac_norm_desc_t(R, _row_stride(x), _row_stride(residual), _row_stride(h), _row_stride(y), C, _float_type(x, "x"), eps)
+    _check(lib().tac_residual_norm(
+        ctypes.addressof(desc), _view_ptr(x, x, "x"), _view_ptr(residual, x, "residual", x.shape), _shaped(gain, torch.float32, "gain", C),
+        _view_ptr(h, x, "h", x.shape), _view_ptr(y, x, "y", x.shape), scaled and scaled[0].data_ptr(), scaled and scaled[1].data_ptr(),
+        None if rstd is None else rstd.data_ptr(), _stream(stream)))
+    return dict(h=h, y=y, scaled=scaled, rstd=rstd)
+
+
+def tac_residual_norm_backward(h, gain, rstd, grad_y, grad_h=None, *, grad_x=None, want_grad_gain=True, stream=None):
+    """Backward pass of tac_residual_norm from the stream h and the rstd it stored.  Returns dict(grad_x, grad_gain); grad_x is the
+    gradient of x and of the residual, and may be given (also grad_y or grad_h)."""
+    import torch
+    if h.dim() != 2:
+        raise ValueError("h must be a matrix")
+    R, C = h.shape
+    if grad_x is None:
+        grad_x = torch.empty((R, C), dtype=h.dtype, device=h.device)
+    desc = tac_norm_desc_t(R, _row_stride(grad_x), _row_stride(grad_h), _row_stride(h), _row_stride(grad_y), C, _float_type(h, "h"), 1.0)
+    at = ctypes.addressof(desc)
+    grad_gain = torch.empty((C,), dtype=torch.float32, device=h.device) if want_grad_gain else None
+    work = _workspace(lib().tac_residual_norm_workspace_bytes(at), h.device, stream) if want_grad_gain else None
+    _check(lib().tac_residual_norm_backward(
+        at, _view_ptr(h, h, "h"), _shaped(gain, torch.float32, "gain", C), _shaped(rstd, torch.float32, "rstd", R),
+        _view_ptr(grad_y, h, "grad_y", h.shape), _view_ptr(grad_h, h, "grad_h", h.shape), _view_ptr(grad_x, h, "grad_x", h.shape),
+        None if grad_gain is None else grad_gain.data_ptr(), None if work is None else work.data_ptr(), _stream(stream)))
+    return dict(grad_x=grad_x, grad_gain=grad_gain)
+
+
+def tac_scaled_product(a_codes, a_scales, b_codes, b_scales, K, *, bias=None, dtype=None, out=None, stream=None):
+    """a b^T (+ bias) of the 8-bit matrices a [M, K] and b [N, K], in bfloat16 (or `dtype`, or into `out` [M, N])."""
+    import torch
+    M, N = a_codes.shape[0], b_codes.shape[0]
+    if out is None:
+        out = torch.empty((M, N), dtype=dtype or torch.bfloat16, device=a_codes.device)
+    a, b = _matrix_ptrs((a_codes, a_scales), M, K, "a"), _matrix_ptrs((b_codes, b_scales), N, K, "b")
+    desc = tac_product_desc_t(M, N, K, _row_stride(out), _float_type(out, "out"))
+    at = ctypes.addressof(desc)
+    work = _workspace(lib().tac_scaled_product_workspace_bytes(at), a_codes.device, stream)
+    _check(lib().tac_scaled_product(at, a[0], a[1], b[0], b[1], _shaped(bias, torch.float32, "bias", N),
+                                    _view_ptr(out, out, "out", (M, N)), None if work is None else work.data_ptr(), _stream(stream)))
+    return out
+
+
+def _scan_desc(gate, out, grad=None):
+    T, B, D = gate.shape
+    return tac_scan_desc_t(T, B, D, gate.stride(0), gate.stride(1), out.stride(0), out.stride(1),
+                           grad.stride(0) if grad is not None else 0, grad.stride(1) if grad is not None else 0, _float_type(gate, "gate"))
+
+
+def _same_layout(a, b, names):
+    """Strides of axes with more than one entry."""
+    if any(x != y for x, y, n in zip(a.stride(), b.stride(), a.shape) if n > 1):
+        raise ValueError("%s must have the same strides" % names)
+
+
+def tac_gated_scan(gate, value, *, lengths=None, h0=None, out=None, want_h_last=True, want_states=False, stream=None):
+    """h_t = a_t h_{t-1} + (1 - a_t) value_t with a = sigmoid(gate).  gate, value: float32 / bfloat16 [T, B, D] of the same strides, the
+    last axis contiguous; lengths: int32 [B]; h0: float32 [B, D].  Returns dict(out, h_last, states); `states` is what the backward
+    pass needs."""
+    import torch
+    if gate.dim() != 3:
+        raise ValueError("gate must be [T, B, D]")
+    T, B, D = gate.shape
+    if out is None:
+        out = torch.empty((T, B, D), dtype=gate.dtype, device=gate.device)
+    f32 = torch.float32
+    h_last = torch.empty((B, D), dtype=f32, device=gate.device) if want_h_last else None
+    states = torch.empty((-(-T // TAC_SCAN_CHUNK), B, D), dtype=f32, device=gate.device) if want_states else None
+    g, v = _view_ptr(gate, gate, "gate"), _view_ptr(value, gate, "value", gate.shape)
+    _same_layout(gate, value, "gate and value")
+    desc = _scan_desc(gate, out)
+    at = ctypes.addressof(desc)
+    work = _workspace(lib().tac_gated_scan_workspace_bytes(at), gate.device, stream)
+    _check(lib().tac_gated_scan(
+        at, g, v, _shaped(lengths, torch.int32, "lengths", B), _shaped(h0, f32, "h0", B, D), _view_ptr(out, gate, "out", gate.shape),
+        None if h_last is None else h_last.data_ptr(), None if states is None else states.data_ptr(),
+        None if work is None else work.data_ptr(), _stream(stream)))
+    return dict(out=out, h_last=h_last, states=states)
+
+
+def tac_gated_scan_backward(gate, value, states, grad_out, *, lengths=None, grad_h_last=None, grad_gate=None, grad_value=None,
+                            want_grad_h0=True, stream=None):
+    """Backward pass of tac_gated_scan from its inputs and `states`.  Returns dict(grad_gate, grad_value, grad_h0); the first two may be
+    given (of the same strides as each other)."""
+    import torch
+    if gate.dim() != 3:
+        raise ValueError("gate must be [T, B, D]")
+    T, B, D = gate.shape
+    if grad_gate is None:
+        grad_gate = torch.empty((T, B, D), dtype=gate.dtype, device=gate.device)
+    if grad_value is None:
+        grad_value = torch.empty_strided(gate.shape, grad_gate.stride(), dtype=gate.dtype, device=gate.device)
+    f32 = torch.float32
+    grad_h0 = torch.empty((B, D), dtype=f32, device=gate.device) if want_grad_h0 else None
+    ptrs = [_view_ptr(t, gate, n, gate.shape) for t, n in ((gate, "gate"), (value, "value"), (grad_out, "grad_out"),
+                                                           (grad_gate, "grad_gate"), (grad_value, "grad_value"))]
+    _same_layout(gate, value, "gate and value")
+    _same_layout(grad_gate, grad_value, "grad_gate and grad_value")
+    desc = _scan_desc(gate, grad_out, grad_gate)
+    at = ctypes.addressof(desc)
+    work = _workspace(lib().tac_gated_scan_workspace_bytes(at), gate.device, stream)
+    _check(lib().tac_gated_scan_backward(
+        at, ptrs[0], ptrs[1], _shaped(lengths, torch.int32, "lengths", B), _shaped(states, f32, "states", -(-T // TAC_SCAN_CHUNK), B, D),
+        ptrs[2], _shaped(grad_h_last, f32, "grad_h_last", B, D), ptrs[3], ptrs[4], None if grad_h0 is None else grad_h0.data_ptr(),
+        None if work is None else work.data_ptr(), _stream(stream)))
+    return dict(grad_gate=grad_gate, grad_value=grad_value, grad_h0=grad_h0)
+
+
+def tac_gated_step(gate, value, pool, slots=None, *, out=None, stream=None):
+    """One step of tac_gated_scan for B running sequences whose states stand in `pool` (float32 [slots, D], updated in place).  gate,
+    value: [B, D]; slots: int32 [B], each slot at most once, outside the pool for rows without a sequence; None: row b has slot b.
+    Returns out [B, D]."""
+    import torch
+    if gate.dim() != 2 or pool.dim() != 2:
+        raise ValueError("gate must be [B, D] and pool [slots, D]")
+    B, D = gate.shape
+    if out is None:
+        out = torch.empty((B, D), dtype=gate.dtype, device=gate.device)
+    g, v = _view_ptr(gate, gate, "gate"), _view_ptr(value, gate, "value", gate.shape)
+    _same_layout(gate, value, "gate and value")
+    desc = tac_scan_desc_t(1, B, D, 0, gate.stride(0), 0, out.stride(0), 0, 0, _float_type(gate, "gate"))
+    _check(lib().tac_gated_step(ctypes.addressof(desc), g, v, _shaped(pool, torch.float32, "pool", pool.shape[0], D), pool.shape[0],
+                                _shaped(slots, torch.int32, "slots", B), _view_ptr(out, gate, "out", gate.shape), _stream(stream)))
+    return out

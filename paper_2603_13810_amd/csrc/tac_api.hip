@@ -25,10 +25,7 @@ constexpr int kMaxDevices = 64;
 std::mutex g_scratch_mutex;
 float* g_scratch_ptr[kMaxDevices] = {};
 
-int hip_fail(hipError_t e, const char* where) {
-  std::snprintf(g_last_error, sizeof(g_last_error), "%s: %s", where, hipGetErrorString(e));
-  return TAC_ERR_HIP;
-}
+using tac::hip_fail;
 
 constexpr int kMaxRowPixels = 2048;
 
@@ -85,6 +82,11 @@ int select_kernel(const tac_layer_desc_t* d) {
 }
 
 }  // namespace
+
+int tac::hip_fail(hipError_t e, const char* where) {
+  std::snprintf(g_last_error, sizeof(g_last_error), "%s: %s", where, hipGetErrorString(e));
+  return TAC_ERR_HIP;
+}
 
 extern "C" {
 
@@ -471,11 +473,11 @@ const char* tac_status_string(int status) {
   switch (status) {
     case TAC_OK: return "ok";
     case TAC_ERR_NULL: return "a required pointer is NULL";
-    case TAC_ERR_BAD_SHAPE: return "bad shape (dimension <= 0, kernel not 3x3, stride not 1/2, pad not 1, or tensor too large)";
+    case TAC_ERR_BAD_SHAPE: return "bad shape (dimension <= 0, kernel not 3x3, stride not 1/2, pad not 1, row stride below the row, or tensor too large)";
     case TAC_ERR_BAD_K: return "bad group size K (K < 1 or K > 32)";
     case TAC_ERR_NEED_STATE: return "T is not a multiple of K: the shorter last group needs v_inout, whichever kernel runs (in some it is a launch of its own)";
-    case TAC_ERR_BAD_PARAM: return "bad parameter (beta outside [0,1], theta <= 0 or not finite, or unknown enum value)";
-    case TAC_ERR_UNSUPPORTED: return "the requested kernel family does not support this layer";
+    case TAC_ERR_BAD_PARAM: return "bad parameter (beta outside [0,1], theta or eps <= 0 or not finite, or unknown enum value)";
+    case TAC_ERR_UNSUPPORTED: return "the requested kernel family does not support this layer, or no kernel supports these sizes";
     case TAC_ERR_HIP: return "a HIP call failed (see tac_last_error)";
     case TAC_ERR_ALIGN: return "a device pointer is not aligned as documented";
     default: return "unknown status";

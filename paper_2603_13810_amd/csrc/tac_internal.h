@@ -6,6 +6,9 @@
 
 namespace tac {
 
+// keeps the text of a failed HIP call for tac_last_error; returns TAC_ERR_HIP
+int hip_fail(hipError_t e, const char* where);
+
 // Compute units of the chip that the host rules' time estimates are fitted to, with everything else in them (an MI355X; on the CPU, where tests ask these rules, there is
 // none to ask).  Launchers that only count workgroups ask the device.
 constexpr int kFittedUnits = 256;

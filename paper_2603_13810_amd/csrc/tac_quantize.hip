@@ -1,0 +1,169 @@
+// Matrices to 8 bits with a power of two per 128 values, along their rows, transposed or both, and back.
+//
+// Memory-bound.  A workgroup of 256 threads takes a tile of 128 x 128: a thread holds 8 rows x 8 columns of it in registers, so its 8 codes of
+// a row are one store of the straight matrix, and its 8 codes of a column go through LDS to become rows of 128 codes of the transposed one.
+#include "tac_head_common.h"
+
+namespace tac {
+
+namespace {
+
+constexpr int kPitch = 132;        // bytes of a transposed row in LDS: 16 lanes that write 8 columns further each are 66 words apart
+
+// DT: 0 float32, 1 bfloat16, 2 8-bit codes.  VEC: rows of whole 16-byte pieces.
+template <int DT, bool VEC>
+__global__ __launch_bounds__(256) void quantize_kernel(const QuantizeParams p, int row_tiles) {
+  __shared__ float col_max[4][kBlock];
+  __shared__ __align__(16) uint8_t turned[kBlock * kPitch];
+  const int64_t r0 = (int64_t)(blockIdx.x % row_tiles) * kBlock, c0 = (int64_t)(blockIdx.x / row_tiles) * kBlock;
+  const int rt = threadIdx.x / 16, ct = threadIdx.x % 16;
+  const int64_t c = c0 + 8 * ct;
+  float v[8][8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int64_t r = r0 + 8 * rt + i;
+    if (r < p.rows && c < p.cols) {
+      if constexpr (DT == 2) {
+        const int64_t pitch = code_pitch(p.cols);
+        const u32x2_t w = *reinterpret_cast<const u32x2_t*>((const uint8_t*)p.src + r * pitch + c);
+        const float scale = scale_value(p.src_scales[r * scale_pitch(p.cols) + c / kBlock]);
+        float lo[4], hi[4];
+        four_values(w[0], lo);
+        four_values(w[1], hi);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[i][e] = lo[e] * scale;
+          v[i][4 + e] = hi[e] * scale;
+        }
+      } else if constexpr (DT == 1) {
+        load_floats<bf16, 8, VEC>((const bf16*)p.src + r * p.src_stride + c, p.cols - c, v[i]);
+      } else {
+        load_floats<float, 8, VEC>((const float*)p.src + r * p.src_stride + c, p.cols - c, v[i]);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] = 0.0f;
+    }
+  }
+  float col[8] = {};
+  float tile = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      v[i][e] = finite_or_nan(v[i][e]);
+      col[e] = fmaxf(col[e], fabsf(v[i][e]));
+    }
+  // the largest of each column over the four row groups of a wave, then over the waves
+  if (p.codes_t || p.tiles) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      col[e] = fmaxf(col[e], __shfl_xor(col[e], 16));
+      col[e] = fmaxf(col[e], __shfl_xor(col[e], 32));
+      if ((threadIdx.x & 48) == 0) col_max[threadIdx.x >> 6][8 * ct + e] = col[e];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      col[e] = fmaxf(fmaxf(col_max[0][8 * ct + e], col_max[1][8 * ct + e]), fmaxf(col_max[2][8 * ct + e], col_max[3][8 * ct + e]));
+      tile = fmaxf(tile, col[e]);
+    }
+    if (p.tiles) tile = max_over<16>(tile);
+  }
+  if (p.codes) {
+    const int64_t pitch = code_pitch(p.cols), spitch = scale_pitch(p.cols);
+    const bool last = c0 + kBlock >= p.cols;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t r = r0 + 8 * rt + i;
+      float amax = tile;
+      if (!p.tiles) {
+        amax = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(v[i][e]));
+        amax = max_over<16>(amax);
+      }
+      const uint32_t byte = scale_byte(amax);
+      const float inv = scale_inverse(byte);
+      if (r < p.rows) {
+        *reinterpret_cast<u32x2_t*>(p.codes + r * pitch + c) =
+            u32x2_t{four_codes(v[i][0] * inv, v[i][1] * inv, v[i][2] * inv, v[i][3] * inv),
+                    four_codes(v[i][4] * inv, v[i][5] * inv, v[i][6] * inv, v[i][7] * inv)};
+        const int64_t at = c0 / kBlock + ct;               // the first lane writes the block's byte, the next ones the row's pad bytes
+        if (ct == 0 || (last && at < spitch)) p.scales[r * spitch + at] = ct == 0 ? (uint8_t)byte : (uint8_t)0;
+      }
+    }
+  }
+  if (p.codes_t) {
+    const int64_t pitch = code_pitch(p.rows), spitch = scale_pitch(p.rows);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t byte = scale_byte(p.tiles ? tile : col[e]);
+      const float inv = scale_inverse(byte);
+      uint32_t* to = reinterpret_cast<uint32_t*>(turned + (8 * ct + e) * kPitch + 8 * rt);
+      to[0] = four_codes(v[0][e] * inv, v[1][e] * inv, v[2][e] * inv, v[3][e] * inv);
+      to[1] = four_codes(v[4][e] * inv, v[5][e] * inv, v[6][e] * inv, v[7][e] * inv);
+      const int64_t at = r0 / kBlock + rt;
+      const bool last = r0 + kBlock >= p.rows;
+      if (c + e < p.cols && (rt == 0 || (last && at < spitch))) p.scales_t[(c + e) * spitch + at] = rt == 0 ? (uint8_t)byte : (uint8_t)0;
+    }
+    __syncthreads();
+    // rows of the transposed matrix: 8 lanes write one row's 128 codes
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = i * 32 + threadIdx.x / 8, part = threadIdx.x % 8;
+      const uint32_t* from = reinterpret_cast<const uint32_t*>(turned + row * kPitch + 16 * part);
+      if (c0 + row < p.cols)
+        *reinterpret_cast<u32x4_t*>(p.codes_t + (c0 + row) * pitch + r0 + 16 * part) = u32x4_t{from[0], from[1], from[2], from[3]};
+    }
+  }
+}
+
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
+                                                         T* __restrict__ dst, int64_t rows, int64_t cols, int64_t stride) {
+  const int64_t pitch = code_pitch(cols), spitch = scale_pitch(cols), pieces = (cols + 7) / 8;
+  const int64_t step = (int64_t)gridDim.x * blockDim.x;
+  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < rows * pieces; i += step) {
+    const int64_t r = i / pieces, c = (i - r * pieces) * 8;
+    const u32x2_t w = *reinterpret_cast<const u32x2_t*>(codes + r * pitch + c);
+    const float scale = scale_value(scales[r * spitch + c / kBlock]);
+    float lo[4], hi[4], v[8];
+    four_values(w[0], lo);
+    four_values(w[1], hi);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = lo[e] * scale;
+      v[4 + e] = hi[e] * scale;
+    }
+    store_floats<T, 8, VEC>(dst + r * stride + c, cols - c, v);
+  }
+}
+
+}  // namespace
+
+hipError_t quantize_launch(const QuantizeParams& p, hipStream_t s) {
+  const int64_t rt = (p.rows + kBlock - 1) / kBlock, ct = (p.cols + kBlock - 1) / kBlock;
+  const dim3 grid((unsigned)(rt * ct));
+  const bool vec = p.dtype != TAC_SCALED && p.cols % 8 == 0 && rows_aligned(p.src, p.src_stride, p.dtype == TAC_BF16 ? 2 : 4);
+  if (p.dtype == TAC_SCALED) hipLaunchKernelGGL((quantize_kernel<2, false>), grid, dim3(256), 0, s, p, (int)rt);
+  else if (p.dtype == TAC_BF16 && vec) hipLaunchKernelGGL((quantize_kernel<1, true>), grid, dim3(256), 0, s, p, (int)rt);
+  else if (p.dtype == TAC_BF16) hipLaunchKernelGGL((quantize_kernel<1, false>), grid, dim3(256), 0, s, p, (int)rt);
+  else if (vec) hipLaunchKernelGGL((quantize_kernel<0, true>), grid, dim3(256), 0, s, p, (int)rt);
+  else hipLaunchKernelGGL((quantize_kernel<0, false>), grid, dim3(256), 0, s, p, (int)rt);
+  return hipGetLastError();
+}
+
+hipError_t dequantize_launch(const uint8_t* codes, const uint8_t* scales, void* dst, int64_t rows, int64_t cols, int64_t stride,
+                             int bf, hipStream_t s) {
+  const int64_t work = (rows * ((cols + 7) / 8) + 255) / 256;
+  const dim3 grid((unsigned)(work < 256 * 32 ? work : 256 * 32));
+  const bool vec = cols % 8 == 0 && rows_aligned(dst, stride, bf ? 2 : 4);
+  if (bf && vec) hipLaunchKernelGGL((dequantize_kernel<bf16, true>), grid, dim3(256), 0, s, codes, scales, (bf16*)dst, rows, cols, stride);
+  else if (bf) hipLaunchKernelGGL((dequantize_kernel<bf16, false>), grid, dim3(256), 0, s, codes, scales, (bf16*)dst, rows, cols, stride);
+  else if (vec) hipLaunchKernelGGL((dequantize_kernel<float, true>), grid, dim3(256), 0, s, codes, scales, (float*)dst, rows, cols, stride);
+  else hipLaunchKernelGGL((dequantize_kernel<float, false>), grid, dim3(256), 0, s, codes, scales, (float*)dst, rows, cols, stride);
+  return hipGetLastError();
+}
+
+}  // namespace tac

@@ -1,0 +1,141 @@
+"""Products of 8-bit matrices against 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import head_util as O
+from paper_2603_13810_amd import api
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = [torch.float32, torch.bfloat16]
+
+
+def matrix(rows, cols, seed, tiles=False, spread=1.0):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    v = torch.randn(rows, cols, generator=g, device=DEV) * torch.exp(spread * torch.randn(rows, 1, generator=g, device=DEV))
+    v *= torch.exp(spread * torch.randn(cols, generator=g, device=DEV))
+    return api.tac_quantize(v, tiles=tiles)["rows"]
+
+
+def exact(a, b, K, bias=None):
+    """The product and the sum of its terms' magnitudes, 64 bits (on the GPU, from values decoded on the CPU for small sizes)."""
+    a64, b64 = (torch.from_numpy(O.decode(m, K)[0]).to(DEV) for m in (a, b))
+    y, size = a64 @ b64.t(), a64.abs() @ b64.t().abs()
+    if bias is not None:
+        y, size = y + bias.double(), size + bias.double().abs()
+    return y, size
+
+
+def check(got, y, size, K):
+    # codes multiply exactly; sums of K terms in float32, at worst one rounding (here: truncation, 2^-23) a term, of at most the
+    # sum of magnitudes; then the rounding of the output.  bfloat16 output: the 8-bit instruction adds eight products at a time and drops
+    # what is below 2^-13 of the largest of them (seen by giving it 2^16 and one smaller term), which is in `size` too
+    tol = O.HALF[got.dtype] * y.abs() + (K + 20) * 2 * O.U * size
+    if got.dtype == torch.bfloat16:
+        tol = tol + 7 * 2.0 ** -13 * size
+    assert bool(((got.double() - y).abs() <= tol * (1 + 1e-6)).all()), float(((got.double() - y).abs() / (tol + 1e-300)).max())
+
+
+SHAPES = [(1, 1, 1), (1, 16, 128), (3, 5, 100), (16, 16, 129), (17, 33, 512), (20, 48, 640), (31, 100, 1000), (64, 64, 256), (65, 127, 385),
+          (128, 128, 128), (130, 260, 700), (256, 256, 1024), (257, 300, 513), (500, 129, 2049), (1000, 520, 384), (12, 700, 9000), (700, 12, 9000),
+          (40, 40, 33000), (300, 4100, 256), (2048, 2048, 300)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_against_64_bits(M, N, K, dtype):
+    a, b = matrix(M, K, 1), matrix(N, K, 2)
+    bias = torch.randn(N, device=DEV) if (M + N) % 2 else None
+    got = api.tac_scaled_product(*a, *b, K, bias=bias, dtype=dtype)
+    y, size = exact(a, b, K, bias)
+    check(got, y, size, K)
+    assert torch.equal(got, api.tac_scaled_product(*a, *b, K, bias=bias, dtype=dtype))        # no order of arrival
+    wide = torch.full((M, N + 5), float("nan"), dtype=dtype, device=DEV)
+    api.tac_scaled_product(*a, *b, K, bias=bias, out=wide[:, :N])
+    assert torch.equal(wide[:, :N], got) and bool(torch.isnan(wide[:, N:]).all())
+
+
+@pytest.mark.parametrize("M,N,K", [(5, 40, 700), (300, 260, 700), (600, 700, 1400)])
+def test_every_place_has_its_own_value(M, N, K):
+    # one term per place, a different power of two or small whole number for each row, column and block: any row, column, block
+    # or byte that is taken for another shows up exactly
+    a, b = torch.zeros(M, K, device=DEV), torch.zeros(N, K, device=DEV)
+    rows, cols = torch.arange(M, device=DEV), torch.arange(N, device=DEV)
+    for k in range(0, K, 37):
+        a[rows, (k + rows) % K] = (1 + rows % 7) * 2.0 ** ((k // 128 + rows) % 7 - 3)
+        b[cols, (k + 3 * cols) % K] = (1 + cols % 15) * 2.0 ** ((k // 128 + 2 * cols) % 7 - 3)
+    qa, qb = api.tac_quantize(a)["rows"], api.tac_quantize(b)["rows"]
+    y, size = exact(qa, qb, K)
+    got = api.tac_scaled_product(*qa, *qb, K, dtype=torch.float32)
+    # terms are multiples of 2^-6, and their magnitudes add up to less than 2^18: every partial sum is a float32 number
+    assert float(size.max()) < 2.0 ** 18 and torch.equal(got.double(), y)
+
+
+@pytest.mark.parametrize("M", [1, 17, 300])
+def test_nan_stays_in_its_row_and_column(M):
+    N, K = 150, 600
+    a, b = torch.randn(M, K, device=DEV), torch.randn(N, K, device=DEV)
+    a[M - 1, 500], b[7, 3] = float("nan"), float("inf")
+    qa, qb = api.tac_quantize(a)["rows"], api.tac_quantize(b)["rows"]
+    got = torch.isnan(api.tac_scaled_product(*qa, *qb, K, dtype=torch.float32))
+    want = torch.zeros_like(got)
+    want[M - 1], want[:, 7] = True, True
+    assert torch.equal(got, want)
+
+
+def test_smallest_and_largest_scales():
+    K = 256
+    a, b = torch.randn(40, K, device=DEV) * 2.0 ** 100, torch.randn(50, K, device=DEV) * 2.0 ** -100
+    qa, qb = api.tac_quantize(a)["rows"], api.tac_quantize(b)["rows"]
+    y, size = exact(qa, qb, K)
+    check(api.tac_scaled_product(*qa, *qb, K, dtype=torch.float32), y, size, K)
+
+
+@pytest.mark.parametrize("rows,cols,n", [(70, 300, 200), (520, 384, 640), (900, 129, 257)])
+def test_the_three_products_of_a_dense_layer(rows, cols, n):
+    g = torch.Generator(device=DEV).manual_seed(4)
+    x, w, gy = (torch.randn(*s, generator=g, device=DEV) for s in ((rows, cols), (n, cols), (rows, n)))
+    qx, qw, qg = api.tac_quantize(x)["rows"], api.tac_quantize(w, tiles=True, columns=True), api.tac_quantize(gy, columns=True)
+    x64, w64, g64 = (torch.from_numpy(O.decode(m, c)[0]).to(DEV) for m, c in ((qx, cols), (qw["rows"], cols), (qg["rows"], n)))
+    f32 = torch.float32
+    check(api.tac_scaled_product(*qx, *qw["rows"], cols, dtype=f32), x64 @ w64.t(), x64.abs() @ w64.abs().t(), cols)
+    # the transposed weights hold the same values as the weights
+    check(api.tac_scaled_product(*qg["rows"], *qw["columns"], n, dtype=f32), g64 @ w64, g64.abs() @ w64.abs(), n)
+    kept = api.tac_quantize(qx, cols=cols, rows=False, columns=True)["columns"]
+    gt, xt = (torch.from_numpy(O.decode(m, rows)[0]).to(DEV) for m in (qg["columns"], kept))
+    check(api.tac_scaled_product(*qg["columns"], *kept, rows, dtype=f32), gt @ xt.t(), gt.abs() @ xt.abs().t(), rows)
+
+
+@pytest.mark.parametrize("M,N,K", [(9, 300, 2000), (300, 200, 700), (64, 64, 20000)])
+def test_on_another_stream_and_in_a_graph(M, N, K):
+    a, b = matrix(M, K, 5), matrix(N, K, 6)
+    want = api.tac_scaled_product(*a, *b, K)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = api.tac_scaled_product(*a, *b, K, stream=side.cuda_stream)
+    side.synchronize()
+    assert torch.equal(got, want)
+    for g in O.captured(lambda: api.tac_scaled_product(*a, *b, K)):
+        assert torch.equal(g, want)
+        g.zero_()
+
+
+@pytest.mark.parametrize("M", [7, 300])
+def test_offsets_beyond_32_bits(M):
+    N, K = 150_000, 32768                                          # 4.9 GB of codes
+    codes = torch.randint(0, 120, (N, K), dtype=torch.uint8, device=DEV)
+    scales = torch.randint(110, 130, (N, 4 * (-(-K // 512))), dtype=torch.uint8, device=DEV)
+    a = matrix(M, K, 7)
+    got = api.tac_scaled_product(*a, codes, scales, K, dtype=torch.float32)
+    for at in (0, N - 70):
+        y, size = exact(a, (codes[at:at + 70], scales[at:at + 70]), K)
+        check(got[:, at:at + 70], y, size, K)
+
+
+def test_output_beyond_32_bits():
+    M, N, K = 70_000, 20_000, 128                                   # 5.6 GB of float32
+    a, b = matrix(M, K, 8), matrix(N, K, 9)
+    got = api.tac_scaled_product(*a, *b, K, dtype=torch.float32)
+    y, size = exact((a[0][-50:], a[1][-50:]), b, K)
+    check(got[-50:], y, size, K)
