@@ -473,7 +473,7 @@ int tac_scaled_product(const tac_product_desc_t* desc, const uint8_t* a_codes, c
  * (the membrane of Eq. 1 with a leak of its own at each step, and no reset).  Sequences may have different lengths: out is zero from a
  * sequence's length on, what stands behind it is read into no result, and its last state is that of its last step (h0 where the
  * length is 0). */
-#define TAC_SCAN_CHUNK 32
+#define TAC_SCAN_CHUNK 16
 typedef struct tac_scan_desc {
   int64_t T;                     /* steps of the tensors */
   int32_t B, D;                  /* sequences, channels */

@@ -513,7 +513,7 @@ def tac_reset_counters() -> None:
 
 TAC_SCALED = 2
 TAC_BLOCK_ROW, TAC_BLOCK_TILE = 0, 1
-TAC_SCALE_BLOCK, TAC_SCAN_CHUNK, TAC_NORM_MAX_COLS = 128, 32, 32768
+TAC_SCALE_BLOCK, TAC_SCAN_CHUNK, TAC_NORM_MAX_COLS = 128, 16, 32768
 
 
 class tac_quantize_desc_t(ctypes.Structure):

@@ -1,87 +1,338 @@
 // Gated linear recurrence h_t = a_t h_{t-1} + (1 - a_t) value_t with a_t = 1 / (1 + exp(-gate_t)), its backward pass, and one step of it
 // on a pool of states.
+//
+// Memory-bound: six bytes a channel and step forwards in bfloat16, ten backwards, against some 25 vector instructions.  Steps in a row are
+// an affine map h -> A h + H, and two such maps in a row are one, so time is cut as the hardware wants it: a wave takes kChunk steps of 64 lanes'
+// channels into registers, forms its map, the waves of a workgroup pass theirs through LDS, and each goes over its steps once
+// more, in registers, from the state that it now knows.  Inputs are read once and outputs written once.  Where the channels are too few for
+// the chip, workgroups share the length as well: a launch that only forms the maps of the parts, then one that starts every part from those before it.
 #include "tac_head_common.h"
 
 namespace tac {
 
 namespace {
 
-constexpr int kChunk = TAC_SCAN_CHUNK;
+constexpr int kChunk = TAC_SCAN_CHUNK;       // steps of a wave
+constexpr int kWaves = 8;                    // most waves of a workgroup
 
-// a and 1 - a, the second without cancellation.  Gates below -80 count as -80 (exp stays finite; a < 2e-35 there).
-struct Leak {
-  float a, rest;
-};
-__device__ __forceinline__ Leak leak(float gate) {
-  const float e = __expf(-fmaxf(gate, -80.0f));
-  const float r = __builtin_amdgcn_rcpf(1.0f + e);
-  return Leak{r, e * r};
+// w = min(a, 1 - a) = 1 / (1 + exp(|gate|)), negative (as -0 too) where a is the smaller.  Updates are written around the nearer of the two ends,
+//   a >= 1/2:  h' = h + w (value - h)        a < 1/2:  h' = value - w (value - h)
+// so that a leak of nearly 1 does not lose the digits of 1 - a: a itself rounded to float32 leaves 1e-6 in states that remember a thousand steps.
+__device__ __forceinline__ float leak(float gate) {
+  const float e = __expf(-fabsf(gate));
+  const float w = e * __builtin_amdgcn_rcpf(1.0f + e);
+  return gate < 0.0f ? -w : w;               // a NaN stays one
 }
+__device__ __forceinline__ bool forgets(float s) { return (int)float_bits(s) < 0; }
+__device__ __forceinline__ float step_state(float s, float h, float u) { return fmaf(s, u - h, forgets(s) ? u : h); }
+__device__ __forceinline__ float times_a(float s, float x) { return fmaf(-s, x, forgets(s) ? 0.0f : x); }
 
 __device__ __forceinline__ int64_t length_of(const int32_t* lengths, int b, int64_t T) {
   return lengths ? min(max((int64_t)lengths[b], (int64_t)0), T) : T;
 }
 
-// a thread per channel
-template <typename T>
-__global__ __launch_bounds__(256) void scan_kernel(const ScanParams p) {
-  const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (n >= (int64_t)p.B * p.D) return;
-  const int b = (int)(n / p.D), d = (int)(n - (int64_t)b * p.D);
-  const int64_t len = length_of(p.lengths, b, p.T);
-  float h = p.h0 ? p.h0[n] : 0.0f;
-  const T *g = (const T*)p.gate + b * p.in_b + d, *u = (const T*)p.value + b * p.in_b + d;
-  T* out = (T*)p.out + b * p.out_b + d;
-  for (int64_t t = 0; t < p.T; ++t) {
-    if (p.states && t % kChunk == 0) p.states[t / kChunk * p.B * p.D + n] = h;
-    float o = 0.0f;
-    if (t < len) {
-      const Leak k = leak((float)g[t * p.in_t]);
-      o = h = fmaf(k.a, h, k.rest * (float)u[t * p.in_t]);
-    }
-    out[t * p.out_t] = (T)o;
+// V channels of a lane: one load of 4 bytes (two bfloat16 or one float32) or of 2
+template <typename T, int V>
+struct Lane {
+  static_assert(sizeof(T) * V <= 4);
+  using Raw = std::conditional_t<sizeof(T) * V == 4, uint32_t, uint16_t>;
+  static __device__ __forceinline__ Raw load(const T* p) { return *reinterpret_cast<const Raw*>(p); }
+  static __device__ __forceinline__ float value(Raw r, int e) {
+    if constexpr (sizeof(T) == 4) return bits_float(r);
+    else return bits_float(e ? (uint32_t)r & 0xffff0000u : (uint32_t)r << 16);
   }
-  if (p.h_last) p.h_last[n] = h;
+  static __device__ __forceinline__ Raw pack(const float (&v)[V]) {
+    if constexpr (sizeof(T) == 4) return float_bits(v[0]);
+    else return (Raw)pack_bf16(v[0], v[V - 1]);
+  }
+  static __device__ __forceinline__ void store(T* p, Raw r) { *reinterpret_cast<Raw*>(p) = r; }
+  // a gate of +infinity: the step leaves the state as it is
+  static constexpr Raw kKeep = (Raw)(sizeof(T) == 4 ? 0x7f800000u : 0x7f807f80u);
+};
+
+// Which channels and which part of the length a workgroup has.
+struct Place {
+  int b, d, tiles, first, last;      // sequence, the lane's first channel, tiles of the whole length, the part's tiles [first, last)
+  bool on;
+};
+template <int V>
+__device__ __forceinline__ Place place_of(int64_t T, int D) {
+  const int per_b = (D + 64 * V - 1) / (64 * V), steps = (blockDim.x >> 6) * kChunk;
+  Place q;
+  q.b = blockIdx.x / per_b;
+  q.d = ((blockIdx.x - q.b * per_b) * 64 + (threadIdx.x & 63)) * V;
+  q.on = q.d < D;
+  if (!q.on) q.d = 0;                // reads what is there, writes nothing
+  q.tiles = (int)((T + steps - 1) / steps);
+  q.first = (int)((int64_t)q.tiles * blockIdx.y / gridDim.y);
+  q.last = (int)((int64_t)q.tiles * (blockIdx.y + 1) / gridDim.y);
+  return q;
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void scan_backward_kernel(const ScanBackwardParams p) {
-  const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (n >= (int64_t)p.B * p.D) return;
-  const int b = (int)(n / p.D), d = (int)(n - (int64_t)b * p.D);
-  const int64_t len = length_of(p.lengths, b, p.T);
-  const T *g = (const T*)p.gate + b * p.in_b + d, *u = (const T*)p.value + b * p.in_b + d, *go = (const T*)p.grad_out + b * p.out_b + d;
-  T *gg = (T*)p.grad_gate + b * p.grad_b + d, *gv = (T*)p.grad_value + b * p.grad_b + d;
-  float c = p.grad_h_last ? p.grad_h_last[n] : 0.0f;
-  for (int64_t chunk = (p.T + kChunk - 1) / kChunk - 1; chunk >= 0; --chunk) {
-    const int64_t t0 = chunk * kChunk;
-    float before[kChunk];
-    float h = p.states[chunk * p.B * p.D + n];
+template <int V>
+struct Map {                         // x -> a x + b
+  float a[V], b[V];
+};
+
+// MAPS: only the map of the part, into workspace [part][2][B][D], from its last tile to its first (the tiles that the second launch starts with are
+// then those that the caches have seen last); the last part's is not needed.
+template <typename T, int V, bool MAPS>
+__global__ __launch_bounds__(64 * kWaves) void scan_kernel(const ScanParams p) {
+  using L = Lane<T, V>;
+  __shared__ Map<V> maps[2][kWaves][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+  if (MAPS && blockIdx.y == gridDim.y - 1) return;
+  const Place q = place_of<V>(p.T, p.D);
+  const int64_t len = length_of(p.lengths, q.b, p.T), channels = (int64_t)p.B * p.D, n = (int64_t)q.b * p.D + q.d;
+  const T *gate = (const T*)p.gate + q.b * p.in_b, *value = (const T*)p.value + q.b * p.in_b;
+  T* out = (T*)p.out + q.b * p.out_b;
+  typename L::Raw g[kChunk] = {}, u[kChunk] = {};
+  auto load = [&](int tile) {
+    const int64_t t0 = ((int64_t)tile * waves + wave) * kChunk;
+    if (t0 >= len) return;
+#pragma unroll
+    for (int i = 0; i < kChunk; ++i) {         // behind the end the last step again; what it brings is replaced below
+      const int64_t t = min(t0 + i, len - 1);
+      g[i] = L::load(gate + t * p.in_t + q.d);
+      u[i] = L::load(value + t * p.in_t + q.d);
+    }
+  };
+  float carry[V], total[V];          // MAPS: the map of the tiles behind, else the state before the tile
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    total[e] = 1.0f;
+    carry[e] = MAPS || !p.h0 ? 0.0f : p.h0[n + e];
+    if constexpr (!MAPS)
+      for (int k = 0; k < (int)blockIdx.y; ++k)
+        carry[e] = fmaf(p.workspace[2 * k * channels + n + e], carry[e], p.workspace[(2 * k + 1) * channels + n + e]);
+  }
+  load(MAPS ? q.last - 1 : q.first);
+  for (int k = 0; k < q.last - q.first; ++k) {
+    const int tile = MAPS ? q.last - 1 - k : q.first + k;
+    const int64_t t0 = ((int64_t)tile * waves + wave) * kChunk;
+    float s[kChunk][V];
+    typename L::Raw x[kChunk];
+    Map<V> mine;
+    if (t0 + kChunk > len) {                   // steps behind the length keep the state
+#pragma unroll
+      for (int i = 0; i < kChunk; ++i)
+        if (t0 + i >= len) {
+          g[i] = L::kKeep;
+          u[i] = 0;
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      mine.a[e] = 1.0f;
+      mine.b[e] = 0.0f;
+    }
 #pragma unroll
     for (int i = 0; i < kChunk; ++i) {
-      before[i] = h;
-      if (t0 + i < len) {
-        const Leak k = leak((float)g[(t0 + i) * p.in_t]);
-        h = fmaf(k.a, h, k.rest * (float)u[(t0 + i) * p.in_t]);
+      x[i] = u[i];
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        s[i][e] = leak(L::value(g[i], e));
+        mine.b[e] = step_state(s[i][e], mine.b[e], L::value(x[i], e));
+        mine.a[e] = times_a(s[i][e], mine.a[e]);
+      }
+    }
+    maps[k & 1][wave][lane] = mine;
+    if (k + 1 < q.last - q.first) load(MAPS ? tile - 1 : tile + 1);
+    __syncthreads();                 // one a tile: what is written next is the other half, read before the barrier in between
+    float h[V];
+    if constexpr (MAPS) {
+      for (int w = waves - 1; w >= 0; --w) {
+        const Map<V> m = maps[k & 1][w][lane];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          carry[e] = fmaf(total[e], m.b[e], carry[e]);
+          total[e] *= m.a[e];
+        }
+      }
+    } else {
+      for (int w = 0; w < waves; ++w) {
+        const Map<V> m = maps[k & 1][w][lane];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          if (w == wave) h[e] = carry[e];
+          carry[e] = fmaf(m.a[e], carry[e], m.b[e]);
+        }
+      }
+      if (p.states && t0 < p.T && q.on) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) p.states[t0 / kChunk * channels + n + e] = h[e];
+      }
+#pragma unroll
+      for (int i = 0; i < kChunk; ++i) {
+        float o[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          h[e] = step_state(s[i][e], h[e], L::value(x[i], e));
+          o[e] = h[e];
+        }
+        x[i] = L::pack(o);
+      }
+      if (t0 + kChunk <= len) {
+        if (q.on) {
+#pragma unroll
+          for (int i = 0; i < kChunk; ++i) L::store(out + (t0 + i) * p.out_t + q.d, x[i]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i)
+          if (t0 + i < p.T && q.on) L::store(out + (t0 + i) * p.out_t + q.d, t0 + i < len ? x[i] : (typename L::Raw)0);
+      }
+    }
+  }
+  if (wave || !q.on) return;
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    if constexpr (MAPS) {
+      p.workspace[2 * blockIdx.y * channels + n + e] = total[e];
+      p.workspace[(2 * blockIdx.y + 1) * channels + n + e] = carry[e];
+    } else if (p.h_last && blockIdx.y == gridDim.y - 1) {
+      p.h_last[n + e] = carry[e];
+    }
+  }
+}
+
+// The same backwards: the gradient c that arrives at a step's state obeys c <- a (c + grad_out).  With w = min(a, 1 - a) the gate's
+// gradient is c w (1 - w) (h_{t-1} - value).  The states before the steps are formed again from the chunk's first, which the forward pass kept.
+template <typename T, int V, bool MAPS>
+__global__ __launch_bounds__(64 * kWaves) void scan_backward_kernel(const ScanBackwardParams p) {
+  using L = Lane<T, V>;
+  __shared__ Map<V> maps[2][kWaves][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+  if (MAPS && blockIdx.y == 0) return;
+  const Place q = place_of<V>(p.T, p.D);
+  const int64_t len = length_of(p.lengths, q.b, p.T), channels = (int64_t)p.B * p.D, n = (int64_t)q.b * p.D + q.d;
+  const T *gate = (const T*)p.gate + q.b * p.in_b, *value = (const T*)p.value + q.b * p.in_b, *grad_out = (const T*)p.grad_out + q.b * p.out_b;
+  T *grad_gate = (T*)p.grad_gate + q.b * p.grad_b, *grad_value = (T*)p.grad_value + q.b * p.grad_b;
+  typename L::Raw g[kChunk] = {}, u[kChunk] = {}, go[kChunk] = {};
+  float first[V];                    // the state before the chunk
+  auto load = [&](int tile) {
+    const int64_t t0 = ((int64_t)tile * waves + wave) * kChunk;
+#pragma unroll
+    for (int e = 0; e < V; ++e) first[e] = !MAPS && t0 < p.T ? p.states[t0 / kChunk * channels + n + e] : 0.0f;
+    if (t0 >= len) return;
+#pragma unroll
+    for (int i = 0; i < kChunk; ++i) {
+      const int64_t t = min(t0 + i, len - 1);
+      g[i] = L::load(gate + t * p.in_t + q.d);
+      if constexpr (!MAPS) u[i] = L::load(value + t * p.in_t + q.d);
+      go[i] = L::load(grad_out + t * p.out_t + q.d);
+    }
+  };
+  float carry[V], total[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    total[e] = 1.0f;
+    carry[e] = MAPS || !p.grad_h_last ? 0.0f : p.grad_h_last[n + e];
+    if constexpr (!MAPS)
+      for (int k = gridDim.y - 1; k > (int)blockIdx.y; --k)
+        carry[e] = fmaf(p.workspace[2 * k * channels + n + e], carry[e], p.workspace[(2 * k + 1) * channels + n + e]);
+  }
+  load(MAPS ? q.first : q.last - 1);
+  for (int k = 0; k < q.last - q.first; ++k) {
+    const int tile = MAPS ? q.first + k : q.last - 1 - k;
+    const int64_t t0 = ((int64_t)tile * waves + wave) * kChunk;
+    float s[kChunk][V], before[kChunk][V];
+    typename L::Raw x[kChunk], y[kChunk];
+    Map<V> mine;
+    if (t0 + kChunk > len) {
+#pragma unroll
+      for (int i = 0; i < kChunk; ++i)
+        if (t0 + i >= len) {
+          g[i] = L::kKeep;
+          u[i] = go[i] = 0;
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      mine.a[e] = 1.0f;
+      mine.b[e] = 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < kChunk; ++i) {
+      x[i] = u[i];
+      y[i] = go[i];
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        s[i][e] = leak(L::value(g[i], e));
+        if constexpr (!MAPS) before[i][e] = i ? step_state(s[i - 1][e], before[i - 1][e], L::value(x[i - 1], e)) : first[e];
       }
     }
 #pragma unroll
-    for (int i = kChunk - 1; i >= 0; --i) {
-      const int64_t t = t0 + i;
-      if (t >= p.T) continue;
-      float dg = 0.0f, dv = 0.0f;
-      if (t < len) {
-        const Leak k = leak((float)g[t * p.in_t]);
-        c += (float)go[t * p.out_t];
-        dv = k.rest * c;
-        dg = dv * k.a * (before[i] - (float)u[t * p.in_t]);
-        c *= k.a;
+    for (int i = kChunk - 1; i >= 0; --i)
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        mine.b[e] = times_a(s[i][e], mine.b[e] + L::value(y[i], e));
+        mine.a[e] = times_a(s[i][e], mine.a[e]);
       }
-      gg[t * p.grad_t] = (T)dg;
-      gv[t * p.grad_t] = (T)dv;
+    maps[k & 1][wave][lane] = mine;
+    if (k + 1 < q.last - q.first) load(MAPS ? tile + 1 : tile - 1);
+    __syncthreads();
+    float c[V];
+    if constexpr (MAPS) {
+      for (int w = 0; w < waves; ++w) {
+        const Map<V> m = maps[k & 1][w][lane];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          carry[e] = fmaf(total[e], m.b[e], carry[e]);
+          total[e] *= m.a[e];
+        }
+      }
+    } else {
+      for (int w = waves - 1; w >= 0; --w) {
+        const Map<V> m = maps[k & 1][w][lane];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          if (w == wave) c[e] = carry[e];
+          carry[e] = fmaf(m.a[e], carry[e], m.b[e]);
+        }
+      }
+#pragma unroll
+      for (int i = kChunk - 1; i >= 0; --i) {
+        float dg[V], dv[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const float w = fabsf(s[i][e]), now = c[e] + L::value(y[i], e);
+          dv[e] = now * (forgets(s[i][e]) ? 1.0f - w : w);
+          dg[e] = now * (w * (1.0f - w)) * (before[i][e] - L::value(x[i], e));
+          c[e] = times_a(s[i][e], now);
+        }
+        x[i] = L::pack(dg);
+        y[i] = L::pack(dv);
+      }
+      if (t0 + kChunk <= len) {
+        if (q.on) {
+#pragma unroll
+          for (int i = 0; i < kChunk; ++i) {
+            L::store(grad_gate + (t0 + i) * p.grad_t + q.d, x[i]);
+            L::store(grad_value + (t0 + i) * p.grad_t + q.d, y[i]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i)
+          if (t0 + i < p.T && q.on) {
+            const bool live = t0 + i < len;
+            L::store(grad_gate + (t0 + i) * p.grad_t + q.d, live ? x[i] : (typename L::Raw)0);
+            L::store(grad_value + (t0 + i) * p.grad_t + q.d, live ? y[i] : (typename L::Raw)0);
+          }
+      }
     }
   }
-  if (p.grad_h0) p.grad_h0[n] = c;
+  if (wave || !q.on) return;
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    if constexpr (MAPS) {
+      p.workspace[2 * blockIdx.y * channels + n + e] = total[e];
+      p.workspace[(2 * blockIdx.y + 1) * channels + n + e] = carry[e];
+    } else if (p.grad_h0 && blockIdx.y == 0) {
+      p.grad_h0[n + e] = carry[e];
+    }
+  }
 }
 
 // a thread per channel of a row
@@ -93,29 +344,72 @@ __global__ __launch_bounds__(256) void step_kernel(const StepParams p) {
   float h = 0.0f;
   if (slot >= 0 && slot < p.n_slots) {
     float* state = p.pool + slot * p.D + d;
-    const Leak k = leak((float)((const T*)p.gate)[b * p.in_b + d]);
-    h = fmaf(k.a, *state, k.rest * (float)((const T*)p.value)[b * p.in_b + d]);
+    h = step_state(leak((float)((const T*)p.gate)[b * p.in_b + d]), *state, (float)((const T*)p.value)[b * p.in_b + d]);
     *state = h;
   }
   ((T*)p.out)[b * p.out_b + d] = (T)h;
 }
 
-}  // namespace
+int wave_count(int64_t T) { return (int)(T > kWaves * kChunk ? kWaves : (T + kChunk - 1) / kChunk); }
+int64_t channel_groups(int B, int D, int v) { return (int64_t)B * ((D + 64 * v - 1) / (64 * v)); }
 
-size_t scan_workspace(int64_t, int, int, int) { return 0; }
+// Parts of the length: one where the channels alone give three workgroups to every four compute units, else enough for two to each.
+int length_parts(int64_t T, int B, int D, int bf) {
+  const int64_t groups = channel_groups(B, D, bf ? 2 : 1), tiles = (T + kWaves * kChunk - 1) / (kWaves * kChunk);
+  if (groups >= kFittedUnits * 3 / 4) return 1;
+  const int64_t want = (2 * kFittedUnits + groups - 1) / groups;
+  return (int)(want < tiles ? want : tiles);
+}
 
-hipError_t scan_launch(const ScanParams& p, hipStream_t s) {
-  const dim3 grid((unsigned)(((int64_t)p.B * p.D + 255) / 256));
-  if (p.bf16) hipLaunchKernelGGL(scan_kernel<bf16>, grid, dim3(256), 0, s, p);
-  else hipLaunchKernelGGL(scan_kernel<float>, grid, dim3(256), 0, s, p);
+// two bfloat16 at once: an even number of channels, and rows that start at multiples of 4 bytes
+bool pairs(int D, int64_t a, int64_t b, const void* p, const void* q) {
+  return D % 2 == 0 && ((a | b) & 1) == 0 && (((uintptr_t)p | (uintptr_t)q) & 3u) == 0;
+}
+
+template <typename T, int V>
+hipError_t scan_typed(const ScanParams& p, hipStream_t s) {
+  const int parts = length_parts(p.T, p.B, p.D, p.bf16), threads = 64 * wave_count(p.T);
+  const unsigned groups = (unsigned)channel_groups(p.B, p.D, V);
+  if (parts > 1) {
+    hipLaunchKernelGGL((scan_kernel<T, V, true>), dim3(groups, parts), dim3(threads), 0, s, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((scan_kernel<T, V, false>), dim3(groups, parts), dim3(threads), 0, s, p);
   return hipGetLastError();
 }
 
-hipError_t scan_backward_launch(const ScanBackwardParams& p, hipStream_t s) {
-  const dim3 grid((unsigned)(((int64_t)p.B * p.D + 255) / 256));
-  if (p.bf16) hipLaunchKernelGGL(scan_backward_kernel<bf16>, grid, dim3(256), 0, s, p);
-  else hipLaunchKernelGGL(scan_backward_kernel<float>, grid, dim3(256), 0, s, p);
+template <typename T, int V>
+hipError_t scan_backward_typed(const ScanBackwardParams& p, hipStream_t s) {
+  const int parts = length_parts(p.T, p.B, p.D, p.bf16), threads = 64 * wave_count(p.T);
+  const unsigned groups = (unsigned)channel_groups(p.B, p.D, V);
+  if (parts > 1) {
+    hipLaunchKernelGGL((scan_backward_kernel<T, V, true>), dim3(groups, parts), dim3(threads), 0, s, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((scan_backward_kernel<T, V, false>), dim3(groups, parts), dim3(threads), 0, s, p);
   return hipGetLastError();
+}
+
+}  // namespace
+
+size_t scan_workspace(int64_t T, int B, int D, int bf) {
+  const int parts = length_parts(T, B, D, bf);
+  return parts > 1 ? (size_t)parts * 2 * (size_t)B * (size_t)D * sizeof(float) : 0;
+}
+
+hipError_t scan_launch(const ScanParams& p, hipStream_t s) {
+  if (!p.bf16) return scan_typed<float, 1>(p, s);
+  const bool two = pairs(p.D, p.in_t, p.in_b, p.gate, p.value) && pairs(p.D, p.out_t, p.out_b, p.out, nullptr);
+  return two ? scan_typed<bf16, 2>(p, s) : scan_typed<bf16, 1>(p, s);
+}
+
+hipError_t scan_backward_launch(const ScanBackwardParams& p, hipStream_t s) {
+  if (!p.bf16) return scan_backward_typed<float, 1>(p, s);
+  const bool two = pairs(p.D, p.in_t, p.in_b, p.gate, p.value) && pairs(p.D, p.out_t, p.out_b, p.grad_out, nullptr) &&
+                   pairs(p.D, p.grad_t, p.grad_b, p.grad_gate, p.grad_value);
+  return two ? scan_backward_typed<bf16, 2>(p, s) : scan_backward_typed<bf16, 1>(p, s);
 }
 
 hipError_t step_launch(const StepParams& p, hipStream_t s) {
