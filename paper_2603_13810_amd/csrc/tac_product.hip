@@ -1,35 +1,43 @@
 // Product of two 8-bit matrices with a power of two per 128 columns, on the matrix cores.
 //
-// v_mfma_scale_f32_16x16x128_f8f6f4 multiplies 16 rows by 16 rows over 128 columns and applies, per row and 32 columns, a power of two
-// that each lane passes in a byte: a block's scale costs no instruction of its own, and all blocks of a sum stay in one accumulator.
-// Lane l holds 32 consecutive codes of row l % 16, those from 32 (l / 16) on.
+// v_mfma_scale_f32_{16x16x128,32x32x64}_f8f6f4 multiply 16 or 32 rows by as many over 128 or 64 columns and apply, per row and 32 columns, a power
+// of two that each lane passes in a byte: a block's scale costs no instruction of its own, and all blocks of a sum stay in one accumulator.
+// A lane holds 32 consecutive codes of one row.
 //
-// That instruction adds eight consecutive products at a time and keeps only what reaches 2^-13 of the largest of them (measured: 2^16 and
+// Those instructions add eight consecutive products at a time and keep only what reaches 2^-13 of the largest of them (measured: 2^16 and
 // one smaller term; normal operands leave a relative error of 1.5e-5 in a sum, wide ones 7e-5).  A bfloat16 result rounds by 2^-8 and does not
 // notice; for a float32 result the codes are turned into bfloat16 in registers, exactly and with their scale (v_cvt_scalef32_pk_bf16_fp8),
-// and multiplied by v_mfma_f32_16x16x32_bf16, which keeps float32 sums (1e-8), at half the rate.
+// and multiplied by v_mfma_f32_*_bf16, which keep float32 sums (1e-8), at half the rate.
+//
+// The rows of b are the instructions' first operand: a lane then ends with four consecutive n of one m.
 #include "tac_head_common.h"
+#include "tac_mfma_common.h"
 
 namespace tac {
 
 namespace {
 
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
-
-__device__ __forceinline__ i32x8_t load_codes(const uint8_t* p) {
-  const u32x4_t lo = reinterpret_cast<const u32x4_t*>(p)[0], hi = reinterpret_cast<const u32x4_t*>(p)[1];
-  return i32x8_t{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
-}
-
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 
-// eight codes as bfloat16 times 2^e (its float in `scale`)
-__device__ __forceinline__ bf16x8_t widen(uint32_t lo, uint32_t hi, float scale) {
+__device__ __forceinline__ i32x8_t join_codes(u32x4_t lo, u32x4_t hi) {
+  return i32x8_t{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+}
+__device__ __forceinline__ i32x8_t load_codes(const uint8_t* p) {
+  return join_codes(reinterpret_cast<const u32x4_t*>(p)[0], reinterpret_cast<const u32x4_t*>(p)[1]);
+}
+
+// the 8 q-th to 8 q + 7-th of 32 codes as bfloat16 times 2^e (its float in `scale`)
+__device__ __forceinline__ bf16x8_t widen(i32x8_t codes, int q, float scale) {
+  const uint32_t lo = (uint32_t)codes[2 * q], hi = (uint32_t)codes[2 * q + 1];
   const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
   const bf16x2_t c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
   return bf16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
+
+// ---- few rows -------------------------------------------------------------------------------------
 
 template <bool EXACT>
 __device__ __forceinline__ f32x4_t multiply(i32x8_t a, i32x8_t b, f32x4_t c, uint32_t a_scale, uint32_t b_scale) {
@@ -38,17 +46,14 @@ __device__ __forceinline__ f32x4_t multiply(i32x8_t a, i32x8_t b, f32x4_t c, uin
   } else {
     const float as = scale_value(a_scale), bs = scale_value(b_scale);
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen((uint32_t)a[2 * q], (uint32_t)a[2 * q + 1], as),
-                                                  widen((uint32_t)b[2 * q], (uint32_t)b[2 * q + 1], bs), c, 0, 0, 0);
+    for (int q = 0; q < 4; ++q) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(a, q, as), widen(b, q, bs), c, 0, 0, 0);
     return c;
   }
 }
 
 // Four waves share 16 rows of b and 16 of a and take every fourth block of columns each; their sums are added up in LDS in a fixed order.
-// The rows of b are the instruction's first operand: a lane then ends with four consecutive n of one m.
 template <typename T>
-__global__ __launch_bounds__(256) void product_kernel(const ProductParams p) {
+__global__ __launch_bounds__(256) void product_rows_kernel(const ProductParams p) {
   __shared__ f32x4_t room[4][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t n0 = (int64_t)blockIdx.x * 16, m0 = (int64_t)blockIdx.y * 16;
@@ -58,7 +63,8 @@ __global__ __launch_bounds__(256) void product_kernel(const ProductParams p) {
   const uint8_t *bp = p.b + n * pitch + 32 * (lane / 16), *ap = p.a + m * pitch + 32 * (lane / 16);
   f32x4_t sum = {0.0f, 0.0f, 0.0f, 0.0f};
   for (int64_t k = wave; k < blocks; k += 4)
-    sum = multiply<sizeof(T) == 4>(load_codes(bp + k * kBlock), load_codes(ap + k * kBlock), sum, p.b_scales[n * spitch + k], p.a_scales[m * spitch + k]);
+    sum = multiply<sizeof(T) == 4>(load_codes(bp + k * kBlock), load_codes(ap + k * kBlock), sum, p.b_scales[n * spitch + k],
+                                   p.a_scales[m * spitch + k]);
   room[wave][lane] = sum;
   __syncthreads();
   if (wave) return;
@@ -71,11 +77,173 @@ __global__ __launch_bounds__(256) void product_kernel(const ProductParams p) {
   }
 }
 
+// ---- many rows ------------------------------------------------------------------------------------
+
+// Tiles of TM rows of a x TN rows of b, WM x WN waves.  One block of 128 columns of the tile's rows (128 bytes each) is a stage in LDS; two stages:
+// while the waves multiply one, direct-to-LDS loads fill the other, and one barrier a block parts them.  A row's eight pieces of 16
+// bytes stand at their number XOR bits 1 to 3 of the row, so that the 16 rows that a fragment read takes at once fall into different
+// banks.  blockIdx.y: the part of the columns where those are shared (`partial`, float32 [part][M][N]).
+template <int TM, int TN, int WM, int WN, bool EXACT, typename T>
+__global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(const ProductParams p, int parts) {
+  constexpr int kWaves = WM * WN, FM = TM / WM / 32, FN = TN / WN / 32, kStage = (TM + TN) * kBlock;
+  constexpr int kLoads = (TM + TN) / 8 / kWaves;         // a load instruction brings 8 rows
+  static_assert(TM % (32 * WM) == 0 && TN % (32 * WN) == 0 && TM % 8 == 0 && (TM + TN) % (8 * kWaves) == 0);
+  extern __shared__ __align__(1024) uint8_t stages[];    // two of them
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t pitch = code_pitch(p.K), spitch = scale_pitch(p.K);
+  const int blocks = (int)(pitch / kBlock);
+  const int first = (int)((int64_t)blocks * blockIdx.y / parts), last = (int)((int64_t)blocks * (blockIdx.y + 1) / parts);
+  // Workgroups i, i + 8, i + 16 ... run on one of the eight dies, which have an L2 each: a die takes consecutive tiles, in strips of four tile rows of a,
+  // so that the tiles that it has in hand at a time share their rows.
+  const int tiles_m = (int)((p.M + TM - 1) / TM), tiles_n = (int)((p.N + TN - 1) / TN), tiles = tiles_m * tiles_n;
+  int tile = blockIdx.x;
+  {
+    const int die = tile % 8, at = tile / 8, whole = tiles / 8, more = tiles % 8;
+    tile = die * whole + min(die, more) + at;
+  }
+  const int strip = tile / (4 * tiles_n), rows = min(4, tiles_m - 4 * strip), in = tile - strip * 4 * tiles_n;
+  const int64_t m0 = (int64_t)(4 * strip + in % rows) * TM, n0 = (int64_t)(in / rows) * TN;
+
+  // rows beyond the matrices read the last one; what comes of them is not stored
+  const uint8_t* from[kLoads];
+#pragma unroll
+  for (int j = 0; j < kLoads; ++j) {
+    const int r = 8 * (wave + j * kWaves) + lane / 8;
+    const uint8_t* row = r < TM ? p.a + min(m0 + r, p.M - 1) * pitch : p.b + min(n0 + r - TM, p.N - 1) * pitch;
+    from[j] = row + (int64_t)first * kBlock + 16 * ((lane % 8) ^ ((r >> 1) & 7));
+  }
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)stages;
+  auto load = [&](int stage) {
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      lds_dma16<1, 0>(from[j], lds0 + stage * kStage + (wave + j * kWaves) * 1024);
+      from[j] += kBlock;
+    }
+  };
+
+  const int wm = wave % WM, wn = wave / WM;
+  const uint8_t *sm[FM], *sn[FN];
+#pragma unroll
+  for (int f = 0; f < FM; ++f) sm[f] = p.a_scales + min(m0 + (wm * FM + f) * 32 + lane % 32, p.M - 1) * spitch;
+#pragma unroll
+  for (int f = 0; f < FN; ++f) sn[f] = p.b_scales + min(n0 + (wn * FN + f) * 32 + lane % 32, p.N - 1) * spitch;
+  uint32_t em[FM], en[FN];                                // scale bytes of four blocks, the current one lowest
+
+  f32x16_t sum[FN][FM];
+#pragma unroll
+  for (int i = 0; i < FN; ++i)
+#pragma unroll
+    for (int j = 0; j < FM; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sum[i][j][e] = 0.0f;
+
+  load(0);
+  for (int k = first; k < last; ++k) {
+    const int stage = (k - first) & 1;
+    if (k == first || k % 4 == 0) {
+#pragma unroll
+      for (int f = 0; f < FM; ++f) em[f] = *reinterpret_cast<const uint32_t*>(sm[f] + (k & ~3)) >> (8 * (k & 3));
+#pragma unroll
+      for (int f = 0; f < FN; ++f) en[f] = *reinterpret_cast<const uint32_t*>(sn[f] + (k & ~3)) >> (8 * (k & 3));
+    }
+    lds_dma_wait();
+    __syncthreads();
+    if (k + 1 < last) load(stage ^ 1);
+    const uint8_t *am = stages + stage * kStage + wm * FM * 32 * kBlock, *bn = stages + stage * kStage + (TM + wn * FN * 32) * kBlock;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {                // 64 columns an instruction
+      const int c = 4 * half + 2 * (lane / 32), x = (lane >> 1) & 7, row = (lane % 32) * kBlock;
+      const int lo = row + 16 * (c ^ x), hi = row + 16 * ((c + 1) ^ x);
+      i32x8_t a[FM], b[FN];
+#pragma unroll
+      for (int f = 0; f < FM; ++f)
+        a[f] = join_codes(*reinterpret_cast<const u32x4_t*>(am + f * 32 * kBlock + lo), *reinterpret_cast<const u32x4_t*>(am + f * 32 * kBlock + hi));
+#pragma unroll
+      for (int f = 0; f < FN; ++f)
+        b[f] = join_codes(*reinterpret_cast<const u32x4_t*>(bn + f * 32 * kBlock + lo), *reinterpret_cast<const u32x4_t*>(bn + f * 32 * kBlock + hi));
+      if constexpr (EXACT) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          bf16x8_t av[FM];
+#pragma unroll
+          for (int f = 0; f < FM; ++f) av[f] = widen(a[f], q, scale_value(em[f] & 255u));
+#pragma unroll
+          for (int i = 0; i < FN; ++i) {
+            const bf16x8_t bv = widen(b[i], q, scale_value(en[i] & 255u));
+#pragma unroll
+            for (int j = 0; j < FM; ++j) sum[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bv, av[j], sum[i][j], 0, 0, 0);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < FN; ++i)
+#pragma unroll
+          for (int j = 0; j < FM; ++j)
+            sum[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b[i], a[j], sum[i][j], 0, 0, 0, (int)en[i], 0, (int)em[j]);
+      }
+    }
+#pragma unroll
+    for (int f = 0; f < FM; ++f) em[f] >>= 8;
+#pragma unroll
+    for (int f = 0; f < FN; ++f) en[f] >>= 8;
+  }
+
+  // element e of a lane: n = 8 (e / 4) + 4 (lane / 32) + e % 4, m = lane % 32
+#pragma unroll
+  for (int j = 0; j < FM; ++j) {
+    const int64_t m = m0 + (wm * FM + j) * 32 + lane % 32;
+    if (m >= p.M) continue;
+#pragma unroll
+    for (int i = 0; i < FN; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int64_t n = n0 + (wn * FN + i) * 32 + 8 * q + 4 * (lane / 32);
+        if (n >= p.N) continue;
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = sum[i][j][4 * q + e];
+        if (parts > 1) {
+          float* to = p.partial + ((int64_t)blockIdx.y * p.M + m) * p.N + n;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (n + e < p.N) to[e] = v[e];
+          continue;
+        }
+        if (p.bias) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (n + e < p.N) v[e] += p.bias[n + e];
+        }
+        T* to = (T*)p.y + m * p.y_stride + n;
+        if (p.wide_stores && n + 4 <= p.N) store_floats<T, 4, true>(to, 4, v);
+        else store_floats<T, 4, false>(to, p.N - n, v);
+      }
+  }
+}
+
+template <int TM, int TN, int WM, int WN, typename T>
+hipError_t tile_launch(const ProductParams& p, int parts, hipStream_t s) {
+  const int64_t tiles = ((p.M + TM - 1) / TM) * ((p.N + TN - 1) / TN);
+  auto* kernel = product_tile_kernel<TM, TN, WM, WN, sizeof(T) == 4, T>;
+  constexpr int lds = 2 * (TM + TN) * kBlock;
+  static const hipError_t room = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (room != hipSuccess) return room;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)tiles, (unsigned)parts), dim3(64 * WM * WN), lds, s, p, parts);
+  return hipGetLastError();
+}
+
 }  // namespace
 
 size_t product_workspace(int64_t, int64_t, int64_t) { return 0; }
 
-hipError_t product_launch(const ProductParams& p, hipStream_t s) {
+hipError_t product_launch(const ProductParams& given, hipStream_t s) {
+  ProductParams p = given;
+  p.wide_stores = rows_aligned(p.y, p.y_stride, p.bf16 ? 2 : 4) ||
+                  (p.bf16 && (((uintptr_t)p.y | (uintptr_t)(p.y_stride * 2)) & 7u) == 0);
+  if (p.M > 64 && p.N > 64) {
+    if (p.M > 128 && p.N > 128) return p.bf16 ? tile_launch<256, 256, 4, 2, bf16>(p, 1, s) : tile_launch<256, 256, 4, 2, float>(p, 1, s);
+    return p.bf16 ? tile_launch<128, 128, 2, 2, bf16>(p, 1, s) : tile_launch<128, 128, 2, 2, float>(p, 1, s);
+  }
   for (int64_t m = 0; m < p.M; m += 16 * 65535) {        // the grid's second axis ends at 65535
     ProductParams q = p;
     q.M = p.M - m < 16 * 65535 ? p.M - m : 16 * 65535;
@@ -83,8 +251,8 @@ hipError_t product_launch(const ProductParams& p, hipStream_t s) {
     q.a_scales += m * scale_pitch(p.K);
     q.y = (char*)p.y + m * p.y_stride * (p.bf16 ? 2 : 4);
     const dim3 grid((unsigned)((p.N + 15) / 16), (unsigned)((q.M + 15) / 16));
-    if (p.bf16) hipLaunchKernelGGL(product_kernel<bf16>, grid, dim3(256), 0, s, q);
-    else hipLaunchKernelGGL(product_kernel<float>, grid, dim3(256), 0, s, q);
+    if (p.bf16) hipLaunchKernelGGL(product_rows_kernel<bf16>, grid, dim3(256), 0, s, q);
+    else hipLaunchKernelGGL(product_rows_kernel<float>, grid, dim3(256), 0, s, q);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
