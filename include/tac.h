@@ -457,13 +457,14 @@ typedef struct tac_product_desc {
   int64_t y_stride;          /* elements from row to row, >= N */
   int32_t dtype;             /* of y: TAC_FP32 / TAC_BF16 */
 } tac_product_desc_t;
+#define TAC_PRODUCT_MAX_K (1 << 23)
 /*   a_codes, a_scales  DEVICE, read-only, 8-bit matrix [M][K]
  *   b_codes, b_scales  DEVICE, read-only, 8-bit matrix [N][K]
  *   bias       DEVICE, read-only, float32 [N], or NULL
  *   y          DEVICE, written
  *   workspace  DEVICE, scratch, tac_scaled_product_workspace_bytes(desc) bytes, 16-byte aligned; NULL where those are 0
  * The same bits from call to call.
- * Errors: TAC_ERR_NULL, TAC_ERR_BAD_SHAPE (also M, N or K beyond 2^31 - 1), TAC_ERR_BAD_PARAM, TAC_ERR_ALIGN, TAC_ERR_HIP. */
+ * Errors: TAC_ERR_NULL, TAC_ERR_BAD_SHAPE (also M, N or K beyond 2^31 - 1), TAC_ERR_UNSUPPORTED (K beyond TAC_PRODUCT_MAX_K), TAC_ERR_BAD_PARAM, TAC_ERR_ALIGN, TAC_ERR_HIP. */
 size_t tac_scaled_product_workspace_bytes(const tac_product_desc_t* desc);
 int tac_scaled_product(const tac_product_desc_t* desc, const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes,
                        const uint8_t* b_scales, const float* bias, void* y, void* workspace, void* stream);

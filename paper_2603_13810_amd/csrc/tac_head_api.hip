@@ -125,6 +125,7 @@ static int check_product(const tac_product_desc_t* d) {
   if (!d) return TAC_ERR_NULL;
   if (d->M < 1 || d->N < 1 || d->K < 1 || d->M > kMost || d->N > kMost || d->K > kMost) return TAC_ERR_BAD_SHAPE;
   if (d->y_stride < d->N || !in_reach(d->M, d->y_stride)) return TAC_ERR_BAD_SHAPE;
+  if (d->K > TAC_PRODUCT_MAX_K) return TAC_ERR_UNSUPPORTED;
   return float_type(d->dtype) ? TAC_OK : TAC_ERR_BAD_PARAM;
 }
 

@@ -79,15 +79,37 @@ __global__ __launch_bounds__(256) void product_rows_kernel(const ProductParams p
 
 // ---- many rows ------------------------------------------------------------------------------------
 
+// 16 bytes a lane from a buffer into LDS at lds_base + 16 lane (addresses beyond the buffer are not read), and 4 bytes a lane from an address of its
+// own to lds_base + 4 lane.  `lanes`: all ones or zero, all of them or none, so that a load which is not wanted needs no branch; a branch would let the compiler move
+// the multiplications around it behind it.  Like lds_dma16 they are not known to the compiler: the reader waits (lds_dma_wait) in front of the barrier
+// that parts it from the loads.  All lanes of a wave run wherever these stand.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void lds_dma_rows(uint32_t offset, u32x4_t buffer, uint32_t lds_base, uint32_t lanes) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds\n\ts_mov_b64 exec, -1"
+               :: "v"(offset), "s"(buffer), "s"(lds_base), "s"(lanes) : "m0", "memory");
+}
+__device__ __forceinline__ void lds_dma_dword(const void* from, uint32_t lds_base, uint32_t lanes) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_mov_b32 exec_lo, %2\n\ts_mov_b32 exec_hi, %2\n\tglobal_load_lds_dword %0, off\n\ts_mov_b64 exec, -1"
+               :: "v"(from), "s"(lds_base), "s"(lanes) : "m0", "memory");
+}
+#pragma clang diagnostic pop
+
+// a buffer of `bytes` bytes (at most 2^32 - 1 are asked for) from `at` on
+__device__ __forceinline__ u32x4_t buffer_at(uint64_t at, int64_t bytes) {
+  return u32x4_t{(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, (uint32_t)bytes, 0x00020000u};
+}
+
 // Tiles of TM rows of a x TN rows of b, WM x WN waves.  One block of 128 columns of the tile's rows (128 bytes each) is a stage in LDS; two stages:
-// while the waves multiply one, direct-to-LDS loads fill the other, and one barrier a block parts them.  A row's eight pieces of 16
+// while the waves multiply one, direct-to-LDS loads fill the other.  Fragments are read two steps ahead of their use, across blocks too: the one
+// barrier a block stands two steps before its end, where all of the stage has been read and the next one is there.  A row's eight pieces of 16
 // bytes stand at their number XOR bits 1 to 3 of the row, so that the 16 rows that a fragment read takes at once fall into different
 // banks.  blockIdx.y: the part of the columns where those are shared (`partial`, float32 [part][M][N]).
 template <int TM, int TN, int WM, int WN, bool EXACT, typename T>
-__global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(const ProductParams p, int parts) {
+__global__ __launch_bounds__(64 * WM * WN, 2) void product_tile_kernel(const ProductParams p, int parts) {
   constexpr int kWaves = WM * WN, FM = TM / WM / 32, FN = TN / WN / 32, kStage = (TM + TN) * kBlock;
-  constexpr int kLoads = (TM + TN) / 8 / kWaves;         // a load instruction brings 8 rows
-  static_assert(TM % (32 * WM) == 0 && TN % (32 * WN) == 0 && TM % 8 == 0 && (TM + TN) % (8 * kWaves) == 0);
+  constexpr int kLoadsM = TM / 8 / kWaves, kLoadsN = TN / 8 / kWaves;         // a load instruction brings 8 rows
+  static_assert(TM % (32 * WM) == 0 && TN % (32 * WN) == 0 && TM % (8 * kWaves) == 0 && TN % (8 * kWaves) == 0 && kWaves % 2 == 0);
   extern __shared__ __align__(1024) uint8_t stages[];    // two of them
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t pitch = code_pitch(p.K), spitch = scale_pitch(p.K);
@@ -104,30 +126,38 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(const Produc
   const int strip = tile / (4 * tiles_n), rows = min(4, tiles_m - 4 * strip), in = tile - strip * 4 * tiles_n;
   const int64_t m0 = (int64_t)(4 * strip + in % rows) * TM, n0 = (int64_t)(in / rows) * TN;
 
-  // rows beyond the matrices read the last one; what comes of them is not stored
-  const uint8_t* from[kLoads];
+  const uint32_t offset = (uint32_t)((8 * wave + lane / 8) * pitch) + 16 * ((lane % 8) ^ ((4 * wave + (lane >> 4)) & 7));
+  const uint32_t step = (uint32_t)(8 * kWaves * pitch);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)stages + wave * 1024;
+  // scale bytes of four blocks a row, in LDS behind the stages, also in two
+  static_assert(TM + TN == 64 * kWaves);
+  const int64_t scale_row = 64 * wave + lane;
+  const uint8_t* scales_from = scale_row < TM ? p.a_scales + min(m0 + scale_row, p.M - 1) * spitch : p.b_scales + min(n0 + scale_row - TM, p.N - 1) * spitch;
+  const uint32_t scales_to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)stages + 2 * kStage + wave * 256;
+  // the tile's rows of either matrix: the rows that are there, from their first byte (rows of at most 2^23 codes: 32-bit offsets)
+  const uint64_t am_at = (uint64_t)(uintptr_t)p.a + (uint64_t)(m0 * pitch), bn_at = (uint64_t)(uintptr_t)p.b + (uint64_t)(n0 * pitch);
+  const uint32_t am_bytes = (uint32_t)(min((int64_t)TM, p.M - m0) * pitch), bn_bytes = (uint32_t)(min((int64_t)TN, p.N - n0) * pitch);
+  auto load = [&](int k) {
+    const uint32_t lanes = __builtin_amdgcn_readfirstlane(k < last ? ~0u : 0u);
+    const uint32_t scale_lanes = __builtin_amdgcn_readfirstlane(k == first || k % 4 == 0 ? lanes : 0u);
+    const u32x4_t am = buffer_at(am_at + (uint32_t)k * kBlock, am_bytes - k * kBlock), bn = buffer_at(bn_at + (uint32_t)k * kBlock, bn_bytes - k * kBlock);
+    const uint32_t to = lds0 + ((k - first) & 1) * kStage;
 #pragma unroll
-  for (int j = 0; j < kLoads; ++j) {
-    const int r = 8 * (wave + j * kWaves) + lane / 8;
-    const uint8_t* row = r < TM ? p.a + min(m0 + r, p.M - 1) * pitch : p.b + min(n0 + r - TM, p.N - 1) * pitch;
-    from[j] = row + (int64_t)first * kBlock + 16 * ((lane % 8) ^ ((r >> 1) & 7));
-  }
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)stages;
-  auto load = [&](int stage) {
+    for (int j = 0; j < kLoadsM; ++j) lds_dma_rows(offset + j * step, am, to + j * kWaves * 1024, lanes);
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) {
-      lds_dma16<1, 0>(from[j], lds0 + stage * kStage + (wave + j * kWaves) * 1024);
-      from[j] += kBlock;
-    }
+    for (int j = 0; j < kLoadsN; ++j) lds_dma_rows(offset + j * step, bn, to + TM * kBlock + j * kWaves * 1024, lanes);
+    lds_dma_dword(scales_from + (k & ~3), scales_to + ((k >> 2) & 1) * (4 * (TM + TN)), scale_lanes);
   };
 
   const int wm = wave % WM, wn = wave / WM;
-  const uint8_t *sm[FM], *sn[FN];
+  uint32_t em[FM], en[FN];                                // scale bytes of the block in hand
+  auto fetch_scales = [&](int k, uint32_t (&m)[FM], uint32_t (&n)[FN]) {
+    const uint8_t* at = stages + 2 * kStage + ((k >> 2) & 1) * (4 * (TM + TN)) + (k & 3) + 4 * (lane % 32);
 #pragma unroll
-  for (int f = 0; f < FM; ++f) sm[f] = p.a_scales + min(m0 + (wm * FM + f) * 32 + lane % 32, p.M - 1) * spitch;
+    for (int f = 0; f < FM; ++f) m[f] = at[(wm * FM + f) * 128];
 #pragma unroll
-  for (int f = 0; f < FN; ++f) sn[f] = p.b_scales + min(n0 + (wn * FN + f) * 32 + lane % 32, p.N - 1) * spitch;
-  uint32_t em[FM], en[FN];                                // scale bytes of four blocks, the current one lowest
+    for (int f = 0; f < FN; ++f) n[f] = at[4 * TM + (wn * FN + f) * 128];
+  };
 
   f32x16_t sum[FN][FM];
 #pragma unroll
@@ -137,56 +167,76 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(const Produc
 #pragma unroll
       for (int e = 0; e < 16; ++e) sum[i][j][e] = 0.0f;
 
-  load(0);
-  for (int k = first; k < last; ++k) {
-    const int stage = (k - first) & 1;
-    if (k == first || k % 4 == 0) {
-#pragma unroll
-      for (int f = 0; f < FM; ++f) em[f] = *reinterpret_cast<const uint32_t*>(sm[f] + (k & ~3)) >> (8 * (k & 3));
-#pragma unroll
-      for (int f = 0; f < FN; ++f) en[f] = *reinterpret_cast<const uint32_t*>(sn[f] + (k & ~3)) >> (8 * (k & 3));
-    }
-    lds_dma_wait();
-    __syncthreads();
-    if (k + 1 < last) load(stage ^ 1);
-    const uint8_t *am = stages + stage * kStage + wm * FM * 32 * kBlock, *bn = stages + stage * kStage + (TM + wn * FN * 32) * kBlock;
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {                // 64 columns an instruction
-      const int c = 4 * half + 2 * (lane / 32), x = (lane >> 1) & 7, row = (lane % 32) * kBlock;
-      const int lo = row + 16 * (c ^ x), hi = row + 16 * ((c + 1) ^ x);
-      i32x8_t a[FM], b[FN];
+  // A block is kSteps steps, each a fragment of b against all of the wave's fragments of a; every step first reads what the step after next needs.
+  constexpr int kSteps = 2 * FN;
+  static_assert(kSteps % 4 == 0);
+  i32x8_t a[2][FM], b[4];
+  bf16x8_t wide[EXACT ? FM : 1][4];
+  const int x = (lane >> 1) & 7, at_m = (wm * FM * 32 + lane % 32) * kBlock, at_n = (TM + wn * FN * 32 + lane % 32) * kBlock;
+  const int piece[2][2] = {{16 * ((2 * (lane / 32)) ^ x), 16 * ((2 * (lane / 32) + 1) ^ x)},
+                           {16 * ((2 * (lane / 32) + 4) ^ x), 16 * ((2 * (lane / 32) + 5) ^ x)}};
+  auto fetch = [&](const uint8_t* at, auto step_number) {
+    constexpr int S = decltype(step_number)::value, H = S / FN, I = S % FN;
+    if constexpr (I == 0) {
 #pragma unroll
       for (int f = 0; f < FM; ++f)
-        a[f] = join_codes(*reinterpret_cast<const u32x4_t*>(am + f * 32 * kBlock + lo), *reinterpret_cast<const u32x4_t*>(am + f * 32 * kBlock + hi));
-#pragma unroll
-      for (int f = 0; f < FN; ++f)
-        b[f] = join_codes(*reinterpret_cast<const u32x4_t*>(bn + f * 32 * kBlock + lo), *reinterpret_cast<const u32x4_t*>(bn + f * 32 * kBlock + hi));
+        a[H][f] = join_codes(*reinterpret_cast<const u32x4_t*>(at + at_m + f * 32 * kBlock + piece[H][0]),
+                             *reinterpret_cast<const u32x4_t*>(at + at_m + f * 32 * kBlock + piece[H][1]));
+    }
+    b[S % 4] = join_codes(*reinterpret_cast<const u32x4_t*>(at + at_n + I * 32 * kBlock + piece[H][0]),
+                          *reinterpret_cast<const u32x4_t*>(at + at_n + I * 32 * kBlock + piece[H][1]));
+  };
+
+  auto block = [&](int k, auto more) {
+    const uint8_t *here = stages + ((k - first) & 1) * kStage, *there = stages + ((k - first + 1) & 1) * kStage;
+    uint32_t next_m[FM], next_n[FN];
+    static_for<0, kSteps>([&](auto step_number) {
+      constexpr int S = decltype(step_number)::value, H = S / FN, I = S % FN;
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (S == kSteps - 2 && decltype(more)::value) {          // all of this stage has been read: it becomes the one after next
+        lds_dma_wait();
+        __syncthreads();
+        load(k + 2);
+        fetch_scales(k + 1, next_m, next_n);
+      }
+      if constexpr (S < kSteps - 2) fetch(here, std::integral_constant<int, (S + 2) % kSteps>());
+      else if constexpr (decltype(more)::value) fetch(there, std::integral_constant<int, (S + 2) % kSteps>());
       if constexpr (EXACT) {
+        if constexpr (I == 0) {
+#pragma unroll
+          for (int f = 0; f < FM; ++f)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) wide[f][q] = widen(a[H][f], q, scale_value(em[f]));
+        }
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          bf16x8_t av[FM];
+          const bf16x8_t bv = widen(b[S % 4], q, scale_value(en[I]));
 #pragma unroll
-          for (int f = 0; f < FM; ++f) av[f] = widen(a[f], q, scale_value(em[f] & 255u));
-#pragma unroll
-          for (int i = 0; i < FN; ++i) {
-            const bf16x8_t bv = widen(b[i], q, scale_value(en[i] & 255u));
-#pragma unroll
-            for (int j = 0; j < FM; ++j) sum[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bv, av[j], sum[i][j], 0, 0, 0);
-          }
+          for (int j = 0; j < FM; ++j) sum[I][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bv, wide[j][q], sum[I][j], 0, 0, 0);
         }
       } else {
 #pragma unroll
-        for (int i = 0; i < FN; ++i)
-#pragma unroll
-          for (int j = 0; j < FM; ++j)
-            sum[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b[i], a[j], sum[i][j], 0, 0, 0, (int)en[i], 0, (int)em[j]);
+        for (int j = 0; j < FM; ++j)
+          sum[I][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b[S % 4], a[H][j], sum[I][j], 0, 0, 0, (int)en[I], 0, (int)em[j]);
       }
+    });
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (decltype(more)::value) {
+#pragma unroll
+      for (int f = 0; f < FM; ++f) em[f] = next_m[f];
+#pragma unroll
+      for (int f = 0; f < FN; ++f) en[f] = next_n[f];
     }
-#pragma unroll
-    for (int f = 0; f < FM; ++f) em[f] >>= 8;
-#pragma unroll
-    for (int f = 0; f < FN; ++f) en[f] >>= 8;
-  }
+  };
+  load(first);
+  lds_dma_wait();
+  __syncthreads();
+  load(first + 1);
+  fetch_scales(first, em, en);
+  fetch(stages, std::integral_constant<int, 0>());
+  fetch(stages, std::integral_constant<int, 1>());
+  for (int k = first; k + 1 < last; ++k) block(k, std::true_type());
+  block(last - 1, std::false_type());
 
   // element e of a lane: n = 8 (e / 4) + 4 (lane / 32) + e % 4, m = lane % 32
 #pragma unroll
@@ -225,7 +275,7 @@ template <int TM, int TN, int WM, int WN, typename T>
 hipError_t tile_launch(const ProductParams& p, int parts, hipStream_t s) {
   const int64_t tiles = ((p.M + TM - 1) / TM) * ((p.N + TN - 1) / TN);
   auto* kernel = product_tile_kernel<TM, TN, WM, WN, sizeof(T) == 4, T>;
-  constexpr int lds = 2 * (TM + TN) * kBlock;
+  constexpr int lds = 2 * (TM + TN) * (kBlock + 4);
   static const hipError_t room = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (room != hipSuccess) return room;
   hipLaunchKernelGGL(kernel, dim3((unsigned)tiles, (unsigned)parts), dim3(64 * WM * WN), lds, s, p, parts);
