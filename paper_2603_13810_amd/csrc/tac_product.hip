@@ -97,62 +97,82 @@ __device__ __forceinline__ void lds_dma_dword(const void* from, uint32_t lds_bas
 
 // a buffer of `bytes` bytes (at most 2^32 - 1 are asked for) from `at` on
 __device__ __forceinline__ u32x4_t buffer_at(uint64_t at, int64_t bytes) {
-  return u32x4_t{(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, (uint32_t)bytes, 0x00020000u};
+  return u32x4_t{(uint32_t)__builtin_amdgcn_readfirstlane((int)at), (uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32)) & 0xffffu,
+                 (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), 0x00020000u};
 }
+
+// LDS of the kernel below: two stages, of which the second's place also takes the results on their way out (32 rows of up to 256 bytes and 16 for each
+// wave), then two sets of scale bytes of four blocks.
+constexpr int tile_scales_at(int TM, int TN, int waves) {
+  const int stage = (TM + TN) * kBlock, out = waves * 32 * (256 + 16);
+  return stage + (stage > out ? stage : out);
+}
+constexpr int tile_lds(int TM, int TN, int waves) { return tile_scales_at(TM, TN, waves) + 8 * (TM + TN); }
 
 // Tiles of TM rows of a x TN rows of b, WM x WN waves.  One block of 128 columns of the tile's rows (128 bytes each) is a stage in LDS; two stages:
 // while the waves multiply one, direct-to-LDS loads fill the other.  Fragments are read two steps ahead of their use, across blocks too: the one
 // barrier a block stands two steps before its end, where all of the stage has been read and the next one is there.  A row's eight pieces of 16
 // bytes stand at their number XOR bits 1 to 3 of the row, so that the 16 rows that a fragment read takes at once fall into different
-// banks.  blockIdx.y: the part of the columns where those are shared (`partial`, float32 [part][M][N]).
-template <int TM, int TN, int WM, int WN, bool EXACT, typename T>
+// banks.  A workgroup takes items (a tile, or one of `parts` parts of a tile's columns, whose results are [part][M][N]) until there are
+// none, and has the next item's first block on its way while it writes the results of the one before: they are turned through LDS, so that
+// rows leave in pieces of 256 bytes.
+template <int TM, int TN, int WM, int WN, bool EXACT, typename U>
 __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile_kernel(const ProductParams p, int parts) {
   constexpr int kWaves = WM * WN, FM = TM / WM / 32, FN = TN / WN / 32, kStage = (TM + TN) * kBlock;
   constexpr int kLoadsM = TM / 8 / kWaves, kLoadsN = TN / 8 / kWaves;         // a load instruction brings 8 rows
   static_assert(TM % (32 * WM) == 0 && TN % (32 * WN) == 0 && TM % (8 * kWaves) == 0 && TN % (8 * kWaves) == 0 && kWaves % 2 == 0);
-  extern __shared__ __align__(1024) uint8_t stages[];    // two of them
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  static_assert(TM + TN == 64 * kWaves);
+  constexpr int kScales = tile_scales_at(TM, TN, kWaves);
+  extern __shared__ __align__(1024) uint8_t stages[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave % WM, wn = wave / WM;
   const int64_t pitch = code_pitch(p.K), spitch = scale_pitch(p.K);
   const int blocks = (int)(pitch / kBlock);
-  const int first = (int)((int64_t)blocks * blockIdx.y / parts), last = (int)((int64_t)blocks * (blockIdx.y + 1) / parts);
-  // Workgroups i, i + 8, i + 16 ... run on one of the eight dies, which have an L2 each: a die takes consecutive tiles, in strips of four tile rows of a,
-  // so that the tiles that it has in hand at a time share their rows.
-  const int tiles_m = (int)((p.M + TM - 1) / TM), tiles_n = (int)((p.N + TN - 1) / TN), tiles = tiles_m * tiles_n;
-  int tile = blockIdx.x;
-  {
-    const int die = tile % 8, at = tile / 8, whole = tiles / 8, more = tiles % 8;
-    tile = die * whole + min(die, more) + at;
-  }
-  const int strip = tile / (4 * tiles_n), rows = min(4, tiles_m - 4 * strip), in = tile - strip * 4 * tiles_n;
-  const int64_t m0 = (int64_t)(4 * strip + in % rows) * TM, n0 = (int64_t)(in / rows) * TN;
+  const int tiles_m = (int)((p.M + TM - 1) / TM), tiles_n = (int)((p.N + TN - 1) / TN), items = tiles_m * tiles_n * parts;
+
+  // the item in hand: its rows and blocks of columns
+  int64_t m0, n0;
+  int part, first, last;
+  uint64_t am_at, bn_at;             // the tile's rows of either matrix: those that are there, from their first byte (rows of at most
+  uint32_t am_bytes, bn_bytes;       // 2^23 codes: 32-bit offsets)
+  const uint8_t* scales_from;        // a lane brings one row's scales; rows beyond the matrices take the last one's, what comes of them is not stored
+  auto take = [&](int item) {
+    // Workgroups i, i + 8, i + 16 ... run on one of the eight dies, which have an L2 each: a die takes consecutive tiles, in strips of four tile
+    // rows of a, so that the tiles that it has in hand at a time share their rows.
+    const int die = item % 8, at = item / 8, whole = items / 8, more = items % 8;
+    item = die * whole + min(die, more) + at;
+    part = item / (tiles_m * tiles_n);
+    const int tile = item - part * (tiles_m * tiles_n);
+    const int strip = tile / (4 * tiles_n), rows = min(4, tiles_m - 4 * strip), in = tile - strip * 4 * tiles_n;
+    m0 = (int64_t)(4 * strip + in % rows) * TM;
+    n0 = (int64_t)(in / rows) * TN;
+    first = (int)((int64_t)blocks * part / parts);
+    last = (int)((int64_t)blocks * (part + 1) / parts);
+    am_at = (uint64_t)(uintptr_t)p.a + (uint64_t)(m0 * pitch);
+    bn_at = (uint64_t)(uintptr_t)p.b + (uint64_t)(n0 * pitch);
+    am_bytes = (uint32_t)(min((int64_t)TM, p.M - m0) * pitch);
+    bn_bytes = (uint32_t)(min((int64_t)TN, p.N - n0) * pitch);
+    const int64_t row = 64 * wave + lane;
+    scales_from = row < TM ? p.a_scales + min(m0 + row, p.M - 1) * spitch : p.b_scales + min(n0 + row - TM, p.N - 1) * spitch;
+  };
 
   const uint32_t offset = (uint32_t)((8 * wave + lane / 8) * pitch) + 16 * ((lane % 8) ^ ((4 * wave + (lane >> 4)) & 7));
   const uint32_t step = (uint32_t)(8 * kWaves * pitch);
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)stages + wave * 1024;
-  // scale bytes of four blocks a row, in LDS behind the stages, also in two
-  static_assert(TM + TN == 64 * kWaves);
-  const int64_t scale_row = 64 * wave + lane;
-  const uint8_t* scales_from = scale_row < TM ? p.a_scales + min(m0 + scale_row, p.M - 1) * spitch : p.b_scales + min(n0 + scale_row - TM, p.N - 1) * spitch;
-  const uint32_t scales_to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)stages + 2 * kStage + wave * 256;
-  // the tile's rows of either matrix: the rows that are there, from their first byte (rows of at most 2^23 codes: 32-bit offsets)
-  const uint64_t am_at = (uint64_t)(uintptr_t)p.a + (uint64_t)(m0 * pitch), bn_at = (uint64_t)(uintptr_t)p.b + (uint64_t)(n0 * pitch);
-  const uint32_t am_bytes = (uint32_t)(min((int64_t)TM, p.M - m0) * pitch), bn_bytes = (uint32_t)(min((int64_t)TN, p.N - n0) * pitch);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)stages;
   auto load = [&](int k) {
     const uint32_t lanes = __builtin_amdgcn_readfirstlane(k < last ? ~0u : 0u);
     const uint32_t scale_lanes = __builtin_amdgcn_readfirstlane(k == first || k % 4 == 0 ? lanes : 0u);
     const u32x4_t am = buffer_at(am_at + (uint32_t)k * kBlock, am_bytes - k * kBlock), bn = buffer_at(bn_at + (uint32_t)k * kBlock, bn_bytes - k * kBlock);
-    const uint32_t to = lds0 + ((k - first) & 1) * kStage;
+    const uint32_t to = lds0 + wave * 1024 + ((k - first) & 1) * kStage;
 #pragma unroll
     for (int j = 0; j < kLoadsM; ++j) lds_dma_rows(offset + j * step, am, to + j * kWaves * 1024, lanes);
 #pragma unroll
     for (int j = 0; j < kLoadsN; ++j) lds_dma_rows(offset + j * step, bn, to + TM * kBlock + j * kWaves * 1024, lanes);
-    lds_dma_dword(scales_from + (k & ~3), scales_to + ((k >> 2) & 1) * (4 * (TM + TN)), scale_lanes);
+    lds_dma_dword(scales_from + (k & ~3), lds0 + kScales + wave * 256 + ((k >> 2) & 1) * (4 * (TM + TN)), scale_lanes);
   };
 
-  const int wm = wave % WM, wn = wave / WM;
   uint32_t em[FM], en[FN];                                // scale bytes of the block in hand
   auto fetch_scales = [&](int k, uint32_t (&m)[FM], uint32_t (&n)[FN]) {
-    const uint8_t* at = stages + 2 * kStage + ((k >> 2) & 1) * (4 * (TM + TN)) + (k & 3) + 4 * (lane % 32);
+    const uint8_t* at = stages + kScales + ((k >> 2) & 1) * (4 * (TM + TN)) + (k & 3) + 4 * (lane % 32);
 #pragma unroll
     for (int f = 0; f < FM; ++f) m[f] = at[(wm * FM + f) * 128];
 #pragma unroll
@@ -160,12 +180,6 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile_kernel(const Pro
   };
 
   f32x16_t sum[FN][FM];
-#pragma unroll
-  for (int i = 0; i < FN; ++i)
-#pragma unroll
-    for (int j = 0; j < FM; ++j)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) sum[i][j][e] = 0.0f;
 
   // A block is kSteps steps, each a fragment of b against all of the wave's fragments of a; every step first reads what the step after next needs.
   constexpr int kSteps = 2 * FN;
@@ -228,57 +242,100 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile_kernel(const Pro
       for (int f = 0; f < FN; ++f) en[f] = next_n[f];
     }
   };
-  load(first);
-  lds_dma_wait();
-  __syncthreads();
-  load(first + 1);
-  fetch_scales(first, em, en);
-  fetch(stages, std::integral_constant<int, 0>());
-  fetch(stages, std::integral_constant<int, 1>());
-  for (int k = first; k + 1 < last; ++k) block(k, std::true_type());
-  block(last - 1, std::false_type());
-
-  // element e of a lane: n = 8 (e / 4) + 4 (lane / 32) + e % 4, m = lane % 32
-#pragma unroll
-  for (int j = 0; j < FM; ++j) {
-    const int64_t m = m0 + (wm * FM + j) * 32 + lane % 32;
-    if (m >= p.M) continue;
-#pragma unroll
-    for (int i = 0; i < FN; ++i)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int64_t n = n0 + (wn * FN + i) * 32 + 8 * q + 4 * (lane / 32);
-        if (n >= p.N) continue;
+  // Results of 32 m x 32 FN n through the wave's own piece of LDS: element e of a lane is n = 8 (e / 4) + 4 (lane / 32) + e % 4, m = lane % 32.
+  auto store_rows = [&](int64_t mw, int64_t nw, U* y, auto fragment) {
+    constexpr int J = decltype(fragment)::value;
+    constexpr int kPerPass = sizeof(U) == 4 ? (FN + 1) / 2 : FN;                    // fragments that fit
+    constexpr int kRow = kPerPass * 32 * (int)sizeof(U) + 16, kPieces = kPerPass * 32 * (int)sizeof(U) / 16, kIn = 16 / (int)sizeof(U);
+    static_assert(kRow <= 256 + 16 && 64 % kPieces == 0);
+    uint8_t* room = stages + kStage + wave * (32 * kRow);
+    const int rows_left = (int)min(p.M - mw, (int64_t)32), cols_left = (int)min(p.N - nw, (int64_t)(32 * FN));
+    if (rows_left <= 0 || cols_left <= 0) return;
+    // columns beyond the matrix read zeros
+    const auto bias = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(p.bias + (p.bias ? nw : 0)), 0, 4 * cols_left, 0x00020000);
+    static_for<0, FN / kPerPass>([&](auto pass) {
+      constexpr int I0 = decltype(pass)::value * kPerPass;
+      __builtin_amdgcn_sched_barrier(0);
+      static_for<0, kPerPass * 4>([&](auto quarter) {
+        constexpr int I = I0 + decltype(quarter)::value / 4, Q = decltype(quarter)::value % 4;
         float v[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = sum[i][j][4 * q + e];
-        if (parts > 1) {
-          float* to = p.partial + ((int64_t)blockIdx.y * p.M + m) * p.N + n;
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (n + e < p.N) to[e] = v[e];
-          continue;
-        }
+        for (int e = 0; e < 4; ++e) v[e] = sum[I][J][4 * Q + e];
         if (p.bias) {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (n + e < p.N) v[e] += p.bias[n + e];
+            v[e] += bits_float((uint32_t)__builtin_amdgcn_raw_buffer_load_b32(bias, 16 * (lane / 32) + 4 * (32 * I + 8 * Q + e), 0, 0));
         }
-        T* to = (T*)p.y + m * p.y_stride + n;
-        if (p.wide_stores && n + 4 <= p.N) store_floats<T, 4, true>(to, 4, v);
-        else store_floats<T, 4, false>(to, p.N - n, v);
+        store_floats<U, 4, true>(reinterpret_cast<U*>(room + (lane % 32) * kRow) + 32 * (I - I0) + 8 * Q + 4 * (lane / 32), 4, v);
+      });
+      __builtin_amdgcn_sched_barrier(0);
+      const int piece = lane % kPieces, left = cols_left - 32 * I0 - kIn * piece;
+      int row = lane / kPieces;
+      U* to = y + (mw + row) * p.y_stride + nw + 32 * I0 + kIn * piece;
+      const uint8_t* from = room + row * kRow + 16 * piece;
+      if (p.wide_stores && cols_left == 32 * FN && rows_left == 32) {
+#pragma unroll 4
+        for (int r = 0; r < 32 * kPieces / 64; ++r) {
+          *reinterpret_cast<u32x4_t*>(to) = *reinterpret_cast<const u32x4_t*>(from);
+          to += (64 / kPieces) * p.y_stride;
+          from += (64 / kPieces) * kRow;
+        }
+      } else {
+#pragma unroll 1
+        for (; row < rows_left; row += 64 / kPieces) {
+          if (p.wide_stores && left >= kIn) {
+            *reinterpret_cast<u32x4_t*>(to) = *reinterpret_cast<const u32x4_t*>(from);
+          } else {
+#pragma unroll 1
+            for (int e = 0; e < min(kIn, left); ++e) to[e] = reinterpret_cast<const U*>(from)[e];
+          }
+          to += (64 / kPieces) * p.y_stride;
+          from += (64 / kPieces) * kRow;
+        }
       }
+    });
+  };
+
+  int item = blockIdx.x;
+  take(item);
+  load(first);
+  while (true) {
+#pragma unroll
+    for (int i = 0; i < FN; ++i)
+#pragma unroll
+      for (int j = 0; j < FM; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sum[i][j][e] = 0.0f;
+    lds_dma_wait();
+    __syncthreads();
+    load(first + 1);
+    fetch_scales(first, em, en);
+    fetch(stages, std::integral_constant<int, 0>());
+    fetch(stages, std::integral_constant<int, 1>());
+    for (int k = first; k + 1 < last; ++k) block(k, std::true_type());
+    block(last - 1, std::false_type());
+    __syncthreads();                                      // both stages have been read
+    const int64_t mw = m0 + wm * FM * 32, nw = n0 + wn * FN * 32;
+    U* y = (U*)p.y + (int64_t)part * p.M * p.N;
+    item += gridDim.x;
+    if (item < items) {
+      take(item);
+      load(first);
+    }
+    static_for<0, FM>([&](auto j) { store_rows(mw + 32 * decltype(j)::value, nw, y, j); });
+    if (item >= items) return;
   }
 }
 
 template <int TM, int TN, int WM, int WN, typename T>
 hipError_t tile_launch(const ProductParams& p, int parts, hipStream_t s) {
-  const int64_t tiles = ((p.M + TM - 1) / TM) * ((p.N + TN - 1) / TN);
+  const int64_t items = ((p.M + TM - 1) / TM) * ((p.N + TN - 1) / TN) * parts;
+  constexpr int kAtOnce = kFittedUnits * (TM + TN <= 256 ? 2 : 1);       // workgroups that the LDS holds
   auto* kernel = product_tile_kernel<TM, TN, WM, WN, sizeof(T) == 4, T>;
-  constexpr int lds = 2 * (TM + TN) * (kBlock + 4);
+  constexpr int lds = tile_lds(TM, TN, WM * WN);
   static const hipError_t room = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (room != hipSuccess) return room;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)tiles, (unsigned)parts), dim3(64 * WM * WN), lds, s, p, parts);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(items < kAtOnce ? items : kAtOnce)), dim3(64 * WM * WN), lds, s, p, parts);
   return hipGetLastError();
 }
 
@@ -288,8 +345,7 @@ size_t product_workspace(int64_t, int64_t, int64_t) { return 0; }
 
 hipError_t product_launch(const ProductParams& given, hipStream_t s) {
   ProductParams p = given;
-  p.wide_stores = rows_aligned(p.y, p.y_stride, p.bf16 ? 2 : 4) ||
-                  (p.bf16 && (((uintptr_t)p.y | (uintptr_t)(p.y_stride * 2)) & 7u) == 0);
+  p.wide_stores = rows_aligned(p.y, p.y_stride, p.bf16 ? 2 : 4);
   if (p.M > 64 && p.N > 64) {
     if (p.M > 128 && p.N > 128) return p.bf16 ? tile_launch<256, 256, 4, 2, bf16>(p, 1, s) : tile_launch<256, 256, 4, 2, float>(p, 1, s);
     return p.bf16 ? tile_launch<128, 128, 2, 2, bf16>(p, 1, s) : tile_launch<128, 128, 2, 2, float>(p, 1, s);
