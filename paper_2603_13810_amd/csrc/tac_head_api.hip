@@ -130,7 +130,7 @@ static int check_product(const tac_product_desc_t* d) {
 }
 
 size_t tac_scaled_product_workspace_bytes(const tac_product_desc_t* d) {
-  return check_product(d) ? 0 : tac::product_workspace(d->M, d->N, d->K);
+  return check_product(d) ? 0 : tac::product_workspace(d->M, d->N, d->K, d->dtype == TAC_BF16);
 }
 
 int tac_scaled_product(const tac_product_desc_t* d, const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes,
@@ -138,7 +138,7 @@ int tac_scaled_product(const tac_product_desc_t* d, const uint8_t* a_codes, cons
   const int rc = check_product(d);
   if (rc) return rc;
   if (!a_codes || !a_scales || !b_codes || !b_scales || !y) return TAC_ERR_NULL;
-  if (!workspace && tac::product_workspace(d->M, d->N, d->K)) return TAC_ERR_NULL;
+  if (!workspace && tac::product_workspace(d->M, d->N, d->K, d->dtype == TAC_BF16)) return TAC_ERR_NULL;
   if (misaligned(a_codes, 16) || misaligned(b_codes, 16) || misaligned(a_scales, 4) || misaligned(b_scales, 4) ||
       misaligned(bias, 4) || misaligned(y, bytes_of(d->dtype)) || misaligned(workspace, 16))
     return TAC_ERR_ALIGN;

@@ -176,7 +176,7 @@ struct ProductParams {
   int bf16;
   int wide_stores;          // rows of y start at multiples of 16 bytes (set by product_launch)
 };
-size_t product_workspace(int64_t M, int64_t N, int64_t K);
+size_t product_workspace(int64_t M, int64_t N, int64_t K, int bf16);
 hipError_t product_launch(const ProductParams& p, hipStream_t s);
 
 struct ScanParams {

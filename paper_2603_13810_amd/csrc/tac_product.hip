@@ -1,15 +1,15 @@
 // Product of two 8-bit matrices with a power of two per 128 columns, on the matrix cores.
 //
-// v_mfma_scale_f32_{16x16x128,32x32x64}_f8f6f4 multiply 16 or 32 rows by as many over 128 or 64 columns and apply, per row and 32 columns, a power
-// of two that each lane passes in a byte: a block's scale costs no instruction of its own, and all blocks of a sum stay in one accumulator.
-// A lane holds 32 consecutive codes of one row.
+// v_mfma_scale_f32_32x32x64_f8f6f4 multiplies 32 rows by 32 rows over 64 columns and applies, per row and 32 columns, a power of two that each
+// lane passes in a byte: a block's scale costs no instruction of its own, and all blocks of a sum stay in one accumulator.  Lane l holds 32
+// consecutive codes of row l % 32.
 //
-// Those instructions add eight consecutive products at a time and keep only what reaches 2^-13 of the largest of them (measured: 2^16 and
+// That instruction adds eight consecutive products at a time and keep only what reaches 2^-13 of the largest of them (measured: 2^16 and
 // one smaller term; normal operands leave a relative error of 1.5e-5 in a sum, wide ones 7e-5).  A bfloat16 result rounds by 2^-8 and does not
 // notice; for a float32 result the codes are turned into bfloat16 in registers, exactly and with their scale (v_cvt_scalef32_pk_bf16_fp8),
-// and multiplied by v_mfma_f32_*_bf16, which keep float32 sums (1e-8), at half the rate.
+// and multiplied by v_mfma_f32_32x32x16_bf16, which keeps float32 sums (1e-8), at half the rate.
 //
-// The rows of b are the instructions' first operand: a lane then ends with four consecutive n of one m.
+// The rows of b are the instruction's first operand: a lane then ends with four consecutive n of one m.
 #include "tac_head_common.h"
 #include "tac_mfma_common.h"
 
@@ -25,9 +25,6 @@ typedef bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ i32x8_t join_codes(u32x4_t lo, u32x4_t hi) {
   return i32x8_t{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
 }
-__device__ __forceinline__ i32x8_t load_codes(const uint8_t* p) {
-  return join_codes(reinterpret_cast<const u32x4_t*>(p)[0], reinterpret_cast<const u32x4_t*>(p)[1]);
-}
 
 // the 8 q-th to 8 q + 7-th of 32 codes as bfloat16 times 2^e (its float in `scale`)
 __device__ __forceinline__ bf16x8_t widen(i32x8_t codes, int q, float scale) {
@@ -37,63 +34,25 @@ __device__ __forceinline__ bf16x8_t widen(i32x8_t codes, int q, float scale) {
   return bf16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// ---- few rows -------------------------------------------------------------------------------------
-
-template <bool EXACT>
-__device__ __forceinline__ f32x4_t multiply(i32x8_t a, i32x8_t b, f32x4_t c, uint32_t a_scale, uint32_t b_scale) {
-  if constexpr (!EXACT) {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, (int)a_scale, 0, (int)b_scale);
-  } else {
-    const float as = scale_value(a_scale), bs = scale_value(b_scale);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(a, q, as), widen(b, q, bs), c, 0, 0, 0);
-    return c;
-  }
-}
-
-// Four waves share 16 rows of b and 16 of a and take every fourth block of columns each; their sums are added up in LDS in a fixed order.
-template <typename T>
-__global__ __launch_bounds__(256) void product_rows_kernel(const ProductParams p) {
-  __shared__ f32x4_t room[4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t n0 = (int64_t)blockIdx.x * 16, m0 = (int64_t)blockIdx.y * 16;
-  const int64_t pitch = code_pitch(p.K), spitch = scale_pitch(p.K), blocks = pitch / kBlock;
-  // rows beyond the matrices read the last one; what comes of them is not stored
-  const int64_t n = min(n0 + lane % 16, p.N - 1), m = min(m0 + lane % 16, p.M - 1);
-  const uint8_t *bp = p.b + n * pitch + 32 * (lane / 16), *ap = p.a + m * pitch + 32 * (lane / 16);
-  f32x4_t sum = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int64_t k = wave; k < blocks; k += 4)
-    sum = multiply<sizeof(T) == 4>(load_codes(bp + k * kBlock), load_codes(ap + k * kBlock), sum, p.b_scales[n * spitch + k],
-                                   p.a_scales[m * spitch + k]);
-  room[wave][lane] = sum;
-  __syncthreads();
-  if (wave) return;
-  sum = (room[0][lane] + room[1][lane]) + (room[2][lane] + room[3][lane]);
-  if (m0 + lane % 16 >= p.M) return;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const int64_t at = n0 + 4 * (lane / 16) + e;
-    if (at < p.N) ((T*)p.y)[m * p.y_stride + at] = (T)(sum[e] + (p.bias ? p.bias[at] : 0.0f));
-  }
-}
-
-// ---- many rows ------------------------------------------------------------------------------------
-
-// 16 bytes a lane from a buffer into LDS at lds_base + 16 lane (addresses beyond the buffer are not read), and 4 bytes a lane from an address of its
-// own to lds_base + 4 lane.  `lanes`: all ones or zero, all of them or none, so that a load which is not wanted needs no branch; a branch would let the compiler move
-// the multiplications around it behind it.  Like lds_dma16 they are not known to the compiler: the reader waits (lds_dma_wait) in front of the barrier
-// that parts it from the loads.  All lanes of a wave run wherever these stand.
+// 16 bytes a lane from a buffer into LDS at lds_base + 16 lane, and 4 bytes a lane from an address of its own to lds_base + 4 lane.  Addresses beyond the
+// buffer are not read and bring zeros: a load that is not wanted has a buffer of no bytes, which takes no branch (a branch would let the compiler
+// move the multiplications around it behind it) and counts like the others.  Like lds_dma16 they are not known to the compiler: the reader
+// waits (dma_wait) in front of the barrier that parts it from the loads.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void lds_dma_rows(uint32_t offset, u32x4_t buffer, uint32_t lds_base, uint32_t lanes) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds\n\ts_mov_b64 exec, -1"
-               :: "v"(offset), "s"(buffer), "s"(lds_base), "s"(lanes) : "m0", "memory");
+__device__ __forceinline__ void lds_dma_rows(uint32_t offset, u32x4_t buffer, uint32_t lds_base) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" :: "v"(offset), "s"(buffer), "s"(lds_base) : "m0", "memory");
 }
-__device__ __forceinline__ void lds_dma_dword(const void* from, uint32_t lds_base, uint32_t lanes) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_mov_b32 exec_lo, %2\n\ts_mov_b32 exec_hi, %2\n\tglobal_load_lds_dword %0, off\n\ts_mov_b64 exec, -1"
-               :: "v"(from), "s"(lds_base), "s"(lanes) : "m0", "memory");
+__device__ __forceinline__ void lds_dma_dword(const void* from, uint32_t lds_base) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" :: "v"(from), "s"(lds_base) : "m0", "memory");
 }
 #pragma clang diagnostic pop
+// until all but the last N of the wave's loads have arrived
+template <int N>
+__device__ __forceinline__ void dma_wait() {
+  static_assert(N < 64);
+  __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4) << 14);
+}
 
 // a buffer of `bytes` bytes (at most 2^32 - 1 are asked for) from `at` on
 __device__ __forceinline__ u32x4_t buffer_at(uint64_t at, int64_t bytes) {
@@ -101,28 +60,28 @@ __device__ __forceinline__ u32x4_t buffer_at(uint64_t at, int64_t bytes) {
                  (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), 0x00020000u};
 }
 
-// LDS of the kernel below: two stages, of which the second's place also takes the results on their way out (32 rows of up to 256 bytes and 16 for each
-// wave), then two sets of scale bytes of four blocks.
-constexpr int tile_scales_at(int TM, int TN, int waves) {
+// LDS of the kernel below: STAGES stages of the tile's rows, of which the last one's place also takes the results on their way out (32 rows of up to
+// 256 bytes and 16 for each wave), then as many sets of scale bytes of four blocks.
+constexpr int tile_scales_at(int TM, int TN, int waves, int STAGES) {
   const int stage = (TM + TN) * kBlock, out = waves * 32 * (256 + 16);
-  return stage + (stage > out ? stage : out);
+  return (STAGES - 1) * stage + (stage > out ? stage : out);
 }
-constexpr int tile_lds(int TM, int TN, int waves) { return tile_scales_at(TM, TN, waves) + 8 * (TM + TN); }
+constexpr int tile_lds(int TM, int TN, int waves, int STAGES) { return tile_scales_at(TM, TN, waves, STAGES) + 4 * STAGES * (TM + TN); }
 
-// Tiles of TM rows of a x TN rows of b, WM x WN waves.  One block of 128 columns of the tile's rows (128 bytes each) is a stage in LDS; two stages:
-// while the waves multiply one, direct-to-LDS loads fill the other.  Fragments are read two steps ahead of their use, across blocks too: the one
+// Tiles of TM rows of a x TN rows of b, WM x WN waves.  One block of 128 columns of the tile's rows (128 bytes each) is a stage in LDS: while the waves
+// multiply one, direct-to-LDS loads fill the others.  Fragments are read two steps ahead of their use, across blocks too: the one
 // barrier a block stands two steps before its end, where all of the stage has been read and the next one is there.  A row's eight pieces of 16
 // bytes stand at their number XOR bits 1 to 3 of the row, so that the 16 rows that a fragment read takes at once fall into different
 // banks.  A workgroup takes items (a tile, or one of `parts` parts of a tile's columns, whose results are [part][M][N]) until there are
-// none, and has the next item's first block on its way while it writes the results of the one before: they are turned through LDS, so that
-// rows leave in pieces of 256 bytes.
-template <int TM, int TN, int WM, int WN, bool EXACT, typename U>
+// none, and has the next item's first blocks on their way while it writes the results of the one before: they are turned through LDS, so that
+// rows leave in pieces of up to 256 bytes.
+template <int TM, int TN, int WM, int WN, int STAGES, bool EXACT, typename U>
 __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile_kernel(const ProductParams p, int parts) {
   constexpr int kWaves = WM * WN, FM = TM / WM / 32, FN = TN / WN / 32, kStage = (TM + TN) * kBlock;
   constexpr int kLoadsM = TM / 8 / kWaves, kLoadsN = TN / 8 / kWaves;         // a load instruction brings 8 rows
   static_assert(TM % (32 * WM) == 0 && TN % (32 * WN) == 0 && TM % (8 * kWaves) == 0 && TN % (8 * kWaves) == 0 && kWaves % 2 == 0);
   static_assert(TM + TN == 64 * kWaves);
-  constexpr int kScales = tile_scales_at(TM, TN, kWaves);
+  constexpr int kScales = tile_scales_at(TM, TN, kWaves, STAGES), kLoads = kLoadsM + kLoadsN + 1;
   extern __shared__ __align__(1024) uint8_t stages[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave % WM, wn = wave / WM;
   const int64_t pitch = code_pitch(p.K), spitch = scale_pitch(p.K);
@@ -159,20 +118,20 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile_kernel(const Pro
   const uint32_t step = (uint32_t)(8 * kWaves * pitch);
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)stages;
   auto load = [&](int k) {
-    const uint32_t lanes = __builtin_amdgcn_readfirstlane(k < last ? ~0u : 0u);
-    const uint32_t scale_lanes = __builtin_amdgcn_readfirstlane(k == first || k % 4 == 0 ? lanes : 0u);
-    const u32x4_t am = buffer_at(am_at + (uint32_t)k * kBlock, am_bytes - k * kBlock), bn = buffer_at(bn_at + (uint32_t)k * kBlock, bn_bytes - k * kBlock);
-    const uint32_t to = lds0 + wave * 1024 + ((k - first) & 1) * kStage;
+    const int slot = (uint32_t)(k - first) % STAGES, at = min(k, last - 1);
+    const u32x4_t am = buffer_at(am_at + (uint32_t)at * kBlock, k < last ? am_bytes - at * kBlock : 0);
+    const u32x4_t bn = buffer_at(bn_at + (uint32_t)at * kBlock, k < last ? bn_bytes - at * kBlock : 0);
+    const uint32_t to = lds0 + wave * 1024 + slot * kStage;
 #pragma unroll
-    for (int j = 0; j < kLoadsM; ++j) lds_dma_rows(offset + j * step, am, to + j * kWaves * 1024, lanes);
+    for (int j = 0; j < kLoadsM; ++j) lds_dma_rows(offset + j * step, am, to + j * kWaves * 1024);
 #pragma unroll
-    for (int j = 0; j < kLoadsN; ++j) lds_dma_rows(offset + j * step, bn, to + TM * kBlock + j * kWaves * 1024, lanes);
-    lds_dma_dword(scales_from + (k & ~3), lds0 + kScales + wave * 256 + ((k >> 2) & 1) * (4 * (TM + TN)), scale_lanes);
+    for (int j = 0; j < kLoadsN; ++j) lds_dma_rows(offset + j * step, bn, to + TM * kBlock + j * kWaves * 1024);
+    lds_dma_dword(scales_from + (at & ~3), lds0 + kScales + slot * (4 * (TM + TN)) + wave * 256);
   };
 
   uint32_t em[FM], en[FN];                                // scale bytes of the block in hand
   auto fetch_scales = [&](int k, uint32_t (&m)[FM], uint32_t (&n)[FN]) {
-    const uint8_t* at = stages + kScales + ((k >> 2) & 1) * (4 * (TM + TN)) + (k & 3) + 4 * (lane % 32);
+    const uint8_t* at = stages + kScales + (uint32_t)(k - first) % STAGES * (4 * (TM + TN)) + (k & 3) + 4 * (lane % 32);
 #pragma unroll
     for (int f = 0; f < FM; ++f) m[f] = at[(wm * FM + f) * 128];
 #pragma unroll
@@ -202,15 +161,15 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile_kernel(const Pro
   };
 
   auto block = [&](int k, auto more) {
-    const uint8_t *here = stages + ((k - first) & 1) * kStage, *there = stages + ((k - first + 1) & 1) * kStage;
+    const uint8_t *here = stages + (uint32_t)(k - first) % STAGES * kStage, *there = stages + (uint32_t)(k - first + 1) % STAGES * kStage;
     uint32_t next_m[FM], next_n[FN];
     static_for<0, kSteps>([&](auto step_number) {
       constexpr int S = decltype(step_number)::value, H = S / FN, I = S % FN;
       __builtin_amdgcn_sched_barrier(0);
-      if constexpr (S == kSteps - 2 && decltype(more)::value) {          // all of this stage has been read: it becomes the one after next
-        lds_dma_wait();
+      if constexpr (S == kSteps - 2 && decltype(more)::value) {          // all of this stage has been read: its place takes the next block that is not on its way
+        dma_wait<(STAGES - 2) * kLoads>();
         __syncthreads();
-        load(k + 2);
+        load(k + STAGES);
         fetch_scales(k + 1, next_m, next_n);
       }
       if constexpr (S < kSteps - 2) fetch(here, std::integral_constant<int, (S + 2) % kSteps>());
@@ -248,7 +207,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile_kernel(const Pro
     constexpr int kPerPass = sizeof(U) == 4 ? (FN + 1) / 2 : FN;                    // fragments that fit
     constexpr int kRow = kPerPass * 32 * (int)sizeof(U) + 16, kPieces = kPerPass * 32 * (int)sizeof(U) / 16, kIn = 16 / (int)sizeof(U);
     static_assert(kRow <= 256 + 16 && 64 % kPieces == 0);
-    uint8_t* room = stages + kStage + wave * (32 * kRow);
+    uint8_t* room = stages + (STAGES - 1) * kStage + wave * (32 * kRow);
     const int rows_left = (int)min(p.M - mw, (int64_t)32), cols_left = (int)min(p.N - nw, (int64_t)(32 * FN));
     if (rows_left <= 0 || cols_left <= 0) return;
     // columns beyond the matrix read zeros
@@ -298,7 +257,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile_kernel(const Pro
 
   int item = blockIdx.x;
   take(item);
-  load(first);
+  for (int i = 0; i < STAGES - 1; ++i) load(first + i);
   while (true) {
 #pragma unroll
     for (int i = 0; i < FN; ++i)
@@ -306,63 +265,143 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile_kernel(const Pro
       for (int j = 0; j < FM; ++j)
 #pragma unroll
         for (int e = 0; e < 16; ++e) sum[i][j][e] = 0.0f;
-    lds_dma_wait();
+    dma_wait<0>();
     __syncthreads();
-    load(first + 1);
+    load(first + STAGES - 1);
     fetch_scales(first, em, en);
     fetch(stages, std::integral_constant<int, 0>());
     fetch(stages, std::integral_constant<int, 1>());
     for (int k = first; k + 1 < last; ++k) block(k, std::true_type());
     block(last - 1, std::false_type());
-    __syncthreads();                                      // both stages have been read
+    __syncthreads();                                      // all stages have been read
     const int64_t mw = m0 + wm * FM * 32, nw = n0 + wn * FN * 32;
     U* y = (U*)p.y + (int64_t)part * p.M * p.N;
     item += gridDim.x;
     if (item < items) {
       take(item);
-      load(first);
+      for (int i = 0; i < STAGES - 1; ++i) load(first + i);
     }
     static_for<0, FM>([&](auto j) { store_rows(mw + 32 * decltype(j)::value, nw, y, j); });
     if (item >= items) return;
   }
 }
 
-template <int TM, int TN, int WM, int WN, typename T>
+// `parts` > 1: float32 results of every part
+template <int TM, int TN, int WM, int WN, int STAGES, bool EXACT, typename U>
 hipError_t tile_launch(const ProductParams& p, int parts, hipStream_t s) {
   const int64_t items = ((p.M + TM - 1) / TM) * ((p.N + TN - 1) / TN) * parts;
-  constexpr int kAtOnce = kFittedUnits * (TM + TN <= 256 ? 2 : 1);       // workgroups that the LDS holds
-  auto* kernel = product_tile_kernel<TM, TN, WM, WN, sizeof(T) == 4, T>;
-  constexpr int lds = tile_lds(TM, TN, WM * WN);
+  auto* kernel = product_tile_kernel<TM, TN, WM, WN, STAGES, EXACT, U>;
+  constexpr int lds = tile_lds(TM, TN, WM * WN, STAGES);
+  constexpr int at_once = kFittedUnits * (lds <= 80 * 1024 ? 2 : 1);       // workgroups that the LDS holds
   static const hipError_t room = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (room != hipSuccess) return room;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(items < kAtOnce ? items : kAtOnce)), dim3(64 * WM * WN), lds, s, p, parts);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(items < at_once ? items : at_once)), dim3(64 * WM * WN), lds, s, p, parts);
   return hipGetLastError();
+}
+
+// sums of the parts, in their order; four n a thread where the rows allow it
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void join_kernel(const ProductParams p, int parts) {
+  constexpr int E = VEC ? 4 : 1;
+  const int64_t per_row = (p.N + E - 1) / E, all = p.M * per_row, step = (int64_t)gridDim.x * 256;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += step) {
+    const int64_t m = i / per_row, n = (i - m * per_row) * E;
+    float v[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = p.bias ? p.bias[n + e] : 0.0f;
+    for (int part = 0; part < parts; ++part) {
+      const float* from = p.partial + ((int64_t)part * p.M + m) * p.N + n;
+      if constexpr (VEC) {
+        const f32x4_t t = *reinterpret_cast<const f32x4_t*>(from);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += t[e];
+      } else {
+        v[0] += *from;
+      }
+    }
+    T* to = (T*)p.y + m * p.y_stride + n;
+    if constexpr (VEC) store_floats<T, 4, true>(to, 4, v);
+    else *to = (T)v[0];
+  }
+}
+
+template <int TM, int TN, int WM, int WN, int STAGES>
+hipError_t tiles(const ProductParams& p, int parts, hipStream_t s) {
+  if (parts == 1) return p.bf16 ? tile_launch<TM, TN, WM, WN, STAGES, false, bf16>(p, 1, s) : tile_launch<TM, TN, WM, WN, STAGES, true, float>(p, 1, s);
+  ProductParams q = p;
+  q.y = p.partial;
+  q.y_stride = p.N;
+  q.bias = nullptr;
+  q.wide_stores = p.N % 4 == 0;
+  const hipError_t e = p.bf16 ? tile_launch<TM, TN, WM, WN, STAGES, false, float>(q, parts, s) : tile_launch<TM, TN, WM, WN, STAGES, true, float>(q, parts, s);
+  if (e != hipSuccess) return e;
+  const bool vec = p.N % 4 == 0 && p.wide_stores;
+  const int64_t work = (p.M * ((p.N + 3) / 4) + 255) / 256;
+  const dim3 grid((unsigned)(work < 8192 ? work : 8192));
+  if (p.bf16 && vec) hipLaunchKernelGGL((join_kernel<bf16, true>), grid, dim3(256), 0, s, p, parts);
+  else if (p.bf16) hipLaunchKernelGGL((join_kernel<bf16, false>), grid, dim3(256), 0, s, p, parts);
+  else if (vec) hipLaunchKernelGGL((join_kernel<float, true>), grid, dim3(256), 0, s, p, parts);
+  else hipLaunchKernelGGL((join_kernel<float, false>), grid, dim3(256), 0, s, p, parts);
+  return hipGetLastError();
+}
+
+// The tile and the number of parts, by an estimate in microseconds: a launch, then for every round of workgroups a beginning and an end and the blocks
+// of columns of an item.  Fitted to products on 256 compute units, one and two workgroups to each (bfloat16 and float32 results):
+//   256 x 256, 2 stages  16384 x 8192 x 4096 459 us, 8192 x 8192 x 256 37;        float32 8192 x 4096 x 8192 408
+//   128 x 128, 4 stages  4096^3 84, 1024 x 4096 x 4096 23, 8192 x 8192 x 256 64;   float32 8192 x 4096 x 8192 540, 3200 x 500 x 3136 29
+//   128 x 128, 2 stages  4096^3 74, 1024 x 4096 x 4096 29, 8192 x 8192 x 256 41;   float32 8192 x 4096 x 8192 474, 3200 x 500 x 3136 28
+//   64 x 64, 4 stages    4096^3 125, 512 x 4096 x 4096 18, 256 x 4096 x 4096 13;   float32 8192 x 4096 x 8192 837, 3200 x 500 x 3136 26
+// Large tiles read less per product, small ones give more workgroups and shorter blocks.  Parts cost their sums' way through memory:
+// 128 x 3136 x 3200 float32 on tiles of 64 in one part 17 us, in two 14, in four 15; 16 x 8192 x 4096 12, 11, 11.
+struct Plan {
+  int tile, parts;
+};
+Plan plan_of(int64_t M, int64_t N, int64_t K, int bf) {
+  struct Tile {
+    int size, more;                  // more: two workgroups share a compute unit
+    double ends, block, block_shared;
+  };
+  static constexpr Tile kTiles[2][4] = {{{256, 0, 6.0, 3.05, 3.05}, {128, 0, 3.0, 1.02, 1.02}, {128, 1, 3.0, 1.0, 1.8}, {64, 1, 2.0, 0.58, 0.79}},
+                                        {{256, 0, 6.0, 1.6, 1.6}, {128, 0, 3.0, 0.56, 0.56}, {128, 1, 3.0, 0.7, 1.07}, {64, 1, 2.0, 0.3, 0.45}}};
+  const int64_t blocks = (K + kBlock - 1) / kBlock;
+  Plan best = {0, 1};
+  double least = 1e300;
+  for (int tile = 0; tile < 4; ++tile) {
+    const Tile& q = kTiles[bf != 0][tile];
+    const int64_t tiles = ((M + q.size - 1) / q.size) * ((N + q.size - 1) / q.size);
+    for (int parts : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
+      if (parts > 1 && (2 * parts > blocks || tiles * parts > 2 * kFittedUnits)) break;
+      const int64_t items = tiles * parts, each = (blocks + parts - 1) / parts, whole = kFittedUnits * (1 + q.more);
+      const int64_t rounds = items / whole, left = items % whole;
+      double us = (double)rounds * (q.ends + (double)each * q.block_shared);
+      if (left) us += q.ends + (double)each * (left > kFittedUnits ? q.block_shared : q.block);
+      if (parts > 1) us += 3.0 + (double)M * (double)N * (8.0 * parts + (bf ? 2.0 : 4.0)) / 4e6;
+      if (us < least) {
+        least = us;
+        best = Plan{tile, parts};
+      }
+    }
+  }
+  return best;
 }
 
 }  // namespace
 
-size_t product_workspace(int64_t, int64_t, int64_t) { return 0; }
+size_t product_workspace(int64_t M, int64_t N, int64_t K, int bf) {
+  const Plan plan = plan_of(M, N, K, bf);
+  return plan.parts > 1 ? (size_t)plan.parts * (size_t)M * (size_t)N * sizeof(float) : 0;
+}
 
 hipError_t product_launch(const ProductParams& given, hipStream_t s) {
   ProductParams p = given;
   p.wide_stores = rows_aligned(p.y, p.y_stride, p.bf16 ? 2 : 4);
-  if (p.M > 64 && p.N > 64) {
-    if (p.M > 128 && p.N > 128) return p.bf16 ? tile_launch<256, 256, 4, 2, bf16>(p, 1, s) : tile_launch<256, 256, 4, 2, float>(p, 1, s);
-    return p.bf16 ? tile_launch<128, 128, 2, 2, bf16>(p, 1, s) : tile_launch<128, 128, 2, 2, float>(p, 1, s);
+  const Plan plan = plan_of(p.M, p.N, p.K, p.bf16);
+  switch (plan.tile) {
+    case 0: return tiles<256, 256, 4, 2, 2>(p, plan.parts, s);
+    case 1: return tiles<128, 128, 2, 2, 4>(p, plan.parts, s);
+    case 2: return tiles<128, 128, 2, 2, 2>(p, plan.parts, s);
+    default: return tiles<64, 64, 2, 1, 4>(p, plan.parts, s);
   }
-  for (int64_t m = 0; m < p.M; m += 16 * 65535) {        // the grid's second axis ends at 65535
-    ProductParams q = p;
-    q.M = p.M - m < 16 * 65535 ? p.M - m : 16 * 65535;
-    q.a += m * code_pitch(p.K);
-    q.a_scales += m * scale_pitch(p.K);
-    q.y = (char*)p.y + m * p.y_stride * (p.bf16 ? 2 : 4);
-    const dim3 grid((unsigned)((p.N + 15) / 16), (unsigned)((q.M + 15) / 16));
-    if (p.bf16) hipLaunchKernelGGL(product_rows_kernel<bf16>, grid, dim3(256), 0, s, q);
-    else hipLaunchKernelGGL(product_rows_kernel<float>, grid, dim3(256), 0, s, q);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  return hipSuccess;
 }
 
 }  // namespace tac
