@@ -539,64 +539,72 @@ class tac_scan_desc_t(ctypes.Structure):
                 ("grad_stride_t", ctypes.c_int64), ("grad_stride_b", ctypes.c_int64), ("dtype", ctypes.c_int32)]
 
 
+_TYPES = None           # TAC_FP32 / TAC_BF16 of torch's types
+
+
 def _float_type(t, name) -> int:
-    import torch
-    if t.dtype == torch.bfloat16:
-        return TAC_BF16
-    if t.dtype == torch.float32:
-        return TAC_FP32
-    raise ValueError("%s must be float32 or bfloat16" % name)
+    global _TYPES
+    if _TYPES is None:
+        import torch
+        _TYPES = {torch.float32: TAC_FP32, torch.bfloat16: TAC_BF16}
+    try:
+        return _TYPES[t.dtype]
+    except KeyError:
+        raise ValueError("%s must be float32 or bfloat16" % name) from None
 
 
-def _view_ptr(t, like, name, shape=None):
-    """Address of a device tensor whose last axis is contiguous (any strides before it), of `like`'s type and `shape`."""
+# Small calls are bound by what happens here, so a tensor is looked at once: address and strides come from one check.
+def _rows_of(t, name, dtype, shape):
+    """Address and row stride of a device matrix of this type and shape whose rows are contiguous; (None, 0) for None."""
     if t is None:
-        return None
-    if not t.is_cuda or (t.stride(-1) != 1 and t.shape[-1] > 1):
-        raise ValueError("%s must be a device tensor with a contiguous last axis" % name)
-    if t.dtype != like.dtype:
-        raise ValueError("%s must have dtype %s" % (name, like.dtype))
-    if shape is not None and t.shape != shape:
-        raise ValueError("%s must be %s" % (name, list(shape)))
-    return t.data_ptr()
+        return None, 0
+    if t.shape != shape or t.dtype != dtype or not t.is_cuda:
+        raise ValueError("%s must be a device tensor %s of %s" % (name, list(shape), dtype))
+    stride = t.stride()
+    if stride[1] != 1 and shape[1] > 1:
+        raise ValueError("%s must have a contiguous last axis" % name)
+    return t.data_ptr(), stride[0] if shape[0] > 1 else shape[1]       # a matrix of one row has no stride that matters
 
 
-def _row_stride(t):
-    """Elements from row to row; a matrix of one row has none that matters."""
-    return 0 if t is None else t.stride(0) if t.shape[0] > 1 else t.shape[1]
+def _steps_of(t, name, dtype, shape):
+    """Address and strides of a device sequence [T, B, D] whose last axis is contiguous."""
+    if t.shape != shape or t.dtype != dtype or not t.is_cuda:
+        raise ValueError("%s must be a device tensor %s of %s" % (name, list(shape), dtype))
+    stride = t.stride()
+    if stride[2] != 1 and shape[2] > 1:
+        raise ValueError("%s must have a contiguous last axis" % name)
+    return t.data_ptr(), stride
 
 
 def _shaped(t, dtype, name, *shape):
+    """Address of a contiguous device tensor of this type and shape, or None."""
     if t is None:
         return None
-    if tuple(t.shape) != shape:
-        raise ValueError("%s must be %s" % (name, list(shape)))
-    return _dev_ptr(t, dtype, name)
+    if t.shape != shape or t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous device tensor %s of %s" % (name, list(shape), dtype))
+    return t.data_ptr()
 
 
-def _matrix(rows, cols, device):
-    """A new 8-bit matrix."""
+def _new_matrix(rows, cols, like):
+    """A new 8-bit matrix on `like`'s device."""
     import torch
-    return (torch.empty((rows, -(-cols // 128) * 128), dtype=torch.uint8, device=device),
-            torch.empty((rows, -(-cols // 512) * 4), dtype=torch.uint8, device=device))
+    return (like.new_empty((rows, -(-cols // 128) * 128), dtype=torch.uint8), like.new_empty((rows, -(-cols // 512) * 4), dtype=torch.uint8))
 
 
-def _matrix_ptrs(m, rows, cols, name):
+def _matrix_at(codes, scales, rows, cols, name):
     import torch
-    if m is None:
-        return None, None
-    return (_shaped(m[0], torch.uint8, name + " codes", rows, -(-cols // 128) * 128),
-            _shaped(m[1], torch.uint8, name + " scales", rows, -(-cols // 512) * 4))
+    return (_shaped(codes, torch.uint8, name + " codes", rows, -(-cols // 128) * 128),
+            _shaped(scales, torch.uint8, name + " scales", rows, -(-cols // 512) * 4))
 
 
-def _workspace(nbytes, device, stream):
+def _workspace(nbytes, like, stream):
     """Scratch for one call.  It is torch's again when the call has been enqueued, so a stream of the caller's own is told to torch's allocator."""
     import torch
     if not nbytes:
         return None
-    w = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    if stream is not None and int(stream) != torch.cuda.current_stream(device).cuda_stream:
-        w.record_stream(torch.cuda.ExternalStream(int(stream), device=device))
+    w = like.new_empty(nbytes, dtype=torch.uint8)
+    if stream is not None and int(stream) != torch.cuda.current_stream(like.device).cuda_stream:
+        w.record_stream(torch.cuda.ExternalStream(int(stream), device=like.device))
     return w
 
 
@@ -616,17 +624,17 @@ def tac_quantize(src, *, cols=None, tiles=False, rows=True, columns=False, strea
     t = src[0] if scaled else src
     if t.dim() != 2 or (scaled and cols is None):
         raise ValueError("src must be a matrix, and an 8-bit one needs its number of columns")
-    R, C = t.shape[0], int(cols) if scaled else t.shape[1]
     if scaled:
-        at, at_scales = _matrix_ptrs(src, R, C, "src")
+        R, C, kind, stride = t.shape[0], int(cols), TAC_SCALED, 0
+        at, at_scales = _matrix_at(t, src[1], R, C, "src")
     else:
-        at, at_scales = _view_ptr(t, t, "src"), None
-    desc = tac_quantize_desc_t(R, C, 0 if scaled else _row_stride(t), TAC_SCALED if scaled else _float_type(t, "src"),
-                               TAC_BLOCK_TILE if tiles else TAC_BLOCK_ROW)
-    straight = _matrix(R, C, t.device) if rows else None
-    turned = _matrix(C, R, t.device) if columns else None
-    to = (None, None) if straight is None else (straight[0].data_ptr(), straight[1].data_ptr())
-    to_t = (None, None) if turned is None else (turned[0].data_ptr(), turned[1].data_ptr())
+        (R, C), kind, at_scales = t.shape, _float_type(t, "src"), None
+        at, stride = _rows_of(t, "src", t.dtype, t.shape)
+    desc = tac_quantize_desc_t(R, C, stride, kind, TAC_BLOCK_TILE if tiles else TAC_BLOCK_ROW)
+    straight = _new_matrix(R, C, t) if rows else None
+    turned = _new_matrix(C, R, t) if columns else None
+    to = (straight[0].data_ptr(), straight[1].data_ptr()) if rows else (None, None)
+    to_t = (turned[0].data_ptr(), turned[1].data_ptr()) if columns else (None, None)
     _check(lib().tac_quantize(ctypes.addressof(desc), at, at_scales, to[0], to[1], to_t[0], to_t[1], _stream(stream)))
     return dict(rows=straight, columns=turned)
 
@@ -637,9 +645,10 @@ def tac_dequantize(matrix, cols, *, dtype=None, out=None, stream=None):
     R = matrix[0].shape[0]
     if out is None:
         out = torch.empty((R, cols), dtype=dtype or torch.float32, device=matrix[0].device)
-    codes, scales = _matrix_ptrs(matrix, R, cols, "matrix")
-    _check(lib().tac_dequantize(R, cols, codes, scales, _float_type(out, "out"), _view_ptr(out, out, "out", (R, cols)),
-                                _row_stride(out), _stream(stream)))
+    codes, scales = _matrix_at(matrix[0], matrix[1], R, cols, "matrix")
+    kind = _float_type(out, "out")
+    to, stride = _rows_of(out, "out", out.dtype, (R, cols))
+    _check(lib().tac_dequantize(R, cols, codes, scales, kind, to, stride, _stream(stream)))
     return out
 
 
@@ -649,20 +658,39 @@ def tac_residual_norm(x, residual=None, gain=None, *, eps, h=None, y=None, want_
     want_h: the sum x + residual (as it is where there is a residual).  Returns dict(h, y, scaled, rstd), `scaled` an 8-bit matrix of y;
     what is not asked for is None.  h and y may be given (h may be x or residual)."""
     import torch
-    if x.dim() != 2:
+    shape, dtype = x.shape, x.dtype
+    if len(shape) != 2:
         raise ValueError("x must be a matrix")
-    R, C = x.shape
-    if h is None and (residual is not None if want_h is None else want_h):
-        h = torch.empty((R, C), dtype=x.dtype, device=x.device)
-    if y is None and want_y:
-        y = torch.empty((R, C), dtype=x.dtype, device=x.device)
-    scaled = _matrix(R, C, x.device) if want_scaled else None
-    rstd = torch.empty((R,), dtype=torch.float32, device=x.device) if want_rstd else None
-    desc = tac_norm_desc_t(R, _row_stride(x), _row_stride(residual), _row_stride(h), _row_stride(y), C, _float_type(x, "x"), eps)
-    _check(lib().tac_residual_norm(
-        ctypes.addressof(desc), _view_ptr(x, x, "x"), _view_ptr(residual, x, "residual", x.shape), _shaped(gain, torch.float32, "gain", C),
-        _view_ptr(h, x, "h", x.shape), _view_ptr(y, x, "y", x.shape), scaled and scaled[0].data_ptr(), scaled and scaled[1].data_ptr(),
-        None if rstd is None else rstd.data_ptr(), _stream(stream)))
+    R, C = shape
+    kind = _float_type(x, "x")
+    x_at, x_stride = _rows_of(x, "x", dtype, shape)
+    r_at, r_stride = _rows_of(residual, "residual", dtype, shape)
+    if h is not None:
+        h_at, h_stride = _rows_of(h, "h", dtype, shape)
+    elif residual is not None if want_h is None else want_h:
+        h = x.new_empty(shape)
+        h_at, h_stride = h.data_ptr(), C
+    else:
+        h_at, h_stride = None, 0
+    if y is not None:
+        y_at, y_stride = _rows_of(y, "y", dtype, shape)
+    elif want_y:
+        y = x.new_empty(shape)
+        y_at, y_stride = y.data_ptr(), C
+    else:
+        y_at, y_stride = None, 0
+    scaled = codes = scales = rstd = rstd_at = None
+    if want_scaled:
+        scaled = _new_matrix(R, C, x)
+        codes, scales = scaled[0].data_ptr(), scaled[1].data_ptr()
+    if want_rstd:
+        rstd = x.new_empty((R,), dtype=torch.float32)
+        rstd_at = rstd.data_ptr()
+    desc = tac_norm_desc_t(R, x_stride, r_stride, h_stride, y_stride, C, kind, eps)
+    status = lib().tac_residual_norm(ctypes.addressof(desc), x_at, r_at, _shaped(gain, torch.float32, "gain", C), h_at, y_at, codes, scales,
+                                     rstd_at, _stream(stream))
+    if status:
+        _check(status)
     return dict(h=h, y=y, scaled=scaled, rstd=rstd)
 
 
@@ -670,18 +698,25 @@ def tac_residual_norm_backward(h, gain, rstd, grad_y, grad_h=None, *, grad_x=Non
     """Backward pass of tac_residual_norm from the stream h and the rstd it stored.  Returns dict(grad_x, grad_gain); grad_x is the
     gradient of x and of the residual, and may be given (also grad_y or grad_h)."""
     import torch
-    if h.dim() != 2:
+    shape, dtype = h.shape, h.dtype
+    if len(shape) != 2:
         raise ValueError("h must be a matrix")
-    R, C = h.shape
+    R, C = shape
+    kind = _float_type(h, "h")
     if grad_x is None:
-        grad_x = torch.empty((R, C), dtype=h.dtype, device=h.device)
-    desc = tac_norm_desc_t(R, _row_stride(grad_x), _row_stride(grad_h), _row_stride(h), _row_stride(grad_y), C, _float_type(h, "h"), 1.0)
+        grad_x = h.new_empty(shape)
+    h_at, h_stride = _rows_of(h, "h", dtype, shape)
+    gy_at, gy_stride = _rows_of(grad_y, "grad_y", dtype, shape)
+    gh_at, gh_stride = _rows_of(grad_h, "grad_h", dtype, shape)
+    gx_at, gx_stride = _rows_of(grad_x, "grad_x", dtype, shape)
+    desc = tac_norm_desc_t(R, gx_stride, gh_stride, h_stride, gy_stride, C, kind, 1.0)
     at = ctypes.addressof(desc)
-    grad_gain = torch.empty((C,), dtype=torch.float32, device=h.device) if want_grad_gain else None
-    work = _workspace(lib().tac_residual_norm_workspace_bytes(at), h.device, stream) if want_grad_gain else None
+    grad_gain = work = None
+    if want_grad_gain:
+        grad_gain = h.new_empty((C,), dtype=torch.float32)
+        work = _workspace(lib().tac_residual_norm_workspace_bytes(at), h, stream)
     _check(lib().tac_residual_norm_backward(
-        at, _view_ptr(h, h, "h"), _shaped(gain, torch.float32, "gain", C), _shaped(rstd, torch.float32, "rstd", R),
-        _view_ptr(grad_y, h, "grad_y", h.shape), _view_ptr(grad_h, h, "grad_h", h.shape), _view_ptr(grad_x, h, "grad_x", h.shape),
+        at, h_at, _shaped(gain, torch.float32, "gain", C), _shaped(rstd, torch.float32, "rstd", R), gy_at, gh_at, gx_at,
         None if grad_gain is None else grad_gain.data_ptr(), None if work is None else work.data_ptr(), _stream(stream)))
     return dict(grad_x=grad_x, grad_gain=grad_gain)
 
@@ -690,26 +725,25 @@ def tac_scaled_product(a_codes, a_scales, b_codes, b_scales, K, *, bias=None, dt
     """a b^T (+ bias) of the 8-bit matrices a [M, K] and b [N, K], in bfloat16 (or `dtype`, or into `out` [M, N])."""
     import torch
     M, N = a_codes.shape[0], b_codes.shape[0]
+    a_at, as_at = _matrix_at(a_codes, a_scales, M, K, "a")
+    b_at, bs_at = _matrix_at(b_codes, b_scales, N, K, "b")
     if out is None:
-        out = torch.empty((M, N), dtype=dtype or torch.bfloat16, device=a_codes.device)
-    a, b = _matrix_ptrs((a_codes, a_scales), M, K, "a"), _matrix_ptrs((b_codes, b_scales), N, K, "b")
-    desc = tac_product_desc_t(M, N, K, _row_stride(out), _float_type(out, "out"))
-    at = ctypes.addressof(desc)
-    work = _workspace(lib().tac_scaled_product_workspace_bytes(at), a_codes.device, stream)
-    _check(lib().tac_scaled_product(at, a[0], a[1], b[0], b[1], _shaped(bias, torch.float32, "bias", N),
-                                    _view_ptr(out, out, "out", (M, N)), None if work is None else work.data_ptr(), _stream(stream)))
+        out = a_codes.new_empty((M, N), dtype=dtype or torch.bfloat16)
+    kind = _float_type(out, "out")
+    y_at, y_stride = _rows_of(out, "out", out.dtype, (M, N))
+    desc = tac_product_desc_t(M, N, K, y_stride, kind)
+    at, L = ctypes.addressof(desc), lib()
+    work = _workspace(L.tac_scaled_product_workspace_bytes(at), a_codes, stream)
+    status = L.tac_scaled_product(at, a_at, as_at, b_at, bs_at, _shaped(bias, torch.float32, "bias", N), y_at,
+                                  None if work is None else work.data_ptr(), _stream(stream))
+    if status:
+        _check(status)
     return out
 
 
-def _scan_desc(gate, out, grad=None):
-    T, B, D = gate.shape
-    return tac_scan_desc_t(T, B, D, gate.stride(0), gate.stride(1), out.stride(0), out.stride(1),
-                           grad.stride(0) if grad is not None else 0, grad.stride(1) if grad is not None else 0, _float_type(gate, "gate"))
-
-
-def _same_layout(a, b, names):
-    """Strides of axes with more than one entry."""
-    if any(x != y for x, y, n in zip(a.stride(), b.stride(), a.shape) if n > 1):
+def _same_strides(a, b, shape, names):
+    """Strides of axes with more than one entry have to agree."""
+    if a != b and any(x != y for x, y, n in zip(a, b, shape) if n > 1):
         raise ValueError("%s must have the same strides" % names)
 
 
@@ -718,21 +752,24 @@ def tac_gated_scan(gate, value, *, lengths=None, h0=None, out=None, want_h_last=
     last axis contiguous; lengths: int32 [B]; h0: float32 [B, D].  Returns dict(out, h_last, states); `states` is what the backward
     pass needs."""
     import torch
-    if gate.dim() != 3:
+    shape, dtype, f32 = gate.shape, gate.dtype, torch.float32
+    if len(shape) != 3:
         raise ValueError("gate must be [T, B, D]")
-    T, B, D = gate.shape
+    T, B, D = shape
+    kind = _float_type(gate, "gate")
+    g_at, strides = _steps_of(gate, "gate", dtype, shape)
+    v_at, v_strides = _steps_of(value, "value", dtype, shape)
+    _same_strides(strides, v_strides, shape, "gate and value")
     if out is None:
-        out = torch.empty((T, B, D), dtype=gate.dtype, device=gate.device)
-    f32 = torch.float32
-    h_last = torch.empty((B, D), dtype=f32, device=gate.device) if want_h_last else None
-    states = torch.empty((-(-T // TAC_SCAN_CHUNK), B, D), dtype=f32, device=gate.device) if want_states else None
-    g, v = _view_ptr(gate, gate, "gate"), _view_ptr(value, gate, "value", gate.shape)
-    _same_layout(gate, value, "gate and value")
-    desc = _scan_desc(gate, out)
-    at = ctypes.addressof(desc)
-    work = _workspace(lib().tac_gated_scan_workspace_bytes(at), gate.device, stream)
-    _check(lib().tac_gated_scan(
-        at, g, v, _shaped(lengths, torch.int32, "lengths", B), _shaped(h0, f32, "h0", B, D), _view_ptr(out, gate, "out", gate.shape),
+        out = gate.new_empty(shape)
+    o_at, o_strides = _steps_of(out, "out", dtype, shape)
+    h_last = gate.new_empty((B, D), dtype=f32) if want_h_last else None
+    states = gate.new_empty((-(-T // TAC_SCAN_CHUNK), B, D), dtype=f32) if want_states else None
+    desc = tac_scan_desc_t(T, B, D, strides[0], strides[1], o_strides[0], o_strides[1], 0, 0, kind)
+    at, L = ctypes.addressof(desc), lib()
+    work = _workspace(L.tac_gated_scan_workspace_bytes(at), gate, stream)
+    _check(L.tac_gated_scan(
+        at, g_at, v_at, _shaped(lengths, torch.int32, "lengths", B), _shaped(h0, f32, "h0", B, D), o_at,
         None if h_last is None else h_last.data_ptr(), None if states is None else states.data_ptr(),
         None if work is None else work.data_ptr(), _stream(stream)))
     return dict(out=out, h_last=h_last, states=states)
@@ -743,25 +780,29 @@ def tac_gated_scan_backward(gate, value, states, grad_out, *, lengths=None, grad
     """Backward pass of tac_gated_scan from its inputs and `states`.  Returns dict(grad_gate, grad_value, grad_h0); the first two may be
     given (of the same strides as each other)."""
     import torch
-    if gate.dim() != 3:
+    shape, dtype, f32 = gate.shape, gate.dtype, torch.float32
+    if len(shape) != 3:
         raise ValueError("gate must be [T, B, D]")
-    T, B, D = gate.shape
+    T, B, D = shape
+    kind = _float_type(gate, "gate")
     if grad_gate is None:
-        grad_gate = torch.empty((T, B, D), dtype=gate.dtype, device=gate.device)
+        grad_gate = gate.new_empty(shape)
     if grad_value is None:
-        grad_value = torch.empty_strided(gate.shape, grad_gate.stride(), dtype=gate.dtype, device=gate.device)
-    f32 = torch.float32
-    grad_h0 = torch.empty((B, D), dtype=f32, device=gate.device) if want_grad_h0 else None
-    ptrs = [_view_ptr(t, gate, n, gate.shape) for t, n in ((gate, "gate"), (value, "value"), (grad_out, "grad_out"),
-                                                           (grad_gate, "grad_gate"), (grad_value, "grad_value"))]
-    _same_layout(gate, value, "gate and value")
-    _same_layout(grad_gate, grad_value, "grad_gate and grad_value")
-    desc = _scan_desc(gate, grad_out, grad_gate)
-    at = ctypes.addressof(desc)
-    work = _workspace(lib().tac_gated_scan_workspace_bytes(at), gate.device, stream)
-    _check(lib().tac_gated_scan_backward(
-        at, ptrs[0], ptrs[1], _shaped(lengths, torch.int32, "lengths", B), _shaped(states, f32, "states", -(-T // TAC_SCAN_CHUNK), B, D),
-        ptrs[2], _shaped(grad_h_last, f32, "grad_h_last", B, D), ptrs[3], ptrs[4], None if grad_h0 is None else grad_h0.data_ptr(),
+        grad_value = torch.empty_strided(shape, grad_gate.stride(), dtype=dtype, device=gate.device)
+    grad_h0 = gate.new_empty((B, D), dtype=f32) if want_grad_h0 else None
+    g_at, strides = _steps_of(gate, "gate", dtype, shape)
+    v_at, v_strides = _steps_of(value, "value", dtype, shape)
+    _same_strides(strides, v_strides, shape, "gate and value")
+    go_at, go_strides = _steps_of(grad_out, "grad_out", dtype, shape)
+    gg_at, gg_strides = _steps_of(grad_gate, "grad_gate", dtype, shape)
+    gv_at, gv_strides = _steps_of(grad_value, "grad_value", dtype, shape)
+    _same_strides(gg_strides, gv_strides, shape, "grad_gate and grad_value")
+    desc = tac_scan_desc_t(T, B, D, strides[0], strides[1], go_strides[0], go_strides[1], gg_strides[0], gg_strides[1], kind)
+    at, L = ctypes.addressof(desc), lib()
+    work = _workspace(L.tac_gated_scan_workspace_bytes(at), gate, stream)
+    _check(L.tac_gated_scan_backward(
+        at, g_at, v_at, _shaped(lengths, torch.int32, "lengths", B), _shaped(states, f32, "states", -(-T // TAC_SCAN_CHUNK), B, D),
+        go_at, _shaped(grad_h_last, f32, "grad_h_last", B, D), gg_at, gv_at, None if grad_h0 is None else grad_h0.data_ptr(),
         None if work is None else work.data_ptr(), _stream(stream)))
     return dict(grad_gate=grad_gate, grad_value=grad_value, grad_h0=grad_h0)
 
@@ -771,14 +812,22 @@ def tac_gated_step(gate, value, pool, slots=None, *, out=None, stream=None):
     value: [B, D]; slots: int32 [B], each slot at most once, outside the pool for rows without a sequence; None: row b has slot b.
     Returns out [B, D]."""
     import torch
-    if gate.dim() != 2 or pool.dim() != 2:
+    shape, dtype = gate.shape, gate.dtype
+    if len(shape) != 2 or pool.dim() != 2:
         raise ValueError("gate must be [B, D] and pool [slots, D]")
-    B, D = gate.shape
+    B, D = shape
+    kind = _float_type(gate, "gate")
+    g_at, stride = _rows_of(gate, "gate", dtype, shape)
+    v_at, v_stride = _rows_of(value, "value", dtype, shape)
+    if stride != v_stride:
+        raise ValueError("gate and value must have the same strides")
     if out is None:
-        out = torch.empty((B, D), dtype=gate.dtype, device=gate.device)
-    g, v = _view_ptr(gate, gate, "gate"), _view_ptr(value, gate, "value", gate.shape)
-    _same_layout(gate, value, "gate and value")
-    desc = tac_scan_desc_t(1, B, D, 0, gate.stride(0), 0, out.stride(0), 0, 0, _float_type(gate, "gate"))
-    _check(lib().tac_gated_step(ctypes.addressof(desc), g, v, _shaped(pool, torch.float32, "pool", pool.shape[0], D), pool.shape[0],
-                                _shaped(slots, torch.int32, "slots", B), _view_ptr(out, gate, "out", gate.shape), _stream(stream)))
+        out = gate.new_empty(shape)
+    o_at, o_stride = _rows_of(out, "out", dtype, shape)
+    n_slots = pool.shape[0]
+    desc = tac_scan_desc_t(1, B, D, 0, stride, 0, o_stride, 0, 0, kind)
+    status = lib().tac_gated_step(ctypes.addressof(desc), g_at, v_at, _shaped(pool, torch.float32, "pool", n_slots, D), n_slots,
+                                  _shaped(slots, torch.int32, "slots", B), o_at, _stream(stream))
+    if status:
+        _check(status)
     return out

@@ -12,6 +12,7 @@
 // The rows of b are the instruction's first operand: a lane then ends with four consecutive n of one m.
 #include "tac_head_common.h"
 #include "tac_mfma_common.h"
+#include "tac_plan_memo.h"
 
 namespace tac {
 
@@ -356,7 +357,7 @@ hipError_t tiles(const ProductParams& p, int parts, hipStream_t s) {
 struct Plan {
   int tile, parts;
 };
-Plan plan_of(int64_t M, int64_t N, int64_t K, int bf) {
+Plan choose_plan(int64_t M, int64_t N, int64_t K, int bf) {
   struct Tile {
     int size, more;                  // more: two workgroups share a compute unit
     double ends, block, block_shared;
@@ -375,7 +376,7 @@ Plan plan_of(int64_t M, int64_t N, int64_t K, int bf) {
       const int64_t rounds = items / whole, left = items % whole;
       double us = (double)rounds * (q.ends + (double)each * q.block_shared);
       if (left) us += q.ends + (double)each * (left > kFittedUnits ? q.block_shared : q.block);
-      if (parts > 1) us += 3.0 + (double)M * (double)N * (8.0 * parts + (bf ? 2.0 : 4.0)) / 4e6;
+      if (parts > 1) us += 4.5 + (double)M * (double)N * (8.0 * parts + (bf ? 2.0 : 4.0)) / 4e6;
       if (us < least) {
         least = us;
         best = Plan{tile, parts};
@@ -383,6 +384,14 @@ Plan plan_of(int64_t M, int64_t N, int64_t K, int bf) {
     }
   }
   return best;
+}
+
+Plan plan_of(int64_t M, int64_t N, int64_t K, int bf) {
+  static thread_local PlanMemo<4, Plan> memo;      // a call asks twice, and the estimates take a microsecond
+  return *memo.of({(int)M, (int)N, (int)K, bf}, [&](Plan& q) {
+    q = choose_plan(M, N, K, bf);
+    return true;
+  });
 }
 
 }  // namespace
