@@ -274,7 +274,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile_kernel(const Pro
     fetch(stages, std::integral_constant<int, 1>());
     for (int k = first; k + 1 < last; ++k) block(k, std::true_type());
     block(last - 1, std::false_type());
-    __syncthreads();                                      // all stages have been read
+    dma_wait<0>();                                        // the empty loads behind the last block write zeros: they have to be there
+    __syncthreads();                                      // before the stages are used again, and all stages have been read
     const int64_t mw = m0 + wm * FM * 32, nw = n0 + wn * FN * 32;
     U* y = (U*)p.y + (int64_t)part * p.M * p.N;
     item += gridDim.x;
@@ -293,7 +294,7 @@ hipError_t tile_launch(const ProductParams& p, int parts, hipStream_t s) {
   const int64_t items = ((p.M + TM - 1) / TM) * ((p.N + TN - 1) / TN) * parts;
   auto* kernel = product_tile_kernel<TM, TN, WM, WN, STAGES, EXACT, U>;
   constexpr int lds = tile_lds(TM, TN, WM * WN, STAGES);
-  constexpr int at_once = kFittedUnits * (lds <= 80 * 1024 ? 2 : 1);       // workgroups that the LDS holds
+  constexpr int at_once = kFittedUnits * (160 * 1024 / lds);       // workgroups that the LDS holds
   static const hipError_t room = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (room != hipSuccess) return room;
   hipLaunchKernelGGL(kernel, dim3((unsigned)(items < at_once ? items : at_once)), dim3(64 * WM * WN), lds, s, p, parts);
@@ -347,35 +348,36 @@ hipError_t tiles(const ProductParams& p, int parts, hipStream_t s) {
 }
 
 // The tile and the number of parts, by an estimate in microseconds: a launch, then for every round of workgroups a beginning and an end and the blocks
-// of columns of an item.  Fitted to products on 256 compute units, one and two workgroups to each (bfloat16 and float32 results):
-//   256 x 256, 2 stages  16384 x 8192 x 4096 459 us, 8192 x 8192 x 256 37;        float32 8192 x 4096 x 8192 408
-//   128 x 128, 4 stages  4096^3 84, 1024 x 4096 x 4096 23, 8192 x 8192 x 256 64;   float32 8192 x 4096 x 8192 540, 3200 x 500 x 3136 29
-//   128 x 128, 2 stages  4096^3 74, 1024 x 4096 x 4096 29, 8192 x 8192 x 256 41;   float32 8192 x 4096 x 8192 474, 3200 x 500 x 3136 28
-//   64 x 64, 4 stages    4096^3 125, 512 x 4096 x 4096 18, 256 x 4096 x 4096 13;   float32 8192 x 4096 x 8192 837, 3200 x 500 x 3136 26
-// Large tiles read less per product, small ones give more workgroups and shorter blocks.  Parts cost their sums' way through memory:
-// 128 x 3136 x 3200 float32 on tiles of 64 in one part 17 us, in two 14, in four 15; 16 x 8192 x 4096 12, 11, 11.
+// of columns of an item.  Fitted to products on 256 compute units, with one to four workgroups on each (bfloat16 and float32 results):
+//   256 x 256, 2 stages  16384 x 8192 x 4096 459 us, 8192 x 8192 x 256 37;         float32 8192 x 4096 x 8192 408
+//   128 x 128, 4 stages  4096^3 84, 1024 x 4096 x 4096 23, 1500^3 15.0;            float32 8192 x 4096 x 8192 540, 3200 x 500 x 3136 30, 1500^3 17.4
+//   128 x 128, 2 stages  4096^3 74, 1024 x 4096 x 4096 29, 1500^3 14.3;            float32 8192 x 4096 x 8192 474, 3200 x 500 x 3136 28, 1500^3 16.6
+//   64 x 64, 4 stages    4096^3 125, 256 x 4096 x 4096 12.8, 16 x 8192 x 4096 12;  float32 8192 x 4096 x 8192 837, 3200 x 500 x 3136 25.5, 1500^3 19.8
+//   64 x 64, 2 stages    256 x 4096 x 4096 12.1, 16 x 8192 x 4096 17, 1500^3 12.8; float32 3200 x 500 x 3136 25.1, 1500^3 15.4
+// Large tiles read less per product, small ones give more workgroups and shorter blocks; stages hide memory where few workgroups do.  Parts cost their
+// sums' way through memory: 128 x 3136 x 3200 float32 on tiles of 64 in one part 17 us, in two 14, in four 15; 16 x 8192 x 4096 12, 11, 11.
 struct Plan {
   int tile, parts;
 };
 Plan choose_plan(int64_t M, int64_t N, int64_t K, int bf) {
   struct Tile {
-    int size, more;                  // more: two workgroups share a compute unit
-    double ends, block, block_shared;
+    int size, shared;                // shared: workgroups that a compute unit takes
+    double ends, block[4];           // block: of a workgroup that shares its unit with none, one, two, three others
   };
-  static constexpr Tile kTiles[2][4] = {{{256, 0, 6.0, 3.05, 3.05}, {128, 0, 3.0, 1.02, 1.02}, {128, 1, 3.0, 1.0, 1.8}, {64, 1, 2.0, 0.58, 0.79}},
-                                        {{256, 0, 6.0, 1.6, 1.6}, {128, 0, 3.0, 0.56, 0.56}, {128, 1, 3.0, 0.7, 1.07}, {64, 1, 2.0, 0.3, 0.45}}};
+  static constexpr Tile kTiles[2][5] = {{{256, 1, 6.0, {3.05}}, {128, 1, 3.0, {1.02}}, {128, 2, 3.0, {1.0, 1.8}}, {64, 2, 2.0, {0.58, 0.79}}, {64, 4, 2.0, {0.62, 0.77, 0.93, 1.25}}},
+                                        {{256, 1, 6.0, {1.6}}, {128, 1, 3.0, {0.56}}, {128, 2, 3.0, {0.7, 1.07}}, {64, 2, 2.0, {0.3, 0.45}}, {64, 4, 2.0, {0.33, 0.47, 0.65, 0.85}}}};
   const int64_t blocks = (K + kBlock - 1) / kBlock;
   Plan best = {0, 1};
   double least = 1e300;
-  for (int tile = 0; tile < 4; ++tile) {
+  for (int tile = 0; tile < 5; ++tile) {
     const Tile& q = kTiles[bf != 0][tile];
     const int64_t tiles = ((M + q.size - 1) / q.size) * ((N + q.size - 1) / q.size);
     for (int parts : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
       if (parts > 1 && (2 * parts > blocks || tiles * parts > 2 * kFittedUnits)) break;
-      const int64_t items = tiles * parts, each = (blocks + parts - 1) / parts, whole = kFittedUnits * (1 + q.more);
-      const int64_t rounds = items / whole, left = items % whole;
-      double us = (double)rounds * (q.ends + (double)each * q.block_shared);
-      if (left) us += q.ends + (double)each * (left > kFittedUnits ? q.block_shared : q.block);
+      const int64_t items = tiles * parts, whole = kFittedUnits * q.shared, left = items % whole;
+      const double each = (double)((blocks + parts - 1) / parts);
+      double us = (double)(items / whole) * (q.ends + each * q.block[q.shared - 1]);
+      if (left) us += q.ends + each * q.block[(left - 1) / kFittedUnits];
       if (parts > 1) us += 4.5 + (double)M * (double)N * (8.0 * parts + (bf ? 2.0 : 4.0)) / 4e6;
       if (us < least) {
         least = us;
@@ -409,7 +411,8 @@ hipError_t product_launch(const ProductParams& given, hipStream_t s) {
     case 0: return tiles<256, 256, 4, 2, 2>(p, plan.parts, s);
     case 1: return tiles<128, 128, 2, 2, 4>(p, plan.parts, s);
     case 2: return tiles<128, 128, 2, 2, 2>(p, plan.parts, s);
-    default: return tiles<64, 64, 2, 1, 4>(p, plan.parts, s);
+    case 3: return tiles<64, 64, 2, 1, 4>(p, plan.parts, s);
+    default: return tiles<64, 64, 2, 1, 2>(p, plan.parts, s);
   }
 }
 
