@@ -112,18 +112,24 @@ __device__ __forceinline__ void four_values(uint32_t codes, float (&v)[4]) {
   v[3] = hi[1];
 }
 
-// largest and sum over groups of LANES consecutive lanes; every lane gets it
-template <int LANES>
-__device__ __forceinline__ float max_over(float v) {
-#pragma unroll
-  for (int d = 1; d < LANES; d <<= 1) v = fmaxf(v, __shfl_xor(v, d));
-  return v;
+// largest over 16 consecutive lanes, and sum over a wave; every lane gets it.  Within 16 lanes by rotation (one instruction each, no LDS).
+template <int BY>
+__device__ __forceinline__ float rotated(float v) {
+  return bits_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)float_bits(v), 0x120 + BY, 0xf, 0xf, false));      // row_ror
 }
-template <int LANES>
-__device__ __forceinline__ float sum_over(float v) {
-#pragma unroll
-  for (int d = 1; d < LANES; d <<= 1) v += __shfl_xor(v, d);
-  return v;
+__device__ __forceinline__ float max_over_16(float v) {
+  v = fmaxf(v, rotated<8>(v));
+  v = fmaxf(v, rotated<4>(v));
+  v = fmaxf(v, rotated<2>(v));
+  return fmaxf(v, rotated<1>(v));
+}
+__device__ __forceinline__ float sum_over_wave(float v) {
+  v += rotated<8>(v);
+  v += rotated<4>(v);
+  v += rotated<2>(v);
+  v += rotated<1>(v);
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
 }
 
 // whether every row of a matrix starts at a multiple of 16 bytes

@@ -15,7 +15,7 @@ constexpr int64_t kMostGroups = 1 << 20;       // workgroups of a launch; more r
 // sum over the LANES lanes that share a row; `room` is LDS for LANES / 64 floats (unused for one wave)
 template <int LANES>
 __device__ __forceinline__ float row_sum(float v, float* room) {
-  v = sum_over<64>(v);
+  v = sum_over_wave(v);
   if constexpr (LANES > 64) {
     const int wave = threadIdx.x >> 6;
     __syncthreads();                       // the row before has been read
@@ -36,8 +36,15 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(const N
   // every lane of a workgroup makes the same number of turns: LANES > 64 has one row a turn, LANES = 64 has no barrier inside
   for (int64_t row = (int64_t)blockIdx.x * (blockDim.x / LANES) + threadIdx.x / LANES; row < p.rows;
        row += (int64_t)gridDim.x * (blockDim.x / LANES)) {
-    float v[PASSES][kCols];
+    float v[PASSES][kCols], g[PASSES][kCols];
     float squares = 0.0f;
+#pragma unroll
+    for (int q = 0; q < PASSES; ++q) {                    // asked for with the row, not after its sum
+      const int c = (q * LANES + lane) * kCols;
+#pragma unroll
+      for (int e = 0; e < kCols; ++e) g[q][e] = 1.0f;
+      if (p.gain && (p.y || p.codes) && c < p.cols) load_floats<float, kCols, VEC>(p.gain + c, p.cols - c, g[q]);
+    }
   #pragma unroll
     for (int q = 0; q < PASSES; ++q) {
       const int c = (q * LANES + lane) * kCols;
@@ -65,15 +72,8 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(const N
     for (int q = 0; q < PASSES; ++q) {
       const int c = (q * LANES + lane) * kCols;
       const int n = p.cols - c;
-      float g[kCols];
-      if (p.gain && n > 0) {
-        load_floats<float, kCols, VEC>(p.gain + c, n, g);
-      } else {
-  #pragma unroll
-        for (int e = 0; e < kCols; ++e) g[e] = 1.0f;
-      }
-  #pragma unroll
-      for (int e = 0; e < kCols; ++e) v[q][e] = v[q][e] * rstd * g[e];
+#pragma unroll
+      for (int e = 0; e < kCols; ++e) v[q][e] = v[q][e] * rstd * g[q][e];
       if (p.y && n > 0) store_floats<T, kCols, VEC>((T*)p.y + row * p.y_stride + c, n, v[q]);
       if (p.codes) {
         float amax = 0.0f;
@@ -82,7 +82,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(const N
           v[q][e] = finite_or_nan(v[q][e]);
           amax = fmaxf(amax, fabsf(v[q][e]));
         }
-        const uint32_t byte = scale_byte(max_over<16>(amax));
+        const uint32_t byte = scale_byte(max_over_16(amax));
         const float inv = scale_inverse(byte);
         if (c < pitch)
           *reinterpret_cast<u32x2_t*>(p.codes + row * pitch + c) =
@@ -176,21 +176,27 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_backward_kerne
   }
 }
 
-// column sums of partial [groups][cols]: 16 columns and 16 slices of the groups a workgroup
+// Column sums of partial [groups][cols]: 16 lanes x 4 columns and 16 slices of the groups a workgroup, then the slices in their order.
+template <bool VEC>
 __global__ __launch_bounds__(256) void gain_sum_kernel(const float* __restrict__ partial, float* __restrict__ grad_gain, int groups, int cols) {
-  __shared__ float room[16][17];
-  const int c = blockIdx.x * 16 + threadIdx.x % 16, slice = threadIdx.x / 16;
-  float t = 0.0f;
-  if (c < cols)
-    for (int g = slice; g < groups; g += 16) t += partial[(int64_t)g * cols + c];
-  room[slice][threadIdx.x % 16] = t;
-  __syncthreads();
-  if (slice == 0 && c < cols) {
-    t = 0.0f;
-#pragma unroll
-    for (int s = 0; s < 16; ++s) t += room[s][threadIdx.x];
-    grad_gain[c] = t;
+  __shared__ f32x4_t room[16][16];
+  const int lane = threadIdx.x % 16, slice = threadIdx.x / 16, c = (blockIdx.x * 16 + lane) * 4;
+  f32x4_t t = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (c < cols) {
+#pragma unroll 8
+    for (int g = slice; g < groups; g += 16) {
+      float v[4];
+      load_floats<float, 4, VEC>(partial + (int64_t)g * cols + c, cols - c, v);
+      t += f32x4_t{v[0], v[1], v[2], v[3]};
+    }
   }
+  room[slice][lane] = t;
+  __syncthreads();
+  if (slice || c >= cols) return;
+#pragma unroll
+  for (int s = 1; s < 16; ++s) t += room[s][lane];
+  const float v[4] = {t[0], t[1], t[2], t[3]};
+  store_floats<float, 4, VEC>(grad_gain + c, cols - c, v);
 }
 
 // Lanes and passes of a row of `cols` columns: f(lanes, passes) with both as constants.
@@ -234,7 +240,9 @@ hipError_t norm_backward_typed(const NormBackwardParams& p, hipStream_t s) {
     return hipGetLastError();
   });
   if (e != hipSuccess || !p.grad_gain) return e;
-  hipLaunchKernelGGL(gain_sum_kernel, dim3((p.cols + 15) / 16), dim3(256), 0, s, p.partial, p.grad_gain, (int)groups, p.cols);
+  const dim3 grid((p.cols + 63) / 64);
+  if (p.cols % 4 == 0 && rows_aligned(p.grad_gain, 0, 4)) hipLaunchKernelGGL(gain_sum_kernel<true>, grid, dim3(256), 0, s, p.partial, p.grad_gain, (int)groups, p.cols);
+  else hipLaunchKernelGGL(gain_sum_kernel<false>, grid, dim3(256), 0, s, p.partial, p.grad_gain, (int)groups, p.cols);
   return hipGetLastError();
 }
 

@@ -10,12 +10,13 @@ namespace {
 
 constexpr int kPitch = 132;        // bytes of a transposed row in LDS: 16 lanes that write 8 columns further each are 66 words apart
 
-// DT: 0 float32, 1 bfloat16, 2 8-bit codes.  VEC: rows of whole 16-byte pieces.
-template <int DT, bool VEC>
-__global__ __launch_bounds__(256) void quantize_kernel(const QuantizeParams p, int row_tiles) {
-  __shared__ float col_max[4][kBlock];
-  __shared__ __align__(16) uint8_t turned[kBlock * kPitch];
-  const int64_t r0 = (int64_t)(blockIdx.x % row_tiles) * kBlock, c0 = (int64_t)(blockIdx.x / row_tiles) * kBlock;
+// DT: 0 float32, 1 bfloat16, 2 8-bit codes.  VEC: rows of whole 16-byte pieces.  ROWS: the straight matrix alone, with a scale per row (an activation or
+// gradient on its way into a product), which needs nothing of the columns.
+template <int DT, bool VEC, bool ROWS>
+__global__ __launch_bounds__(256) void quantize_kernel(const QuantizeParams p, int col_tiles) {
+  __shared__ float col_max[ROWS ? 1 : 4][kBlock];
+  __shared__ __align__(16) uint8_t turned[ROWS ? 16 : kBlock * kPitch];
+  const int64_t r0 = (int64_t)(blockIdx.x / col_tiles) * kBlock, c0 = (int64_t)(blockIdx.x % col_tiles) * kBlock;
   const int rt = threadIdx.x / 16, ct = threadIdx.x % 16;
   const int64_t c = c0 + 8 * ct;
   float v[8][8];
@@ -52,10 +53,10 @@ __global__ __launch_bounds__(256) void quantize_kernel(const QuantizeParams p, i
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       v[i][e] = finite_or_nan(v[i][e]);
-      col[e] = fmaxf(col[e], fabsf(v[i][e]));
+      if constexpr (!ROWS) col[e] = fmaxf(col[e], fabsf(v[i][e]));
     }
   // the largest of each column over the four row groups of a wave, then over the waves
-  if (p.codes_t || p.tiles) {
+  if (!ROWS && (p.codes_t || p.tiles)) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       col[e] = fmaxf(col[e], __shfl_xor(col[e], 16));
@@ -68,20 +69,20 @@ __global__ __launch_bounds__(256) void quantize_kernel(const QuantizeParams p, i
       col[e] = fmaxf(fmaxf(col_max[0][8 * ct + e], col_max[1][8 * ct + e]), fmaxf(col_max[2][8 * ct + e], col_max[3][8 * ct + e]));
       tile = fmaxf(tile, col[e]);
     }
-    if (p.tiles) tile = max_over<16>(tile);
+    if (p.tiles) tile = max_over_16(tile);
   }
-  if (p.codes) {
+  if (ROWS || p.codes) {
     const int64_t pitch = code_pitch(p.cols), spitch = scale_pitch(p.cols);
     const bool last = c0 + kBlock >= p.cols;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int64_t r = r0 + 8 * rt + i;
       float amax = tile;
-      if (!p.tiles) {
+      if (ROWS || !p.tiles) {
         amax = 0.0f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(v[i][e]));
-        amax = max_over<16>(amax);
+        amax = max_over_16(amax);
       }
       const uint32_t byte = scale_byte(amax);
       const float inv = scale_inverse(byte);
@@ -94,7 +95,7 @@ __global__ __launch_bounds__(256) void quantize_kernel(const QuantizeParams p, i
       }
     }
   }
-  if (p.codes_t) {
+  if (!ROWS && p.codes_t) {
     const int64_t pitch = code_pitch(p.rows), spitch = scale_pitch(p.rows);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -142,15 +143,21 @@ __global__ __launch_bounds__(256) void dequantize_kernel(const uint8_t* __restri
 
 }  // namespace
 
+template <int DT, bool VEC>
+static void quantize_typed(const QuantizeParams& p, dim3 grid, int ct, hipStream_t s) {
+  if (!p.codes_t && !p.tiles) hipLaunchKernelGGL((quantize_kernel<DT, VEC, true>), grid, dim3(256), 0, s, p, ct);
+  else hipLaunchKernelGGL((quantize_kernel<DT, VEC, false>), grid, dim3(256), 0, s, p, ct);
+}
+
 hipError_t quantize_launch(const QuantizeParams& p, hipStream_t s) {
   const int64_t rt = (p.rows + kBlock - 1) / kBlock, ct = (p.cols + kBlock - 1) / kBlock;
   const dim3 grid((unsigned)(rt * ct));
   const bool vec = p.dtype != TAC_SCALED && p.cols % 8 == 0 && rows_aligned(p.src, p.src_stride, p.dtype == TAC_BF16 ? 2 : 4);
-  if (p.dtype == TAC_SCALED) hipLaunchKernelGGL((quantize_kernel<2, false>), grid, dim3(256), 0, s, p, (int)rt);
-  else if (p.dtype == TAC_BF16 && vec) hipLaunchKernelGGL((quantize_kernel<1, true>), grid, dim3(256), 0, s, p, (int)rt);
-  else if (p.dtype == TAC_BF16) hipLaunchKernelGGL((quantize_kernel<1, false>), grid, dim3(256), 0, s, p, (int)rt);
-  else if (vec) hipLaunchKernelGGL((quantize_kernel<0, true>), grid, dim3(256), 0, s, p, (int)rt);
-  else hipLaunchKernelGGL((quantize_kernel<0, false>), grid, dim3(256), 0, s, p, (int)rt);
+  if (p.dtype == TAC_SCALED) quantize_typed<2, false>(p, grid, (int)ct, s);
+  else if (p.dtype == TAC_BF16 && vec) quantize_typed<1, true>(p, grid, (int)ct, s);
+  else if (p.dtype == TAC_BF16) quantize_typed<1, false>(p, grid, (int)ct, s);
+  else if (vec) quantize_typed<0, true>(p, grid, (int)ct, s);
+  else quantize_typed<0, false>(p, grid, (int)ct, s);
   return hipGetLastError();
 }
 
