@@ -2,6 +2,7 @@
 // element types, 8-bit codes and their scales, sums over lanes, launch parameters.
 #pragma once
 #include "tac_internal.h"
+#include "tac_product_plan.h"
 
 namespace tac {
 
@@ -9,8 +10,6 @@ typedef __bf16 bf16;
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
-
-constexpr int kBlock = TAC_SCALE_BLOCK;      // columns that share a scale
 
 // a row of codes is padded to whole blocks, a row of scales to whole dwords
 inline __host__ __device__ int64_t code_pitch(int64_t cols) { return (cols + kBlock - 1) / kBlock * kBlock; }

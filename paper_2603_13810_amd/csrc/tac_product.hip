@@ -13,6 +13,7 @@
 #include "tac_head_common.h"
 #include "tac_mfma_common.h"
 #include "tac_plan_memo.h"
+#include "tac_product_plan.h"
 
 namespace tac {
 
@@ -61,14 +62,6 @@ __device__ __forceinline__ u32x4_t buffer_at(uint64_t at, int64_t bytes) {
                  (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), 0x00020000u};
 }
 
-// LDS of the kernel below: STAGES stages of the tile's rows, of which the last one's place also takes the results on their way out (32 rows of up to
-// 256 bytes and 16 for each wave), then as many sets of scale bytes of four blocks.
-constexpr int tile_scales_at(int TM, int TN, int waves, int STAGES) {
-  const int stage = (TM + TN) * kBlock, out = waves * 32 * (256 + 16);
-  return (STAGES - 1) * stage + (stage > out ? stage : out);
-}
-constexpr int tile_lds(int TM, int TN, int waves, int STAGES) { return tile_scales_at(TM, TN, waves, STAGES) + 4 * STAGES * (TM + TN); }
-
 // Tiles of TM rows of a x TN rows of b, WM x WN waves.  One block of 128 columns of the tile's rows (128 bytes each) is a stage in LDS: while the waves
 // multiply one, direct-to-LDS loads fill the others.  Fragments are read two steps ahead of their use, across blocks too: the one
 // barrier a block stands two steps before its end, where all of the stage has been read and the next one is there.  A row's eight pieces of 16
@@ -81,7 +74,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile_kernel(const Pro
   constexpr int kWaves = WM * WN, FM = TM / WM / 32, FN = TN / WN / 32, kStage = (TM + TN) * kBlock;
   constexpr int kLoadsM = TM / 8 / kWaves, kLoadsN = TN / 8 / kWaves;         // a load instruction brings 8 rows
   static_assert(TM % (32 * WM) == 0 && TN % (32 * WN) == 0 && TM % (8 * kWaves) == 0 && TN % (8 * kWaves) == 0 && kWaves % 2 == 0);
-  static_assert(TM + TN == 64 * kWaves);
+  static_assert((TM + TN) % 64 == 0 && TM + TN <= 64 * kWaves);
   constexpr int kScales = tile_scales_at(TM, TN, kWaves, STAGES), kLoads = kLoadsM + kLoadsN + 1;
   extern __shared__ __align__(1024) uint8_t stages[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave % WM, wn = wave / WM;
@@ -111,7 +104,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile_kernel(const Pro
     bn_at = (uint64_t)(uintptr_t)p.b + (uint64_t)(n0 * pitch);
     am_bytes = (uint32_t)(min((int64_t)TM, p.M - m0) * pitch);
     bn_bytes = (uint32_t)(min((int64_t)TN, p.N - n0) * pitch);
-    const int64_t row = 64 * wave + lane;
+    const int64_t row = (64 * wave + lane) % (TM + TN);      // waves that have none of their own bring others' again, to a place that nobody reads
     scales_from = row < TM ? p.a_scales + min(m0 + row, p.M - 1) * spitch : p.b_scales + min(n0 + row - TM, p.N - 1) * spitch;
   };
 
@@ -127,12 +120,12 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile_kernel(const Pro
     for (int j = 0; j < kLoadsM; ++j) lds_dma_rows(offset + j * step, am, to + j * kWaves * 1024);
 #pragma unroll
     for (int j = 0; j < kLoadsN; ++j) lds_dma_rows(offset + j * step, bn, to + TM * kBlock + j * kWaves * 1024);
-    lds_dma_dword(scales_from + (at & ~3), lds0 + kScales + slot * (4 * (TM + TN)) + wave * 256);
+    lds_dma_dword(scales_from + (at & ~3), lds0 + kScales + (slot * kWaves + wave) * 256);
   };
 
   uint32_t em[FM], en[FN];                                // scale bytes of the block in hand
   auto fetch_scales = [&](int k, uint32_t (&m)[FM], uint32_t (&n)[FN]) {
-    const uint8_t* at = stages + kScales + (uint32_t)(k - first) % STAGES * (4 * (TM + TN)) + (k & 3) + 4 * (lane % 32);
+    const uint8_t* at = stages + kScales + (uint32_t)(k - first) % STAGES * (256 * kWaves) + (k & 3) + 4 * (lane % 32);
 #pragma unroll
     for (int f = 0; f < FM; ++f) m[f] = at[(wm * FM + f) * 128];
 #pragma unroll
@@ -142,9 +135,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile_kernel(const Pro
   f32x16_t sum[FN][FM];
 
   // A block is kSteps steps, each a fragment of b against all of the wave's fragments of a; every step first reads what the step after next needs.
-  constexpr int kSteps = 2 * FN;
-  static_assert(kSteps % 4 == 0);
-  i32x8_t a[2][FM], b[4];
+  constexpr int kSteps = 2 * FN, kRing = kSteps < 4 ? kSteps : 4;
+  static_assert(kSteps % kRing == 0);
+  i32x8_t a[2][FM], b[kRing];
   bf16x8_t wide[EXACT ? FM : 1][4];
   const int x = (lane >> 1) & 7, at_m = (wm * FM * 32 + lane % 32) * kBlock, at_n = (TM + wn * FN * 32 + lane % 32) * kBlock;
   const int piece[2][2] = {{16 * ((2 * (lane / 32)) ^ x), 16 * ((2 * (lane / 32) + 1) ^ x)},
@@ -157,7 +150,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile_kernel(const Pro
         a[H][f] = join_codes(*reinterpret_cast<const u32x4_t*>(at + at_m + f * 32 * kBlock + piece[H][0]),
                              *reinterpret_cast<const u32x4_t*>(at + at_m + f * 32 * kBlock + piece[H][1]));
     }
-    b[S % 4] = join_codes(*reinterpret_cast<const u32x4_t*>(at + at_n + I * 32 * kBlock + piece[H][0]),
+    b[S % kRing] = join_codes(*reinterpret_cast<const u32x4_t*>(at + at_n + I * 32 * kBlock + piece[H][0]),
                           *reinterpret_cast<const u32x4_t*>(at + at_n + I * 32 * kBlock + piece[H][1]));
   };
 
@@ -173,8 +166,11 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile_kernel(const Pro
         load(k + STAGES);
         fetch_scales(k + 1, next_m, next_n);
       }
-      if constexpr (S < kSteps - 2) fetch(here, std::integral_constant<int, (S + 2) % kSteps>());
-      else if constexpr (decltype(more)::value) fetch(there, std::integral_constant<int, (S + 2) % kSteps>());
+      auto ahead = [&] {
+        if constexpr (S < kSteps - 2) fetch(here, std::integral_constant<int, (S + 2) % kSteps>());
+        else if constexpr (decltype(more)::value) fetch(there, std::integral_constant<int, (S + 2) % kSteps>());
+      };
+      if constexpr (kSteps > 2) ahead();                  // with two steps a block the step after next has this step's registers
       if constexpr (EXACT) {
         if constexpr (I == 0) {
 #pragma unroll
@@ -184,15 +180,16 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile_kernel(const Pro
         }
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const bf16x8_t bv = widen(b[S % 4], q, scale_value(en[I]));
+          const bf16x8_t bv = widen(b[S % kRing], q, scale_value(en[I]));
 #pragma unroll
           for (int j = 0; j < FM; ++j) sum[I][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bv, wide[j][q], sum[I][j], 0, 0, 0);
         }
       } else {
 #pragma unroll
         for (int j = 0; j < FM; ++j)
-          sum[I][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b[S % 4], a[H][j], sum[I][j], 0, 0, 0, (int)en[I], 0, (int)em[j]);
+          sum[I][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b[S % kRing], a[H][j], sum[I][j], 0, 0, 0, (int)en[I], 0, (int)em[j]);
       }
+      if constexpr (kSteps == 2) ahead();
     });
     __builtin_amdgcn_sched_barrier(0);
     if constexpr (decltype(more)::value) {
@@ -327,71 +324,47 @@ __global__ __launch_bounds__(256) void join_kernel(const ProductParams p, int pa
   }
 }
 
-template <int TM, int TN, int WM, int WN, int STAGES>
+// a tile with results of type T
+template <typename T, int TM, int TN, int WM, int WN, int STAGES>
 hipError_t tiles(const ProductParams& p, int parts, hipStream_t s) {
-  if (parts == 1) return p.bf16 ? tile_launch<TM, TN, WM, WN, STAGES, false, bf16>(p, 1, s) : tile_launch<TM, TN, WM, WN, STAGES, true, float>(p, 1, s);
+  constexpr bool exact = sizeof(T) == 4;
+  if (parts == 1) return tile_launch<TM, TN, WM, WN, STAGES, exact, T>(p, 1, s);
   ProductParams q = p;
   q.y = p.partial;
   q.y_stride = p.N;
   q.bias = nullptr;
   q.wide_stores = p.N % 4 == 0;
-  const hipError_t e = p.bf16 ? tile_launch<TM, TN, WM, WN, STAGES, false, float>(q, parts, s) : tile_launch<TM, TN, WM, WN, STAGES, true, float>(q, parts, s);
+  const hipError_t e = tile_launch<TM, TN, WM, WN, STAGES, exact, float>(q, parts, s);
   if (e != hipSuccess) return e;
   const bool vec = p.N % 4 == 0 && p.wide_stores;
   const int64_t work = (p.M * ((p.N + 3) / 4) + 255) / 256;
   const dim3 grid((unsigned)(work < 8192 ? work : 8192));
-  if (p.bf16 && vec) hipLaunchKernelGGL((join_kernel<bf16, true>), grid, dim3(256), 0, s, p, parts);
-  else if (p.bf16) hipLaunchKernelGGL((join_kernel<bf16, false>), grid, dim3(256), 0, s, p, parts);
-  else if (vec) hipLaunchKernelGGL((join_kernel<float, true>), grid, dim3(256), 0, s, p, parts);
-  else hipLaunchKernelGGL((join_kernel<float, false>), grid, dim3(256), 0, s, p, parts);
+  if (vec) hipLaunchKernelGGL((join_kernel<T, true>), grid, dim3(256), 0, s, p, parts);
+  else hipLaunchKernelGGL((join_kernel<T, false>), grid, dim3(256), 0, s, p, parts);
   return hipGetLastError();
 }
 
-// The tile and the number of parts, by an estimate in microseconds: a launch, then for every round of workgroups a beginning and an end and the blocks
-// of columns of an item.  Fitted to products on 256 compute units, with one to four workgroups on each (bfloat16 and float32 results):
-//   256 x 256, 2 stages  16384 x 8192 x 4096 459 us, 8192 x 8192 x 256 37;         float32 8192 x 4096 x 8192 408
-//   128 x 128, 4 stages  4096^3 84, 1024 x 4096 x 4096 23, 1500^3 15.0;            float32 8192 x 4096 x 8192 540, 3200 x 500 x 3136 30, 1500^3 17.4
-//   128 x 128, 2 stages  4096^3 74, 1024 x 4096 x 4096 29, 1500^3 14.3;            float32 8192 x 4096 x 8192 474, 3200 x 500 x 3136 28, 1500^3 16.6
-//   64 x 64, 4 stages    4096^3 125, 256 x 4096 x 4096 12.8, 16 x 8192 x 4096 12;  float32 8192 x 4096 x 8192 837, 3200 x 500 x 3136 25.5, 1500^3 19.8
-//   64 x 64, 2 stages    256 x 4096 x 4096 12.1, 16 x 8192 x 4096 17, 1500^3 12.8; float32 3200 x 500 x 3136 25.1, 1500^3 15.4
-// Large tiles read less per product, small ones give more workgroups and shorter blocks; stages hide memory where few workgroups do.  Parts cost their
-// sums' way through memory: 128 x 3136 x 3200 float32 on tiles of 64 in one part 17 us, in two 14, in four 15; 16 x 8192 x 4096 12, 11, 11.
-struct Plan {
-  int tile, parts;
-};
-Plan choose_plan(int64_t M, int64_t N, int64_t K, int bf) {
-  struct Tile {
-    int size, shared;                // shared: workgroups that a compute unit takes
-    double ends, block[4];           // block: of a workgroup that shares its unit with none, one, two, three others
-  };
-  static constexpr Tile kTiles[2][5] = {{{256, 1, 6.0, {3.05}}, {128, 1, 3.0, {1.02}}, {128, 2, 3.0, {1.0, 1.8}}, {64, 2, 2.0, {0.58, 0.79}}, {64, 4, 2.0, {0.62, 0.77, 0.93, 1.25}}},
-                                        {{256, 1, 6.0, {1.6}}, {128, 1, 3.0, {0.56}}, {128, 2, 3.0, {0.7, 1.07}}, {64, 2, 2.0, {0.3, 0.45}}, {64, 4, 2.0, {0.33, 0.47, 0.65, 0.85}}}};
-  const int64_t blocks = (K + kBlock - 1) / kBlock;
-  Plan best = {0, 1};
-  double least = 1e300;
-  for (int tile = 0; tile < 5; ++tile) {
-    const Tile& q = kTiles[bf != 0][tile];
-    const int64_t tiles = ((M + q.size - 1) / q.size) * ((N + q.size - 1) / q.size);
-    for (int parts : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
-      if (parts > 1 && (2 * parts > blocks || tiles * parts > 2 * kFittedUnits)) break;
-      const int64_t items = tiles * parts, whole = kFittedUnits * q.shared, left = items % whole;
-      const double each = (double)((blocks + parts - 1) / parts);
-      double us = (double)(items / whole) * (q.ends + each * q.block[q.shared - 1]);
-      if (left) us += q.ends + each * q.block[(left - 1) / kFittedUnits];
-      if (parts > 1) us += 4.5 + (double)M * (double)N * (8.0 * parts + (bf ? 2.0 : 4.0)) / 4e6;
-      if (us < least) {
-        least = us;
-        best = Plan{tile, parts};
-      }
-    }
+hipError_t launch_plan(const ProductPlan& plan, const ProductParams& p, hipStream_t s) {
+  if (p.bf16) switch (plan.tile) {
+    case 0: return tiles<bf16, 256, 256, 4, 2, 2>(p, plan.parts, s);
+    case 1: return tiles<bf16, 128, 128, 2, 2, 4>(p, plan.parts, s);
+    case 2: return tiles<bf16, 128, 128, 2, 2, 2>(p, plan.parts, s);
+    case 4: return tiles<bf16, 64, 64, 2, 1, 2>(p, plan.parts, s);
+    case 5: return tiles<bf16, 64, 64, 2, 1, 4>(p, plan.parts, s);
+    default: return tiles<bf16, 64, 64, 2, 2, 4>(p, plan.parts, s);
   }
-  return best;
+  switch (plan.tile) {
+    case 0: return tiles<float, 256, 256, 4, 2, 2>(p, plan.parts, s);
+    case 2: return tiles<float, 128, 128, 2, 2, 2>(p, plan.parts, s);
+    case 3: return tiles<float, 128, 64, 2, 2, 2>(p, plan.parts, s);
+    default: return tiles<float, 64, 64, 2, 2, 2>(p, plan.parts, s);
+  }
 }
 
-Plan plan_of(int64_t M, int64_t N, int64_t K, int bf) {
-  static thread_local PlanMemo<4, Plan> memo;      // a call asks twice, and the estimates take a microsecond
-  return *memo.of({(int)M, (int)N, (int)K, bf}, [&](Plan& q) {
-    q = choose_plan(M, N, K, bf);
+ProductPlan plan_of(int64_t M, int64_t N, int64_t K, int bf) {
+  static thread_local PlanMemo<4, ProductPlan> memo;      // a call asks twice, and the estimates take a microsecond
+  return *memo.of({(int)M, (int)N, (int)K, bf}, [&](ProductPlan& q) {
+    q = choose_product_plan(M, N, K, bf);
     return true;
   });
 }
@@ -399,21 +372,14 @@ Plan plan_of(int64_t M, int64_t N, int64_t K, int bf) {
 }  // namespace
 
 size_t product_workspace(int64_t M, int64_t N, int64_t K, int bf) {
-  const Plan plan = plan_of(M, N, K, bf);
+  const ProductPlan plan = plan_of(M, N, K, bf);
   return plan.parts > 1 ? (size_t)plan.parts * (size_t)M * (size_t)N * sizeof(float) : 0;
 }
 
 hipError_t product_launch(const ProductParams& given, hipStream_t s) {
   ProductParams p = given;
   p.wide_stores = rows_aligned(p.y, p.y_stride, p.bf16 ? 2 : 4);
-  const Plan plan = plan_of(p.M, p.N, p.K, p.bf16);
-  switch (plan.tile) {
-    case 0: return tiles<256, 256, 4, 2, 2>(p, plan.parts, s);
-    case 1: return tiles<128, 128, 2, 2, 4>(p, plan.parts, s);
-    case 2: return tiles<128, 128, 2, 2, 2>(p, plan.parts, s);
-    case 3: return tiles<64, 64, 2, 1, 4>(p, plan.parts, s);
-    default: return tiles<64, 64, 2, 1, 2>(p, plan.parts, s);
-  }
+  return launch_plan(plan_of(p.M, p.N, p.K, p.bf16), p, s);
 }
 
 }  // namespace tac
