@@ -111,6 +111,12 @@ __device__ __forceinline__ void four_values(uint32_t codes, float (&v)[4]) {
   v[3] = hi[1];
 }
 
+// eight codes of a row
+__device__ __forceinline__ void store_codes(uint8_t* to, const float (&v)[8], float inv) {
+  *reinterpret_cast<u32x2_t*>(to) = u32x2_t{four_codes(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv),
+                                            four_codes(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv)};
+}
+
 // largest over 16 consecutive lanes, and sum over a wave; every lane gets it.  Within 16 lanes by rotation (one instruction each, no LDS).
 template <int BY>
 __device__ __forceinline__ float rotated(float v) {
@@ -122,13 +128,21 @@ __device__ __forceinline__ float max_over_16(float v) {
   v = fmaxf(v, rotated<2>(v));
   return fmaxf(v, rotated<1>(v));
 }
+// v of this lane and of those 16, 32 and 48 further: two swaps of lane rows bring the two of a pair (v_permlane16_swap, v_permlane32_swap)
+template <class F>
+__device__ __forceinline__ float over_rows(float v, F f) {
+  auto r = __builtin_amdgcn_permlane16_swap(float_bits(v), float_bits(v), false, false);
+  v = f(bits_float(r[0]), bits_float(r[1]));
+  r = __builtin_amdgcn_permlane32_swap(float_bits(v), float_bits(v), false, false);
+  return f(bits_float(r[0]), bits_float(r[1]));
+}
+__device__ __forceinline__ float max_over_rows(float v) { return over_rows(v, [](float a, float b) { return fmaxf(a, b); }); }
 __device__ __forceinline__ float sum_over_wave(float v) {
   v += rotated<8>(v);
   v += rotated<4>(v);
   v += rotated<2>(v);
   v += rotated<1>(v);
-  v += __shfl_xor(v, 16);
-  return v + __shfl_xor(v, 32);
+  return over_rows(v, [](float a, float b) { return a + b; });
 }
 
 // whether every row of a matrix starts at a multiple of 16 bytes

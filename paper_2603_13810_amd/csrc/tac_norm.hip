@@ -84,11 +84,8 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(const N
         }
         const uint32_t byte = scale_byte(max_over_16(amax));
         const float inv = scale_inverse(byte);
-        if (c < pitch)
-          *reinterpret_cast<u32x2_t*>(p.codes + row * pitch + c) =
-              u32x2_t{four_codes(v[q][0] * inv, v[q][1] * inv, v[q][2] * inv, v[q][3] * inv),
-                      four_codes(v[q][4] * inv, v[q][5] * inv, v[q][6] * inv, v[q][7] * inv)};
-        if (lane % 16 == 0 && c / kBlock < spitch) p.scales[row * spitch + c / kBlock] = (uint8_t)byte;
+        if (c < pitch) store_codes(p.codes + row * pitch + c, v[q], inv);
+      if (lane % 16 == 0 && c / kBlock < spitch) p.scales[row * spitch + c / kBlock] = (uint8_t)byte;
       }
     }
   }
