@@ -176,15 +176,21 @@ def tac_prepared_weight_bytes(desc: tac_layer_desc_t) -> int:
 
 # The two below run up to seven times per call: plain integers for the void* arguments, and the current stream's handle without a
 # Stream object (1.0 us) where torch has the function that gives it.
+_here = None            # torch's current device and that device's current stream
+
+
 def _stream(stream=None):
+    global _here
     if stream is not None:
         return int(stream)
-    import torch
-    try:
-        handle = torch._C._cuda_getCurrentRawStream
-    except AttributeError:
-        return torch.cuda.current_stream().cuda_stream
-    return handle(torch.cuda.current_device())
+    if _here is None:
+        import torch
+        torch.cuda.current_device()                  # torch's own set-up, once
+        try:
+            _here = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+        except AttributeError:
+            _here = (lambda device: torch.cuda.current_stream(device).cuda_stream), torch.cuda.current_device
+    return _here[0](_here[1]())
 
 
 def _dev_ptr(t, dtype=None, name="tensor"):
@@ -597,15 +603,24 @@ def _matrix_at(codes, scales, rows, cols, name):
             _shaped(scales, torch.uint8, name + " scales", rows, -(-cols // 512) * 4))
 
 
-def _workspace(nbytes, like, stream):
-    """Scratch for one call.  It is torch's again when the call has been enqueued, so a stream of the caller's own is told to torch's allocator."""
+def _on(stream, call):
+    """`call` with `stream` as torch's current one: what it allocates then belongs to that stream, and no block comes back to work that is still
+    reading it on another."""
     import torch
-    if not nbytes:
-        return None
-    w = like.new_empty(nbytes, dtype=torch.uint8)
-    if stream is not None and int(stream) != torch.cuda.current_stream(like.device).cuda_stream:
-        w.record_stream(torch.cuda.ExternalStream(int(stream), device=like.device))
-    return w
+    with torch.cuda.stream(torch.cuda.ExternalStream(int(stream))):
+        return call()
+
+
+def _new_like(t, shape):
+    """A new contiguous tensor of t's type, shape and device (the shorter way where t is contiguous itself)."""
+    import torch
+    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(shape)
+
+
+def _workspace(nbytes, like):
+    """Scratch for one call, torch's again when the call has been enqueued on the current stream."""
+    import torch
+    return like.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
 
 
 def tac_code_bytes(rows, cols) -> int:
@@ -620,6 +635,8 @@ def tac_quantize(src, *, cols=None, tiles=False, rows=True, columns=False, strea
     """A matrix to 8 bits.  src: float32 / bfloat16 [R, C] with a contiguous last axis, or an 8-bit matrix (codes, scales) of `cols`
     columns.  tiles: one scale per 128 x 128 instead of per row and 128 columns.  Returns dict(rows, columns) of 8-bit matrices:
     `rows` is src itself, `columns` its transpose [C, R] (None where not asked for)."""
+    if stream is not None:
+        return _on(stream, lambda: tac_quantize(src, cols=cols, tiles=tiles, rows=rows, columns=columns))
     scaled = isinstance(src, (tuple, list))
     t = src[0] if scaled else src
     if t.dim() != 2 or (scaled and cols is None):
@@ -635,12 +652,14 @@ def tac_quantize(src, *, cols=None, tiles=False, rows=True, columns=False, strea
     turned = _new_matrix(C, R, t) if columns else None
     to = (straight[0].data_ptr(), straight[1].data_ptr()) if rows else (None, None)
     to_t = (turned[0].data_ptr(), turned[1].data_ptr()) if columns else (None, None)
-    _check(lib().tac_quantize(ctypes.addressof(desc), at, at_scales, to[0], to[1], to_t[0], to_t[1], _stream(stream)))
+    _check(lib().tac_quantize(ctypes.addressof(desc), at, at_scales, to[0], to[1], to_t[0], to_t[1], _stream()))
     return dict(rows=straight, columns=turned)
 
 
 def tac_dequantize(matrix, cols, *, dtype=None, out=None, stream=None):
     """The values of an 8-bit matrix (codes, scales) of `cols` columns, float32 (or `dtype`, or into `out`)."""
+    if stream is not None:
+        return _on(stream, lambda: tac_dequantize(matrix, cols, dtype=dtype, out=out))
     import torch
     R = matrix[0].shape[0]
     if out is None:
@@ -648,7 +667,7 @@ def tac_dequantize(matrix, cols, *, dtype=None, out=None, stream=None):
     codes, scales = _matrix_at(matrix[0], matrix[1], R, cols, "matrix")
     kind = _float_type(out, "out")
     to, stride = _rows_of(out, "out", out.dtype, (R, cols))
-    _check(lib().tac_dequantize(R, cols, codes, scales, kind, to, stride, _stream(stream)))
+    _check(lib().tac_dequantize(R, cols, codes, scales, kind, to, stride, _stream()))
     return out
 
 
@@ -657,6 +676,9 @@ def tac_residual_norm(x, residual=None, gain=None, *, eps, h=None, y=None, want_
     """y = rms_norm(x + residual) gain over rows.  x: float32 / bfloat16 [R, C] with a contiguous last axis; gain: float32 [C].
     want_h: the sum x + residual (as it is where there is a residual).  Returns dict(h, y, scaled, rstd), `scaled` an 8-bit matrix of y;
     what is not asked for is None.  h and y may be given (h may be x or residual)."""
+    if stream is not None:
+        return _on(stream, lambda: tac_residual_norm(x, residual, gain, eps=eps, h=h, y=y, want_h=want_h, want_y=want_y,
+                                                      want_scaled=want_scaled, want_rstd=want_rstd))
     import torch
     shape, dtype = x.shape, x.dtype
     if len(shape) != 2:
@@ -668,14 +690,14 @@ def tac_residual_norm(x, residual=None, gain=None, *, eps, h=None, y=None, want_
     if h is not None:
         h_at, h_stride = _rows_of(h, "h", dtype, shape)
     elif residual is not None if want_h is None else want_h:
-        h = x.new_empty(shape)
+        h = _new_like(x, shape)
         h_at, h_stride = h.data_ptr(), C
     else:
         h_at, h_stride = None, 0
     if y is not None:
         y_at, y_stride = _rows_of(y, "y", dtype, shape)
     elif want_y:
-        y = x.new_empty(shape)
+        y = _new_like(x, shape)
         y_at, y_stride = y.data_ptr(), C
     else:
         y_at, y_stride = None, 0
@@ -688,15 +710,17 @@ def tac_residual_norm(x, residual=None, gain=None, *, eps, h=None, y=None, want_
         rstd_at = rstd.data_ptr()
     desc = tac_norm_desc_t(R, x_stride, r_stride, h_stride, y_stride, C, kind, eps)
     status = lib().tac_residual_norm(ctypes.addressof(desc), x_at, r_at, _shaped(gain, torch.float32, "gain", C), h_at, y_at, codes, scales,
-                                     rstd_at, _stream(stream))
+                                     rstd_at, _stream())
     if status:
         _check(status)
-    return dict(h=h, y=y, scaled=scaled, rstd=rstd)
+    return {"h": h, "y": y, "scaled": scaled, "rstd": rstd}
 
 
 def tac_residual_norm_backward(h, gain, rstd, grad_y, grad_h=None, *, grad_x=None, want_grad_gain=True, stream=None):
     """Backward pass of tac_residual_norm from the stream h and the rstd it stored.  Returns dict(grad_x, grad_gain); grad_x is the
     gradient of x and of the residual, and may be given (also grad_y or grad_h)."""
+    if stream is not None:
+        return _on(stream, lambda: tac_residual_norm_backward(h, gain, rstd, grad_y, grad_h, grad_x=grad_x, want_grad_gain=want_grad_gain))
     import torch
     shape, dtype = h.shape, h.dtype
     if len(shape) != 2:
@@ -704,7 +728,7 @@ def tac_residual_norm_backward(h, gain, rstd, grad_y, grad_h=None, *, grad_x=Non
     R, C = shape
     kind = _float_type(h, "h")
     if grad_x is None:
-        grad_x = h.new_empty(shape)
+        grad_x = _new_like(h, shape)
     h_at, h_stride = _rows_of(h, "h", dtype, shape)
     gy_at, gy_stride = _rows_of(grad_y, "grad_y", dtype, shape)
     gh_at, gh_stride = _rows_of(grad_h, "grad_h", dtype, shape)
@@ -714,15 +738,17 @@ def tac_residual_norm_backward(h, gain, rstd, grad_y, grad_h=None, *, grad_x=Non
     grad_gain = work = None
     if want_grad_gain:
         grad_gain = h.new_empty((C,), dtype=torch.float32)
-        work = _workspace(lib().tac_residual_norm_workspace_bytes(at), h, stream)
+        work = _workspace(lib().tac_residual_norm_workspace_bytes(at), h)
     _check(lib().tac_residual_norm_backward(
         at, h_at, _shaped(gain, torch.float32, "gain", C), _shaped(rstd, torch.float32, "rstd", R), gy_at, gh_at, gx_at,
-        None if grad_gain is None else grad_gain.data_ptr(), None if work is None else work.data_ptr(), _stream(stream)))
+        None if grad_gain is None else grad_gain.data_ptr(), None if work is None else work.data_ptr(), _stream()))
     return dict(grad_x=grad_x, grad_gain=grad_gain)
 
 
 def tac_scaled_product(a_codes, a_scales, b_codes, b_scales, K, *, bias=None, dtype=None, out=None, stream=None):
     """a b^T (+ bias) of the 8-bit matrices a [M, K] and b [N, K], in bfloat16 (or `dtype`, or into `out` [M, N])."""
+    if stream is not None:
+        return _on(stream, lambda: tac_scaled_product(a_codes, a_scales, b_codes, b_scales, K, bias=bias, dtype=dtype, out=out))
     import torch
     M, N = a_codes.shape[0], b_codes.shape[0]
     a_at, as_at = _matrix_at(a_codes, a_scales, M, K, "a")
@@ -733,9 +759,9 @@ def tac_scaled_product(a_codes, a_scales, b_codes, b_scales, K, *, bias=None, dt
     y_at, y_stride = _rows_of(out, "out", out.dtype, (M, N))
     desc = tac_product_desc_t(M, N, K, y_stride, kind)
     at, L = ctypes.addressof(desc), lib()
-    work = _workspace(L.tac_scaled_product_workspace_bytes(at), a_codes, stream)
+    work = _workspace(L.tac_scaled_product_workspace_bytes(at), a_codes)
     status = L.tac_scaled_product(at, a_at, as_at, b_at, bs_at, _shaped(bias, torch.float32, "bias", N), y_at,
-                                  None if work is None else work.data_ptr(), _stream(stream))
+                                  None if work is None else work.data_ptr(), _stream())
     if status:
         _check(status)
     return out
@@ -751,6 +777,8 @@ def tac_gated_scan(gate, value, *, lengths=None, h0=None, out=None, want_h_last=
     """h_t = a_t h_{t-1} + (1 - a_t) value_t with a = sigmoid(gate).  gate, value: float32 / bfloat16 [T, B, D] of the same strides, the
     last axis contiguous; lengths: int32 [B]; h0: float32 [B, D].  Returns dict(out, h_last, states); `states` is what the backward
     pass needs."""
+    if stream is not None:
+        return _on(stream, lambda: tac_gated_scan(gate, value, lengths=lengths, h0=h0, out=out, want_h_last=want_h_last, want_states=want_states))
     import torch
     shape, dtype, f32 = gate.shape, gate.dtype, torch.float32
     if len(shape) != 3:
@@ -761,17 +789,17 @@ def tac_gated_scan(gate, value, *, lengths=None, h0=None, out=None, want_h_last=
     v_at, v_strides = _steps_of(value, "value", dtype, shape)
     _same_strides(strides, v_strides, shape, "gate and value")
     if out is None:
-        out = gate.new_empty(shape)
+        out = gate.new_empty(tuple(shape))
     o_at, o_strides = _steps_of(out, "out", dtype, shape)
     h_last = gate.new_empty((B, D), dtype=f32) if want_h_last else None
     states = gate.new_empty((-(-T // TAC_SCAN_CHUNK), B, D), dtype=f32) if want_states else None
     desc = tac_scan_desc_t(T, B, D, strides[0], strides[1], o_strides[0], o_strides[1], 0, 0, kind)
     at, L = ctypes.addressof(desc), lib()
-    work = _workspace(L.tac_gated_scan_workspace_bytes(at), gate, stream)
+    work = _workspace(L.tac_gated_scan_workspace_bytes(at), gate)
     _check(L.tac_gated_scan(
         at, g_at, v_at, _shaped(lengths, torch.int32, "lengths", B), _shaped(h0, f32, "h0", B, D), o_at,
         None if h_last is None else h_last.data_ptr(), None if states is None else states.data_ptr(),
-        None if work is None else work.data_ptr(), _stream(stream)))
+        None if work is None else work.data_ptr(), _stream()))
     return dict(out=out, h_last=h_last, states=states)
 
 
@@ -779,6 +807,9 @@ def tac_gated_scan_backward(gate, value, states, grad_out, *, lengths=None, grad
                             want_grad_h0=True, stream=None):
     """Backward pass of tac_gated_scan from its inputs and `states`.  Returns dict(grad_gate, grad_value, grad_h0); the first two may be
     given (of the same strides as each other)."""
+    if stream is not None:
+        return _on(stream, lambda: tac_gated_scan_backward(gate, value, states, grad_out, lengths=lengths, grad_h_last=grad_h_last,
+                                                            grad_gate=grad_gate, grad_value=grad_value, want_grad_h0=want_grad_h0))
     import torch
     shape, dtype, f32 = gate.shape, gate.dtype, torch.float32
     if len(shape) != 3:
@@ -786,7 +817,7 @@ def tac_gated_scan_backward(gate, value, states, grad_out, *, lengths=None, grad
     T, B, D = shape
     kind = _float_type(gate, "gate")
     if grad_gate is None:
-        grad_gate = gate.new_empty(shape)
+        grad_gate = gate.new_empty(tuple(shape))
     if grad_value is None:
         grad_value = torch.empty_strided(shape, grad_gate.stride(), dtype=dtype, device=gate.device)
     grad_h0 = gate.new_empty((B, D), dtype=f32) if want_grad_h0 else None
@@ -799,11 +830,11 @@ def tac_gated_scan_backward(gate, value, states, grad_out, *, lengths=None, grad
     _same_strides(gg_strides, gv_strides, shape, "grad_gate and grad_value")
     desc = tac_scan_desc_t(T, B, D, strides[0], strides[1], go_strides[0], go_strides[1], gg_strides[0], gg_strides[1], kind)
     at, L = ctypes.addressof(desc), lib()
-    work = _workspace(L.tac_gated_scan_workspace_bytes(at), gate, stream)
+    work = _workspace(L.tac_gated_scan_workspace_bytes(at), gate)
     _check(L.tac_gated_scan_backward(
         at, g_at, v_at, _shaped(lengths, torch.int32, "lengths", B), _shaped(states, f32, "states", -(-T // TAC_SCAN_CHUNK), B, D),
         go_at, _shaped(grad_h_last, f32, "grad_h_last", B, D), gg_at, gv_at, None if grad_h0 is None else grad_h0.data_ptr(),
-        None if work is None else work.data_ptr(), _stream(stream)))
+        None if work is None else work.data_ptr(), _stream()))
     return dict(grad_gate=grad_gate, grad_value=grad_value, grad_h0=grad_h0)
 
 
@@ -811,6 +842,8 @@ def tac_gated_step(gate, value, pool, slots=None, *, out=None, stream=None):
     """One step of tac_gated_scan for B running sequences whose states stand in `pool` (float32 [slots, D], updated in place).  gate,
     value: [B, D]; slots: int32 [B], each slot at most once, outside the pool for rows without a sequence; None: row b has slot b.
     Returns out [B, D]."""
+    if stream is not None:
+        return _on(stream, lambda: tac_gated_step(gate, value, pool, slots, out=out))
     import torch
     shape, dtype = gate.shape, gate.dtype
     if len(shape) != 2 or pool.dim() != 2:
@@ -822,12 +855,12 @@ def tac_gated_step(gate, value, pool, slots=None, *, out=None, stream=None):
     if stride != v_stride:
         raise ValueError("gate and value must have the same strides")
     if out is None:
-        out = gate.new_empty(shape)
+        out = gate.new_empty(tuple(shape))
     o_at, o_stride = _rows_of(out, "out", dtype, shape)
     n_slots = pool.shape[0]
     desc = tac_scan_desc_t(1, B, D, 0, stride, 0, o_stride, 0, 0, kind)
     status = lib().tac_gated_step(ctypes.addressof(desc), g_at, v_at, _shaped(pool, torch.float32, "pool", n_slots, D), n_slots,
-                                  _shaped(slots, torch.int32, "slots", B), o_at, _stream(stream))
+                                  _shaped(slots, torch.int32, "slots", B), o_at, _stream())
     if status:
         _check(status)
     return out
