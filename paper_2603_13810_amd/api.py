@@ -176,21 +176,15 @@ def tac_prepared_weight_bytes(desc: tac_layer_desc_t) -> int:
 
 # The two below run up to seven times per call: plain integers for the void* arguments, and the current stream's handle without a
 # Stream object (1.0 us) where torch has the function that gives it.
-_here = None            # torch's current device and that device's current stream
-
-
 def _stream(stream=None):
-    global _here
     if stream is not None:
         return int(stream)
-    if _here is None:
-        import torch
-        torch.cuda.current_device()                  # torch's own set-up, once
-        try:
-            _here = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
-        except AttributeError:
-            _here = (lambda device: torch.cuda.current_stream(device).cuda_stream), torch.cuda.current_device
-    return _here[0](_here[1]())
+    import torch
+    try:
+        handle = torch._C._cuda_getCurrentRawStream
+    except AttributeError:
+        return torch.cuda.current_stream().cuda_stream
+    return handle(torch.cuda.current_device())
 
 
 def _dev_ptr(t, dtype=None, name="tensor"):
