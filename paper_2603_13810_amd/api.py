@@ -539,62 +539,28 @@ class tac_scan_desc_t(ctypes.Structure):
                 ("grad_stride_t", ctypes.c_int64), ("grad_stride_b", ctypes.c_int64), ("dtype", ctypes.c_int32)]
 
 
-_TYPES = None           # TAC_FP32 / TAC_BF16 of torch's types
+_operators = None
 
 
-def _float_type(t, name) -> int:
-    global _TYPES
-    if _TYPES is None:
-        import torch
-        _TYPES = {torch.float32: TAC_FP32, torch.bfloat16: TAC_BF16}
-    try:
-        return _TYPES[t.dtype]
-    except KeyError:
-        raise ValueError("%s must be float32 or bfloat16" % name) from None
+def _native():
+    """The module whose functions check, allocate and launch (csrc/tac_torch.cpp): small calls are bound by what happens on the host."""
+    global _operators
+    if _operators is None:
+        import torch  # noqa: F401  (the module is linked against torch's libraries)
+        lib()
+        try:
+            from . import _operators as module
+        except ImportError as e:
+            raise RuntimeError("the operators' module has not been built: %s" % e) from None
+        _operators = module
+    return _operators
 
 
-# Small calls are bound by what happens here, so a tensor is looked at once: address and strides come from one check.
-def _rows_of(t, name, dtype, shape):
-    """Address and row stride of a device matrix of this type and shape whose rows are contiguous; (None, 0) for None."""
-    if t is None:
-        return None, 0
-    if t.shape != shape or t.dtype != dtype or not t.is_cuda:
-        raise ValueError("%s must be a device tensor %s of %s" % (name, list(shape), dtype))
-    stride = t.stride()
-    if stride[1] != 1 and shape[1] > 1:
-        raise ValueError("%s must have a contiguous last axis" % name)
-    return t.data_ptr(), stride[0] if shape[0] > 1 else shape[1]       # a matrix of one row has no stride that matters
-
-
-def _steps_of(t, name, dtype, shape):
-    """Address and strides of a device sequence [T, B, D] whose last axis is contiguous."""
-    if t.shape != shape or t.dtype != dtype or not t.is_cuda:
-        raise ValueError("%s must be a device tensor %s of %s" % (name, list(shape), dtype))
-    stride = t.stride()
-    if stride[2] != 1 and shape[2] > 1:
-        raise ValueError("%s must have a contiguous last axis" % name)
-    return t.data_ptr(), stride
-
-
-def _shaped(t, dtype, name, *shape):
-    """Address of a contiguous device tensor of this type and shape, or None."""
-    if t is None:
-        return None
-    if t.shape != shape or t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous device tensor %s of %s" % (name, list(shape), dtype))
-    return t.data_ptr()
-
-
-def _new_matrix(rows, cols, like):
-    """A new 8-bit matrix on `like`'s device."""
-    import torch
-    return (like.new_empty((rows, -(-cols // 128) * 128), dtype=torch.uint8), like.new_empty((rows, -(-cols // 512) * 4), dtype=torch.uint8))
-
-
-def _matrix_at(codes, scales, rows, cols, name):
-    import torch
-    return (_shaped(codes, torch.uint8, name + " codes", rows, -(-cols // 128) * 128),
-            _shaped(scales, torch.uint8, name + " scales", rows, -(-cols // 512) * 4))
+def _result(r):
+    """What a native call returns, or the error of the status it returns instead."""
+    if type(r) is int:
+        _check(r)
+    return r
 
 
 def _on(stream, call):
@@ -603,18 +569,6 @@ def _on(stream, call):
     import torch
     with torch.cuda.stream(torch.cuda.ExternalStream(int(stream))):
         return call()
-
-
-def _new_like(t, shape):
-    """A new contiguous tensor of t's type, shape and device (the shorter way where t is contiguous itself)."""
-    import torch
-    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(shape)
-
-
-def _workspace(nbytes, like):
-    """Scratch for one call, torch's again when the call has been enqueued on the current stream."""
-    import torch
-    return like.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
 
 
 def tac_code_bytes(rows, cols) -> int:
@@ -631,38 +585,18 @@ def tac_quantize(src, *, cols=None, tiles=False, rows=True, columns=False, strea
     `rows` is src itself, `columns` its transpose [C, R] (None where not asked for)."""
     if stream is not None:
         return _on(stream, lambda: tac_quantize(src, cols=cols, tiles=tiles, rows=rows, columns=columns))
-    scaled = isinstance(src, (tuple, list))
-    t = src[0] if scaled else src
-    if t.dim() != 2 or (scaled and cols is None):
-        raise ValueError("src must be a matrix, and an 8-bit one needs its number of columns")
-    if scaled:
-        R, C, kind, stride = t.shape[0], int(cols), TAC_SCALED, 0
-        at, at_scales = _matrix_at(t, src[1], R, C, "src")
-    else:
-        (R, C), kind, at_scales = t.shape, _float_type(t, "src"), None
-        at, stride = _rows_of(t, "src", t.dtype, t.shape)
-    desc = tac_quantize_desc_t(R, C, stride, kind, TAC_BLOCK_TILE if tiles else TAC_BLOCK_ROW)
-    straight = _new_matrix(R, C, t) if rows else None
-    turned = _new_matrix(C, R, t) if columns else None
-    to = (straight[0].data_ptr(), straight[1].data_ptr()) if rows else (None, None)
-    to_t = (turned[0].data_ptr(), turned[1].data_ptr()) if columns else (None, None)
-    _check(lib().tac_quantize(ctypes.addressof(desc), at, at_scales, to[0], to[1], to_t[0], to_t[1], _stream()))
-    return dict(rows=straight, columns=turned)
+    if isinstance(src, (tuple, list)):
+        if cols is None:
+            raise ValueError("an 8-bit matrix needs its number of columns")
+        return _result(_native().quantize(src[0], src[1], cols, tiles, rows, columns))
+    return _result(_native().quantize(src, None, None, tiles, rows, columns))
 
 
 def tac_dequantize(matrix, cols, *, dtype=None, out=None, stream=None):
     """The values of an 8-bit matrix (codes, scales) of `cols` columns, float32 (or `dtype`, or into `out`)."""
     if stream is not None:
         return _on(stream, lambda: tac_dequantize(matrix, cols, dtype=dtype, out=out))
-    import torch
-    R = matrix[0].shape[0]
-    if out is None:
-        out = torch.empty((R, cols), dtype=dtype or torch.float32, device=matrix[0].device)
-    codes, scales = _matrix_at(matrix[0], matrix[1], R, cols, "matrix")
-    kind = _float_type(out, "out")
-    to, stride = _rows_of(out, "out", out.dtype, (R, cols))
-    _check(lib().tac_dequantize(R, cols, codes, scales, kind, to, stride, _stream()))
-    return out
+    return _result(_native().dequantize(matrix[0], matrix[1], cols, dtype, out))
 
 
 def tac_residual_norm(x, residual=None, gain=None, *, eps, h=None, y=None, want_h=None, want_y=True, want_scaled=False,
@@ -673,41 +607,7 @@ def tac_residual_norm(x, residual=None, gain=None, *, eps, h=None, y=None, want_
     if stream is not None:
         return _on(stream, lambda: tac_residual_norm(x, residual, gain, eps=eps, h=h, y=y, want_h=want_h, want_y=want_y,
                                                       want_scaled=want_scaled, want_rstd=want_rstd))
-    import torch
-    shape, dtype = x.shape, x.dtype
-    if len(shape) != 2:
-        raise ValueError("x must be a matrix")
-    R, C = shape
-    kind = _float_type(x, "x")
-    x_at, x_stride = _rows_of(x, "x", dtype, shape)
-    r_at, r_stride = _rows_of(residual, "residual", dtype, shape)
-    if h is not None:
-        h_at, h_stride = _rows_of(h, "h", dtype, shape)
-    elif residual is not None if want_h is None else want_h:
-        h = _new_like(x, shape)
-        h_at, h_stride = h.data_ptr(), C
-    else:
-        h_at, h_stride = None, 0
-    if y is not None:
-        y_at, y_stride = _rows_of(y, "y", dtype, shape)
-    elif want_y:
-        y = _new_like(x, shape)
-        y_at, y_stride = y.data_ptr(), C
-    else:
-        y_at, y_stride = None, 0
-    scaled = codes = scales = rstd = rstd_at = None
-    if want_scaled:
-        scaled = _new_matrix(R, C, x)
-        codes, scales = scaled[0].data_ptr(), scaled[1].data_ptr()
-    if want_rstd:
-        rstd = x.new_empty((R,), dtype=torch.float32)
-        rstd_at = rstd.data_ptr()
-    desc = tac_norm_desc_t(R, x_stride, r_stride, h_stride, y_stride, C, kind, eps)
-    status = lib().tac_residual_norm(ctypes.addressof(desc), x_at, r_at, _shaped(gain, torch.float32, "gain", C), h_at, y_at, codes, scales,
-                                     rstd_at, _stream())
-    if status:
-        _check(status)
-    return {"h": h, "y": y, "scaled": scaled, "rstd": rstd}
+    return _result(_native().residual_norm(x, residual, gain, eps, h, y, want_h, want_y, want_scaled, want_rstd))
 
 
 def tac_residual_norm_backward(h, gain, rstd, grad_y, grad_h=None, *, grad_x=None, want_grad_gain=True, stream=None):
@@ -715,56 +615,14 @@ def tac_residual_norm_backward(h, gain, rstd, grad_y, grad_h=None, *, grad_x=Non
     gradient of x and of the residual, and may be given (also grad_y or grad_h)."""
     if stream is not None:
         return _on(stream, lambda: tac_residual_norm_backward(h, gain, rstd, grad_y, grad_h, grad_x=grad_x, want_grad_gain=want_grad_gain))
-    import torch
-    shape, dtype = h.shape, h.dtype
-    if len(shape) != 2:
-        raise ValueError("h must be a matrix")
-    R, C = shape
-    kind = _float_type(h, "h")
-    if grad_x is None:
-        grad_x = _new_like(h, shape)
-    h_at, h_stride = _rows_of(h, "h", dtype, shape)
-    gy_at, gy_stride = _rows_of(grad_y, "grad_y", dtype, shape)
-    gh_at, gh_stride = _rows_of(grad_h, "grad_h", dtype, shape)
-    gx_at, gx_stride = _rows_of(grad_x, "grad_x", dtype, shape)
-    desc = tac_norm_desc_t(R, gx_stride, gh_stride, h_stride, gy_stride, C, kind, 1.0)
-    at = ctypes.addressof(desc)
-    grad_gain = work = None
-    if want_grad_gain:
-        grad_gain = h.new_empty((C,), dtype=torch.float32)
-        work = _workspace(lib().tac_residual_norm_workspace_bytes(at), h)
-    _check(lib().tac_residual_norm_backward(
-        at, h_at, _shaped(gain, torch.float32, "gain", C), _shaped(rstd, torch.float32, "rstd", R), gy_at, gh_at, gx_at,
-        None if grad_gain is None else grad_gain.data_ptr(), None if work is None else work.data_ptr(), _stream()))
-    return dict(grad_x=grad_x, grad_gain=grad_gain)
+    return _result(_native().residual_norm_backward(h, gain, rstd, grad_y, grad_h, grad_x, want_grad_gain))
 
 
 def tac_scaled_product(a_codes, a_scales, b_codes, b_scales, K, *, bias=None, dtype=None, out=None, stream=None):
     """a b^T (+ bias) of the 8-bit matrices a [M, K] and b [N, K], in bfloat16 (or `dtype`, or into `out` [M, N])."""
     if stream is not None:
         return _on(stream, lambda: tac_scaled_product(a_codes, a_scales, b_codes, b_scales, K, bias=bias, dtype=dtype, out=out))
-    import torch
-    M, N = a_codes.shape[0], b_codes.shape[0]
-    a_at, as_at = _matrix_at(a_codes, a_scales, M, K, "a")
-    b_at, bs_at = _matrix_at(b_codes, b_scales, N, K, "b")
-    if out is None:
-        out = a_codes.new_empty((M, N), dtype=dtype or torch.bfloat16)
-    kind = _float_type(out, "out")
-    y_at, y_stride = _rows_of(out, "out", out.dtype, (M, N))
-    desc = tac_product_desc_t(M, N, K, y_stride, kind)
-    at, L = ctypes.addressof(desc), lib()
-    work = _workspace(L.tac_scaled_product_workspace_bytes(at), a_codes)
-    status = L.tac_scaled_product(at, a_at, as_at, b_at, bs_at, _shaped(bias, torch.float32, "bias", N), y_at,
-                                  None if work is None else work.data_ptr(), _stream())
-    if status:
-        _check(status)
-    return out
-
-
-def _same_strides(a, b, shape, names):
-    """Strides of axes with more than one entry have to agree."""
-    if a != b and any(x != y for x, y, n in zip(a, b, shape) if n > 1):
-        raise ValueError("%s must have the same strides" % names)
+    return _result(_native().scaled_product(a_codes, a_scales, b_codes, b_scales, K, bias, dtype, out))
 
 
 def tac_gated_scan(gate, value, *, lengths=None, h0=None, out=None, want_h_last=True, want_states=False, stream=None):
@@ -773,28 +631,7 @@ def tac_gated_scan(gate, value, *, lengths=None, h0=None, out=None, want_h_last=
     pass needs."""
     if stream is not None:
         return _on(stream, lambda: tac_gated_scan(gate, value, lengths=lengths, h0=h0, out=out, want_h_last=want_h_last, want_states=want_states))
-    import torch
-    shape, dtype, f32 = gate.shape, gate.dtype, torch.float32
-    if len(shape) != 3:
-        raise ValueError("gate must be [T, B, D]")
-    T, B, D = shape
-    kind = _float_type(gate, "gate")
-    g_at, strides = _steps_of(gate, "gate", dtype, shape)
-    v_at, v_strides = _steps_of(value, "value", dtype, shape)
-    _same_strides(strides, v_strides, shape, "gate and value")
-    if out is None:
-        out = gate.new_empty(tuple(shape))
-    o_at, o_strides = _steps_of(out, "out", dtype, shape)
-    h_last = gate.new_empty((B, D), dtype=f32) if want_h_last else None
-    states = gate.new_empty((-(-T // TAC_SCAN_CHUNK), B, D), dtype=f32) if want_states else None
-    desc = tac_scan_desc_t(T, B, D, strides[0], strides[1], o_strides[0], o_strides[1], 0, 0, kind)
-    at, L = ctypes.addressof(desc), lib()
-    work = _workspace(L.tac_gated_scan_workspace_bytes(at), gate)
-    _check(L.tac_gated_scan(
-        at, g_at, v_at, _shaped(lengths, torch.int32, "lengths", B), _shaped(h0, f32, "h0", B, D), o_at,
-        None if h_last is None else h_last.data_ptr(), None if states is None else states.data_ptr(),
-        None if work is None else work.data_ptr(), _stream()))
-    return dict(out=out, h_last=h_last, states=states)
+    return _result(_native().gated_scan(gate, value, lengths, h0, out, want_h_last, want_states))
 
 
 def tac_gated_scan_backward(gate, value, states, grad_out, *, lengths=None, grad_h_last=None, grad_gate=None, grad_value=None,
@@ -804,32 +641,7 @@ def tac_gated_scan_backward(gate, value, states, grad_out, *, lengths=None, grad
     if stream is not None:
         return _on(stream, lambda: tac_gated_scan_backward(gate, value, states, grad_out, lengths=lengths, grad_h_last=grad_h_last,
                                                             grad_gate=grad_gate, grad_value=grad_value, want_grad_h0=want_grad_h0))
-    import torch
-    shape, dtype, f32 = gate.shape, gate.dtype, torch.float32
-    if len(shape) != 3:
-        raise ValueError("gate must be [T, B, D]")
-    T, B, D = shape
-    kind = _float_type(gate, "gate")
-    if grad_gate is None:
-        grad_gate = gate.new_empty(tuple(shape))
-    if grad_value is None:
-        grad_value = torch.empty_strided(shape, grad_gate.stride(), dtype=dtype, device=gate.device)
-    grad_h0 = gate.new_empty((B, D), dtype=f32) if want_grad_h0 else None
-    g_at, strides = _steps_of(gate, "gate", dtype, shape)
-    v_at, v_strides = _steps_of(value, "value", dtype, shape)
-    _same_strides(strides, v_strides, shape, "gate and value")
-    go_at, go_strides = _steps_of(grad_out, "grad_out", dtype, shape)
-    gg_at, gg_strides = _steps_of(grad_gate, "grad_gate", dtype, shape)
-    gv_at, gv_strides = _steps_of(grad_value, "grad_value", dtype, shape)
-    _same_strides(gg_strides, gv_strides, shape, "grad_gate and grad_value")
-    desc = tac_scan_desc_t(T, B, D, strides[0], strides[1], go_strides[0], go_strides[1], gg_strides[0], gg_strides[1], kind)
-    at, L = ctypes.addressof(desc), lib()
-    work = _workspace(L.tac_gated_scan_workspace_bytes(at), gate)
-    _check(L.tac_gated_scan_backward(
-        at, g_at, v_at, _shaped(lengths, torch.int32, "lengths", B), _shaped(states, f32, "states", -(-T // TAC_SCAN_CHUNK), B, D),
-        go_at, _shaped(grad_h_last, f32, "grad_h_last", B, D), gg_at, gv_at, None if grad_h0 is None else grad_h0.data_ptr(),
-        None if work is None else work.data_ptr(), _stream()))
-    return dict(grad_gate=grad_gate, grad_value=grad_value, grad_h0=grad_h0)
+    return _result(_native().gated_scan_backward(gate, value, states, grad_out, lengths, grad_h_last, grad_gate, grad_value, want_grad_h0))
 
 
 def tac_gated_step(gate, value, pool, slots=None, *, out=None, stream=None):
@@ -838,23 +650,4 @@ def tac_gated_step(gate, value, pool, slots=None, *, out=None, stream=None):
     Returns out [B, D]."""
     if stream is not None:
         return _on(stream, lambda: tac_gated_step(gate, value, pool, slots, out=out))
-    import torch
-    shape, dtype = gate.shape, gate.dtype
-    if len(shape) != 2 or pool.dim() != 2:
-        raise ValueError("gate must be [B, D] and pool [slots, D]")
-    B, D = shape
-    kind = _float_type(gate, "gate")
-    g_at, stride = _rows_of(gate, "gate", dtype, shape)
-    v_at, v_stride = _rows_of(value, "value", dtype, shape)
-    if stride != v_stride:
-        raise ValueError("gate and value must have the same strides")
-    if out is None:
-        out = gate.new_empty(tuple(shape))
-    o_at, o_stride = _rows_of(out, "out", dtype, shape)
-    n_slots = pool.shape[0]
-    desc = tac_scan_desc_t(1, B, D, 0, stride, 0, o_stride, 0, 0, kind)
-    status = lib().tac_gated_step(ctypes.addressof(desc), g_at, v_at, _shaped(pool, torch.float32, "pool", n_slots, D), n_slots,
-                                  _shaped(slots, torch.int32, "slots", B), o_at, _stream())
-    if status:
-        _check(status)
-    return out
+    return _result(_native().gated_step(gate, value, pool, slots, out))

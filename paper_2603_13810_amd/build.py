@@ -1,4 +1,4 @@
-"""Build libtac.so (HIP, gfx950 only) in-tree with hipcc."""
+"""Build libtac.so (HIP, gfx950 only) in-tree with hipcc, and the Python module that calls its dense operators."""
 from __future__ import annotations
 
 import os
@@ -9,6 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libtac.so")
+OPERATORS = os.path.join(HERE, "_operators.so")
 # the large matrix-core kernel is compiled in one translation unit per geometry (input width, stride) and trace variant,
 # so that its many instantiations build side by side; the slowest files come first
 SOURCES = ["tac_mfma_w64s1.hip", "tac_mfma_w64s1_trace.hip", "tac_mfma_w32s1.hip", "tac_mfma_w32s1_trace.hip",
@@ -56,7 +57,23 @@ def build(verbose: bool = True) -> str:
     tmp = LIB + ".tmp%d" % os.getpid()
     subprocess.check_call([hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp] + objs)
     os.replace(tmp, LIB)
+    build_operators()
     return LIB
+
+
+def build_operators() -> str:
+    """The Python module of the dense operators: host code alone, against torch's headers, linked to the library beside it."""
+    import sysconfig
+    import torch
+    at = os.path.dirname(torch.__file__)
+    tmp = OPERATORS + ".tmp%d" % os.getpid()
+    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+                           "-I", INCLUDE, "-isystem", os.path.join(at, "include"), "-isystem", os.path.join(at, "include/torch/csrc/api/include"),
+                           "-isystem", "/opt/rocm/include", "-isystem", sysconfig.get_paths()["include"], os.path.join(CSRC, "tac_torch.cpp"),
+                           "-o", tmp, "-L", os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-ltorch_hip", "-lc10", "-lc10_hip",
+                           "-L", HERE, "-ltac", "-Wl,-rpath,$ORIGIN"])
+    os.replace(tmp, OPERATORS)
+    return OPERATORS
 
 
 if __name__ == "__main__":
