@@ -74,7 +74,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile_kernel(const Pro
   constexpr int kWaves = WM * WN, FM = TM / WM / 32, FN = TN / WN / 32, kStage = (TM + TN) * kBlock;
   constexpr int kLoadsM = TM / 8 / kWaves, kLoadsN = TN / 8 / kWaves;         // a load instruction brings 8 rows
   static_assert(TM % (32 * WM) == 0 && TN % (32 * WN) == 0 && TM % (8 * kWaves) == 0 && TN % (8 * kWaves) == 0 && kWaves % 2 == 0);
-  static_assert((TM + TN) % 64 == 0 && TM + TN <= 64 * kWaves);
+  static_assert(TM + TN <= 64 * kWaves);
   constexpr int kScales = tile_scales_at(TM, TN, kWaves, STAGES), kLoads = kLoadsM + kLoadsN + 1;
   extern __shared__ __align__(1024) uint8_t stages[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave % WM, wn = wave / WM;
@@ -308,15 +308,17 @@ __global__ __launch_bounds__(256) void join_kernel(const ProductParams p, int pa
     float v[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) v[e] = p.bias ? p.bias[n + e] : 0.0f;
-    for (int part = 0; part < parts; ++part) {
-      const float* from = p.partial + ((int64_t)part * p.M + m) * p.N + n;
-      if constexpr (VEC) {
-        const f32x4_t t = *reinterpret_cast<const f32x4_t*>(from);
+    const float* from = p.partial + m * p.N + n;
+    for (int first = 0; first < parts; first += 8) {      // eight loads on their way, their sums in order
+      float t[8][E];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] += t[e];
-      } else {
-        v[0] += *from;
-      }
+      for (int q = 0; q < 8; ++q) load_floats<float, E, VEC>(from + min(first + q, parts - 1) * (p.M * p.N), E, t[q]);
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        if (first + q < parts) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) v[e] += t[q][e];
+        }
     }
     T* to = (T*)p.y + m * p.y_stride + n;
     if constexpr (VEC) store_floats<T, 4, true>(to, 4, v);
@@ -351,7 +353,8 @@ hipError_t launch_plan(const ProductPlan& plan, const ProductParams& p, hipStrea
     case 2: return tiles<bf16, 128, 128, 2, 2, 2>(p, plan.parts, s);
     case 4: return tiles<bf16, 64, 64, 2, 1, 2>(p, plan.parts, s);
     case 5: return tiles<bf16, 64, 64, 2, 1, 4>(p, plan.parts, s);
-    default: return tiles<bf16, 64, 64, 2, 2, 4>(p, plan.parts, s);
+    case 6: return tiles<bf16, 64, 64, 2, 2, 4>(p, plan.parts, s);
+    default: return tiles<bf16, 64, 32, 2, 1, 8>(p, plan.parts, s);
   }
   switch (plan.tile) {
     case 0: return tiles<float, 256, 256, 4, 2, 2>(p, plan.parts, s);

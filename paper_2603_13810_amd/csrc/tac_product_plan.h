@@ -23,13 +23,16 @@ constexpr int tile_lds(int TM, int TN, int waves, int STAGES) { return tile_scal
 //   64 x 64, 2 waves, 2 stages                 -     117                  31      17      13                 20                 12                17
 //   64 x 64, 2 waves, 4 stages               983     126                  34      20      17                 18                 13                12
 //   64 x 64, 4 waves, 4 stages                 -     152                  40      23      20                 21                 12                11
+//   64 x 32, 2 waves, 8 stages                 -       -                   -       -       -                 -                  -                 9
 //   float32 results          8192 x 4096 x 8192  2000 x 3000 x 1000  512 x 4096 x 4096  1500^3  3200 x 500 x 3136  128 x 3136 x 3200  500 x 700 x 900
 //   256 x 256, 8 waves                      408                   -                  -       -                 62                 58               24
 //   128 x 128, 2 stages                     474                  20                 33      17                 27                 25               12
 //   128 x 64                                  -                  19                 24      16                 18                 16                8
 //   64 x 64, 4 waves, 2 stages                -                  22                 26      15                 20                 12                6
 // Large tiles read less per product, small ones give more workgroups and shorter blocks; stages hide memory where few workgroups do.  Parts cost
-// their sums' way through memory: 128 x 3136 x 3200 in one part 12.0 us, in two 11.3; 16 x 8192 x 4096 10.8 and 10.2; 3200 x 500 x 3136 18 and 23.
+// their sums' way through memory: 128 x 3136 x 3200 in one part 12.0 us, in two 11.3; 3200 x 500 x 3136 18 and 23.
+// The last tile is for few rows, where the other matrix's bytes count: seven blocks on their way per compute unit. With it, weights from memory, bfloat16
+// results: 16 x 8192 x 4096 14.9 -> 11.9 us, 64 x 8192 x 4096 16.8 -> 13.4, 100 x 4096 x 4096 12.9 -> 11.0.
 struct ProductPlan {
   int tile, parts;
 };
@@ -44,7 +47,8 @@ constexpr ProductTile kProductTiles[] = {{256, 256, 1, 6.0, {{3.05}, {1.6}}},
                            {64, 64, 4, 2.0, {{}, {0.33, 0.47, 0.67, 0.85}}},
                            {64, 64, 2, 2.0, {{}, {0.3, 0.45}}},
                            {64, 64, 1, 2.0, {{}, {0.23}}},
-                           {64, 64, 3, 2.0, {{0.45, 0.64, 0.9}, {}}}};
+                           {64, 64, 3, 2.0, {{0.45, 0.64, 0.9}, {}}},
+                           {64, 32, 1, 2.0, {{}, {0.22}}}};
 
 inline ProductPlan choose_product_plan(int64_t M, int64_t N, int64_t K, int bf) {
   const int64_t blocks = (K + kBlock - 1) / kBlock;

@@ -17,7 +17,8 @@ CASES = [(0, 0, 5518, 2181, 266, 1, False), (0, 0, 6313, 3998, 279, 1, True), (0
          (1, 2, 1584, 2599, 267, 1, False), (1, 2, 6703, 2463, 283, 1, True), (1, 2, 5520, 140, 9678, 4, False),
          (1, 4, 6608, 263, 279, 1, False), (1, 4, 4611, 1674, 289, 1, True),
          (1, 5, 132, 5636, 281, 1, False), (1, 5, 1, 647, 10751, 32, False),
-         (1, 6, 46, 41, 262, 1, False), (1, 6, 1, 1, 2866, 8, False)]
+         (1, 6, 73, 4411, 263, 1, False), (1, 6, 1, 323, 6067, 24, False),
+         (1, 8, 46, 41, 262, 1, False), (1, 8, 33, 8170, 513, 1, False), (1, 8, 40, 700, 5000, 8, False)]
 
 
 def values(m, cols):

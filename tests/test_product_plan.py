@@ -11,7 +11,7 @@ from paper_2603_13810_amd import api, build
 from test_gpu_product_tiles import CASES
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-STAGES = {0: (8, 2), 1: (4, 4), 2: (4, 2), 3: (4, 2), 4: (2, 2), 5: (2, 4), 6: (4, 4), 7: (4, 2)}       # waves and stages of a tile
+STAGES = {0: (8, 2), 1: (4, 4), 2: (4, 2), 3: (4, 2), 4: (2, 2), 5: (2, 4), 6: (4, 4), 7: (4, 2), 8: (2, 8)}       # waves and stages of a tile
 
 
 @pytest.fixture(scope="module")
