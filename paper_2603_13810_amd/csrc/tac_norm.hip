@@ -28,7 +28,7 @@ __device__ __forceinline__ float row_sum(float v, float* room) {
   return v;
 }
 
-template <typename T, int LANES, int PASSES, bool VEC>
+template <typename T, int LANES, int PASSES, bool VEC, bool PAST>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(const NormParams p) {
   __shared__ float room[LANES / 64];
   const int lane = threadIdx.x % LANES;
@@ -57,7 +57,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(const N
   #pragma unroll
           for (int e = 0; e < kCols; ++e) v[q][e] += r[e];
         }
-        if (p.h) store_floats<T, kCols, VEC>((T*)p.h + row * p.h_stride + c, n, v[q]);
+        if (p.h) store_floats<T, kCols, VEC, PAST>((T*)p.h + row * p.h_stride + c, n, v[q]);
       } else {
   #pragma unroll
         for (int e = 0; e < kCols; ++e) v[q][e] = 0.0f;
@@ -74,7 +74,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(const N
       const int n = p.cols - c;
 #pragma unroll
       for (int e = 0; e < kCols; ++e) v[q][e] = v[q][e] * rstd * g[q][e];
-      if (p.y && n > 0) store_floats<T, kCols, VEC>((T*)p.y + row * p.y_stride + c, n, v[q]);
+      if (p.y && n > 0) store_floats<T, kCols, VEC, PAST>((T*)p.y + row * p.y_stride + c, n, v[q]);
       if (p.codes) {
         float amax = 0.0f;
   #pragma unroll
@@ -93,7 +93,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(const N
 
 // A workgroup takes rows blockIdx, blockIdx + gridDim, ...: a lane keeps its columns from row to row, so the sum over rows of
 // grad_y n stays in registers and leaves once per workgroup (partial [workgroup][cols]); gain_sum_kernel adds those up in their order.
-template <typename T, int LANES, int PASSES, bool VEC>
+template <typename T, int LANES, int PASSES, bool VEC, bool PAST>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_backward_kernel(const NormBackwardParams p) {
   constexpr int kRows = LANES < 256 ? 256 / LANES : 1;      // rows that a workgroup has in hand
   __shared__ float room[LANES / 64];
@@ -147,7 +147,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_backward_kerne
         }
 #pragma unroll
         for (int e = 0; e < kCols; ++e) g[e] = fmaf(rstd, w[q][e] - n[q][e] * mean, g[e]);
-        store_floats<T, kCols, VEC>((T*)p.grad_x + row * p.grad_x_stride + c, left, g);
+        store_floats<T, kCols, VEC, PAST>((T*)p.grad_x + row * p.grad_x_stride + c, left, g);
       }
     }
   }
@@ -217,23 +217,23 @@ int64_t backward_groups(int64_t rows, int cols) {
   return units < 1024 ? units : 1024;
 }
 
-template <typename T, bool VEC>
+template <typename T, bool VEC, bool PAST>
 hipError_t norm_typed(const NormParams& p, hipStream_t s) {
   return by_columns(p.cols, [&](auto lanes, auto passes) {
     constexpr int L = decltype(lanes)::value, P = decltype(passes)::value;
     constexpr int threads = L < 256 ? 256 : L, rows = threads / L;
     const int64_t groups = (p.rows + rows - 1) / rows;
-    hipLaunchKernelGGL((norm_kernel<T, L, P, VEC>), dim3((unsigned)(groups < kMostGroups ? groups : kMostGroups)), dim3(threads), 0, s, p);
+    hipLaunchKernelGGL((norm_kernel<T, L, P, VEC, PAST>), dim3((unsigned)(groups < kMostGroups ? groups : kMostGroups)), dim3(threads), 0, s, p);
     return hipGetLastError();
   });
 }
 
-template <typename T, bool VEC>
+template <typename T, bool VEC, bool PAST>
 hipError_t norm_backward_typed(const NormBackwardParams& p, hipStream_t s) {
   const int64_t groups = backward_groups(p.rows, p.cols);
   hipError_t e = by_columns(p.cols, [&](auto lanes, auto passes) {
     constexpr int L = decltype(lanes)::value, P = decltype(passes)::value;
-    hipLaunchKernelGGL((norm_backward_kernel<T, L, P, VEC>), dim3((unsigned)groups), dim3(L < 256 ? 256 : L), 0, s, p);
+    hipLaunchKernelGGL((norm_backward_kernel<T, L, P, VEC, PAST>), dim3((unsigned)groups), dim3(L < 256 ? 256 : L), 0, s, p);
     return hipGetLastError();
   });
   if (e != hipSuccess || !p.grad_gain) return e;
@@ -247,21 +247,23 @@ hipError_t norm_backward_typed(const NormBackwardParams& p, hipStream_t s) {
 
 hipError_t norm_launch(const NormParams& p, hipStream_t s) {
   const size_t el = p.bf16 ? 2 : 4;
+  const bool past = streamed(p.rows * p.cols * (int64_t)el);
   const bool vec = p.cols % kCols == 0 && rows_aligned(p.x, p.x_stride, el) && rows_aligned(p.residual, p.residual_stride, el) &&
                    rows_aligned(p.h, p.h_stride, el) && rows_aligned(p.y, p.y_stride, el) && rows_aligned(p.gain, 0, 4);
-  if (p.bf16) return vec ? norm_typed<bf16, true>(p, s) : norm_typed<bf16, false>(p, s);
-  return vec ? norm_typed<float, true>(p, s) : norm_typed<float, false>(p, s);
+  if (p.bf16) return !vec ? norm_typed<bf16, false, false>(p, s) : past ? norm_typed<bf16, true, true>(p, s) : norm_typed<bf16, true, false>(p, s);
+  return !vec ? norm_typed<float, false, false>(p, s) : past ? norm_typed<float, true, true>(p, s) : norm_typed<float, true, false>(p, s);
 }
 
 size_t norm_backward_workspace(int64_t rows, int cols) { return (size_t)backward_groups(rows, cols) * (size_t)cols * sizeof(float); }
 
 hipError_t norm_backward_launch(const NormBackwardParams& p, hipStream_t s) {
   const size_t el = p.bf16 ? 2 : 4;
+  const bool past = streamed(p.rows * p.cols * (int64_t)el);
   const bool vec = p.cols % kCols == 0 && rows_aligned(p.h, p.h_stride, el) && rows_aligned(p.grad_y, p.grad_y_stride, el) &&
                    rows_aligned(p.grad_h, p.grad_h_stride, el) && rows_aligned(p.grad_x, p.grad_x_stride, el) &&
                    rows_aligned(p.gain, 0, 4);
-  if (p.bf16) return vec ? norm_backward_typed<bf16, true>(p, s) : norm_backward_typed<bf16, false>(p, s);
-  return vec ? norm_backward_typed<float, true>(p, s) : norm_backward_typed<float, false>(p, s);
+  if (p.bf16) return !vec ? norm_backward_typed<bf16, false, false>(p, s) : past ? norm_backward_typed<bf16, true, true>(p, s) : norm_backward_typed<bf16, true, false>(p, s);
+  return !vec ? norm_backward_typed<float, false, false>(p, s) : past ? norm_backward_typed<float, true, true>(p, s) : norm_backward_typed<float, true, false>(p, s);
 }
 
 }  // namespace tac

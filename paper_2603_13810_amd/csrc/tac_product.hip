@@ -69,7 +69,7 @@ __device__ __forceinline__ u32x4_t buffer_at(uint64_t at, int64_t bytes) {
 // banks.  A workgroup takes items (a tile, or one of `parts` parts of a tile's columns, whose results are [part][M][N]) until there are
 // none, and has the next item's first blocks on their way while it writes the results of the one before: they are turned through LDS, so that
 // rows leave in pieces of up to 256 bytes.
-template <int TM, int TN, int WM, int WN, int STAGES, bool EXACT, typename U>
+template <int TM, int TN, int WM, int WN, int STAGES, bool EXACT, bool PAST, typename U>
 __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile_kernel(const ProductParams p, int parts) {
   constexpr int kWaves = WM * WN, FM = TM / WM / 32, FN = TN / WN / 32, kStage = (TM + TN) * kBlock;
   constexpr int kLoadsM = TM / 8 / kWaves, kLoadsN = TN / 8 / kWaves;         // a load instruction brings 8 rows
@@ -233,7 +233,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile_kernel(const Pro
       if (p.wide_stores && cols_left == 32 * FN && rows_left == 32) {
 #pragma unroll 4
         for (int r = 0; r < 32 * kPieces / 64; ++r) {
-          *reinterpret_cast<u32x4_t*>(to) = *reinterpret_cast<const u32x4_t*>(from);
+          store_past<PAST>(reinterpret_cast<u32x4_t*>(to), *reinterpret_cast<const u32x4_t*>(from));
           to += (64 / kPieces) * p.y_stride;
           from += (64 / kPieces) * kRow;
         }
@@ -286,10 +286,10 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile_kernel(const Pro
 }
 
 // `parts` > 1: float32 results of every part
-template <int TM, int TN, int WM, int WN, int STAGES, bool EXACT, typename U>
+template <int TM, int TN, int WM, int WN, int STAGES, bool EXACT, bool PAST, typename U>
 hipError_t tile_launch(const ProductParams& p, int parts, hipStream_t s) {
   const int64_t items = ((p.M + TM - 1) / TM) * ((p.N + TN - 1) / TN) * parts;
-  auto* kernel = product_tile_kernel<TM, TN, WM, WN, STAGES, EXACT, U>;
+  auto* kernel = product_tile_kernel<TM, TN, WM, WN, STAGES, EXACT, PAST, U>;
   constexpr int lds = tile_lds(TM, TN, WM * WN, STAGES);
   constexpr int at_once = kFittedUnits * (160 * 1024 / lds);       // workgroups that the LDS holds
   static const hipError_t room = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
@@ -330,13 +330,15 @@ __global__ __launch_bounds__(256) void join_kernel(const ProductParams p, int pa
 template <typename T, int TM, int TN, int WM, int WN, int STAGES>
 hipError_t tiles(const ProductParams& p, int parts, hipStream_t s) {
   constexpr bool exact = sizeof(T) == 4;
-  if (parts == 1) return tile_launch<TM, TN, WM, WN, STAGES, exact, T>(p, 1, s);
+  if constexpr (TM == 256)
+    if (parts == 1 && streamed(p.M * p.N * (int64_t)sizeof(T))) return tile_launch<TM, TN, WM, WN, STAGES, exact, true, T>(p, 1, s);
+  if (parts == 1) return tile_launch<TM, TN, WM, WN, STAGES, exact, false, T>(p, 1, s);
   ProductParams q = p;
   q.y = p.partial;
   q.y_stride = p.N;
   q.bias = nullptr;
   q.wide_stores = p.N % 4 == 0;
-  const hipError_t e = tile_launch<TM, TN, WM, WN, STAGES, exact, float>(q, parts, s);
+  const hipError_t e = tile_launch<TM, TN, WM, WN, STAGES, exact, false, float>(q, parts, s);
   if (e != hipSuccess) return e;
   const bool vec = p.N % 4 == 0 && p.wide_stores;
   const int64_t work = (p.M * ((p.N + 3) / 4) + 255) / 256;
