@@ -30,7 +30,7 @@ constexpr int tile_lds(int TM, int TN, int waves, int STAGES) { return tile_scal
 //   128 x 64                                  -                  19                 24      16                 18                 16                8
 //   64 x 64, 4 waves, 2 stages                -                  22                 26      15                 20                 12                6
 // Large tiles read less per product, small ones give more workgroups and shorter blocks; stages hide memory where few workgroups do.  Parts cost
-// their sums' way through memory: 128 x 3136 x 3200 in one part 12.0 us, in two 11.3; 3200 x 500 x 3136 18 and 23.
+// their sums' way through memory: 128 x 3136 x 3200 float32 in one part 14.1 us, in two 13.1; 3200 x 500 x 3136 18 and 23.
 // The last tile is for few rows, where the other matrix's bytes count: seven blocks on their way per compute unit. With it, weights from memory, bfloat16
 // results: 16 x 8192 x 4096 14.9 -> 11.9 us, 64 x 8192 x 4096 16.8 -> 13.4, 100 x 4096 x 4096 12.9 -> 11.0.
 struct ProductPlan {
@@ -65,7 +65,7 @@ inline ProductPlan choose_product_plan(int64_t M, int64_t N, int64_t K, int bf) 
       const double each = (double)((blocks + parts - 1) / parts);
       double us = (double)(items / whole) * (q.ends + each * block[q.shared - 1]);
       if (left) us += q.ends + each * block[(left - 1) / kFittedUnits];
-      if (parts > 1) us += 4.5 + (double)M * (double)N * (8.0 * parts + (bf ? 2.0 : 4.0)) / 4e6;
+      if (parts > 1) us += 3.0 + (double)M * (double)N * (8.0 * parts + (bf ? 2.0 : 4.0)) / 4e6;
       if (us < least) {
         least = us;
         best = ProductPlan{tile, parts};
