@@ -77,6 +77,8 @@ __global__ __launch_bounds__(COLUMNS ? 256 : 512, COLUMNS && !ROWS && DT ? 5 : 1
           const u32x4_t w = *reinterpret_cast<const u32x4_t*>(row);
 #pragma unroll
           for (int q = 0; q < 4; ++q) v[i].w[q] = w[q];
+        } else if (left >= 8) {
+          __builtin_memcpy(v[i].w, row, 16);
         } else {
 #pragma unroll
           for (int e = 0; e < 8; ++e)
