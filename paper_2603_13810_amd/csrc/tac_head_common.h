@@ -217,7 +217,7 @@ struct ProductParams {
   float* partial;
   int64_t M, N, K, y_stride;
   int bf16;
-  int wide_stores;          // rows of y start at multiples of 16 bytes (set by product_launch)
+  int wide_stores;          // rows of y start at multiples of 16 bytes (set by product_launch): stores past the caches, sums of parts by four
 };
 size_t product_workspace(int64_t M, int64_t N, int64_t K, int bf16);
 hipError_t product_launch(const ProductParams& p, hipStream_t s);

@@ -230,18 +230,20 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile_kernel(const Pro
       int row = lane / kPieces;
       U* to = y + (mw + row) * p.y_stride + nw + 32 * I0 + kIn * piece;
       const uint8_t* from = room + row * kRow + 16 * piece;
-      if (p.wide_stores && cols_left == 32 * FN && rows_left == 32) {
+      // pieces of 16 bytes wherever a row starts: memory is written from any byte (4100 x 3001 x 512 bfloat16 15.4 us, element by element 31.6)
+      if (cols_left == 32 * FN && rows_left == 32) {
 #pragma unroll 4
         for (int r = 0; r < 32 * kPieces / 64; ++r) {
-          store_past<PAST>(reinterpret_cast<u32x4_t*>(to), *reinterpret_cast<const u32x4_t*>(from));
+          if constexpr (PAST) store_past<true>(reinterpret_cast<u32x4_t*>(to), *reinterpret_cast<const u32x4_t*>(from));
+          else __builtin_memcpy(to, __builtin_assume_aligned(from, 16), 16);
           to += (64 / kPieces) * p.y_stride;
           from += (64 / kPieces) * kRow;
         }
       } else {
 #pragma unroll 1
         for (; row < rows_left; row += 64 / kPieces) {
-          if (p.wide_stores && left >= kIn) {
-            *reinterpret_cast<u32x4_t*>(to) = *reinterpret_cast<const u32x4_t*>(from);
+          if (left >= kIn) {
+            __builtin_memcpy(to, __builtin_assume_aligned(from, 16), 16);
           } else {
 #pragma unroll 1
             for (int e = 0; e < min(kIn, left); ++e) to[e] = reinterpret_cast<const U*>(from)[e];
@@ -331,13 +333,12 @@ template <typename T, int TM, int TN, int WM, int WN, int STAGES>
 hipError_t tiles(const ProductParams& p, int parts, hipStream_t s) {
   constexpr bool exact = sizeof(T) == 4;
   if constexpr (TM == 256)
-    if (parts == 1 && streamed(p.M * p.N * (int64_t)sizeof(T))) return tile_launch<TM, TN, WM, WN, STAGES, exact, true, T>(p, 1, s);
+    if (parts == 1 && p.wide_stores && streamed(p.M * p.N * (int64_t)sizeof(T))) return tile_launch<TM, TN, WM, WN, STAGES, exact, true, T>(p, 1, s);
   if (parts == 1) return tile_launch<TM, TN, WM, WN, STAGES, exact, false, T>(p, 1, s);
   ProductParams q = p;
   q.y = p.partial;
   q.y_stride = p.N;
   q.bias = nullptr;
-  q.wide_stores = p.N % 4 == 0;
   const hipError_t e = tile_launch<TM, TN, WM, WN, STAGES, exact, false, float>(q, parts, s);
   if (e != hipSuccess) return e;
   const bool vec = p.N % 4 == 0 && p.wide_stores;
