@@ -1,4 +1,4 @@
-"""Thin ctypes binding over libtac.so: same names as include/tac.h, argument marshalling only.
+"""Thin binding over libtac.so: same names as include/tac.h, argument marshalling only (ctypes; a native module for the dense operators).
 
 Every step of the layer (spike loading, aggregation, convolution, LIF, packing) runs inside
 the library's HIP kernels.  PyTorch is used for device memory and the current stream only.
