@@ -76,15 +76,23 @@ struct Map {                         // x -> a x + b
 };
 
 // MAPS: only the map of the part, into workspace [part][2][B][D], from its last tile to its first (the tiles that the second launch starts with are
-// then those that the caches have seen last); the last part's is not needed.
+// then those that the caches have seen last).  The last part's is not needed: its place takes h0, from where every part of the second launch starts,
+// since that launch writes h_last, which may be h0, in no order with its parts' reads.
 template <typename T, int V, bool MAPS, bool PAST = false>
 __global__ __launch_bounds__(64 * kWaves) void scan_kernel(const ScanParams p) {
   using L = Lane<T, V>;
   __shared__ Map<V> maps[2][kWaves][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-  if (MAPS && blockIdx.y == gridDim.y - 1) return;
   const Place q = place_of<V>(p.T, p.D);
   const int64_t len = length_of(p.lengths, q.b, p.T), channels = (int64_t)p.B * p.D, n = (int64_t)q.b * p.D + q.d;
+  const float* h0 = p.h0 && gridDim.y > 1 ? p.workspace + 2 * (gridDim.y - 1) * channels : p.h0;
+  if (MAPS && blockIdx.y == gridDim.y - 1) {
+    if (p.h0 && !wave && q.on) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) p.workspace[2 * (gridDim.y - 1) * channels + n + e] = p.h0[n + e];
+    }
+    return;
+  }
   const T *gate = (const T*)p.gate + q.b * p.in_b, *value = (const T*)p.value + q.b * p.in_b;
   T* out = (T*)p.out + q.b * p.out_b;
   typename L::Raw g[kChunk] = {}, u[kChunk] = {};
@@ -102,7 +110,7 @@ __global__ __launch_bounds__(64 * kWaves) void scan_kernel(const ScanParams p) {
 #pragma unroll
   for (int e = 0; e < V; ++e) {
     total[e] = 1.0f;
-    carry[e] = MAPS || !p.h0 ? 0.0f : p.h0[n + e];
+    carry[e] = MAPS || !h0 ? 0.0f : h0[n + e];
     if constexpr (!MAPS)
       for (int k = 0; k < (int)blockIdx.y; ++k)
         carry[e] = fmaf(p.workspace[2 * k * channels + n + e], carry[e], p.workspace[(2 * k + 1) * channels + n + e]);
@@ -199,14 +207,22 @@ __global__ __launch_bounds__(64 * kWaves) void scan_kernel(const ScanParams p) {
 
 // The same backwards: the gradient c that arrives at a step's state obeys c <- a (c + grad_out).  With w = min(a, 1 - a) the gate's
 // gradient is c w (1 - w) (h_{t-1} - value).  The states before the steps are formed again from the chunk's first, which the forward pass kept.
+// Here the first part's map is not needed, and its place takes grad_h_last (which grad_h0 may be).
 template <typename T, int V, bool MAPS, bool PAST = false>
 __global__ __launch_bounds__(64 * kWaves) void scan_backward_kernel(const ScanBackwardParams p) {
   using L = Lane<T, V>;
   __shared__ Map<V> maps[2][kWaves][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-  if (MAPS && blockIdx.y == 0) return;
   const Place q = place_of<V>(p.T, p.D);
   const int64_t len = length_of(p.lengths, q.b, p.T), channels = (int64_t)p.B * p.D, n = (int64_t)q.b * p.D + q.d;
+  const float* last = p.grad_h_last && gridDim.y > 1 ? p.workspace : p.grad_h_last;
+  if (MAPS && blockIdx.y == 0) {
+    if (p.grad_h_last && !wave && q.on) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) p.workspace[n + e] = p.grad_h_last[n + e];
+    }
+    return;
+  }
   const T *gate = (const T*)p.gate + q.b * p.in_b, *value = (const T*)p.value + q.b * p.in_b, *grad_out = (const T*)p.grad_out + q.b * p.out_b;
   T *grad_gate = (T*)p.grad_gate + q.b * p.grad_b, *grad_value = (T*)p.grad_value + q.b * p.grad_b;
   typename L::Raw g[kChunk] = {}, u[kChunk] = {}, go[kChunk] = {};
@@ -228,7 +244,7 @@ __global__ __launch_bounds__(64 * kWaves) void scan_backward_kernel(const ScanBa
 #pragma unroll
   for (int e = 0; e < V; ++e) {
     total[e] = 1.0f;
-    carry[e] = MAPS || !p.grad_h_last ? 0.0f : p.grad_h_last[n + e];
+    carry[e] = MAPS || !last ? 0.0f : last[n + e];
     if constexpr (!MAPS)
       for (int k = gridDim.y - 1; k > (int)blockIdx.y; --k)
         carry[e] = fmaf(p.workspace[2 * k * channels + n + e], carry[e], p.workspace[(2 * k + 1) * channels + n + e]);

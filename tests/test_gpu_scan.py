@@ -1,4 +1,6 @@
 """Gated linear recurrence, its backward pass and its single step against 64 bits."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -281,3 +283,29 @@ def test_offsets_beyond_32_bits():
     back = api.tac_gated_scan_backward(gate, value, got["states"], got["out"])
     r = reference(gate[t0:, -1:, :200], value[t0:, -1:, :200], None, start[-1:, :200], got["out"][t0:, -1:, :200])
     close(back["grad_value"][t0:, -1:, :200], r["gv"], r["ctol"], torch.bfloat16)
+
+
+def c_abi(name, T, B, D, dtype, *tensors):
+    """The C entry point on contiguous tensors (None: NULL), scratch behind them."""
+    d = api.tac_scan_desc_t(T, B, D, B * D, D, B * D, D, B * D, D, api.TAC_BF16 if dtype == torch.bfloat16 else api.TAC_FP32)
+    work = torch.empty(max(16, api.lib().tac_gated_scan_workspace_bytes(ctypes.addressof(d))), dtype=torch.uint8, device=DEV)
+    status = getattr(api.lib(), name)(ctypes.addressof(d), *(None if t is None else t.data_ptr() for t in tensors), work.data_ptr(),
+                                      torch.cuda.current_stream().cuda_stream)
+    assert status == api.TAC_OK
+
+
+@pytest.mark.parametrize("ragged", [False, True])
+@pytest.mark.parametrize("T,B,D,dtype", [(32768, 1, 2048, torch.bfloat16), (20000, 3, 1000, torch.float32), (9000, 1, 512, torch.float32),
+                                         (3001, 2, 65, torch.bfloat16), (100, 3, 96, torch.float32)])
+def test_the_last_state_may_take_the_place_of_the_first(T, B, D, dtype, ragged):
+    gate, value, lengths, h0, go, gl = (t if t is None else t.contiguous() for t in make(T, B, D, dtype, 32, ragged))
+    if ragged and B == 1:
+        lengths[0] = T // 3
+    want = api.tac_gated_scan(gate, value, lengths=lengths, h0=h0, want_states=True)
+    want_back = api.tac_gated_scan_backward(gate, value, want["states"], go, lengths=lengths, grad_h_last=gl)
+    state, out, states = h0.clone(), torch.empty_like(go), torch.empty_like(want["states"])
+    c_abi("tac_gated_scan", T, B, D, dtype, gate, value, lengths, state, out, state, states)
+    assert torch.equal(state, want["h_last"]) and torch.equal(out, want["out"]) and torch.equal(states, want["states"])
+    grad, gg, gv = gl.clone(), torch.empty_like(go), torch.empty_like(go)
+    c_abi("tac_gated_scan_backward", T, B, D, dtype, gate, value, lengths, states, go, grad, gg, gv, grad)
+    assert torch.equal(grad, want_back["grad_h0"]) and torch.equal(gg, want_back["grad_gate"]) and torch.equal(gv, want_back["grad_value"])
