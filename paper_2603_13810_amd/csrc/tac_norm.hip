@@ -72,10 +72,18 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(const N
     for (int q = 0; q < PASSES; ++q) {
       const int c = (q * LANES + lane) * kCols;
       const int n = p.cols - c;
+      const float by = !VEC || n > 0 ? rstd : 0.0f;        // pad codes are zero where rstd is NaN too; lanes that are half a pad: below
 #pragma unroll
-      for (int e = 0; e < kCols; ++e) v[q][e] = v[q][e] * rstd * g[q][e];
+      for (int e = 0; e < kCols; ++e) v[q][e] = v[q][e] * by * g[q][e];
       if (p.y && n > 0) store_floats<T, kCols, VEC, PAST>((T*)p.y + row * p.y_stride + c, n, v[q]);
       if (p.codes) {
+        if constexpr (!VEC) {
+          if (rstd != rstd) {
+#pragma unroll
+            for (int e = 0; e < kCols; ++e)
+              if (e >= n) v[q][e] = 0.0f;
+          }
+        }
         float amax = 0.0f;
   #pragma unroll
         for (int e = 0; e < kCols; ++e) {

@@ -193,3 +193,12 @@ def test_offsets_beyond_32_bits():
     api.tac_residual_norm(x, None, None, eps=EPS, y=y)
     for at in (0, rows // 2, rows - 3):
         check_forward(x[at:at + 3], None, None, dict(h=None, y=y[at:at + 3], rstd=None, scaled=None))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols", [1, 100, 400, 1001, 1300, 2049, 9000])
+def test_pad_codes_are_zero_beside_infinities_and_nan(cols, dtype):
+    x, _, gain, _, _ = make(5, cols, dtype, 15, residual=False)
+    x[1, cols // 2], x[2, cols - 1], x[3, :] = float("nan"), float("inf"), -float("inf")
+    scaled = api.tac_residual_norm(x, None, gain, eps=EPS, want_scaled=True)["scaled"]
+    assert np.isnan(O.decode(scaled, cols)[0][[1, 3]]).all() and O.pads_are_zero(scaled, cols)
