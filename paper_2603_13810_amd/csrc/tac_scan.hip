@@ -27,6 +27,22 @@ __device__ __forceinline__ bool forgets(float s) { return (int)float_bits(s) < 0
 __device__ __forceinline__ float step_state(float s, float h, float u) { return fmaf(s, u - h, forgets(s) ? u : h); }
 __device__ __forceinline__ float times_a(float s, float x) { return fmaf(-s, x, forgets(s) ? 0.0f : x); }
 
+// Those forms turn an infinity into inf - inf, and the difference of two values near float32's largest into an infinity; maps multiply infinities
+// by factors that have become 0.  What is infinite or NaN stays one of the two in them, step by step and map by map, so that a look at the end of every
+// chunk finds it.  The steps of such a channel are then taken again one after the other by the formula as it stands wherever the form above is not
+// finite: an infinity goes on as a h + (1 - a) value says, NaN where float32 has its factor as 0.
+__device__ __forceinline__ bool finite(float v) { return fabsf(v) < __builtin_inff(); }
+__device__ __forceinline__ float a_of(float s) { return forgets(s) ? fabsf(s) : 1.0f - fabsf(s); }
+__device__ __forceinline__ float rest_of(float s) { return forgets(s) ? 1.0f - fabsf(s) : fabsf(s); }
+__device__ __forceinline__ float careful_state(float s, float h, float u) {
+  const float r = step_state(s, h, u);
+  return finite(r) ? r : fmaf(a_of(s), h, rest_of(s) * u);
+}
+__device__ __forceinline__ float careful_times(float s, float x) {
+  const float r = times_a(s, x);
+  return finite(r) ? r : a_of(s) * x;
+}
+
 __device__ __forceinline__ int64_t length_of(const int32_t* lengths, int b, int64_t T) {
   return lengths ? min(max((int64_t)lengths[b], (int64_t)0), T) : T;
 }
@@ -56,6 +72,8 @@ struct Place {
   int b, d, tiles, first, last;      // sequence, the lane's first channel, tiles of the whole length, the part's tiles [first, last)
   bool on;
 };
+// first tile of a part, tiles part / parts in 32 bits (there are at most 512 parts)
+__device__ __forceinline__ int part_from(int tiles, int part, int parts) { return tiles / parts * part + tiles % parts * part / parts; }
 template <int V>
 __device__ __forceinline__ Place place_of(int64_t T, int D) {
   const int per_b = (D + 64 * V - 1) / (64 * V), steps = (blockDim.x >> 6) * kChunk;
@@ -65,8 +83,8 @@ __device__ __forceinline__ Place place_of(int64_t T, int D) {
   q.on = q.d < D;
   if (!q.on) q.d = 0;                // reads what is there, writes nothing
   q.tiles = (int)((T + steps - 1) / steps);
-  q.first = (int)((int64_t)q.tiles * blockIdx.y / gridDim.y);
-  q.last = (int)((int64_t)q.tiles * (blockIdx.y + 1) / gridDim.y);
+  q.first = part_from(q.tiles, blockIdx.y, gridDim.y);
+  q.last = part_from(q.tiles, blockIdx.y + 1, gridDim.y);
   return q;
 }
 
@@ -78,10 +96,12 @@ struct Map {                         // x -> a x + b
 // MAPS: only the map of the part, into workspace [part][2][B][D], from its last tile to its first (the tiles that the second launch starts with are
 // then those that the caches have seen last).  The last part's is not needed: its place takes h0, from where every part of the second launch starts,
 // since that launch writes h_last, which may be h0, in no order with its parts' reads.
+// At most 128 registers, so that two workgroups share a compute unit (the walk behind the loop would let the compiler take 160).
 template <typename T, int V, bool MAPS, bool PAST = false>
-__global__ __launch_bounds__(64 * kWaves) void scan_kernel(const ScanParams p) {
+__global__ __launch_bounds__(64 * kWaves, 4) void scan_kernel(const ScanParams p) {
   using L = Lane<T, V>;
   __shared__ Map<V> maps[2][kWaves][64];
+  __shared__ float starts[kWaves][V][64];      // what carry starts from, where it is asked for again: in memory the last state (gradient) may have its place
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const Place q = place_of<V>(p.T, p.D);
   const int64_t len = length_of(p.lengths, q.b, p.T), channels = (int64_t)p.B * p.D, n = (int64_t)q.b * p.D + q.d;
@@ -107,10 +127,13 @@ __global__ __launch_bounds__(64 * kWaves) void scan_kernel(const ScanParams p) {
     }
   };
   float carry[V], total[V];          // MAPS: the map of the tiles behind, else the state before the tile
+  bool good[V];                      // nothing that is not finite so far
 #pragma unroll
   for (int e = 0; e < V; ++e) {
     total[e] = 1.0f;
+    good[e] = true;
     carry[e] = MAPS || !h0 ? 0.0f : h0[n + e];
+    if constexpr (!MAPS) starts[wave][e][lane] = carry[e];
     if constexpr (!MAPS)
       for (int k = 0; k < (int)blockIdx.y; ++k)
         carry[e] = fmaf(p.workspace[2 * k * channels + n + e], carry[e], p.workspace[(2 * k + 1) * channels + n + e]);
@@ -181,6 +204,8 @@ __global__ __launch_bounds__(64 * kWaves) void scan_kernel(const ScanParams p) {
         }
         x[i] = L::pack(o);
       }
+#pragma unroll
+      for (int e = 0; e < V; ++e) good[e] = good[e] && finite(h[e]);
       if (t0 + kChunk <= len) {
         if (q.on) {
 #pragma unroll
@@ -191,6 +216,34 @@ __global__ __launch_bounds__(64 * kWaves) void scan_kernel(const ScanParams p) {
         for (int i = 0; i < kChunk; ++i)
           if (t0 + i < p.T && q.on) L::template store<PAST>(out + (t0 + i) * p.out_t + q.d, t0 + i < len ? x[i] : (typename L::Raw)0);
       }
+    }
+  }
+  if constexpr (!MAPS) {             // channels that are not finite: every wave takes all steps and writes its own again
+    const int64_t steps = (int64_t)waves * kChunk;
+#pragma unroll 1
+    for (int e = 0; e < V; ++e) {
+      if (!q.on || ((e ? good[V - 1] : good[0]) && finite(e ? carry[V - 1] : carry[0]))) continue;
+      float h = starts[wave][e][lane];
+      int from = 0;                  // the first part that ends with something else than a number, or this one
+      for (; from < (int)blockIdx.y; ++from) {
+        const float next = fmaf(p.workspace[2 * from * channels + n + e], h, p.workspace[(2 * from + 1) * channels + n + e]);
+        if (!finite(next)) break;
+        h = next;
+      }
+      // a NaN makes all behind it NaN, and the steps have written that
+      const int64_t first = q.first * steps, end = min(q.last * steps, len);
+#pragma unroll 1
+      for (int64_t t = part_from(q.tiles, from, gridDim.y) * steps; t < end && h == h; ++t) {
+        const bool mine = t >= first && t / kChunk % waves == wave;
+        if (mine && p.states && t % kChunk == 0) p.states[t / kChunk * channels + n + e] = h;
+        h = careful_state(leak((float)gate[t * p.in_t + q.d + e]), h, (float)value[t * p.in_t + q.d + e]);
+        if (mine) out[t * p.out_t + q.d + e] = (T)h;
+      }
+      // chunks behind the length
+      if (p.states)
+        for (int64_t c = max(q.first * (int64_t)waves, (len + kChunk - 1) / kChunk); c < min(q.last * (int64_t)waves, (p.T + kChunk - 1) / kChunk); ++c)
+          if (c % waves == wave) p.states[c * channels + n + e] = h;
+      (e ? carry[V - 1] : carry[0]) = h;
     }
   }
   if (wave || !q.on) return;
@@ -212,6 +265,7 @@ template <typename T, int V, bool MAPS, bool PAST = false>
 __global__ __launch_bounds__(64 * kWaves) void scan_backward_kernel(const ScanBackwardParams p) {
   using L = Lane<T, V>;
   __shared__ Map<V> maps[2][kWaves][64];
+  __shared__ float starts[kWaves][V][64];      // what carry starts from, where it is asked for again: in memory the last state (gradient) may have its place
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const Place q = place_of<V>(p.T, p.D);
   const int64_t len = length_of(p.lengths, q.b, p.T), channels = (int64_t)p.B * p.D, n = (int64_t)q.b * p.D + q.d;
@@ -241,10 +295,13 @@ __global__ __launch_bounds__(64 * kWaves) void scan_backward_kernel(const ScanBa
     }
   };
   float carry[V], total[V];
+  bool good[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) {
     total[e] = 1.0f;
+    good[e] = true;
     carry[e] = MAPS || !last ? 0.0f : last[n + e];
+    if constexpr (!MAPS) starts[wave][e][lane] = carry[e];
     if constexpr (!MAPS)
       for (int k = gridDim.y - 1; k > (int)blockIdx.y; --k)
         carry[e] = fmaf(p.workspace[2 * k * channels + n + e], carry[e], p.workspace[(2 * k + 1) * channels + n + e]);
@@ -287,6 +344,10 @@ __global__ __launch_bounds__(64 * kWaves) void scan_backward_kernel(const ScanBa
         mine.a[e] = times_a(s[i][e], mine.a[e]);
       }
     maps[k & 1][wave][lane] = mine;
+    if constexpr (!MAPS) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) good[e] = good[e] && finite(before[kChunk - 1][e]);
+    }
     if (k + 1 < q.last - q.first) load(MAPS ? tile + 1 : tile - 1);
     __syncthreads();
     float c[V];
@@ -314,13 +375,15 @@ __global__ __launch_bounds__(64 * kWaves) void scan_backward_kernel(const ScanBa
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           const float w = fabsf(s[i][e]), now = c[e] + L::value(y[i], e);
-          dv[e] = now * (forgets(s[i][e]) ? 1.0f - w : w);
+          dv[e] = now * rest_of(s[i][e]);
           dg[e] = now * (w * (1.0f - w)) * (before[i][e] - L::value(x[i], e));
           c[e] = times_a(s[i][e], now);
         }
         x[i] = L::pack(dg);
         y[i] = L::pack(dv);
       }
+#pragma unroll
+      for (int e = 0; e < V; ++e) good[e] = good[e] && finite(c[e]);
       if (t0 + kChunk <= len) {
         if (q.on) {
 #pragma unroll
@@ -338,6 +401,35 @@ __global__ __launch_bounds__(64 * kWaves) void scan_backward_kernel(const ScanBa
             L::template store<PAST>(grad_value + (t0 + i) * p.grad_t + q.d, live ? y[i] : (typename L::Raw)0);
           }
       }
+    }
+  }
+  if constexpr (!MAPS) {             // as forwards
+    const int64_t steps = (int64_t)waves * kChunk;
+#pragma unroll 1
+    for (int e = 0; e < V; ++e) {
+      if (!q.on || ((e ? good[V - 1] : good[0]) && finite(e ? carry[V - 1] : carry[0]))) continue;
+      float c = starts[wave][e][lane];
+      int from = gridDim.y - 1;
+      for (; from > (int)blockIdx.y; --from) {
+        const float next = fmaf(p.workspace[2 * from * channels + n + e], c, p.workspace[(2 * from + 1) * channels + n + e]);
+        if (!finite(next)) break;
+        c = next;
+      }
+      const int64_t first = q.first * steps, end = q.last * steps;
+#pragma unroll 1
+      for (int64_t t = min(part_from(q.tiles, from + 1, gridDim.y) * steps, len) - 1; t >= first && c == c; --t) {
+        const float s = leak((float)gate[t * p.in_t + q.d + e]), now = c + (float)grad_out[t * p.out_t + q.d + e];
+        if (t < end && t / kChunk % waves == wave) {
+          const int64_t t0 = t / kChunk * kChunk;
+          float h = p.states[t / kChunk * channels + n + e];
+          for (int64_t j = t0; j < t; ++j) h = careful_state(leak((float)gate[j * p.in_t + q.d + e]), h, (float)value[j * p.in_t + q.d + e]);
+          const float w = fabsf(s);
+          grad_gate[t * p.grad_t + q.d + e] = (T)(now * (w * (1.0f - w)) * (h - (float)value[t * p.in_t + q.d + e]));
+          grad_value[t * p.grad_t + q.d + e] = (T)(now * rest_of(s));
+        }
+        c = careful_times(s, now);
+      }
+      (e ? carry[V - 1] : carry[0]) = c;
     }
   }
   if (wave || !q.on) return;
@@ -361,7 +453,7 @@ __global__ __launch_bounds__(256) void step_kernel(const StepParams p) {
   float h = 0.0f;
   if (slot >= 0 && slot < p.n_slots) {
     float* state = p.pool + slot * p.D + d;
-    h = step_state(leak((float)((const T*)p.gate)[b * p.in_b + d]), *state, (float)((const T*)p.value)[b * p.in_b + d]);
+    h = careful_state(leak((float)((const T*)p.gate)[b * p.in_b + d]), *state, (float)((const T*)p.value)[b * p.in_b + d]);
     *state = h;
   }
   ((T*)p.out)[b * p.out_b + d] = (T)h;

@@ -309,3 +309,91 @@ def test_the_last_state_may_take_the_place_of_the_first(T, B, D, dtype, ragged):
     grad, gg, gv = gl.clone(), torch.empty_like(go), torch.empty_like(go)
     c_abi("tac_gated_scan_backward", T, B, D, dtype, gate, value, lengths, states, go, grad, gg, gv, grad)
     assert torch.equal(grad, want_back["grad_h0"]) and torch.equal(gg, want_back["grad_gate"]) and torch.equal(gv, want_back["grad_value"])
+
+
+def same_ends(got, want, tol, dtype):
+    """NaN and infinities of either sign in the same places; the numbers within tol (by channel) and a rounding."""
+    got = O.as64(got)
+    assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(np.isposinf(got), np.isposinf(want))
+    assert np.array_equal(np.isneginf(got), np.isneginf(want))
+    ok = np.isfinite(want)
+    half = O.HALF[dtype]
+    assert (np.abs(got - want)[ok] <= (half * np.abs(want) * (1 + 1e-6) + tol * (1 + half) + 1e-37)[ok]).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,B,D,lengths", [(40, 3, 10, (16, 17, 40)), (40, 3, 11, None), (300, 4, 66, (127, 128, 300, 200)), (3001, 2, 64, (3001, 2000)),
+                                           (2500, 1, 12, None), (256, 200, 130, None)])
+def test_infinite_states_and_gradients(T, B, D, lengths, dtype):
+    g = torch.Generator(device=DEV).manual_seed(33)
+    n = lambda *s: torch.randn(*s, generator=g, device=DEV)
+    gate, value, h0, go, gl = (n(T, B, D) + 1).to(dtype), n(T, B, D).to(dtype), n(B, D), n(T, B, D).to(dtype), n(B, D)
+    lens = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    args = dict(lengths=lens, h0=h0)
+    clean = api.tac_gated_scan(gate, value, want_states=True, **args)
+    clean_back = api.tac_gated_scan_backward(gate, value, clean["states"], go, lengths=lens, grad_h_last=gl)
+    h0, value, gate, go, gl = h0.clone(), value.clone(), gate.clone(), go.clone(), gl.clone()
+    inf, top = float("inf"), torch.finfo(dtype).max
+    end = [T] * B if lengths is None else lengths
+    h0[:, 0] = inf                                       # an infinite state that is there from the start
+    h0[:, 1], gate[:, :, 1] = -inf, -8.0                 # through factors whose product is below float32's smallest
+    for b in range(B):
+        value[end[b] // 2, b, 2] = inf
+        value[end[b] // 3, b, 3], value[end[b] // 2, b, 3] = inf, -inf        # NaN from the second on
+        value[end[b] - 1, b, 4] = -inf                   # the last step's
+        go[end[b] // 2, b, 6] = inf
+        go[end[b] // 2, b, 7], go[end[b] // 3, b, 7] = inf, -inf
+    value[::2, :, 5], value[1::2, :, 5] = top, -top      # differences beyond float32, states within it
+    gl[:, 8] = -inf
+    value[T // 4, :, 9] = float("nan")
+    got = api.tac_gated_scan(gate, value, want_states=True, lengths=lens, h0=h0)
+    g64, u64, cut = O.as64(gate), O.as64(value), None if lengths is None else np.array(lengths)
+    with np.errstate(invalid="ignore"):
+        out, before, last = O.scan(g64, u64, cut, O.as64(h0))
+        gg, gv, g0 = O.scan_backward(g64, u64, before, O.as64(go), cut, O.as64(gl))
+    # as in reference(), by channel: per step (16 + 2 |gate|) roundings of the channel's largest finite value, shrinking by the largest a
+    steps = np.minimum(T, 1.0 / (1.0 - 1.0 / (1.0 + np.exp(-g64.max(0)))))
+    most = lambda v: np.where(np.isfinite(v), np.abs(v), 0).max(0)
+    per = (16 + 2 * np.abs(g64).max(0)) * O.U * steps
+    tol = per * np.maximum(np.maximum(most(u64), most(before)), most(last[None]))
+    same_ends(got["out"], out, tol, dtype)
+    same_ends(got["h_last"], last, tol, torch.float32)
+    same_ends(got["states"], before[::api.TAC_SCAN_CHUNK], tol, torch.float32)
+    back = api.tac_gated_scan_backward(gate, value, got["states"], go, lengths=lens, grad_h_last=gl)
+    size = np.maximum(most(O.as64(go)), most(O.as64(gl)[None])) * steps
+    same_ends(back["grad_value"], gv, per * size, dtype)
+    same_ends(back["grad_h0"], g0, per * size, torch.float32)
+    gated = [d for d in range(D) if d != 5]              # h - value itself is beyond float32 there
+    wide = 2 * np.maximum(most(u64), most(before)) * per * size / 4 + size * tol / 4
+    same_ends(back["grad_gate"][..., gated], gg[..., gated], wide[..., gated], dtype)
+    for k in ("out", "h_last", "states"):                # the other channels do not notice
+        assert torch.equal(got[k][..., 10:], clean[k][..., 10:])
+    for k in back:
+        assert torch.equal(back[k][..., 10:], clean_back[k][..., 10:])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_infinite_states_step_by_step(dtype):
+    gate, value = torch.zeros(3, 8, device=DEV, dtype=dtype), torch.ones(3, 8, device=DEV, dtype=dtype)
+    gate[1], gate[2] = 3.0, -3.0
+    pool = torch.full((3, 8), float("inf"), device=DEV)
+    pool[:, 1::2] = -float("inf")
+    want = pool.clone()
+    for _ in range(3):
+        assert torch.equal(api.tac_gated_step(gate, value, pool).float(), want) and torch.equal(pool, want)
+
+
+@pytest.mark.parametrize("T,B,D,dtype", [(100, 3, 96, torch.float32), (130, 70, 200, torch.bfloat16), (9000, 1, 512, torch.bfloat16)])
+def test_infinite_states_where_the_last_takes_the_place_of_the_first(T, B, D, dtype):
+    gate, value, lengths, h0, go, gl = (t if t is None else t.contiguous() for t in make(T, B, D, dtype, 34, ragged=B > 1))
+    h0[:, ::3], gl[:, 1::3] = float("inf"), -float("inf")
+    want = api.tac_gated_scan(gate, value, lengths=lengths, h0=h0, want_states=True)
+    want_back = api.tac_gated_scan_backward(gate, value, want["states"], go, lengths=lengths, grad_h_last=gl)
+    state, out, states = h0.clone(), torch.empty_like(go), torch.empty_like(want["states"])
+    c_abi("tac_gated_scan", T, B, D, dtype, gate, value, lengths, state, out, state, states)
+    grad, gg, gv = gl.clone(), torch.empty_like(go), torch.empty_like(go)
+    c_abi("tac_gated_scan_backward", T, B, D, dtype, gate, value, lengths, states, go, grad, gg, gv, grad)
+    assert torch.isposinf(state[:, ::3]).all() and torch.isneginf(grad[:, 1::3]).all()
+    for got, w in ((state, want["h_last"]), (out, want["out"]), (states, want["states"]), (grad, want_back["grad_h0"]), (gg, want_back["grad_gate"]),
+                   (gv, want_back["grad_value"])):
+        assert torch.allclose(got.float(), w.float(), rtol=0, atol=0, equal_nan=True)
