@@ -563,11 +563,14 @@ def _result(r):
     return r
 
 
-def _on(stream, call):
-    """`call` with `stream` as torch's current one: what it allocates then belongs to that stream, and no block comes back to work that is still
-    reading it on another."""
+def _on(stream, first, call):
+    """`call` with `stream` as torch's current one on the device of the call's first tensor: what it allocates then belongs to that stream, and no
+    block comes back to work that is still reading it on another."""
     import torch
-    with torch.cuda.stream(torch.cuda.ExternalStream(int(stream))):
+    device = getattr(first, "device", None)
+    if device is None or device.type != "cuda":
+        return call()                        # which refuses it
+    with torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=device)):
         return call()
 
 
@@ -584,7 +587,8 @@ def tac_quantize(src, *, cols=None, tiles=False, rows=True, columns=False, strea
     columns.  tiles: one scale per 128 x 128 instead of per row and 128 columns.  Returns dict(rows, columns) of 8-bit matrices:
     `rows` is src itself, `columns` its transpose [C, R] (None where not asked for)."""
     if stream is not None:
-        return _on(stream, lambda: tac_quantize(src, cols=cols, tiles=tiles, rows=rows, columns=columns))
+        return _on(stream, src[0] if isinstance(src, (tuple, list)) else src,
+                   lambda: tac_quantize(src, cols=cols, tiles=tiles, rows=rows, columns=columns))
     if isinstance(src, (tuple, list)):
         if cols is None:
             raise ValueError("an 8-bit matrix needs its number of columns")
@@ -595,7 +599,7 @@ def tac_quantize(src, *, cols=None, tiles=False, rows=True, columns=False, strea
 def tac_dequantize(matrix, cols, *, dtype=None, out=None, stream=None):
     """The values of an 8-bit matrix (codes, scales) of `cols` columns, float32 (or `dtype`, or into `out`)."""
     if stream is not None:
-        return _on(stream, lambda: tac_dequantize(matrix, cols, dtype=dtype, out=out))
+        return _on(stream, matrix[0], lambda: tac_dequantize(matrix, cols, dtype=dtype, out=out))
     return _result(_native().dequantize(matrix[0], matrix[1], cols, dtype, out))
 
 
@@ -605,8 +609,8 @@ def tac_residual_norm(x, residual=None, gain=None, *, eps, h=None, y=None, want_
     want_h: the sum x + residual (as it is where there is a residual).  Returns dict(h, y, scaled, rstd), `scaled` an 8-bit matrix of y;
     what is not asked for is None.  h and y may be given (h may be x or residual)."""
     if stream is not None:
-        return _on(stream, lambda: tac_residual_norm(x, residual, gain, eps=eps, h=h, y=y, want_h=want_h, want_y=want_y,
-                                                      want_scaled=want_scaled, want_rstd=want_rstd))
+        return _on(stream, x, lambda: tac_residual_norm(x, residual, gain, eps=eps, h=h, y=y, want_h=want_h, want_y=want_y,
+                                                         want_scaled=want_scaled, want_rstd=want_rstd))
     return _result(_native().residual_norm(x, residual, gain, eps, h, y, want_h, want_y, want_scaled, want_rstd))
 
 
@@ -614,14 +618,14 @@ def tac_residual_norm_backward(h, gain, rstd, grad_y, grad_h=None, *, grad_x=Non
     """Backward pass of tac_residual_norm from the stream h and the rstd it stored.  Returns dict(grad_x, grad_gain); grad_x is the
     gradient of x and of the residual, and may be given (also grad_y or grad_h)."""
     if stream is not None:
-        return _on(stream, lambda: tac_residual_norm_backward(h, gain, rstd, grad_y, grad_h, grad_x=grad_x, want_grad_gain=want_grad_gain))
+        return _on(stream, h, lambda: tac_residual_norm_backward(h, gain, rstd, grad_y, grad_h, grad_x=grad_x, want_grad_gain=want_grad_gain))
     return _result(_native().residual_norm_backward(h, gain, rstd, grad_y, grad_h, grad_x, want_grad_gain))
 
 
 def tac_scaled_product(a_codes, a_scales, b_codes, b_scales, K, *, bias=None, dtype=None, out=None, stream=None):
     """a b^T (+ bias) of the 8-bit matrices a [M, K] and b [N, K], in bfloat16 (or `dtype`, or into `out` [M, N])."""
     if stream is not None:
-        return _on(stream, lambda: tac_scaled_product(a_codes, a_scales, b_codes, b_scales, K, bias=bias, dtype=dtype, out=out))
+        return _on(stream, a_codes, lambda: tac_scaled_product(a_codes, a_scales, b_codes, b_scales, K, bias=bias, dtype=dtype, out=out))
     return _result(_native().scaled_product(a_codes, a_scales, b_codes, b_scales, K, bias, dtype, out))
 
 
@@ -630,7 +634,7 @@ def tac_gated_scan(gate, value, *, lengths=None, h0=None, out=None, want_h_last=
     last axis contiguous; lengths: int32 [B]; h0: float32 [B, D].  Returns dict(out, h_last, states); `states` is what the backward
     pass needs."""
     if stream is not None:
-        return _on(stream, lambda: tac_gated_scan(gate, value, lengths=lengths, h0=h0, out=out, want_h_last=want_h_last, want_states=want_states))
+        return _on(stream, gate, lambda: tac_gated_scan(gate, value, lengths=lengths, h0=h0, out=out, want_h_last=want_h_last, want_states=want_states))
     return _result(_native().gated_scan(gate, value, lengths, h0, out, want_h_last, want_states))
 
 
@@ -639,8 +643,8 @@ def tac_gated_scan_backward(gate, value, states, grad_out, *, lengths=None, grad
     """Backward pass of tac_gated_scan from its inputs and `states`.  Returns dict(grad_gate, grad_value, grad_h0); the first two may be
     given (of the same strides as each other)."""
     if stream is not None:
-        return _on(stream, lambda: tac_gated_scan_backward(gate, value, states, grad_out, lengths=lengths, grad_h_last=grad_h_last,
-                                                            grad_gate=grad_gate, grad_value=grad_value, want_grad_h0=want_grad_h0))
+        return _on(stream, gate, lambda: tac_gated_scan_backward(gate, value, states, grad_out, lengths=lengths, grad_h_last=grad_h_last,
+                                                                  grad_gate=grad_gate, grad_value=grad_value, want_grad_h0=want_grad_h0))
     return _result(_native().gated_scan_backward(gate, value, states, grad_out, lengths, grad_h_last, grad_gate, grad_value, want_grad_h0))
 
 
@@ -649,5 +653,5 @@ def tac_gated_step(gate, value, pool, slots=None, *, out=None, stream=None):
     value: [B, D]; slots: int32 [B], each slot at most once, outside the pool for rows without a sequence; None: row b has slot b.
     Returns out [B, D]."""
     if stream is not None:
-        return _on(stream, lambda: tac_gated_step(gate, value, pool, slots, out=out))
+        return _on(stream, gate, lambda: tac_gated_step(gate, value, pool, slots, out=out))
     return _result(_native().gated_step(gate, value, pool, slots, out))

@@ -243,3 +243,51 @@ def test_laying_8bit_values_out_again_is_exact_above_the_subnormals():
     normal = np.abs(v.T) >= 2.0 ** -6 * unit
     assert normal.mean() > 0.97 and np.array_equal(again[normal], v.T[normal])
     assert (np.abs(again - v.T) <= 2.0 ** -10 * unit).all()
+
+
+CALLS = {
+    "quantize": lambda t, s: api.tac_quantize(t, stream=s),
+    "quantize codes": lambda t, s: api.tac_quantize((t, t), cols=8, stream=s),
+    "dequantize": lambda t, s: api.tac_dequantize((t, t), 8, stream=s),
+    "residual_norm": lambda t, s: api.tac_residual_norm(t, eps=1e-5, stream=s),
+    "residual_norm_backward": lambda t, s: api.tac_residual_norm_backward(t, None, t, t, stream=s),
+    "scaled_product": lambda t, s: api.tac_scaled_product(t, t, t, t, 8, stream=s),
+    "gated_scan": lambda t, s: api.tac_gated_scan(t, t, stream=s),
+    "gated_scan_backward": lambda t, s: api.tac_gated_scan_backward(t, t, t, t, stream=s),
+    "gated_step": lambda t, s: api.tac_gated_step(t, t, t, stream=s),
+}
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_a_given_stream_is_one_of_the_tensors_device(name, monkeypatch):
+    import contextlib
+    import types
+    import torch
+    seen, inside = [], []
+
+    class Native:
+        def __getattr__(self, function):
+            return lambda *args: (function, list(inside))
+
+    @contextlib.contextmanager
+    def current(stream):
+        inside.append(stream)
+        yield
+        inside.pop()
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle, device=None: seen.append((handle, device)) or (handle, device))
+    monkeypatch.setattr(torch.cuda, "stream", current)
+    monkeypatch.setattr(api, "_native", Native)
+    tensor = types.SimpleNamespace(device=torch.device("cuda:1"))        # not the current device
+    function, streams = CALLS[name](tensor, 77)
+    assert function == name.split()[0] and streams == seen == [(77, torch.device("cuda:1"))]
+    function, streams = CALLS[name](tensor, None)
+    assert function == name.split()[0] and streams == [] and len(seen) == 1
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_a_stream_does_not_change_what_is_refused(name):
+    import torch
+    with pytest.raises(ValueError):
+        CALLS[name](torch.zeros(4, 8), 77)
+    with pytest.raises((ValueError, TypeError)):
+        CALLS[name](None, 77)
