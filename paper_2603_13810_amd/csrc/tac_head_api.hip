@@ -2,6 +2,7 @@
 #include <cmath>
 
 #include "tac_head_common.h"
+#include "tac_quantize_plan.h"
 
 namespace {
 
@@ -64,7 +65,7 @@ int tac_quantize(const tac_quantize_desc_t* d, const void* src, const uint8_t* s
   if (scaled && !src_scales) return TAC_ERR_NULL;
   if (!scaled && bad_stride(src, d->src_stride, d->rows, d->cols)) return TAC_ERR_BAD_SHAPE;
   const int64_t tiles = ((d->rows + 127) / 128) * ((d->cols + 127) / 128);
-  if (tiles >= 1 << 24) return TAC_ERR_BAD_SHAPE;             // a launch has fewer than 2^32 threads
+  if (tiles >= tac::kMostTiles) return TAC_ERR_BAD_SHAPE;
   if (misaligned(src, scaled ? 16 : bytes_of(d->dtype)) || (scaled && misaligned(src_scales, 4)) || misaligned(codes, 16) ||
       misaligned(codes_t, 16) || misaligned(scales, 4) || misaligned(scales_t, 4))
     return TAC_ERR_ALIGN;

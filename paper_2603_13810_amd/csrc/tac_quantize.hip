@@ -5,6 +5,7 @@
 // come first: rows further apart than a few kilobytes share too few memory channels.  8192 x 8192 bfloat16, calls in a row: 32 us along the rows, 31 along
 // the columns, 47 both, and 30 from 8-bit codes (6.3, 6.5, 5.7 and 4.5 TB/s with what the last-level cache keeps; a copy from memory reaches 5.1).
 #include "tac_head_common.h"
+#include "tac_quantize_plan.h"
 
 namespace tac {
 
@@ -218,7 +219,7 @@ __global__ __launch_bounds__(256) void dequantize_kernel(const uint8_t* __restri
 
 template <int DT, bool VEC>
 static void quantize_typed(const QuantizeParams& p, dim3 grid, int ct, hipStream_t s) {
-  if (!p.codes_t && !p.tiles) hipLaunchKernelGGL((quantize_kernel<DT, VEC, true, false>), grid, dim3(512), 0, s, p, ct);
+  if (rows_alone(p.codes_t, p.tiles, grid.x)) hipLaunchKernelGGL((quantize_kernel<DT, VEC, true, false>), grid, dim3(512), 0, s, p, ct);
   else if (!p.codes && !p.tiles) hipLaunchKernelGGL((quantize_kernel<DT, VEC, false, true>), grid, dim3(256), 0, s, p, ct);
   else hipLaunchKernelGGL((quantize_kernel<DT, VEC, true, true>), grid, dim3(256), 0, s, p, ct);
 }

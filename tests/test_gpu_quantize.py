@@ -134,3 +134,14 @@ def test_offsets_beyond_32_bits():
         check((codes.contiguous(), scales.contiguous()), want, e, rows - r0)
     back = api.tac_dequantize(got["rows"], cols, dtype=torch.bfloat16)
     assert np.array_equal(O.as64(back[rows - 2:]), O.decode((got["rows"][0][rows - 2:], got["rows"][1][rows - 2:]), cols)[0])
+
+
+def test_more_tiles_than_512_threads_each_fit_a_launch():
+    square = 1 << 15
+    x = torch.empty((1, square * square + 200), dtype=torch.bfloat16, device=DEV)        # 2^23 + 2 tiles of one row
+    x.normal_()
+    codes, scales = api.tac_quantize(x)["rows"]
+    want = api.tac_quantize(x[:, :square * square].view(square, square))["rows"]
+    assert torch.equal(codes[:, :square * square].view(square, square), want[0])
+    assert torch.equal(scales[:, :square * square // 128].view(square, -1), want[1])
+    check((codes[:, square * square:].contiguous(), scales[:, square * square // 128:].contiguous()), *O.quantized(O.as64(x[:, square * square:])), 200)
