@@ -7,13 +7,14 @@
 // more, in registers, from the state that it now knows.  Inputs are read once and outputs written once.  Where the channels are too few for
 // the chip, workgroups share the length as well: a launch that only forms the maps of the parts, then one that starts every part from those before it.
 #include "tac_head_common.h"
+#include "tac_scan_plan.h"
 
 namespace tac {
 
 namespace {
 
 constexpr int kChunk = TAC_SCAN_CHUNK;       // steps of a wave
-constexpr int kWaves = 8;                    // most waves of a workgroup
+constexpr int kWaves = kScanWaves;
 
 // w = min(a, 1 - a) = 1 / (1 + exp(|gate|)), negative (as -0 too) where a is the smaller.  Updates are written around the nearer of the two ends,
 //   a >= 1/2:  h' = h + w (value - h)        a < 1/2:  h' = value - w (value - h)
@@ -459,7 +460,6 @@ __global__ __launch_bounds__(256) void step_kernel(const StepParams p) {
   ((T*)p.out)[b * p.out_b + d] = (T)h;
 }
 
-int wave_count(int64_t T) { return (int)(T > kWaves * kChunk ? kWaves : (T + kChunk - 1) / kChunk); }
 int64_t channel_groups(int B, int D, int v) { return (int64_t)B * ((D + 64 * v - 1) / (64 * v)); }
 
 // Parts of the length: one where the channels alone give three workgroups to every four compute units, else enough for two to each.
@@ -481,8 +481,8 @@ bool streamed_rows(int64_t steps, int D, int bf) { return D % (bf ? 8 : 4) == 0 
 
 template <typename T, int V>
 hipError_t scan_typed(const ScanParams& p, hipStream_t s) {
-  const int parts = length_parts(p.T, p.B, p.D, p.bf16), threads = 64 * wave_count(p.T);
   const unsigned groups = (unsigned)channel_groups(p.B, p.D, V);
+  const int parts = length_parts(p.T, p.B, p.D, p.bf16), threads = 64 * scan_waves(p.T, groups);
   if (parts > 1) {
     hipLaunchKernelGGL((scan_kernel<T, V, true>), dim3(groups, parts), dim3(threads), 0, s, p);
     const hipError_t e = hipGetLastError();
@@ -495,8 +495,8 @@ hipError_t scan_typed(const ScanParams& p, hipStream_t s) {
 
 template <typename T, int V>
 hipError_t scan_backward_typed(const ScanBackwardParams& p, hipStream_t s) {
-  const int parts = length_parts(p.T, p.B, p.D, p.bf16), threads = 64 * wave_count(p.T);
   const unsigned groups = (unsigned)channel_groups(p.B, p.D, V);
+  const int parts = length_parts(p.T, p.B, p.D, p.bf16), threads = 64 * scan_waves(p.T, groups);
   if (parts > 1) {
     hipLaunchKernelGGL((scan_backward_kernel<T, V, true>), dim3(groups, parts), dim3(threads), 0, s, p);
     const hipError_t e = hipGetLastError();
