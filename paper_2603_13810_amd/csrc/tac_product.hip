@@ -4,9 +4,9 @@
 // lane passes in a byte: a block's scale costs no instruction of its own, and all blocks of a sum stay in one accumulator.  Lane l holds 32
 // consecutive codes of row l % 32.
 //
-// That instruction adds eight consecutive products at a time and keep only what reaches 2^-13 of the largest of them (measured: 2^16 and
-// one smaller term; normal operands leave a relative error of 1.5e-5 in a sum, wide ones 7e-5).  A bfloat16 result rounds by 2^-8 and does not
-// notice; for a float32 result the codes are turned into bfloat16 in registers, exactly and with their scale (v_cvt_scalef32_pk_bf16_fp8),
+// That instruction adds eight consecutive products at a time and keeps only what reaches 2^-13 of the largest of them (measured: 2^16 and
+// one smaller term; the root mean square of a sum's error is 1.3e-5 to 1.7e-5 of the sums' for normal operands of 512 to 16384 columns, 4e-5 to 7e-5 where
+// their columns' sizes spread by a factor e).  A bfloat16 result rounds by 2^-8 and does not notice; for a float32 result the codes are turned into bfloat16 in registers, exactly and with their scale (v_cvt_scalef32_pk_bf16_fp8),
 // and multiplied by v_mfma_f32_32x32x16_bf16, which keeps float32 sums (1e-8), at half the rate.
 //
 // The rows of b are the instruction's first operand: a lane then ends with four consecutive n of one m.

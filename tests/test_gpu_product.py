@@ -139,3 +139,40 @@ def test_output_beyond_32_bits():
     got = api.tac_scaled_product(*a, *b, K, dtype=torch.float32)
     y, size = exact((a[0][-50:], a[1][-50:]), b, K)
     check(got[-50:], y, size, K)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,N,K", [(1, 40, 700), (5, 40, 700), (70, 260, 900), (300, 260, 700), (600, 700, 1400), (2200, 1500, 300)])
+def test_one_product_per_place_is_exact(M, N, K, dtype):
+    # every row of a has one value, so a place is one product of two numbers of four bits: exact in bfloat16 too, whichever instruction multiplies.
+    # Values differ by row, column, block and byte
+    a, rows, cols, k = torch.zeros(M, K, device=DEV), torch.arange(M, device=DEV), torch.arange(N, device=DEV), torch.arange(K, device=DEV)
+    a[rows, 37 * rows % K] = (1 + rows % 15) * 2.0 ** (rows % 9 - 4)
+    b = (1 + (cols[:, None] + 3 * k[None, :]) % 15) * 2.0 ** ((2 * cols[:, None] + k[None, :] // 128) % 11 - 5)
+    qa, qb = api.tac_quantize(a)["rows"], api.tac_quantize(b)["rows"]
+    want = a[rows, 37 * rows % K].double()[:, None] * b.double()[:, 37 * rows % K].t()
+    assert torch.equal(api.tac_scaled_product(*qa, *qb, K, dtype=dtype).double(), want)
+
+
+@pytest.mark.parametrize("M", [1, 20, 300])
+@pytest.mark.parametrize("spread", [0.0, 1.0])
+@pytest.mark.parametrize("N,K", [(2000, 512), (2000, 4096), (300, 20000)])
+def test_digits_of_the_8bit_instruction(M, N, K, spread):
+    # The bias takes the sum away again, so that the bfloat16 result is the sum's error (one row of a, M times).
+    g = torch.Generator(device=DEV).manual_seed(41)
+    scale = torch.exp(spread * torch.randn(2, K, generator=g, device=DEV))
+    a, b = torch.randn(1, K, generator=g, device=DEV) * scale[0], torch.randn(N, K, generator=g, device=DEV) * scale[1]
+    qa, qb = api.tac_quantize(a)["rows"], api.tac_quantize(b)["rows"]
+    terms = torch.from_numpy(O.decode(qa, K)[0] * O.decode(qb, K)[0]).to(DEV)
+    y = terms.sum(1)
+    got = api.tac_scaled_product(*(t.expand(M, -1).contiguous() for t in qa), *qb, K, bias=-y.float())
+    assert all(torch.equal(got[i], got[0]) for i in range(M))
+    error = (got[0].double() - (y - y.float().double())) / (1 + O.HALF[torch.bfloat16])
+    # eight neighbours lose less than 2^-13 of the largest each; signs are mixed, so errors up to q of either sign add up to at most
+    # sqrt(8 / 3) q per eight in the root mean square, over all eights
+    q = 2.0 ** -13 * torch.nn.functional.pad(terms, (0, -K % 8)).abs().view(N, -1, 8).amax(2)
+    f32 = K * O.U * y.abs().max()                        # sums in float32 and the bias's rounding, far below
+    assert bool((error.abs() <= 8 * q.sum(1) + f32).all())
+    assert float(error.square().mean()) <= 8 / 3 * float(q.square().sum(1).mean()) + float(f32) ** 2
+    # what tac.h states of a sum: a relative error of a few 1e-5 (and not float32's 6e-8 either, which this instruction does not have)
+    assert float(error.square().mean().sqrt() / y.square().mean().sqrt()) < 1e-4
