@@ -61,11 +61,20 @@ def build(verbose: bool = True) -> str:
     return LIB
 
 
-def build_operators() -> str:
-    """The Python module of the dense operators: host code alone, against torch's headers, linked to the library beside it."""
+def build_operators():
+    """The Python module of the dense operators: host code alone, against torch's headers, linked to the library beside it.  Where there are none the
+    library is complete without it: None, and the module's calls say that it has not been built."""
     import sysconfig
-    import torch
-    at = os.path.dirname(torch.__file__)
+    try:
+        import torch
+        at = os.path.dirname(torch.__file__)
+    except ImportError:
+        at = None
+    if at is None or not os.path.exists(os.path.join(at, "include/torch/csrc/Dtype.h")):
+        if os.path.exists(OPERATORS):
+            os.remove(OPERATORS)               # of an earlier library
+        print("no torch headers: the Python module of the dense operators is not built", flush=True)
+        return None
     tmp = OPERATORS + ".tmp%d" % os.getpid()
     subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
                            "-I", INCLUDE, "-isystem", os.path.join(at, "include"), "-isystem", os.path.join(at, "include/torch/csrc/api/include"),

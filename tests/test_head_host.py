@@ -291,3 +291,29 @@ def test_a_stream_does_not_change_what_is_refused(name):
         CALLS[name](torch.zeros(4, 8), 77)
     with pytest.raises((ValueError, TypeError)):
         CALLS[name](None, 77)
+
+
+@pytest.mark.parametrize("torch_is", ["missing", "without headers"])
+def test_the_library_is_built_without_torchs_headers(torch_is, tmp_path, monkeypatch):
+    import subprocess
+    import sys
+    import types
+    from paper_2603_13810_amd import build
+    stale, ran = tmp_path / "_operators.so", []
+    stale.write_text("of an earlier library")
+    monkeypatch.setattr(build, "OPERATORS", str(stale))
+    monkeypatch.setattr(build, "LIB", str(tmp_path / "libtac.so"))
+    monkeypatch.setattr(build, "SOURCES", ["tac_head_api.hip"])
+    monkeypatch.setattr(build, "CSRC", str(tmp_path))
+    (tmp_path / "tac_head_api.hip").write_text("")
+
+    def link(cmd):
+        ran.append(cmd)
+        open(cmd[cmd.index("-o") + 1], "w").close()
+    monkeypatch.setattr(subprocess, "run", lambda cmd, **kw: types.SimpleNamespace(stdout="", returncode=0))
+    monkeypatch.setattr(subprocess, "check_call", link)
+    fake = types.ModuleType("torch")
+    fake.__file__ = str(tmp_path / "torch" / "__init__.py")
+    monkeypatch.setitem(sys.modules, "torch", None if torch_is == "missing" else fake)
+    assert build.build(verbose=False) == str(tmp_path / "libtac.so") and os.path.exists(build.LIB)
+    assert len(ran) == 1 and not stale.exists()
