@@ -510,6 +510,8 @@ def tac_reset_counters() -> None:
 
 # ---- dense operators over a stack's features (see include/tac.h) ---------------------------------
 # An 8-bit matrix is a pair (codes, scales) of uint8 tensors, [rows, 128 ceil(cols / 128)] and [rows, 4 ceil(cols / 512)].
+# Like the layers' calls these are not recorded by torch's autograd: results are detached, whatever their inputs require, and gradients come from the
+# *_backward calls.  Tensors that are given to be written (out, h, y, pool, grad_*) count as changed in place, so that autograd notices where it has kept them.
 
 TAC_SCALED = 2
 TAC_BLOCK_ROW, TAC_BLOCK_TILE = 0, 1

@@ -140,6 +140,10 @@ PyObject* same(PyObject* o) {
   Py_INCREF(o);
   return o;
 }
+// the caller's tensor has been written: what autograd has kept of it is out of date (inference tensors keep no count)
+void written(const Tensor* t) {
+  if (t && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+}
 // a dict that takes the values' references
 PyObject* dict_of(std::initializer_list<std::pair<const char*, PyObject*>> items) {
   PyObject* d = PyDict_New();
@@ -216,6 +220,7 @@ PyObject* dequantize(PyObject*, PyObject* const* a, Py_ssize_t count) {
     return tac_dequantize(R, C, from.codes, from.scales, type, at, row_stride(&out, R, C), c.stream());
   });
   if (status) return PyLong_FromLong(status);
+  written(to);
   return to ? same(a[4]) : out_of(out);
   TAC_END
   END_HANDLE_TH_ERRORS
@@ -252,6 +257,8 @@ PyObject* residual_norm(PyObject*, PyObject* const* a, Py_ssize_t count) {
                                        (float*)at_of(rstd), c.stream());
   });
   if (status) return PyLong_FromLong(status);
+  written(h_given);
+  written(y_given);
   return dict_of({{"h", h_given ? same(a[4]) : out_of(h)}, {"y", y_given ? same(a[5]) : out_of(y)}, {"scaled", out_of(scaled)}, {"rstd", out_of(rstd)}});
   TAC_END
   END_HANDLE_TH_ERRORS
@@ -285,6 +292,7 @@ PyObject* residual_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t count
     return tac_residual_norm_backward(&d, h_at, gain_at, rstd_at, gy_at, gh_at, gx_at, (float*)at_of(grad_gain), at_of(work), c.stream());
   });
   if (status) return PyLong_FromLong(status);
+  written(to);
   return dict_of({{"grad_x", to ? same(a[5]) : out_of(grad_x)}, {"grad_gain", out_of(grad_gain)}});
   TAC_END
   END_HANDLE_TH_ERRORS
@@ -311,6 +319,7 @@ PyObject* scaled_product(PyObject*, PyObject* const* a, Py_ssize_t count) {
     return tac_scaled_product(&d, at.codes, at.scales, bt.codes, bt.scales, bias, y, at_of(work), c.stream());
   });
   if (status) return PyLong_FromLong(status);
+  written(to);
   return to ? same(a[7]) : out_of(out);
   TAC_END
   END_HANDLE_TH_ERRORS
@@ -357,6 +366,7 @@ PyObject* gated_scan(PyObject*, PyObject* const* a, Py_ssize_t count) {
     return tac_gated_scan(&d, g, v, lengths, h0, o, (float*)at_of(h_last), (float*)at_of(states), at_of(work), c.stream());
   });
   if (status) return PyLong_FromLong(status);
+  written(to);
   return dict_of({{"out", to ? same(a[4]) : out_of(out)}, {"h_last", out_of(h_last)}, {"states", out_of(states)}});
   TAC_END
   END_HANDLE_TH_ERRORS
@@ -395,6 +405,8 @@ PyObject* gated_scan_backward(PyObject*, PyObject* const* a, Py_ssize_t count) {
     return tac_gated_scan_backward(&d, g, v, lengths, kept, go, last, gg.data_ptr(), gv.data_ptr(), (float*)at_of(h0), at_of(work), c.stream());
   });
   if (status) return PyLong_FromLong(status);
+  written(gg_given);
+  written(gv_given);
   return dict_of({{"grad_gate", gg_given ? same(a[6]) : out_of(gg)}, {"grad_value", gv_given ? same(a[7]) : out_of(gv)}, {"grad_h0", out_of(h0)}});
   TAC_END
   END_HANDLE_TH_ERRORS
@@ -425,6 +437,8 @@ PyObject* gated_step(PyObject*, PyObject* const* a, Py_ssize_t count) {
     return tac_gated_step(&d, g, v, states, slots, of, o, c.stream());
   });
   if (status) return PyLong_FromLong(status);
+  written(to);
+  written(&pool);
   return to ? same(a[4]) : out_of(out);
   TAC_END
   END_HANDLE_TH_ERRORS

@@ -98,3 +98,40 @@ def test_outputs_that_are_given_come_back():
     assert api.tac_gated_scan(out, out, out=out)["out"] is out
     g = api.tac_gated_scan_backward(f32(3, 2, 4), f32(3, 2, 4), f32(1, 2, 4), f32(3, 2, 4), grad_gate=f32(3, 2, 8)[..., :4])
     assert g["grad_value"].stride() == g["grad_gate"].stride() == (16, 8, 1)
+
+
+GIVEN = {
+    "dequantize out": lambda t: api.tac_dequantize(matrix(4, 8), 8, out=t),
+    "norm h": lambda t: api.tac_residual_norm(f32(4, 8), f32(4, 8), eps=1e-5, h=t),
+    "norm y": lambda t: api.tac_residual_norm(f32(4, 8), eps=1e-5, y=t),
+    "norm backward grad_x": lambda t: api.tac_residual_norm_backward(f32(4, 8), None, f32(4), f32(4, 8), grad_x=t),
+    "product out": lambda t: api.tac_scaled_product(*matrix(4, 8), *matrix(8, 8), 8, out=t),
+    "scan out": lambda t: api.tac_gated_scan(f32(2, 2, 8), f32(2, 2, 8), out=t.view(2, 2, 8)),
+    "scan backward grad_gate": lambda t: api.tac_gated_scan_backward(f32(2, 2, 8), f32(2, 2, 8), f32(1, 2, 8), f32(2, 2, 8), grad_gate=t.view(2, 2, 8)),
+    "scan backward grad_value": lambda t: api.tac_gated_scan_backward(f32(2, 2, 8), f32(2, 2, 8), f32(1, 2, 8), f32(2, 2, 8), grad_value=t.view(2, 2, 8)),
+    "step pool": lambda t: api.tac_gated_step(f32(4, 8), f32(4, 8), t),
+    "step out": lambda t: api.tac_gated_step(f32(4, 8), f32(4, 8), f32(4, 8), out=t),
+}
+
+
+@pytest.mark.parametrize("name", GIVEN)
+def test_a_written_tensor_counts_as_changed_in_place(name):
+    t, w = f32(4, 8), f32(4, 8).requires_grad_()
+    loss = (w * t).sum()                                     # autograd keeps t
+    GIVEN[name](t)
+    assert t._version == 1
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    with torch.inference_mode():
+        plain = f32(4, 8)
+        GIVEN[name](plain)
+    GIVEN[name](plain)                                       # and outside, where torch's own in-place operations refuse it
+
+
+def test_results_are_not_recorded_by_autograd():
+    x = torch.randn(4, 8, device=DEV).requires_grad_()
+    got = api.tac_residual_norm(x, x, eps=1e-5, want_rstd=True)
+    assert x._version == 0 and not any(got[k].requires_grad for k in ("h", "y", "rstd"))
+    before = x.detach().clone()
+    api.tac_residual_norm(x, eps=1e-5)
+    assert x._version == 0 and torch.equal(x, before)
