@@ -45,7 +45,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(const N
       for (int e = 0; e < kCols; ++e) g[q][e] = 1.0f;
       if (p.gain && (p.y || p.codes) && c < p.cols) load_floats<float, kCols, VEC>(p.gain + c, p.cols - c, g[q]);
     }
-  #pragma unroll
+#pragma unroll
     for (int q = 0; q < PASSES; ++q) {
       const int c = (q * LANES + lane) * kCols;
       const int n = p.cols - c;
@@ -54,21 +54,21 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(const N
         if (p.residual) {
           float r[kCols];
           load_floats<T, kCols, VEC>((const T*)p.residual + row * p.residual_stride + c, n, r);
-  #pragma unroll
+#pragma unroll
           for (int e = 0; e < kCols; ++e) v[q][e] += r[e];
         }
         if (p.h) store_floats<T, kCols, VEC, PAST>((T*)p.h + row * p.h_stride + c, n, v[q]);
       } else {
-  #pragma unroll
+#pragma unroll
         for (int e = 0; e < kCols; ++e) v[q][e] = 0.0f;
       }
-  #pragma unroll
+#pragma unroll
       for (int e = 0; e < kCols; ++e) squares = fmaf(v[q][e], v[q][e], squares);
     }
     const float rstd = 1.0f / sqrtf(row_sum<LANES>(squares, room) / (float)p.cols + p.eps);
     if (p.rstd && lane == 0) p.rstd[row] = rstd;
     if (!p.y && !p.codes) continue;
-  #pragma unroll
+#pragma unroll
     for (int q = 0; q < PASSES; ++q) {
       const int c = (q * LANES + lane) * kCols;
       const int n = p.cols - c;
@@ -85,7 +85,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(const N
           }
         }
         float amax = 0.0f;
-  #pragma unroll
+#pragma unroll
         for (int e = 0; e < kCols; ++e) {
           v[q][e] = finite_or_nan(v[q][e]);
           amax = fmaxf(amax, fabsf(v[q][e]));
@@ -93,7 +93,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(const N
         const uint32_t byte = scale_byte(max_over_16(amax));
         const float inv = scale_inverse(byte);
         if (c < pitch) store_codes(p.codes + row * pitch + c, v[q], inv);
-      if (lane % 16 == 0 && c / kBlock < spitch) p.scales[row * spitch + c / kBlock] = (uint8_t)byte;
+        if (lane % 16 == 0 && c / kBlock < spitch) p.scales[row * spitch + c / kBlock] = (uint8_t)byte;
       }
     }
   }

@@ -3,7 +3,8 @@
 // Memory-bound.  A workgroup takes a tile of 128 x 128: a thread holds 32 or 64 values of it in registers, so its codes of
 // a row are one store of the straight matrix, and its codes of a column go through LDS to become rows of 128 codes of the transposed one.  Tiles along a row
 // come first: rows further apart than a few kilobytes share too few memory channels.  8192 x 8192 bfloat16, calls in a row: 32 us along the rows, 31 along
-// the columns, 47 both, and 30 from 8-bit codes (6.3, 6.5, 5.7 and 4.5 TB/s with what the last-level cache keeps; a copy from memory reaches 5.1).
+// the columns, 46 both, and 30 from 8-bit codes (6.3, 6.5, 5.8 and 4.5 TB/s with what the last-level cache keeps; a copy from memory reaches 4.9).  In tiles,
+// both ways, as weights are laid out: 8192 x 4096 float32 32 us.  Back to bfloat16 31 us, to float32, past what the cache keeps, 88 (3.8 TB/s).
 #include "tac_head_common.h"
 #include "tac_quantize_plan.h"
 
@@ -44,7 +45,7 @@ struct Eight {
 // VEC: rows of whole 16-byte pieces.  ROWS without COLUMNS: the straight matrix with a scale per row (an activation or gradient on its way into a
 // product); COLUMNS without ROWS: the transposed one with a scale per column (the operands of a weight gradient); both: either, and tiles.
 // A thread has 4 rows x 8 columns where it looks at rows alone (twice as many waves in flight as with 8: 16 x 4096 3.2 us against 4.6) and 8 x 8 for columns,
-// where it then writes 8 codes of one at a time into LDS (8192 x 8192 38 us against 44 with 4).
+// where it then writes 8 codes of one at a time into LDS (8192 x 8192 31 us against 35 with 4).
 // Largest values are taken with infinities first, since next to no matrix has one; a workgroup that finds one looks again without them.  The conversion
 // turns an infinity into NaN by itself.
 template <int DT, bool VEC, bool ROWS, bool COLUMNS>
