@@ -475,7 +475,7 @@ int tac_scaled_product(const tac_product_desc_t* desc, const uint8_t* a_codes, c
  * sequence's length on, what stands behind it is read into no result, and its last state is that of its last step (h0 where the
  * length is 0).  Infinite and NaN values, states and gradients go on by these formulas in float32: an infinite state stays infinite until one of the
  * other sign meets it or float32 has its factor as 0, either of which makes it NaN.  Channels that have one take their steps one after the
- * other, many times slower than the rest. */
+ * other, many times slower than the rest.  (Where an output lies on an input of the same call they are NaN from the next step on.) */
 #define TAC_SCAN_CHUNK 16
 typedef struct tac_scan_desc {
   int64_t T;                     /* steps of the tensors */

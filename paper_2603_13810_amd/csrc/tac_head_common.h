@@ -230,6 +230,7 @@ struct ScanParams {
   float *h_last, *states, *workspace;
   int64_t T, in_t, in_b, out_t, out_b;
   int B, D, bf16;
+  int apart;                // no output lies on an input (set by scan_launch): steps can be taken a second time
 };
 struct ScanBackwardParams {
   const void *gate, *value;
@@ -241,6 +242,7 @@ struct ScanBackwardParams {
   float *grad_h0, *workspace;
   int64_t T, in_t, in_b, out_t, out_b, grad_t, grad_b;
   int B, D, bf16;
+  int apart;
 };
 size_t scan_workspace(int64_t T, int B, int D, int bf16);
 hipError_t scan_launch(const ScanParams& p, hipStream_t s);

@@ -31,7 +31,7 @@ __device__ __forceinline__ float times_a(float s, float x) { return fmaf(-s, x, 
 // Those forms turn an infinity into inf - inf, and the difference of two values near float32's largest into an infinity; maps multiply infinities
 // by factors that have become 0.  What is infinite or NaN stays one of the two in them, step by step and map by map, so that a look at the end of every
 // chunk finds it.  The steps of such a channel are then taken again one after the other by the formula as it stands wherever the form above is not
-// finite: an infinity goes on as a h + (1 - a) value says, NaN where float32 has its factor as 0.
+// finite: an infinity goes on as a h + (1 - a) value says, NaN where float32 has its factor as 0.  (Not where outputs have taken the inputs' place.)
 __device__ __forceinline__ bool finite(float v) { return fabsf(v) < __builtin_inff(); }
 __device__ __forceinline__ float a_of(float s) { return forgets(s) ? fabsf(s) : 1.0f - fabsf(s); }
 __device__ __forceinline__ float rest_of(float s) { return forgets(s) ? 1.0f - fabsf(s) : fabsf(s); }
@@ -223,7 +223,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void scan_kernel(const ScanParams p
     const int64_t steps = (int64_t)waves * kChunk;
 #pragma unroll 1
     for (int e = 0; e < V; ++e) {
-      if (!q.on || ((e ? good[V - 1] : good[0]) && finite(e ? carry[V - 1] : carry[0]))) continue;
+      if (!q.on || !p.apart || ((e ? good[V - 1] : good[0]) && finite(e ? carry[V - 1] : carry[0]))) continue;
       float h = starts[wave][e][lane];
       int from = 0;                  // the first part that ends with something else than a number, or this one
       for (; from < (int)blockIdx.y; ++from) {
@@ -408,7 +408,7 @@ __global__ __launch_bounds__(64 * kWaves) void scan_backward_kernel(const ScanBa
     const int64_t steps = (int64_t)waves * kChunk;
 #pragma unroll 1
     for (int e = 0; e < V; ++e) {
-      if (!q.on || ((e ? good[V - 1] : good[0]) && finite(e ? carry[V - 1] : carry[0]))) continue;
+      if (!q.on || !p.apart || ((e ? good[V - 1] : good[0]) && finite(e ? carry[V - 1] : carry[0]))) continue;
       float c = starts[wave][e][lane];
       int from = gridDim.y - 1;
       for (; from > (int)blockIdx.y; --from) {
@@ -514,13 +514,21 @@ size_t scan_workspace(int64_t T, int B, int D, int bf) {
   return parts > 1 ? (size_t)parts * 2 * (size_t)B * (size_t)D * sizeof(float) : 0;
 }
 
-hipError_t scan_launch(const ScanParams& p, hipStream_t s) {
+hipError_t scan_launch(const ScanParams& given, hipStream_t s) {
+  ScanParams p = given;
+  const Rows out = {p.out, p.out_t, p.out_b};
+  p.apart = true;
+  for (const void* in : {p.gate, p.value}) p.apart &= !rows_overlap({in, p.in_t, p.in_b}, out, p.T, p.B, p.D, p.bf16 ? 2 : 4);
   if (!p.bf16) return scan_typed<float, 1>(p, s);
   const bool two = pairs(p.D, p.in_t, p.in_b, p.gate, p.value) && pairs(p.D, p.out_t, p.out_b, p.out, nullptr);
   return two ? scan_typed<bf16, 2>(p, s) : scan_typed<bf16, 1>(p, s);
 }
 
-hipError_t scan_backward_launch(const ScanBackwardParams& p, hipStream_t s) {
+hipError_t scan_backward_launch(const ScanBackwardParams& given, hipStream_t s) {
+  ScanBackwardParams p = given;
+  p.apart = true;
+  for (const Rows& in : {Rows{p.gate, p.in_t, p.in_b}, Rows{p.value, p.in_t, p.in_b}, Rows{p.grad_out, p.out_t, p.out_b}})
+    for (const void* out : {p.grad_gate, p.grad_value}) p.apart &= !rows_overlap(in, {out, p.grad_t, p.grad_b}, p.T, p.B, p.D, p.bf16 ? 2 : 4);
   if (!p.bf16) return scan_backward_typed<float, 1>(p, s);
   const bool two = pairs(p.D, p.in_t, p.in_b, p.gate, p.value) && pairs(p.D, p.out_t, p.out_b, p.grad_out, nullptr) &&
                    pairs(p.D, p.grad_t, p.grad_b, p.grad_gate, p.grad_value);

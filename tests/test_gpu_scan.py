@@ -397,3 +397,32 @@ def test_infinite_states_where_the_last_takes_the_place_of_the_first(T, B, D, dt
     for got, w in ((state, want["h_last"]), (out, want["out"]), (states, want["states"]), (grad, want_back["grad_h0"]), (gg, want_back["grad_gate"]),
                    (gv, want_back["grad_value"])):
         assert torch.allclose(got.float(), w.float(), rtol=0, atol=0, equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,B,D", [(50, 2, 66), (3000, 1, 64), (300, 200, 32)])
+def test_in_place_a_channel_that_ends_in_nan_keeps_what_was_before(T, B, D, dtype):
+    g = torch.Generator(device=DEV).manual_seed(35)
+    gate, value, go = ((torch.randn(T, B, D, generator=g, device=DEV) + 1).to(dtype) for _ in range(3))
+    clean = api.tac_gated_scan(gate, value, want_states=True)
+    clean_back = api.tac_gated_scan_backward(gate, value, clean["states"], go)
+    at, nan = T // 2, float("nan")
+
+    def check(got, want, nans):
+        """`want`, but NaN in the channels and steps of `nans`"""
+        want = want.clone()
+        for steps, d in nans:
+            want[steps, :, d] = nan
+        assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.nan_to_num(0.5), want.nan_to_num(0.5))
+    value[at, :, 3], go[at, :, 5] = nan, nan
+    for name in ("value", "gate"):
+        a, b = gate.clone(), value.clone()
+        into = b if name == "value" else a
+        got = api.tac_gated_scan(a, b, out=into, want_states=True)
+        check(into, clean["out"], [(slice(at, None), 3)])
+        check(got["h_last"][None], clean["h_last"][None], [(slice(None), 3)])
+        check(got["states"], clean["states"], [(slice(at // api.TAC_SCAN_CHUNK + 1, None), 3)])
+    a, b = gate.clone(), value.clone()
+    api.tac_gated_scan_backward(a, b, got["states"], go, grad_gate=a, grad_value=b)
+    check(a, clean_back["grad_gate"], [(slice(at, None), 3), (slice(0, at + 1), 5)])
+    check(b, clean_back["grad_value"], [(slice(0, at + 1), 5)])

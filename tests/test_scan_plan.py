@@ -29,3 +29,29 @@ def test_a_wave_a_chunk_and_no_more_than_a_launch_holds(shim, T):
         waves = shim.scan_waves_of(T, groups)
         assert 1 <= waves <= usual and 64 * waves * groups < 1 << 32
         assert waves == usual or 64 * (waves + 1) * groups >= 1 << 32
+
+
+def touched(at, st, sb, T, B, D, el):
+    return {at + el * (t * st + b * sb + d) + i for t in range(T) for b in range(B) for d in range(D) for i in range(el)}
+
+
+def test_sequences_that_share_memory_are_seen(shim):
+    shim.rows_overlap_of.argtypes = [ctypes.c_longlong] * 10
+    import random
+    r, apart, slices = random.Random(3), 0, 0
+    for _ in range(4000):
+        T, B, D, el = r.randint(1, 4), r.randint(1, 3), r.randint(1, 5), r.choice([2, 4])
+        wide = D * r.randint(1, 4)
+        layout = lambda: r.choice([(B * wide, wide), (wide, T * wide), (B * D, D), (D, T * D)])
+        x, y = layout(), layout()
+        if r.random() < 0.5:
+            y = x
+        at = 1000 * el
+        other = at + el * r.choice([0, D, -D, 2 * D, r.randint(-60, 60), r.randint(-300, 300)])
+        share = bool(touched(at, *x, T, B, D, el) & touched(other, *y, T, B, D, el))
+        seen = bool(shim.rows_overlap_of(at, *x, other, *y, T, B, D, el))
+        assert seen or not share                         # never missed
+        apart += not seen
+        slices += not seen and x == y and 0 < abs(other - at) < (T - 1) * x[0] * el
+    assert apart > 500 and slices > 100                  # and slices of the same rows are not taken for shared
+    assert not shim.rows_overlap_of(0, 512, 256, 2 * 128, 512, 256, 100, 2, 128, 2)          # halves of rows, bfloat16
