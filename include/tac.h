@@ -369,7 +369,9 @@ int tac_stack_backward(const tac_stack_layer_t* layers, const tac_stack_grads_t*
  *   scales  uint8 [rows][4 ceil(cols / 512)], 4-byte aligned: byte j of a row is 127 + e, and 2^e multiplies the codes of columns
  *           128 j .. 128 j + 127; pad bytes are written as zero and read by nobody
  * e is the smallest from -127 on for which the block's largest magnitude is at most 448 * 2^e, so a code is its value's nearest (even)
- * e4m3 number in units of 2^e, rounded once.  Infinities and NaN become NaN codes; their block's scale is that of its finite values. */
+ * e4m3 number in units of 2^e, rounded once.  Infinities and NaN become NaN codes; their block's scale is that of its finite values.
+ * Magnitudes from 31/32 * 2^128 on (the largest bfloat16 and float32 numbers among them, which masks are made of) are nearest to 2^128, which float32
+ * does not have: tac_dequantize gives an infinity for them, and tac_scaled_product with a float32 y multiplies by one (with a bfloat16 y by 2^128). */
 #define TAC_SCALE_BLOCK 128
 size_t tac_code_bytes(int64_t rows, int64_t cols);      /* 0 if a dimension is <= 0 */
 size_t tac_scale_bytes(int64_t rows, int64_t cols);
