@@ -520,6 +520,121 @@ int tac_gated_scan_backward(const tac_scan_desc_t* desc, const void* gate, const
 int tac_gated_step(const tac_scan_desc_t* desc, const void* gate, const void* value, float* pool, int64_t n_slots,
                    const int32_t* slots, void* out, void* stream);
 
+/* Norm of every head and rotation by position, of queries and keys in one pass:
+ *   n = x / sqrt(mean over the head of x^2 + eps) * gain,   then pairs of features are turned:
+ *   (y0, y1) = (n0 cos t - n1 sin t, n1 cos t + n0 sin t),   t = position[axis] * base^(-i / pairs[axis])
+ * for the i-th of an axis's pairs; the axes' pairs follow each other.  With P pairs in all the first 2 P features of a head are turned, pair p
+ * being features (p, P + p), or (2 p, 2 p + 1) with `interleaved`; the others stay as the norm has them.  Angles are formed in 64 bits,
+ * so that far positions have the angles of near ones' precision; the rest is float32, each result rounded once. */
+#define TAC_ROTATION_AXES 4
+#define TAC_HEAD_MAX_FEATURES 512
+typedef struct tac_head_strides { int64_t row, head; } tac_head_strides_t;      /* elements from row to row and from head to head, >= D where more than one */
+typedef struct tac_head_norm_desc {
+  int64_t rows;
+  tac_head_strides_t query, key;             /* of the heads before the norm */
+  tac_head_strides_t out_query, out_key;     /* of the results, or (backward) of their gradients */
+  tac_head_strides_t grad_query, grad_key;   /* backward only */
+  int32_t query_heads, key_heads;            /* key_heads 0: queries alone, everything of keys is ignored */
+  int32_t D;                                 /* features of a head: even, 2 .. TAC_HEAD_MAX_FEATURES */
+  int32_t dtype;                             /* TAC_FP32 / TAC_BF16 */
+  int32_t axes;                              /* numbers in a position, 0 .. TAC_ROTATION_AXES; 0: no rotation */
+  int32_t pairs[TAC_ROTATION_AXES];          /* pairs of each axis, >= 1; at most D / 2 in all */
+  int32_t interleaved;
+  float eps;                                 /* > 0; 0: no norm, n = x gain */
+  double base;                               /* > 0 (ignored without a rotation) */
+} tac_head_norm_desc_t;
+/*   query, key            DEVICE, read-only, [rows][heads][D]
+ *   gain_query, gain_key  DEVICE, read-only, float32 [D], or NULL: ones
+ *   positions             DEVICE, read-only, int32 [rows][axes] (ignored without a rotation)
+ *   out_query, out_key    DEVICE, written; may be query and key (with their strides)
+ * Errors: TAC_ERR_NULL, TAC_ERR_BAD_SHAPE, TAC_ERR_UNSUPPORTED (more than TAC_HEAD_MAX_FEATURES features), TAC_ERR_BAD_PARAM, TAC_ERR_ALIGN, TAC_ERR_HIP. */
+int tac_head_norm(const tac_head_norm_desc_t* desc, const void* query, const void* key, const float* gain_query, const float* gain_key,
+                  const int32_t* positions, void* out_query, void* out_key, void* stream);
+
+/* Its backward pass: gradients of the results are turned back (g), then with n' = x rstd and w = gain g
+ *   grad_x = rstd (w - n' mean(w n')),  grad_gain = sum over rows and heads of g n'      (without a norm: w, and sum of g x)
+ *   query, key                        DEVICE, read-only: what the forward pass read
+ *   grad_out_query, grad_out_key      DEVICE, read-only, strides out_query, out_key
+ *   grad_query, grad_key              DEVICE, written; may be grad_out_query and grad_out_key (with their strides)
+ *   grad_gain_query, grad_gain_key    DEVICE, written, float32 [D], or NULL
+ *   workspace                         DEVICE, scratch, tac_head_norm_workspace_bytes(desc) bytes, 16-byte aligned; may be NULL where neither gain's gradient is asked for
+ * Sums are formed in an order that depends on the sizes alone: the same bits from call to call. */
+size_t tac_head_norm_workspace_bytes(const tac_head_norm_desc_t* desc);
+int tac_head_norm_backward(const tac_head_norm_desc_t* desc, const void* query, const void* key, const float* gain_query, const float* gain_key,
+                           const int32_t* positions, const void* grad_out_query, const void* grad_out_key, void* grad_query, void* grad_key,
+                           float* grad_gain_query, float* grad_gain_key, void* workspace, void* stream);
+
+/* Gated delta rule: a recurrence whose state is a matrix per head, an associative memory from keys to values.  For every sequence and head,
+ * with a_t = 1 / (1 + exp(-gate_t)) and b_t = 1 / (1 + exp(-write_t)):
+ *   S <- a_t S_{t-1},   u_t = b_t (value_t - S^T key_t),   S_t = S + key_t u_t^T,   out_t = S_t^T query_t
+ * so that S [Dk][Dv] fades by a_t and then moves what it answers to key_t towards value_t (all the way where b_t and |key_t| are 1).  Keys are
+ * wanted no longer than 1 (tac_head_norm with gains of Dk^-1/2): where b_t |key_t|^2 is beyond 2 the recurrence itself grows.  v_heads / k_heads
+ * consecutive heads of values share a head of queries and keys.  Sequences may have different lengths: out is zero from a sequence's length on, what
+ * stands behind it is read into no result, and its last state is that of its last step (h0 where the length is 0).
+ * Steps are taken TAC_DELTA_CHUNK at a time: what the chunk's steps write solves a triangular system, everything else is products on the
+ * matrix cores.  float32 numbers enter these as three bfloat16 parts whose sum they are, sums are float32: states, and results of float32
+ * tensors, are as exact as float32 products.  bfloat16 results, which are rounded to 2^-8 of their value, come from two parts (2^-16).
+ * An input of a sequence's head that is not finite makes that head's results of the chunk it stands in and of those behind it (backwards:
+ * before it) unspecified, NaN for the most part; other heads, sequences and chunks are not touched. */
+#define TAC_DELTA_CHUNK 64
+#define TAC_DELTA_MAX_KEY 128
+#define TAC_DELTA_MAX_VALUE 4096
+typedef struct tac_delta_strides { int64_t t, b, head; } tac_delta_strides_t;   /* elements from step to step, sequence to sequence, head to head */
+typedef struct tac_delta_desc {
+  int64_t T;                                       /* steps of the tensors */
+  int32_t B;                                       /* sequences */
+  int32_t k_heads, v_heads;                        /* v_heads a multiple of k_heads */
+  int32_t Dk, Dv;                                  /* features of a key, of a value; up to TAC_DELTA_MAX_KEY, TAC_DELTA_MAX_VALUE */
+  int32_t dtype;                                   /* TAC_FP32 / TAC_BF16 */
+  tac_delta_strides_t query, key, value;           /* each at least the features of a head, where there is more than one */
+  tac_delta_strides_t gate, write;                 /* of single numbers; `head` must be 1 */
+  tac_delta_strides_t out;                         /* out, or grad_out */
+  tac_delta_strides_t grad_query, grad_key, grad_value, grad_gate, grad_write;      /* backward only */
+} tac_delta_desc_t;
+/*   query, key   DEVICE, read-only, [T][B][k_heads][Dk]
+ *   value        DEVICE, read-only, [T][B][v_heads][Dv]
+ *   gate, write  DEVICE, read-only, [T][B][v_heads]
+ *   lengths      DEVICE, read-only, int32 [B], taken as 0 .. T where outside; NULL: all T
+ *   h0           DEVICE, read-only, float32 [B][v_heads][Dk][Dv], or NULL: zeros
+ *   out          DEVICE, written, [T][B][v_heads][Dv]; no output may lie on an input, but for h_last on h0
+ *   h_last       DEVICE, written, float32 [B][v_heads][Dk][Dv], or NULL; may be h0
+ *   states       DEVICE, written, float32 [ceil(T / TAC_DELTA_CHUNK)][B][v_heads][Dk][Dv]: the state before every chunk of steps, and
+ *   updates      DEVICE, written, float32 [T][B][v_heads][Dv]: u, which are all that the backward pass keeps; both or both NULL.  Of chunks that lie
+ *                behind a sequence's length nothing is written
+ *   workspace    DEVICE, scratch, tac_delta_scan_workspace_bytes(desc) bytes, 16-byte aligned
+ * The same bits from call to call.
+ * Errors: TAC_ERR_NULL, TAC_ERR_BAD_SHAPE, TAC_ERR_UNSUPPORTED (more features than the limits), TAC_ERR_BAD_PARAM, TAC_ERR_ALIGN, TAC_ERR_HIP. */
+size_t tac_delta_scan_workspace_bytes(const tac_delta_desc_t* desc);
+int tac_delta_scan(const tac_delta_desc_t* desc, const void* query, const void* key, const void* value, const void* gate, const void* write,
+                   const int32_t* lengths, const float* h0, void* out, float* h_last, float* states, float* updates, void* workspace, void* stream);
+
+/* Its backward pass.  From behind the last step, where dS = grad_h_last:
+ *   dS += query_t grad_out_t^T,  grad_query_t = S_t grad_out_t,  r_t = dS^T key_t,
+ *   grad_value_t = b_t r_t,  grad_write_t = (1 - b_t) r_t . u_t,  grad_key_t = dS u_t - b_t a_t S_{t-1} r_t,
+ *   dS -= b_t key_t r_t^T,  grad_gate_t = a_t (1 - a_t) <dS, S_{t-1}>,  dS <- a_t dS
+ * in chunks as the forward pass; gradients of shared queries and keys are summed over the heads that share them, in their order.  Gradients
+ * are zero from a sequence's length on.
+ *   states, updates  DEVICE, read-only, as tac_delta_scan wrote them
+ *   grad_out         DEVICE, read-only, strides `out`
+ *   grad_h_last      DEVICE, read-only, float32 [B][v_heads][Dk][Dv], or NULL: zeros
+ *   grad_query, grad_key, grad_value, grad_gate, grad_write   DEVICE, written
+ *   grad_h0          DEVICE, written, float32 [B][v_heads][Dk][Dv], or NULL; may be grad_h_last
+ *   workspace        DEVICE, scratch, tac_delta_scan_backward_workspace_bytes(desc) bytes, 16-byte aligned */
+size_t tac_delta_scan_backward_workspace_bytes(const tac_delta_desc_t* desc);
+int tac_delta_scan_backward(const tac_delta_desc_t* desc, const void* query, const void* key, const void* value, const void* gate, const void* write,
+                            const int32_t* lengths, const float* states, const float* updates, const void* grad_out, const float* grad_h_last,
+                            void* grad_query, void* grad_key, void* grad_value, void* grad_gate, void* grad_write, float* grad_h0,
+                            void* workspace, void* stream);
+
+/* One step of B running sequences whose states stand in a pool.
+ *   desc   B, k_heads, v_heads, Dk, Dv, dtype and the b and head strides of query, key, value, gate, write and out count; T must be 1
+ *   pool   DEVICE, updated, float32 [n_slots][v_heads][Dk][Dv]
+ *   slots  DEVICE, read-only, int32 [B], each slot at most once; a slot outside 0 .. n_slots - 1 stands for no sequence: its rows of out are
+ *          zero and no state changes.  NULL: sequence b has slot b (n_slots >= B)
+ *   out    DEVICE, written, [B][v_heads][Dv] */
+int tac_delta_step(const tac_delta_desc_t* desc, const void* query, const void* key, const void* value, const void* gate, const void* write,
+                   float* pool, int64_t n_slots, const int32_t* slots, void* out, void* stream);
+
 /* Dense 0/1 bytes <-> packed words, `rows` rows of W pixels each (rows = T*B*C*H).
  *   dense01  DEVICE uint8 [rows][W]; any non-zero byte packs as 1
  *   packed   DEVICE uint32 [rows][ceil(W/32)]

@@ -29,7 +29,9 @@ EXPORTS = ("tac_out_shape", "tac_packed_bytes", "tac_select_kernel", "tac_prepar
            "tac_stack_check", "tac_stack_forward", "tac_conv_lif_backward", "tac_conv_lif_backward_static", "tac_stack_backward", "tac_get_counters", "tac_reset_counters", "tac_status_string",
            "tac_last_error", "tac_code_bytes", "tac_scale_bytes", "tac_quantize", "tac_dequantize", "tac_residual_norm",
            "tac_residual_norm_workspace_bytes", "tac_residual_norm_backward", "tac_scaled_product", "tac_scaled_product_workspace_bytes",
-           "tac_gated_scan", "tac_gated_scan_workspace_bytes", "tac_gated_scan_backward", "tac_gated_step")
+           "tac_gated_scan", "tac_gated_scan_workspace_bytes", "tac_gated_scan_backward", "tac_gated_step",
+           "tac_head_norm", "tac_head_norm_workspace_bytes", "tac_head_norm_backward", "tac_delta_scan", "tac_delta_scan_workspace_bytes",
+           "tac_delta_scan_backward", "tac_delta_scan_backward_workspace_bytes", "tac_delta_step")
 
 
 class tac_layer_desc_t(ctypes.Structure):
@@ -111,7 +113,12 @@ def lib() -> ctypes.CDLL:
                 ("tac_scaled_product", [vp] * 9, ctypes.c_int), ("tac_scaled_product_workspace_bytes", [vp], ctypes.c_size_t),
                 ("tac_gated_scan", [vp] * 10, ctypes.c_int), ("tac_gated_scan_workspace_bytes", [vp], ctypes.c_size_t),
                 ("tac_gated_scan_backward", [vp] * 12, ctypes.c_int),
-                ("tac_gated_step", [vp, vp, vp, vp, i64, vp, vp, vp], ctypes.c_int)):
+                ("tac_gated_step", [vp, vp, vp, vp, i64, vp, vp, vp], ctypes.c_int),
+                ("tac_head_norm", [vp] * 9, ctypes.c_int), ("tac_head_norm_workspace_bytes", [vp], ctypes.c_size_t),
+                ("tac_head_norm_backward", [vp] * 14, ctypes.c_int),
+                ("tac_delta_scan", [vp] * 14, ctypes.c_int), ("tac_delta_scan_workspace_bytes", [vp], ctypes.c_size_t),
+                ("tac_delta_scan_backward", [vp] * 19, ctypes.c_int), ("tac_delta_scan_backward_workspace_bytes", [vp], ctypes.c_size_t),
+                ("tac_delta_step", [vp, vp, vp, vp, vp, vp, vp, i64, vp, vp, vp], ctypes.c_int)):
             getattr(L, name).argtypes = args
             getattr(L, name).restype = result
         _lib = L
@@ -516,6 +523,8 @@ def tac_reset_counters() -> None:
 TAC_SCALED = 2
 TAC_BLOCK_ROW, TAC_BLOCK_TILE = 0, 1
 TAC_SCALE_BLOCK, TAC_SCAN_CHUNK, TAC_NORM_MAX_COLS = 128, 16, 32768
+TAC_ROTATION_AXES, TAC_HEAD_MAX_FEATURES = 4, 512
+TAC_DELTA_CHUNK, TAC_DELTA_MAX_KEY, TAC_DELTA_MAX_VALUE = 64, 128, 4096
 
 
 class tac_quantize_desc_t(ctypes.Structure):
@@ -539,6 +548,26 @@ class tac_scan_desc_t(ctypes.Structure):
                 ("in_stride_t", ctypes.c_int64), ("in_stride_b", ctypes.c_int64),
                 ("out_stride_t", ctypes.c_int64), ("out_stride_b", ctypes.c_int64),
                 ("grad_stride_t", ctypes.c_int64), ("grad_stride_b", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
+class tac_head_strides_t(ctypes.Structure):
+    _fields_ = [("row", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class tac_head_norm_desc_t(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64)] + [(n, tac_head_strides_t) for n in ("query", "key", "out_query", "out_key", "grad_query", "grad_key")] + [
+        (n, ctypes.c_int32) for n in ("query_heads", "key_heads", "D", "dtype", "axes")] + [
+        ("pairs", ctypes.c_int32 * TAC_ROTATION_AXES), ("interleaved", ctypes.c_int32), ("eps", ctypes.c_float), ("base", ctypes.c_double)]
+
+
+class tac_delta_strides_t(ctypes.Structure):
+    _fields_ = [("t", ctypes.c_int64), ("b", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class tac_delta_desc_t(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("B", "k_heads", "v_heads", "Dk", "Dv", "dtype")] + [
+        (n, tac_delta_strides_t) for n in ("query", "key", "value", "gate", "write", "out", "grad_query", "grad_key", "grad_value", "grad_gate",
+                                           "grad_write")]
 
 
 _operators = None
@@ -659,3 +688,62 @@ def tac_gated_step(gate, value, pool, slots=None, *, out=None, stream=None):
     if stream is not None:
         return _on(stream, gate, lambda: tac_gated_step(gate, value, pool, slots, out=out))
     return _result(_native().gated_step(gate, value, pool, slots, out))
+
+
+def tac_head_norm(query, key=None, gain_query=None, gain_key=None, *, eps=None, positions=None, sections=None, base=10000.0, interleaved=False,
+                  out_query=None, out_key=None, stream=None):
+    """Norm of every head (eps; None: no norm) times a gain, then the rotation of its pairs of features by position (None: no rotation), of queries and keys
+    in one pass.  query, key: float32 / bfloat16 [rows, heads, D] with a contiguous last axis, slices of one product's rows for instance; gains: float32 [D];
+    positions: int32 [rows], or [rows, axes] (time, height, width, ..); sections: the pairs of each axis, D / 2 in all at most (one axis: all of them).  Pair
+    p is the features (p, P + p) of P pairs in all, or (2 p, 2 p + 1) with `interleaved`; the i-th of an axis's n pairs turns by
+    position * base^(-i / n).  Returns dict(q, k); both may be given (also query and key themselves)."""
+    if stream is not None:
+        return _on(stream, query, lambda: tac_head_norm(query, key, gain_query, gain_key, eps=eps, positions=positions, sections=sections, base=base,
+                                                        interleaved=interleaved, out_query=out_query, out_key=out_key))
+    return _result(_native().head_norm(query, key, gain_query, gain_key, eps, positions, sections, base, interleaved, out_query, out_key))
+
+
+def tac_head_norm_backward(query, key, gain_query, gain_key, grad_out_query, grad_out_key=None, *, eps=None, positions=None, sections=None, base=10000.0,
+                           interleaved=False, grad_query=None, grad_key=None, want_grad_gain=True, stream=None):
+    """Backward pass of tac_head_norm from what it read and the gradients of its results.  Returns dict(grad_q, grad_k, grad_gain_q, grad_gain_k); the
+    first two may be given (also grad_out_query and grad_out_key)."""
+    if stream is not None:
+        return _on(stream, query, lambda: tac_head_norm_backward(
+            query, key, gain_query, gain_key, grad_out_query, grad_out_key, eps=eps, positions=positions, sections=sections, base=base,
+            interleaved=interleaved, grad_query=grad_query, grad_key=grad_key, want_grad_gain=want_grad_gain))
+    return _result(_native().head_norm_backward(query, key, gain_query, gain_key, grad_out_query, grad_out_key, eps, positions, sections, base,
+                                                interleaved, grad_query, grad_key, want_grad_gain))
+
+
+def tac_delta_scan(query, key, value, gate, write, *, lengths=None, h0=None, out=None, want_h_last=True, want_kept=False, stream=None):
+    """Gated delta rule: for every sequence and head, with a = sigmoid(gate) and b = sigmoid(write),
+    S <- a S, u = b (value - S^T key), S <- S + key u^T, out = S^T query.  query, key: float32 / bfloat16 [T, B, k_heads, Dk], Dk up to
+    TAC_DELTA_MAX_KEY, keys no longer than 1 (tac_head_norm with gains of Dk^-1/2); value: [T, B, v_heads, Dv]; gate, write: [T, B, v_heads]; last axes
+    contiguous, the others of any strides; v_heads / k_heads consecutive heads of values share a head of queries and keys.  lengths: int32 [B]; h0: float32
+    [B, v_heads, Dk, Dv].  Returns dict(out, h_last, states, updates); the last two (want_kept) are what the backward pass needs.  `out` may be given, but
+    not an input."""
+    if stream is not None:
+        return _on(stream, query, lambda: tac_delta_scan(query, key, value, gate, write, lengths=lengths, h0=h0, out=out, want_h_last=want_h_last,
+                                                         want_kept=want_kept))
+    return _result(_native().delta_scan(query, key, value, gate, write, lengths, h0, out, want_h_last, want_kept))
+
+
+def tac_delta_scan_backward(query, key, value, gate, write, states, updates, grad_out, *, lengths=None, grad_h_last=None, grad_query=None, grad_key=None,
+                            grad_value=None, grad_gate=None, grad_write=None, want_grad_h0=True, stream=None):
+    """Backward pass of tac_delta_scan from its inputs and what it kept.  Returns dict(grad_query, grad_key, grad_value, grad_gate, grad_write, grad_h0); all
+    but the last may be given (slices of one product's gradient, for instance, but not inputs)."""
+    if stream is not None:
+        return _on(stream, query, lambda: tac_delta_scan_backward(
+            query, key, value, gate, write, states, updates, grad_out, lengths=lengths, grad_h_last=grad_h_last, grad_query=grad_query, grad_key=grad_key,
+            grad_value=grad_value, grad_gate=grad_gate, grad_write=grad_write, want_grad_h0=want_grad_h0))
+    return _result(_native().delta_scan_backward(query, key, value, gate, write, states, updates, grad_out, lengths, grad_h_last, grad_query, grad_key,
+                                                 grad_value, grad_gate, grad_write, want_grad_h0))
+
+
+def tac_delta_step(query, key, value, gate, write, pool, slots=None, *, out=None, stream=None):
+    """One step of tac_delta_scan for B running sequences whose states stand in `pool` (float32 [slots, v_heads, Dk, Dv], updated in place).  query, key:
+    [B, k_heads, Dk]; value: [B, v_heads, Dv]; gate, write: [B, v_heads]; slots: int32 [B], each slot at most once, outside the pool for rows without a
+    sequence; None: row b has slot b.  Returns out [B, v_heads, Dv]."""
+    if stream is not None:
+        return _on(stream, query, lambda: tac_delta_step(query, key, value, gate, write, pool, slots, out=out))
+    return _result(_native().delta_step(query, key, value, gate, write, pool, slots, out))

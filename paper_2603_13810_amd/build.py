@@ -18,7 +18,8 @@ SOURCES = ["tac_mfma_w64s1.hip", "tac_mfma_w64s1_trace.hip", "tac_mfma_w32s1.hip
            "tac_mfma_mid_f32.hip", "tac_mfma_mid_f32_trace.hip", "tac_mfma_row.hip", "tac_mfma_deep.hip", "tac_mfma_deep_trace.hip", "tac_mfma_mid.hip", "tac_mfma.hip", "tac_api.hip",
            "tac_pack.hip", "tac_direct.hip", "tac_backward.hip", "tac_backward_dgrad_tile.hip",
            "tac_backward_wgrad_f32.hip", "tac_backward_wgrad_first.hip", "tac_backward_dgrad_f32.hip",
-           "tac_norm.hip", "tac_quantize.hip", "tac_product.hip", "tac_scan.hip", "tac_head_api.hip"]
+           "tac_norm.hip", "tac_quantize.hip", "tac_product.hip", "tac_scan.hip", "tac_head_api.hip",
+           "tac_heads.hip", "tac_delta_prepare.hip", "tac_delta.hip", "tac_delta_backward.hip", "tac_delta_step.hip", "tac_delta_api.hip"]
 MAX_JOBS = min(16, os.cpu_count() or 4)
 
 

@@ -1,0 +1,44 @@
+// Host rules of the head norm and of the gated delta rule: how work is cut, and what a workspace holds.
+#pragma once
+#include "tac_product_plan.h"
+
+namespace tac {
+
+// ---- head norm -----------------------------------------------------------------------------------
+
+// lanes that share a head: each holds four pairs of features
+inline int head_lanes(int D) { return D <= 64 ? 8 : D <= 128 ? 16 : D <= 256 ? 32 : 64; }
+
+// Slices of a row's heads: the lanes of a slice take every `slices`-th head and turn them all by the angles that they have formed once.  As few slices as
+// give every compute unit four workgroups of 256 lanes.
+inline int head_slices(int64_t rows, int heads, int lanes) {
+  const int64_t wanted = (int64_t)kFittedUnits * 4 * (256 / lanes);
+  const int64_t slices = (wanted + rows - 1) / rows;
+  return (int)(slices < 1 ? 1 : slices > heads ? heads : slices);
+}
+
+// workgroups of a launch; what they do not reach in one turn they take in further ones
+constexpr int64_t kHeadGroups = 8 * kFittedUnits;
+inline int64_t head_groups(int64_t rows, int slices, int lanes, int64_t most) {
+  const int64_t units = rows * slices, each = 256 / lanes;
+  const int64_t groups = (units + each - 1) / each;
+  return groups < most ? groups : most;
+}
+// the backward pass keeps the gains' gradients of a workgroup, 2 D numbers, in a row of the workspace
+constexpr int64_t kHeadBackwardGroups = 4 * kFittedUnits;
+
+// ---- gated delta rule ------------------------------------------------------------------------------
+
+inline int64_t delta_chunks(int64_t T) { return (T + TAC_DELTA_CHUNK - 1) / TAC_DELTA_CHUNK; }
+
+// Columns of a state that a workgroup takes: 32, or 16 where those would leave compute units without work.
+inline bool delta_narrow(int64_t B, int64_t heads, int64_t Dv) { return Dv <= 16 || B * heads * ((Dv + 31) / 32) < 2 * kFittedUnits; }
+
+// A launch has a workgroup of 256 threads for every chunk and head, or for every 16 columns of a head: fewer than 2^32 threads.
+inline bool delta_fits(int64_t T, int64_t B, int64_t heads, int64_t Dv) {
+  const int64_t most = (1ll << 24) - 1;
+  if (B * heads > most) return false;
+  return delta_chunks(T) <= most / (B * heads) && (Dv + 15) / 16 <= most / (B * heads);
+}
+
+}  // namespace tac

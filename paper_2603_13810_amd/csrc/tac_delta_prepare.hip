@@ -1,0 +1,178 @@
+// What the steps of a chunk do to each other, for every chunk and head at once: with G the running sum of log a,
+//   A_tj = b_t e^(G_t - G_j) k_t . k_j  (j < t),   (I + A)^-1,   P_tj = e^(G_t - G_j) q_t . k_j  (j <= t).
+//
+// G is kept in two numbers: a chunk that fades by e^-100 in all may hold neighbours that hardly fade, and one float32 number would have lost their difference.
+// The inverse is formed by blocks of 16: the diagonal ones by substitution, one column a lane, those below from them on the float32 matrix cores.  A product
+// of powers of A would be shorter, but its terms grow with the number of like keys where the inverse does not.
+#include "tac_delta_chunk.h"
+
+namespace tac {
+
+namespace {
+
+constexpr int kPitch = kChunk + 4;       // float32 rows in LDS
+
+// running sum over the wave's lanes of numbers in two parts
+__device__ __forceinline__ void scan_pairs(float& high, float& low, int lane) {
+#pragma unroll
+  for (int by = 1; by < 64; by *= 2) {
+    const float h = __shfl_up(high, by), l = __shfl_up(low, by);
+    if (lane >= by) {
+      const float s = high + h, back = s - high, e = (high - (s - back)) + (h - back);
+      const float rest = low + l + e;
+      high = s + rest;
+      low = rest - (high - s);
+    }
+  }
+}
+
+template <typename T, int DK, bool BACK>
+__global__ __launch_bounds__(256) void prepare_kernel(const DeltaParams p) {
+  constexpr int IN = Kind<T>::in, OUT = BACK ? 3 : Kind<T>::out, KS = DK / 32;
+  __shared__ float A[kChunk][kPitch], P[kChunk][kPitch], inverse[kChunk][kPitch];
+  __shared__ float diagonal[4][16][20];
+  __shared__ float high[kChunk], low[kChunk], beta[kChunk];
+  const int h = blockIdx.x % p.v_heads, b = blockIdx.x / p.v_heads % p.B;
+  const int64_t chunk = blockIdx.x / p.v_heads / p.B, from = chunk * kChunk;
+  const int n = steps_of(p, b, from);
+  if (n == 0) return;
+  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, low16 = lane & 15, quad = lane >> 4;
+  const int hk = h / (p.v_heads / p.k_heads);
+  const T* q = (const T*)p.q + from * p.q_at.t + (int64_t)b * p.q_at.b + (int64_t)hk * p.q_at.head;
+  const T* k = (const T*)p.k + from * p.k_at.t + (int64_t)b * p.k_at.b + (int64_t)hk * p.k_at.head;
+
+  if (wave == 0) {
+    float hi = 0.0f, lo = 0.0f, w = 0.0f;
+    if (lane < n) {
+      const float x = (float)((const T*)p.gate)[(from + lane) * p.gate_at.t + (int64_t)b * p.gate_at.b + h];
+      hi = fminf(x, 0.0f) - log1pf(expf(-fabsf(x)));
+      if (x < -128.0f) hi = -128.0f;                  // e^-128 is 0 in float32; keeps -inf out of the differences
+      if (x != x) hi = x;
+      w = sigmoid((float)((const T*)p.write)[(from + lane) * p.write_at.t + (int64_t)b * p.write_at.b + h]);
+    }
+    scan_pairs(hi, lo, lane);
+    high[lane] = hi;
+    low[lane] = lo;
+    beta[lane] = w;
+  }
+  Parts<IN> own_k[KS], own_q[KS];
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    const int row = 16 * wave + low16, col = 32 * s + 8 * quad, left = row < n ? p.Dk - col : 0;
+    Eight<T> e;
+    e.load(k + (int64_t)row * p.k_at.t + col, left);
+    own_k[s] = e.parts();
+    e.load(q + (int64_t)row * p.q_at.t + col, left);
+    own_q[s] = e.parts();
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    f32x4_t kk = {0.0f, 0.0f, 0.0f, 0.0f}, qk = kk;
+    if (j <= wave) {
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        const int row = 16 * j + low16, col = 32 * s + 8 * quad;
+        Eight<T> e;
+        e.load(k + (int64_t)row * p.k_at.t + col, row < n ? p.Dk - col : 0);
+        const Parts<IN> other = e.parts();
+        multiply<IN>(kk, own_k[s], other);
+        multiply<IN>(qk, own_q[s], other);
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int t = 16 * wave + 4 * quad + r, c = 16 * j + low16;
+      const float decay = fast_exp((high[t] - high[c]) + (low[t] - low[c]));
+      A[t][c] = c < t ? beta[t] * decay * kk[r] : 0.0f;
+      P[t][c] = c <= t ? decay * qk[r] : 0.0f;
+    }
+  }
+  __syncthreads();
+  // a diagonal block's inverse: column low16 of x, row by row
+  float x[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    x[i] = i == low16 ? 1.0f : 0.0f;
+#pragma unroll
+    for (int j = 0; j < i; ++j) x[i] = fmaf(-A[16 * wave + i][16 * wave + j], x[j], x[i]);
+  }
+  f32x4_t block[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) block[i] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+  f32x4_t mine;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) mine[r] = quad == 0 ? x[r] : quad == 1 ? x[4 + r] : quad == 2 ? x[8 + r] : x[12 + r];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) diagonal[wave][4 * quad + r][low16] = mine[r];
+  __syncthreads();
+  // block column `wave`, downwards: T_ij = -T_ii sum_k A_ik T_kj.  A result's registers are the next product's second operand as they are (rows 4 quad + r in step r).
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (i == wave) block[i] = mine;
+    if (i <= wave) continue;
+    f32x4_t sum = {0.0f, 0.0f, 0.0f, 0.0f}, result = sum;
+#pragma unroll
+    for (int m = 0; m < 3; ++m) {
+      if (m < wave || m >= i) continue;
+      const f32x4_t a = *reinterpret_cast<const f32x4_t*>(&A[16 * i + low16][16 * m + 4 * quad]);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sum = __builtin_amdgcn_mfma_f32_16x16x4f32(a[r], block[m][r], sum, 0, 0, 0);
+    }
+    const f32x4_t d = *reinterpret_cast<const f32x4_t*>(&diagonal[i][low16][4 * quad]);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) result = __builtin_amdgcn_mfma_f32_16x16x4f32(-d[r], sum[r], result, 0, 0, 0);
+    block[i] = result;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) inverse[16 * i + 4 * quad + r][16 * wave + low16] = block[i][r];
+  __syncthreads();
+  const ChunkRoom room(p.chunk_room, blockIdx.x, OUT);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int piece = threadIdx.x + 256 * i;
+    const int row = BACK ? piece % 64 : piece / 8, col = BACK ? 8 * (piece / 64) : 8 * (piece % 8);
+    float v[8], w[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      v[e] = BACK ? inverse[col + e][row] : inverse[row][col + e];
+      w[e] = BACK ? P[col + e][row] : P[row][col + e];
+    }
+    const Parts<3> a = split<3>(v);
+    const Parts<OUT> c = split<OUT>(w);
+#pragma unroll
+    for (int part = 0; part < 3; ++part) *reinterpret_cast<bf16x8_t*>(const_cast<bf16*>(room.inverse) + part * ChunkRoom::plane + row * kChunk + col) = a.p[part];
+#pragma unroll
+    for (int part = 0; part < OUT; ++part) *reinterpret_cast<bf16x8_t*>(const_cast<bf16*>(room.products) + part * ChunkRoom::plane + row * kChunk + col) = c.p[part];
+  }
+  if (threadIdx.x < kChunk) {
+    const int t = threadIdx.x;
+    const_cast<float*>(room.start)[t] = fast_exp(high[t] + low[t]);
+    const_cast<float*>(room.rest)[t] = fast_exp((high[kChunk - 1] - high[t]) + (low[kChunk - 1] - low[t]));
+    const_cast<float*>(room.beta)[t] = beta[t];
+    const_cast<float*>(room.high)[t] = high[t];
+    const_cast<float*>(room.low)[t] = low[t];
+  }
+}
+
+template <typename T, bool BACK>
+hipError_t prepare_typed(const DeltaParams& p, hipStream_t s) {
+  const dim3 grid((unsigned)((int64_t)p.chunks * p.B * p.v_heads));
+  switch (padded_key(p.Dk)) {
+    case 32: hipLaunchKernelGGL((prepare_kernel<T, 32, BACK>), grid, dim3(256), 0, s, p); break;
+    case 64: hipLaunchKernelGGL((prepare_kernel<T, 64, BACK>), grid, dim3(256), 0, s, p); break;
+    default: hipLaunchKernelGGL((prepare_kernel<T, 128, BACK>), grid, dim3(256), 0, s, p);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t delta_prepare_launch(const DeltaParams& p, bool back, hipStream_t s) {
+  if (p.bf16) return back ? prepare_typed<bf16, true>(p, s) : prepare_typed<bf16, false>(p, s);
+  return back ? prepare_typed<float, true>(p, s) : prepare_typed<float, false>(p, s);
+}
+
+}  // namespace tac

@@ -1,0 +1,338 @@
+// Norm of every head of queries and keys and the rotation by position, and the backward pass.
+//
+// Memory-bound: every head is read once into registers and written from them.  A lane holds four pairs of features, both features of each, so that a pair is turned
+// without another lane; 8 to 64 lanes share a head, whose sum of squares is three to six exchanges.
+// An angle is position * base^(-i / n) in turns: formed in 64 bits and brought to the nearest turn there, sine and cosine are float32 from then on.  That costs
+// some fifty instructions a pair, so a lane turns several heads of a row by the angles it has.
+#include "tac_delta_common.h"
+
+namespace tac {
+
+namespace {
+
+constexpr int kPairs = 4;            // of a lane
+constexpr int kAtOnce = 4;           // heads whose loads are on their way together
+
+// The two features of pair p: rotated pairs first, then what is left, paired half a remainder apart.
+__device__ __forceinline__ int feature_of(const HeadNormParams& p, int pair, int second) {
+  if (p.interleaved) return 2 * pair + second;
+  const int rest = p.D / 2 - p.rotated;
+  return pair < p.rotated ? pair + second * p.rotated : 2 * p.rotated + (pair - p.rotated) + second * rest;
+}
+
+// How a lane's eight features are read: EACH by itself; QUADS: the first and the second features of its pairs are four neighbours each, aligned; ROW: all eight are neighbours.
+enum { EACH = 0, QUADS = 1, ROW = 2 };
+
+template <int MODE>
+struct Lane {
+  int at[2 * kPairs];                // features: the pairs' first ones, then their second ones (ROW: in their order)
+  int count;                         // pairs that there are
+  double turns[kPairs];              // per unit of position
+  int axis[kPairs];                  // -1: not rotated
+
+  __device__ Lane(const HeadNormParams& p, int lane) {
+    count = min(max(p.D / 2 - kPairs * lane, 0), kPairs);
+#pragma unroll
+    for (int j = 0; j < kPairs; ++j) {
+      const int pair = kPairs * lane + j;
+#pragma unroll
+      for (int second = 0; second < 2; ++second) at[MODE == ROW ? 2 * j + second : j + kPairs * second] = j < count ? feature_of(p, pair, second) : 0;
+      axis[j] = -1;
+      turns[j] = 0.0;
+      int begin = 0;
+      for (int a = 0; a < p.axes; ++a) {
+        if (pair >= begin && pair < begin + p.pairs[a]) {
+          axis[j] = a;
+          turns[j] = exp2(-(double)(pair - begin) / (double)p.pairs[a] * p.log2_base) * 0.15915494309189533577;      // 1 / (2 pi)
+        }
+        begin += p.pairs[a];
+      }
+    }
+  }
+  __device__ __forceinline__ int first(int j) const { return MODE == ROW ? 2 * j : j; }
+  __device__ __forceinline__ int second(int j) const { return MODE == ROW ? 2 * j + 1 : j + kPairs; }
+
+  __device__ __forceinline__ void angles(const HeadNormParams& p, int64_t row, float (&c)[kPairs], float (&s)[kPairs]) const {
+#pragma unroll
+    for (int j = 0; j < kPairs; ++j) {
+      c[j] = 1.0f;
+      s[j] = 0.0f;
+      if (axis[j] >= 0) {
+        const double t = (double)p.positions[row * p.axes + axis[j]] * turns[j];
+        sincospif(2.0f * (float)(t - rint(t)), &s[j], &c[j]);
+      }
+    }
+  }
+  template <typename T>
+  __device__ __forceinline__ void load(const T* x, float (&v)[2 * kPairs]) const {
+    if constexpr (MODE == ROW) {
+      if (count) load_floats<T, 8, true>(x + at[0], 8, v);
+    } else if constexpr (MODE == QUADS) {
+      if (count) {
+        float a[4], b[4];
+        load_floats<T, 4, true>(x + at[0], 4, a);
+        load_floats<T, 4, true>(x + at[4], 4, b);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = a[e], v[e + 4] = b[e];
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e % kPairs < count) v[e] = (float)x[at[e]];
+    }
+  }
+  template <typename T>
+  __device__ __forceinline__ void store(T* y, const float (&v)[2 * kPairs]) const {
+    if constexpr (MODE == ROW) {
+      if (count) store_floats<T, 8, true>(y + at[0], 8, v);
+    } else if constexpr (MODE == QUADS) {
+      if (count) {
+        const float a[4] = {v[0], v[1], v[2], v[3]}, b[4] = {v[4], v[5], v[6], v[7]};
+        store_floats<T, 4, true>(y + at[0], 4, a);
+        store_floats<T, 4, true>(y + at[4], 4, b);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e % kPairs < count) y[at[e]] = (T)v[e];
+    }
+  }
+  __device__ __forceinline__ void gains(const float* gain, float (&v)[2 * kPairs]) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = gain && count > (MODE == ROW ? e / 2 : e % kPairs) ? gain[at[e]] : 1.0f;
+  }
+};
+
+// whatever the order that they are read in, features are summed in this one: results do not depend on addresses
+template <int MODE>
+__device__ __forceinline__ constexpr int in_order(int e) { return MODE == ROW ? 2 * (e % kPairs) + e / kPairs : e; }
+
+__device__ __forceinline__ void zero(float (&v)[2 * kPairs]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+}
+
+template <typename T, int LANES, int MODE>
+__global__ __launch_bounds__(256) void head_norm_kernel(const HeadNormParams p) {
+  const Lane<MODE> lane(p, threadIdx.x % LANES);
+  float gain[2][8];
+  lane.gains(p.q.gain, gain[0]);
+  lane.gains(p.k.gain, gain[1]);
+  const int heads = p.q.heads + p.k.heads;
+  const uint32_t units = (uint32_t)p.rows * (uint32_t)p.slices, step = gridDim.x * (256 / LANES);
+  for (uint32_t unit = blockIdx.x * (256 / LANES) + threadIdx.x / LANES; unit < units; unit += step) {
+    const uint32_t row = unit / (uint32_t)p.slices;
+    const int slice = (int)(unit - row * (uint32_t)p.slices);
+    float c[kPairs], s[kPairs];
+    for (int begin = slice; begin < heads; begin += kAtOnce * p.slices) {
+      float v[kAtOnce][8];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int h = begin + i * p.slices;
+        zero(v[i]);
+        if (h < p.q.heads) lane.load((const T*)p.q.x + (int64_t)row * p.q.x_stride.row + (int64_t)h * p.q.x_stride.head, v[i]);
+        else if (h < heads) lane.load((const T*)p.k.x + (int64_t)row * p.k.x_stride.row + (int64_t)(h - p.q.heads) * p.k.x_stride.head, v[i]);
+      }
+      if (begin == slice) lane.angles(p, row, c, s);
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int h = begin + i * p.slices;
+        if (h >= heads) break;
+        float squares = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) squares = fmaf(v[i][in_order<MODE>(e)], v[i][in_order<MODE>(e)], squares);
+        const float rstd = p.eps > 0.0f ? 1.0f / sqrtf(sum_over_lanes<LANES>(squares) / (float)p.D + p.eps) : 1.0f;
+        const bool key = h >= p.q.heads;
+        float y[8];
+#pragma unroll
+        for (int j = 0; j < kPairs; ++j) {
+          const int f = lane.first(j), g = lane.second(j);
+          const float a = v[i][f] * rstd * (key ? gain[1][f] : gain[0][f]), b = v[i][g] * rstd * (key ? gain[1][g] : gain[0][g]);
+          y[f] = lane.axis[j] >= 0 ? fmaf(a, c[j], -(b * s[j])) : a;       // a NaN beside a feature that is not turned stays where it is
+          y[g] = lane.axis[j] >= 0 ? fmaf(b, c[j], a * s[j]) : b;
+        }
+        if (key) lane.store((T*)p.k.out + (int64_t)row * p.k.out_stride.row + (int64_t)(h - p.q.heads) * p.k.out_stride.head, y);
+        else lane.store((T*)p.q.out + (int64_t)row * p.q.out_stride.row + (int64_t)h * p.q.out_stride.head, y);
+      }
+    }
+  }
+}
+
+// The gains' gradients stay in a lane's registers over all heads that it takes, are added up over the workgroup in LDS and leave as a row of the
+// workspace [workgroup][queries, keys][8 LANES]; head_gain_kernel adds those up in their order.
+template <typename T, int LANES, int MODE>
+__global__ __launch_bounds__(256) void head_norm_backward_kernel(const HeadNormParams p) {
+  __shared__ float room[256 * 8];
+  const Lane<MODE> lane(p, threadIdx.x % LANES);
+  float gain[2][8], sums[2][8];
+  lane.gains(p.q.gain, gain[0]);
+  lane.gains(p.k.gain, gain[1]);
+  zero(sums[0]);
+  zero(sums[1]);
+  const int heads = p.q.heads + p.k.heads;
+  const uint32_t units = (uint32_t)p.rows * (uint32_t)p.slices, step = gridDim.x * (256 / LANES);
+  for (uint32_t unit = blockIdx.x * (256 / LANES) + threadIdx.x / LANES; unit < units; unit += step) {
+    const uint32_t row = unit / (uint32_t)p.slices;
+    const int slice = (int)(unit - row * (uint32_t)p.slices);
+    float c[kPairs], s[kPairs];
+    for (int begin = slice; begin < heads; begin += kAtOnce / 2 * p.slices) {
+      float v[kAtOnce / 2][8], d[kAtOnce / 2][8];
+#pragma unroll
+      for (int i = 0; i < kAtOnce / 2; ++i) {
+        const int h = begin + i * p.slices;
+        zero(v[i]);
+        zero(d[i]);
+        if (h >= heads) continue;
+        const HeadTensor& t = h < p.q.heads ? p.q : p.k;
+        const int at = h < p.q.heads ? h : h - p.q.heads;
+        lane.load((const T*)t.x + (int64_t)row * t.x_stride.row + (int64_t)at * t.x_stride.head, v[i]);
+        lane.load((const T*)t.grad_out + (int64_t)row * t.grad_out_stride.row + (int64_t)at * t.grad_out_stride.head, d[i]);
+      }
+      if (begin == slice) lane.angles(p, row, c, s);
+#pragma unroll
+      for (int i = 0; i < kAtOnce / 2; ++i) {
+        const int h = begin + i * p.slices;
+        if (h >= heads) break;
+        const bool key = h >= p.q.heads;
+        float rstd = 1.0f;
+        if (p.eps > 0.0f) {
+          float squares = 0.0f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) squares = fmaf(v[i][in_order<MODE>(e)], v[i][in_order<MODE>(e)], squares);
+          rstd = 1.0f / sqrtf(sum_over_lanes<LANES>(squares) / (float)p.D + p.eps);
+        }
+        float w[8], dot = 0.0f;
+#pragma unroll
+        for (int j = 0; j < kPairs; ++j) {
+          const int f = lane.first(j), g = lane.second(j);
+          w[f] = lane.axis[j] >= 0 ? fmaf(d[i][f], c[j], d[i][g] * s[j]) : d[i][f];
+          w[g] = lane.axis[j] >= 0 ? fmaf(d[i][g], c[j], -(d[i][f] * s[j])) : d[i][g];
+        }
+#pragma unroll
+        for (int m = 0; m < 8; ++m) {
+          const int e = in_order<MODE>(m);
+          v[i][e] *= rstd;
+          const float one = w[e] * v[i][e];
+          if (key) sums[1][e] += one;
+          else sums[0][e] += one;
+          w[e] *= key ? gain[1][e] : gain[0][e];
+          dot = fmaf(w[e], v[i][e], dot);
+        }
+        if (p.eps > 0.0f) {
+          const float mean = sum_over_lanes<LANES>(dot) / (float)p.D;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) w[e] = rstd * (w[e] - v[i][e] * mean);
+        }
+        if (key) lane.store((T*)p.k.out + (int64_t)row * p.k.out_stride.row + (int64_t)(h - p.q.heads) * p.k.out_stride.head, w);
+        else lane.store((T*)p.q.out + (int64_t)row * p.q.out_stride.row + (int64_t)h * p.q.out_stride.head, w);
+      }
+    }
+  }
+  if (!p.partial) return;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    __syncthreads();                        // the tensor before has been read
+#pragma unroll
+    for (int e = 0; e < 8; ++e) room[e * 256 + threadIdx.x] = sums[t][e];
+    __syncthreads();
+    for (int slot = threadIdx.x; slot < 8 * LANES; slot += 256) {
+      const int e = slot / LANES, l = slot % LANES;
+      float total = 0.0f;
+#pragma unroll
+      for (int g = 0; g < 256 / LANES; ++g) total += room[e * 256 + g * LANES + l];
+      p.partial[((int64_t)blockIdx.x * 2 + t) * (8 * LANES) + slot] = total;
+    }
+  }
+}
+
+// Sums of partial [groups][2][8 LANES]: 16 slots and 16 slices of the groups a workgroup, then the slices in their order.
+template <int MODE>
+__global__ __launch_bounds__(256) void head_gain_kernel(const HeadNormParams p, int groups, int lanes) {
+  __shared__ float room[16][16];
+  const int slot = blockIdx.x * 16 + threadIdx.x % 16, slice = threadIdx.x / 16, t = blockIdx.y, slots = 8 * lanes;
+  float total = 0.0f;
+#pragma unroll 8
+  for (int g = slice; g < groups; g += 16) total += p.partial[((int64_t)g * 2 + t) * slots + slot];
+  room[slice][threadIdx.x % 16] = total;
+  __syncthreads();
+  if (slice) return;
+#pragma unroll
+  for (int s = 1; s < 16; ++s) total += room[s][threadIdx.x % 16];
+  const int e = slot / lanes, pair = kPairs * (slot % lanes) + (MODE == ROW ? e / 2 : e % kPairs), second = MODE == ROW ? e % 2 : e / kPairs;
+  float* to = t ? p.grad_gain_k : p.grad_gain_q;
+  if (to && pair < p.D / 2) to[feature_of(p, pair, second)] = total;
+}
+
+bool quads_aligned(const void* at, const tac_head_strides_t& s, size_t piece, size_t el) {
+  return !at || (((uintptr_t)at | (uintptr_t)(s.row * (int64_t)el) | (uintptr_t)(s.head * (int64_t)el)) & (piece - 1)) == 0;
+}
+
+int mode_of(const HeadNormParams& p) {
+  const size_t el = p.bf16 ? 2 : 4, piece = p.interleaved ? 16 : 4 * el;
+  bool aligned = true;
+  for (const HeadTensor* t : {&p.q, &p.k}) {
+    if (!t->heads) continue;
+    aligned &= quads_aligned(t->x, t->x_stride, piece, el) && quads_aligned(t->grad_out, t->grad_out_stride, piece, el) && quads_aligned(t->out, t->out_stride, piece, el);
+  }
+  if (!aligned) return EACH;
+  if (p.interleaved) return p.D % 8 == 0 ? ROW : EACH;
+  return p.rotated % kPairs == 0 && (p.D / 2 - p.rotated) % kPairs == 0 ? QUADS : EACH;
+}
+
+// f(lanes, mode) with both as constants
+template <typename F>
+hipError_t by_shape(const HeadNormParams& p, F f) {
+  using std::integral_constant;
+  const auto with = [&](auto lanes) {
+    switch (mode_of(p)) {
+      case QUADS: return f(lanes, integral_constant<int, QUADS>());
+      case ROW: return f(lanes, integral_constant<int, ROW>());
+      default: return f(lanes, integral_constant<int, EACH>());
+    }
+  };
+  switch (head_lanes(p.D)) {
+    case 8: return with(integral_constant<int, 8>());
+    case 16: return with(integral_constant<int, 16>());
+    case 32: return with(integral_constant<int, 32>());
+    default: return with(integral_constant<int, 64>());
+  }
+}
+
+}  // namespace
+
+hipError_t head_norm_launch(const HeadNormParams& given, hipStream_t s) {
+  HeadNormParams p = given;
+  const int lanes = head_lanes(p.D);
+  p.slices = head_slices(p.rows, p.q.heads + p.k.heads, lanes);
+  const unsigned groups = (unsigned)head_groups(p.rows, p.slices, lanes, kHeadGroups);
+  return by_shape(p, [&](auto l, auto m) {
+    constexpr int L = decltype(l)::value, M = decltype(m)::value;
+    if (p.bf16) hipLaunchKernelGGL((head_norm_kernel<bf16, L, M>), dim3(groups), dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((head_norm_kernel<float, L, M>), dim3(groups), dim3(256), 0, s, p);
+    return hipGetLastError();
+  });
+}
+
+size_t head_norm_workspace(int64_t rows, int heads, int D) {
+  const int lanes = head_lanes(D);
+  return (size_t)head_groups(rows, head_slices(rows, heads, lanes), lanes, kHeadBackwardGroups) * 2 * 8 * (size_t)lanes * sizeof(float);
+}
+
+hipError_t head_norm_backward_launch(const HeadNormParams& given, hipStream_t s) {
+  HeadNormParams p = given;
+  const int lanes = head_lanes(p.D);
+  p.slices = head_slices(p.rows, p.q.heads + p.k.heads, lanes);
+  const unsigned groups = (unsigned)head_groups(p.rows, p.slices, lanes, kHeadBackwardGroups);
+  if (!p.grad_gain_q && !p.grad_gain_k) p.partial = nullptr;
+  return by_shape(p, [&](auto l, auto m) {
+    constexpr int L = decltype(l)::value, M = decltype(m)::value;
+    if (p.bf16) hipLaunchKernelGGL((head_norm_backward_kernel<bf16, L, M>), dim3(groups), dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((head_norm_backward_kernel<float, L, M>), dim3(groups), dim3(256), 0, s, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !p.partial) return e;
+    hipLaunchKernelGGL((head_gain_kernel<M>), dim3(L / 2, p.k.heads ? 2 : 1), dim3(256), 0, s, p, (int)groups, L);
+    return hipGetLastError();
+  });
+}
+
+}  // namespace tac

@@ -13,6 +13,8 @@
 
 #include <pybind11/pybind11.h>
 
+#include <vector>
+
 #include "tac.h"
 
 namespace {
@@ -444,6 +446,299 @@ PyObject* gated_step(PyObject*, PyObject* const* a, Py_ssize_t count) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---- heads and the gated delta rule ----------------------------------------------------------------
+
+double number(PyObject* o) {
+  const double v = PyFloat_AsDouble(o);
+  if (v == -1.0 && PyErr_Occurred()) throw Refused();
+  return v;
+}
+void head_axes(const Tensor& t, const char* name) {
+  if (t.dim() != 3) refuse("%s must be [rows, heads, features]", name);
+  if (t.size(1) > INT32_MAX || t.size(2) > INT32_MAX) refuse("%s has too many heads or features", name);
+}
+tac_head_strides_t head_strides(const Tensor& t) { return {t.stride(0), t.stride(1)}; }
+
+// What both directions of the head norm share: eps, positions, sections, base, interleaved from a[0] on
+struct Rotation {
+  tac_head_norm_desc_t d = {};
+  const int32_t* positions = nullptr;
+  Rotation(const Call& c, const Tensor& q, const Tensor* k, PyObject* const* a) {
+    d.rows = q.size(0);
+    d.query_heads = (int32_t)q.size(1);
+    d.D = (int32_t)q.size(2);
+    d.dtype = float_type(q, "query");
+    d.query = head_strides(q);
+    if (k) {
+      d.key_heads = (int32_t)k->size(1);
+      d.key = head_strides(*k);
+    }
+    if (a[0] != Py_None) {
+      d.eps = (float)number(a[0]);
+      if (!(d.eps > 0.0f)) refuse("eps must be more than 0 (None: no norm)");
+    }
+    const Tensor* at = maybe(a[1], "positions");
+    if (!at) {
+      if (a[2] != Py_None) refuse("sections need positions");
+      if (a[0] == Py_None) refuse("neither a norm (eps) nor positions");
+      return;
+    }
+    if (at->dim() != 1 && at->dim() != 2) refuse("positions must be [rows] or [rows, axes]");
+    const int64_t axes = at->dim() == 1 ? 1 : at->size(1);
+    if (axes < 1 || axes > TAC_ROTATION_AXES) refuse("positions must have 1 to %d axes", TAC_ROTATION_AXES);
+    if (at->dim() == 1) positions = (const int32_t*)c.whole(at, "positions", ScalarType::Int, {d.rows});
+    else positions = (const int32_t*)c.whole(at, "positions", ScalarType::Int, {d.rows, axes});
+    d.axes = (int32_t)axes;
+    if (a[2] == Py_None) {
+      if (axes > 1) refuse("several axes need sections");
+      d.pairs[0] = d.D / 2;
+    } else {
+      PyObject* items = PySequence_Fast(a[2], "sections must be a sequence of numbers of pairs");
+      if (!items) throw Refused();
+      int64_t pairs[TAC_ROTATION_AXES] = {};
+      const Py_ssize_t count = PySequence_Fast_GET_SIZE(items);
+      bool wrong = count != axes;
+      for (Py_ssize_t i = 0; i < count && !wrong; ++i) {
+        pairs[i] = PyLong_AsLongLong(PySequence_Fast_GET_ITEM(items, i));
+        wrong = pairs[i] < 1 || pairs[i] > INT32_MAX;
+        d.pairs[i] = (int32_t)pairs[i];
+      }
+      Py_DECREF(items);
+      if (PyErr_Occurred()) throw Refused();
+      if (wrong) refuse("sections must be one number of pairs, at least 1, for each axis");
+    }
+    d.base = number(a[3]);
+    d.interleaved = yes(a[4]);
+  }
+};
+
+// query, key, gain_query, gain_key, eps, positions, sections, base, interleaved, out_query, out_key
+PyObject* head_norm(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  HANDLE_TH_ERRORS
+  TAC_ARGUMENTS(11)
+  const Tensor& q = given(a[0], "query");
+  const Tensor *k = maybe(a[1], "key"), *gq = maybe(a[2], "gain_query"), *gk = maybe(a[3], "gain_key"), *oq_given = maybe(a[9], "out_query"), *ok_given = maybe(a[10], "out_key");
+  head_axes(q, "query");
+  if (k) head_axes(*k, "key");
+  if (!k && (gk || ok_given)) refuse("gain_key and out_key need keys");
+  const Call c(q, "query");
+  Rotation r(c, q, k, a + 4);
+  const ScalarType type = q.scalar_type();
+  const int64_t R = q.size(0), D = q.size(2);
+  const void *q_at = c.lines(&q, "query", type, q.sizes()), *k_at = k ? c.lines(k, "key", type, {R, k->size(1), D}) : nullptr;
+  const float *gq_at = (const float*)c.whole(gq, "gain_query", ScalarType::Float, {D}), *gk_at = (const float*)c.whole(gk, "gain_key", ScalarType::Float, {D});
+  const Tensor oq = oq_given ? *oq_given : c.make(q.sizes(), type), ok = !k ? Tensor() : ok_given ? *ok_given : c.make(k->sizes(), type);
+  void *oq_at = c.lines(&oq, "out_query", type, q.sizes()), *ok_at = k ? c.lines(&ok, "out_key", type, k->sizes()) : nullptr;
+  r.d.out_query = head_strides(oq);
+  if (k) r.d.out_key = head_strides(ok);
+  const int status = unlocked([&] { return tac_head_norm(&r.d, q_at, k_at, gq_at, gk_at, r.positions, oq_at, ok_at, c.stream()); });
+  if (status) return PyLong_FromLong(status);
+  written(oq_given);
+  written(ok_given);
+  return dict_of({{"q", oq_given ? same(a[9]) : out_of(oq)}, {"k", ok_given ? same(a[10]) : out_of(ok)}});
+  TAC_END
+  END_HANDLE_TH_ERRORS
+}
+
+// query, key, gain_query, gain_key, grad_out_query, grad_out_key, eps, positions, sections, base, interleaved, grad_query, grad_key, want_grad_gain
+PyObject* head_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  HANDLE_TH_ERRORS
+  TAC_ARGUMENTS(14)
+  const Tensor &q = given(a[0], "query"), &dq = given(a[4], "grad_out_query");
+  const Tensor *k = maybe(a[1], "key"), *gq = maybe(a[2], "gain_query"), *gk = maybe(a[3], "gain_key"), *dk = maybe(a[5], "grad_out_key"),
+               *xq_given = maybe(a[11], "grad_query"), *xk_given = maybe(a[12], "grad_key");
+  head_axes(q, "query");
+  if (k) head_axes(*k, "key");
+  if (!k && (gk || dk || xk_given)) refuse("gain_key, grad_out_key and grad_key need keys");
+  if (k && !dk) refuse("grad_out_key is missing");
+  const Call c(q, "query");
+  Rotation r(c, q, k, a + 6);
+  const ScalarType type = q.scalar_type();
+  const int64_t R = q.size(0), D = q.size(2);
+  const void *q_at = c.lines(&q, "query", type, q.sizes()), *k_at = k ? c.lines(k, "key", type, {R, k->size(1), D}) : nullptr;
+  const void *dq_at = c.lines(&dq, "grad_out_query", type, q.sizes()), *dk_at = k ? c.lines(dk, "grad_out_key", type, k->sizes()) : nullptr;
+  const float *gq_at = (const float*)c.whole(gq, "gain_query", ScalarType::Float, {D}), *gk_at = (const float*)c.whole(gk, "gain_key", ScalarType::Float, {D});
+  const Tensor xq = xq_given ? *xq_given : c.make(q.sizes(), type), xk = !k ? Tensor() : xk_given ? *xk_given : c.make(k->sizes(), type);
+  void *xq_at = c.lines(&xq, "grad_query", type, q.sizes()), *xk_at = k ? c.lines(&xk, "grad_key", type, k->sizes()) : nullptr;
+  r.d.out_query = head_strides(dq);
+  r.d.grad_query = head_strides(xq);
+  if (k) {
+    r.d.out_key = head_strides(*dk);
+    r.d.grad_key = head_strides(xk);
+  }
+  Tensor sum_q, sum_k, work;
+  if (yes(a[13])) {
+    sum_q = c.make({D}, ScalarType::Float);
+    if (k) sum_k = c.make({D}, ScalarType::Float);
+    work = c.scratch(tac_head_norm_workspace_bytes(&r.d));
+  }
+  const int status = unlocked([&] {
+    return tac_head_norm_backward(&r.d, q_at, k_at, gq_at, gk_at, r.positions, dq_at, dk_at, xq_at, xk_at, (float*)at_of(sum_q), (float*)at_of(sum_k), at_of(work),
+                                  c.stream());
+  });
+  if (status) return PyLong_FromLong(status);
+  written(xq_given);
+  written(xk_given);
+  return dict_of({{"grad_q", xq_given ? same(a[11]) : out_of(xq)}, {"grad_k", xk_given ? same(a[12]) : out_of(xk)}, {"grad_gain_q", out_of(sum_q)}, {"grad_gain_k", out_of(sum_k)}});
+  TAC_END
+  END_HANDLE_TH_ERRORS
+}
+
+// query, key, value, gate, write of a delta rule, [T, B, heads, ..] or (a step) [B, heads, ..]
+struct Delta {
+  tac_delta_desc_t d = {};
+  const Tensor &q, &k, &v, &g, &w;
+  bool step;
+  ScalarType type;
+  const void *q_at, *k_at, *v_at, *g_at, *w_at;
+  static const Tensor& axes(PyObject* o, const char* name, int64_t n) {
+    const Tensor& t = given(o, name);
+    if (t.dim() != n) refuse("%s must have %d axes", name, (int)n);
+    for (int64_t i = 0; i < n; ++i)
+      if (t.size(i) > INT32_MAX) refuse("%s is too large", name);
+    return t;
+  }
+  std::vector<int64_t> lead() const { return step ? std::vector<int64_t>{(int64_t)d.B} : std::vector<int64_t>{d.T, (int64_t)d.B}; }
+  std::vector<int64_t> shape(std::initializer_list<int64_t> rest) const {
+    std::vector<int64_t> s = lead();
+    s.insert(s.end(), rest);
+    return s;
+  }
+  std::vector<int64_t> keys() const { return shape({d.k_heads, d.Dk}); }
+  std::vector<int64_t> values() const { return shape({d.v_heads, d.Dv}); }
+  std::vector<int64_t> gates() const { return shape({d.v_heads}); }
+  std::vector<int64_t> state() const { return {d.B, d.v_heads, d.Dk, d.Dv}; }
+  tac_delta_strides_t strides(const Tensor& t) const {
+    return step ? tac_delta_strides_t{0, t.stride(0), t.stride(1)} : tac_delta_strides_t{t.stride(0), t.stride(1), t.stride(2)};
+  }
+  Delta(PyObject* const* a, bool one)
+      : q(axes(a[0], "query", one ? 3 : 4)), k(axes(a[1], "key", one ? 3 : 4)), v(axes(a[2], "value", one ? 3 : 4)), g(axes(a[3], "gate", one ? 2 : 3)),
+        w(axes(a[4], "write", one ? 2 : 3)), step(one), type(q.scalar_type()) {
+    const int64_t first = one ? 0 : 1;
+    d.T = one ? 1 : q.size(0);
+    d.B = (int32_t)q.size(first);
+    d.k_heads = (int32_t)q.size(first + 1);
+    d.Dk = (int32_t)q.size(first + 2);
+    d.v_heads = (int32_t)v.size(first + 1);
+    d.Dv = (int32_t)v.size(first + 2);
+    d.dtype = float_type(q, "query");
+    d.query = strides(q);
+    d.key = strides(k);
+    d.value = strides(v);
+    d.gate = strides(g);
+    d.write = strides(w);
+  }
+  void look(const Call& c) {
+    q_at = c.lines(&q, "query", type, keys());
+    k_at = c.lines(&k, "key", type, keys());
+    v_at = c.lines(&v, "value", type, values());
+    g_at = c.lines(&g, "gate", type, gates());
+    w_at = c.lines(&w, "write", type, gates());
+  }
+};
+
+// query, key, value, gate, write, lengths, h0, out, want_h_last, want_kept
+PyObject* delta_scan(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  HANDLE_TH_ERRORS
+  TAC_ARGUMENTS(10)
+  Delta x(a, false);
+  const Call c(x.q, "query");
+  x.look(c);
+  const auto& d = x.d;
+  const int32_t* lengths = (const int32_t*)c.whole(maybe(a[5], "lengths"), "lengths", ScalarType::Int, {d.B});
+  const float* h0 = (const float*)c.whole(maybe(a[6], "h0"), "h0", ScalarType::Float, x.state());
+  const Tensor* to = maybe(a[7], "out");
+  const Tensor out = to ? *to : c.make(x.values(), x.type);
+  void* o = c.lines(&out, "out", x.type, x.values());
+  x.d.out = x.strides(out);
+  Tensor h_last, states, updates;
+  if (yes(a[8])) h_last = c.make(x.state(), ScalarType::Float);
+  if (yes(a[9])) {
+    states = c.make({up(d.T, TAC_DELTA_CHUNK), d.B, d.v_heads, d.Dk, d.Dv}, ScalarType::Float);
+    updates = c.make(x.values(), ScalarType::Float);
+  }
+  const Tensor work = c.scratch(tac_delta_scan_workspace_bytes(&x.d));
+  const int status = unlocked([&] {
+    return tac_delta_scan(&x.d, x.q_at, x.k_at, x.v_at, x.g_at, x.w_at, lengths, h0, o, (float*)at_of(h_last), (float*)at_of(states), (float*)at_of(updates), at_of(work),
+                          c.stream());
+  });
+  if (status) return PyLong_FromLong(status);
+  written(to);
+  return dict_of({{"out", to ? same(a[7]) : out_of(out)}, {"h_last", out_of(h_last)}, {"states", out_of(states)}, {"updates", out_of(updates)}});
+  TAC_END
+  END_HANDLE_TH_ERRORS
+}
+
+// query, key, value, gate, write, states, updates, grad_out, lengths, grad_h_last, grad_query, grad_key, grad_value, grad_gate, grad_write, want_grad_h0
+PyObject* delta_scan_backward(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  HANDLE_TH_ERRORS
+  TAC_ARGUMENTS(16)
+  Delta x(a, false);
+  const Call c(x.q, "query");
+  x.look(c);
+  const auto& d = x.d;
+  const float* states = (const float*)c.whole(&given(a[5], "states"), "states", ScalarType::Float, {up(d.T, TAC_DELTA_CHUNK), d.B, d.v_heads, d.Dk, d.Dv});
+  const float* updates = (const float*)c.whole(&given(a[6], "updates"), "updates", ScalarType::Float, x.values());
+  const Tensor& go = given(a[7], "grad_out");
+  const void* go_at = c.lines(&go, "grad_out", x.type, x.values());
+  x.d.out = x.strides(go);
+  const int32_t* lengths = (const int32_t*)c.whole(maybe(a[8], "lengths"), "lengths", ScalarType::Int, {d.B});
+  const float* last = (const float*)c.whole(maybe(a[9], "grad_h_last"), "grad_h_last", ScalarType::Float, x.state());
+  const char* const names[5] = {"grad_query", "grad_key", "grad_value", "grad_gate", "grad_write"};
+  const std::vector<int64_t> shapes[5] = {x.keys(), x.keys(), x.values(), x.gates(), x.gates()};
+  tac_delta_strides_t* const strides[5] = {&x.d.grad_query, &x.d.grad_key, &x.d.grad_value, &x.d.grad_gate, &x.d.grad_write};
+  Tensor grads[5];
+  void* at[5];
+  for (int i = 0; i < 5; ++i) {
+    const Tensor* t = maybe(a[10 + i], names[i]);
+    grads[i] = t ? *t : c.make(shapes[i], x.type);
+    at[i] = c.lines(&grads[i], names[i], x.type, shapes[i]);
+    *strides[i] = x.strides(grads[i]);
+  }
+  Tensor h0;
+  if (yes(a[15])) h0 = c.make(x.state(), ScalarType::Float);
+  const Tensor work = c.scratch(tac_delta_scan_backward_workspace_bytes(&x.d));
+  const int status = unlocked([&] {
+    return tac_delta_scan_backward(&x.d, x.q_at, x.k_at, x.v_at, x.g_at, x.w_at, lengths, states, updates, go_at, last, at[0], at[1], at[2], at[3], at[4],
+                                   (float*)at_of(h0), at_of(work), c.stream());
+  });
+  if (status) return PyLong_FromLong(status);
+  PyObject* made[5];
+  for (int i = 0; i < 5; ++i) {
+    written(maybe(a[10 + i], names[i]));
+    made[i] = a[10 + i] != Py_None ? same(a[10 + i]) : out_of(grads[i]);
+  }
+  return dict_of({{names[0], made[0]}, {names[1], made[1]}, {names[2], made[2]}, {names[3], made[3]}, {names[4], made[4]}, {"grad_h0", out_of(h0)}});
+  TAC_END
+  END_HANDLE_TH_ERRORS
+}
+
+// query, key, value, gate, write, pool, slots, out
+PyObject* delta_step(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  HANDLE_TH_ERRORS
+  TAC_ARGUMENTS(8)
+  Delta x(a, true);
+  const Call c(x.q, "query");
+  x.look(c);
+  const auto& d = x.d;
+  const Tensor& pool = given(a[5], "pool");
+  if (pool.dim() != 4) refuse("pool must be [slots, heads, Dk, Dv]");
+  const int64_t n = pool.size(0);
+  float* states = (float*)c.whole(&pool, "pool", ScalarType::Float, {n, d.v_heads, d.Dk, d.Dv});
+  const int32_t* slots = (const int32_t*)c.whole(maybe(a[6], "slots"), "slots", ScalarType::Int, {d.B});
+  const Tensor* to = maybe(a[7], "out");
+  const Tensor out = to ? *to : c.make(x.values(), x.type);
+  void* o = c.lines(&out, "out", x.type, x.values());
+  x.d.out = x.strides(out);
+  const int status = unlocked([&] { return tac_delta_step(&x.d, x.q_at, x.k_at, x.v_at, x.g_at, x.w_at, states, n, slots, o, c.stream()); });
+  if (status) return PyLong_FromLong(status);
+  written(to);
+  written(&pool);
+  return to ? same(a[7]) : out_of(out);
+  TAC_END
+  END_HANDLE_TH_ERRORS
+}
+
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyMethodDef entry(const char* name) {
   return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(F)), METH_FASTCALL, nullptr};
@@ -457,6 +752,11 @@ PyMethodDef kMethods[] = {entry<quantize>("quantize"),
                           entry<gated_scan>("gated_scan"),
                           entry<gated_scan_backward>("gated_scan_backward"),
                           entry<gated_step>("gated_step"),
+                          entry<head_norm>("head_norm"),
+                          entry<head_norm_backward>("head_norm_backward"),
+                          entry<delta_scan>("delta_scan"),
+                          entry<delta_scan_backward>("delta_scan_backward"),
+                          entry<delta_step>("delta_step"),
                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_operators", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
