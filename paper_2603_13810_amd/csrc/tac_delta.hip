@@ -1,6 +1,6 @@
 // Gated delta rule over sequences: the states from chunk to chunk and the outputs.
 //
-// Columns of a state do not touch each other: a workgroup takes 16 or 32 of a head's and goes through the chunks, four waves side by side.  Of a chunk, with S its
+// Columns of a state do not touch each other: a workgroup takes 16 or 32 of a head's and goes through the chunks.  Of a chunk, with S its
 // first state and what prepare_kernel left,
 //   U = (I + A)^-1 b (V - e^G K S),   O = e^G Q S + P U,   S <- e^G_end S + K^T (e^(G_end - G) U).
 // S, the right-hand sides and U go from one product's result to the next one's operand through LDS as bfloat16 parts; S itself stays in registers in float32.
@@ -10,187 +10,224 @@ namespace tac {
 
 namespace {
 
-// LDS of scan_kernel in bfloat16 numbers: S [3][columns][DK + 8], right-hand sides [3][columns][kSteps], U faded [3], U [OUT], K transposed [IN][DK][kSteps]
+// Eight waves: four take the states from chunk to chunk, and four form the outputs from what those leave in LDS.
+
+// LDS of scan_kernel.  float32 [4][columns][kSums]: the waves' shares of K S; then in bfloat16 numbers S [OUT][columns][DK + 8] for the outputs, right-hand sides
+// [3][columns][kSteps], U faded [3], U [OUT], K transposed [IN][DK][kSteps]; and K as it stands, [64][DK + 8] elements.
+constexpr int kSums = kChunk + 4;
 template <typename T, int DK, int NT>
 struct ScanRoom {
   static constexpr int columns = 16 * NT, key = DK + 8;
   static constexpr int s_plane = columns * key, u_plane = columns * kSteps, k_plane = DK * kSteps;
-  static constexpr int s = 0, rhs = s + 3 * s_plane, faded = rhs + 3 * u_plane, u = faded + 3 * u_plane, k = u + Kind<T>::out * u_plane;
-  static constexpr int size = k + Kind<T>::in * k_plane;
+  static constexpr int s = 4 * columns * kSums * 2, rhs = s + Kind<T>::out * s_plane, faded = rhs + 3 * u_plane, u = faded + 3 * u_plane, k = u + Kind<T>::out * u_plane;
+  static constexpr int rows = k + Kind<T>::in * k_plane;
+  static constexpr int bytes = 2 * rows + kChunk * key * (int)sizeof(T);
 };
 
-template <typename T, int DK, int NT>
-__global__ __launch_bounds__(256) void scan_kernel(const DeltaParams p, int tiles) {
-  using Room = ScanRoom<T, DK, NT>;
-  constexpr int IN = Kind<T>::in, OUT = Kind<T>::out, KS = DK / 32, MT = DK / 16, OWN = MT > 4 ? MT / 4 : 1;
-  extern __shared__ __align__(16) uint8_t lds[];
-  bf16* const L = (bf16*)lds;
-  const int index = blockIdx.x, tile = index % tiles, h = index / tiles % p.v_heads, b = index / tiles / p.v_heads;
-  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, low16 = lane & 15, quad = lane >> 4;
-  const int hk = h / (p.v_heads / p.k_heads), first = tile * Room::columns;
-  const int64_t length = p.lengths ? min((int64_t)max(p.lengths[b], 0), p.T) : p.T;
-  const T* const q = (const T*)p.q + (int64_t)b * p.q_at.b + (int64_t)hk * p.q_at.head;
-  const T* const k = (const T*)p.k + (int64_t)b * p.k_at.b + (int64_t)hk * p.k_at.head;
-  const T* const v = (const T*)p.v + (int64_t)b * p.v_at.b + (int64_t)h * p.v_at.head;
-  T* const out = (T*)p.out + (int64_t)b * p.out_at.b + (int64_t)h * p.out_at.head;
-  const int64_t head = (int64_t)b * p.v_heads + h, state = (int64_t)p.Dk * p.Dv;
-  const Identity id(lane);
-  const bool owner = MT >= 4 || wave < MT;             // waves that have rows of S
+// What a workgroup of scan_kernel works on, and where this lane stands: wave w of either four has the chunk's steps from 16 w on as rows.
+template <typename T, int NT>
+struct ScanPlace {
+  int wave, lane, low16, quad, row, rows;      // row: of operands; rows: the first of four of results
+  int first, chunks, last;                     // last: steps of the last chunk
   int col[NT];
+  int64_t head, state;
+  const T *q, *k, *v;
+  T* out;
+  __device__ ScanPlace(const DeltaParams& p, int tiles) {
+    const HeadTile place(blockIdx.x, p.B * p.v_heads, tiles);
+    const int tile = place.tile, h = place.head % p.v_heads, b = place.head / p.v_heads, hk = h / (p.v_heads / p.k_heads);
+    wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64 % 4);
+    lane = threadIdx.x % 64;
+    low16 = lane & 15;
+    quad = lane >> 4;
+    row = 16 * wave + low16;
+    rows = 16 * wave + 4 * quad;
+    first = tile * 16 * NT;
 #pragma unroll
-  for (int t = 0; t < NT; ++t) col[t] = first + 16 * t + low16;
+    for (int t = 0; t < NT; ++t) col[t] = first + 16 * t + low16;
+    const int64_t length = p.lengths ? min((int64_t)max(p.lengths[b], 0), p.T) : p.T;
+    chunks = (int)((length + kChunk - 1) / kChunk);
+    last = (int)(length - (int64_t)(chunks - 1) * kChunk);
+    head = (int64_t)b * p.v_heads + h;
+    state = (int64_t)p.Dk * p.Dv;
+    q = (const T*)p.q + (int64_t)b * p.q_at.b + (int64_t)hk * p.q_at.head;
+    k = (const T*)p.k + (int64_t)b * p.k_at.b + (int64_t)hk * p.k_at.head;
+    v = (const T*)p.v + (int64_t)b * p.v_at.b + (int64_t)h * p.v_at.head;
+    out = (T*)p.out + (int64_t)b * p.out_at.b + (int64_t)h * p.out_at.head;
+  }
+  __device__ __forceinline__ ChunkRoom room(const DeltaParams& p, int c) const { return ChunkRoom(p.chunk_room, (int64_t)c * p.B * p.v_heads + head, Kind<T>::out); }
+  __device__ __forceinline__ int steps(int c) const { return c + 1 < chunks ? kChunk : last; }
+  // step `i` of chunk c, of a tensor whose steps are `stride` apart.  What is behind the last step is read from there: it stands beside b = 0, or is not stored.
+  template <typename E>
+  __device__ __forceinline__ E* step(E* base, int64_t stride, int c, int i) const {
+    base += (int64_t)c * kChunk * stride;
+    return base + (steps(c) == kChunk ? (int64_t)i * stride : (int64_t)min(i, last - 1) * stride);
+  }
+  // a row of the inverse or of the products; nothing stands above the diagonal
+  template <int PARTS>
+  __device__ __forceinline__ void load_matrix(Parts<PARTS> (&m)[2], const bf16* at) const {
+    m[0] = from_planes<PARTS>(at + ChunkRoom::operand(wave, 0, lane), ChunkRoom::plane);
+    m[1] = from_planes<PARTS>(at + ChunkRoom::operand(wave, wave >= 2 ? 1 : 0, lane), ChunkRoom::plane);
+  }
+};
 
+// Loads of the next chunk are asked for as soon as this one's have been used, a chunk before they are waited for; memory operations come in the same number whatever
+// the sizes (behind a branch the compiler waits for all of them), so what is not to be stored goes to a place of the workspace that nobody reads.
+
+// The chain that everything waits for: the states from chunk to chunk.  A wave has 32 rows of S (16 where Dk is at most 64).  As the first product's operand they stay in the wave's
+// registers: the summed index may come in any order, so the result's layout is taken as it is, and K is read to match; the waves' shares of K S are
+// added up through LDS, which moves a third of what S in parts would.  Of the chunk's K the wave reads every step, from LDS: a compute unit takes 64 bytes a cycle from the
+// caches, and every load that is not asked for twice counts.
+template <typename T, int DK, int NT, bool WHOLE, bool KEEP>
+__device__ __forceinline__ void scan_states(const DeltaParams& p, const ScanPlace<T, NT>& at, uint8_t* lds) {
+  using Room = ScanRoom<T, DK, NT>;
+  constexpr int IN = Kind<T>::in, OUT = Kind<T>::out, MT = DK / 16, OWN = MT > 4 ? 2 : 1;
+  float* const sums = (float*)lds;
+  bf16* const L = (bf16*)lds;
+  const int low16 = at.low16, quad = at.quad, rows = at.rows;
+  const bool owner = MT >= 4 || at.wave < MT;             // waves that have rows of S; the others' are zeros behind Dk
+  int state_row[OWN];
+#pragma unroll
+  for (int m = 0; m < OWN; ++m) state_row[m] = 16 * (at.wave * OWN + m) + 4 * quad;
   f32x4_t S[OWN][NT];
 #pragma unroll
   for (int m = 0; m < OWN; ++m)
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int row = 16 * (wave * OWN + m) + 4 * quad + r;
-        S[m][t][r] = p.h0 && row < p.Dk && col[t] < p.Dv ? p.h0[head * state + (int64_t)row * p.Dv + col[t]] : 0.0f;
-      }
+      for (int r = 0; r < 4; ++r)
+        S[m][t][r] = p.h0 && state_row[m] + r < p.Dk && at.col[t] < p.Dv ? p.h0[at.head * at.state + (int64_t)(state_row[m] + r) * p.Dv + at.col[t]] : 0.0f;
 
-  const int chunks = (int)((length + kChunk - 1) / kChunk);
-  for (int c = 0; c < chunks; ++c) {
+  Parts<3> inverse[2];
+  T value[NT][4];
+  f32x4_t start, rest, beta;
+  float whole;
+  const auto load_values = [&](int c) {
+    const ChunkRoom room = at.room(p, c);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const T* from = at.step(at.v, p.v_at.t, c, rows + r);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) value[t][r] = from[min(at.col[t], p.Dv - 1)];
+    }
+    start = *reinterpret_cast<const f32x4_t*>(room.start + rows);
+    beta = *reinterpret_cast<const f32x4_t*>(room.beta + rows);
+  };
+  const auto load_matrix = [&](int c) {
+    const ChunkRoom room = at.room(p, c);
+    at.load_matrix(inverse, room.inverse);
+    rest = *reinterpret_cast<const f32x4_t*>(room.rest + rows);
+  };
+  const auto load_whole = [&](int c) { whole = at.room(p, c).start[kChunk - 1]; };
+  loads_arrive();
+  if (at.chunks) {
+    load_values(0);
+    load_matrix(0);
+    load_whole(0);
+  }
+  __syncthreads();                                        // the first chunk's K
+  for (int c = 0; c < at.chunks; ++c) {
     const int64_t from = (int64_t)c * kChunk;
-    const int n = (int)min((int64_t)kChunk, length - from);
-    const int64_t index_of_chunk = (int64_t)c * p.B * p.v_heads + head;
-    const ChunkRoom room(p.chunk_room, index_of_chunk, OUT);
-    // operands with the chunk's steps as rows
-    Parts<IN> key[KS], query[KS];
-    {
-      const int row = 16 * wave + low16;
+    const int next = c + 1 < at.chunks ? c + 1 : c;
+    float* const nowhere = at.room(p, c).high;            // read backwards only, from a workspace of its own
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const int at = 32 * s + 8 * quad, left = row < n ? p.Dk - at : 0;
-        Eight<T> e;
-        e.load(k + (from + row) * p.k_at.t + at, left);
-        key[s] = e.parts();
-        e.load(q + (from + row) * p.q_at.t + at, left);
-        query[s] = e.parts();
-      }
-    }
-    f32x4_t value[NT];
+    for (int t = 0; t < NT; ++t) {
+      float own[8];
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+      for (int e = 0; e < 8; ++e) own[e] = e / 4 < OWN ? S[e / 4 < OWN ? e / 4 : 0][t][e % 4] : 0.0f;
+      const Parts<3> op = split<3>(own);
+      if (owner) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int row = 16 * wave + 4 * quad + r;
-        value[t][r] = row < n && col[t] < p.Dv ? (float)v[(from + row) * p.v_at.t + col[t]] : 0.0f;
-      }
-    const f32x4_t start = *reinterpret_cast<const f32x4_t*>(room.start + 16 * wave + 4 * quad);
-    const f32x4_t rest = *reinterpret_cast<const f32x4_t*>(room.rest + 16 * wave + 4 * quad);
-    const f32x4_t beta = *reinterpret_cast<const f32x4_t*>(room.beta + 16 * wave + 4 * quad);
-    const float whole = room.start[kChunk - 1];
-
-    if (owner) {
+        for (int m = 0; m < OWN; ++m)
 #pragma unroll
-      for (int m = 0; m < OWN; ++m)
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          const int row = 16 * (wave * OWN + m) + 4 * quad;
-          quad_to_planes<3>(L + Room::s + (16 * t + low16) * Room::key + row, Room::s_plane, S[m][t]);
-          if (p.states && col[t] < p.Dv) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (row + r < p.Dk) p.states[index_of_chunk * state + (int64_t)(row + r) * p.Dv + col[t]] = S[m][t][r];
+          for (int i = 0; i < OUT; ++i) {
+            const u32x4_t w = __builtin_bit_cast(u32x4_t, op.p[i]);
+            *reinterpret_cast<u32x2_t*>(L + Room::s + i * Room::s_plane + (16 * t + low16) * Room::key + state_row[m]) = u32x2_t{w[2 * m], w[2 * m + 1]};
           }
+      }
+      if constexpr (KEEP) {
+#pragma unroll
+        for (int m = 0; m < OWN; ++m) {
+          float* to = p.states + ((int64_t)c * p.B * p.v_heads + at.head) * at.state + (int64_t)state_row[m] * p.Dv + at.col[t];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) store_device(state_row[m] + r < p.Dk && at.col[t] < p.Dv ? to + r * p.Dv : nowhere, S[m][t][r]);
         }
-    }
-    __syncthreads();
-
-    f32x4_t ks[NT], qs[NT];
+      }
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      ks[t] = qs[t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const Parts<3> op = from_planes<3>(L + Room::s + (16 * t + low16) * Room::key + 32 * s + 8 * quad, Room::s_plane);
-        multiply<3>(ks[t], key[s], op);
-        multiply<OUT>(qs[t], query[s], op);
+      for (int i = 0; i < 4; ++i) {
+        f32x4_t share = {0.0f, 0.0f, 0.0f, 0.0f};
+        const T* const from = (const T*)(L + Room::rows) + (16 * i + low16) * Room::key;
+        const Piece<T, 4> a = load_aligned<T, 4>(from + (owner ? state_row[0] : 0));
+        if constexpr (OWN == 2) multiply<3>(share, parts_of(a, load_aligned<T, 4>(from + state_row[1])), op);
+        else multiply<3>(share, parts_of(a, a), op);          // the other half of S's operand is zero
+        *reinterpret_cast<f32x4_t*>(sums + (at.wave * Room::columns + 16 * t + low16) * kSums + 16 * i + 4 * quad) = share;
       }
     }
+    __syncthreads();                                      // S, the shares of K S
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      f32x4_t rhs;
+      f32x4_t ks = {0.0f, 0.0f, 0.0f, 0.0f}, rhs;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) rhs[r] = beta[r] * fmaf(-start[r], ks[t][r], value[t][r]);
-      quad_to_planes<3>(L + Room::rhs + (16 * t + low16) * kSteps + 16 * wave + 4 * quad, Room::u_plane, rhs);
+      for (int w = 0; w < 4; ++w) ks += *reinterpret_cast<const f32x4_t*>(sums + (w * Room::columns + 16 * t + low16) * kSums + rows);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) rhs[r] = beta[r] * fmaf(-start[r], ks[r], (float)value[t][r]);
+      quad_to_planes<3>(L + Room::rhs + (16 * t + low16) * kSteps + rows, Room::u_plane, rhs);
     }
-#pragma unroll
-    for (int s = 0; s < KS; ++s) transpose_to<IN>(L + Room::k, Room::k_plane, key[s], 16 * wave, 32 * s, id, lane);
-    __syncthreads();
-
-    f32x4_t u[NT];
+    in_this_order();
+    load_values(next);
+    __syncthreads();                                      // right-hand sides, K transposed
+    f32x4_t u[NT], faded[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) u[t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      if (32 * s > 16 * wave + 15) continue;           // nothing above the diagonal
-      const Parts<3> a = from_planes<3>(room.inverse + (16 * wave + low16) * kChunk + 32 * s + 8 * quad, ChunkRoom::plane);
+      if (s && at.wave < 2) continue;
 #pragma unroll
-      for (int t = 0; t < NT; ++t) multiply<3>(u[t], a, from_planes<3>(L + Room::rhs + (16 * t + low16) * kSteps + 32 * s + 8 * quad, Room::u_plane));
-    }
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      const int at = (16 * t + low16) * kSteps + 16 * wave + 4 * quad;
-      f32x4_t faded;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) faded[r] = rest[r] * u[t][r];
-      quad_to_planes<3>(L + Room::faded + at, Room::u_plane, faded);
-      quad_to_planes<OUT>(L + Room::u + at, Room::u_plane, u[t]);
-      if (p.updates && col[t] < p.Dv) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int row = 16 * wave + 4 * quad + r;
-          if (from + row < p.T) p.updates[((from + row) * p.B * p.v_heads + head) * p.Dv + col[t]] = u[t][r];
-        }
-      }
-    }
-    __syncthreads();
-
-    if (owner) {
-#pragma unroll
-      for (int m = 0; m < OWN; ++m) {
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) S[m][t][r] *= whole;
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const Parts<IN> a = from_planes<IN>(L + Room::k + (16 * (wave * OWN + m) + low16) * kSteps + 32 * s + 8 * quad, Room::k_plane);
-#pragma unroll
-          for (int t = 0; t < NT; ++t)
-            multiply<3>(S[m][t], a, from_planes<3>(L + Room::faded + (16 * t + low16) * kSteps + 32 * s + 8 * quad, Room::u_plane));
-        }
-      }
+      for (int t = 0; t < NT; ++t) multiply<3>(u[t], inverse[s], from_planes<3>(L + Room::rhs + (16 * t + low16) * kSteps + 32 * s + 8 * quad, Room::u_plane));
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) qs[t][r] *= start[r];
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      if (32 * s > 16 * wave + 15) continue;
-      const Parts<OUT> a = from_planes<OUT>(room.products + (16 * wave + low16) * kChunk + 32 * s + 8 * quad, ChunkRoom::plane);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) multiply<OUT>(qs[t], a, from_planes<OUT>(L + Room::u + (16 * t + low16) * kSteps + 32 * s + 8 * quad, Room::u_plane));
-    }
+      for (int r = 0; r < 4; ++r) faded[t][r] = rest[r] * u[t][r];
+    computed(faded);
+    in_this_order();
+    load_matrix(next);
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      if (col[t] >= p.Dv) continue;
+      const int place = (16 * t + low16) * kSteps + rows;
+      quad_to_planes<3>(L + Room::faded + place, Room::u_plane, faded[t]);
+      quad_to_planes<OUT>(L + Room::u + place, Room::u_plane, u[t]);
+      if constexpr (KEEP) {
+        float* to = p.updates + ((from + rows) * p.B * p.v_heads + at.head) * p.Dv + at.col[t];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int row = 16 * wave + 4 * quad + r;
-        if (from + row < p.T) out[(from + row) * p.out_at.t + col[t]] = (T)(row < n ? qs[t][r] : 0.0f);
+        for (int r = 0; r < 4; ++r) store_device(from + rows + r < p.T && at.col[t] < p.Dv ? to + (int64_t)r * p.B * p.v_heads * p.Dv : nowhere, u[t][r]);
       }
     }
-  }
-  // behind the last chunk's steps
-  for (int64_t t = (int64_t)chunks * kChunk + threadIdx.x / Room::columns; t < p.T; t += 256 / Room::columns) {
-    const int at = first + threadIdx.x % Room::columns;
-    if (at < p.Dv) out[t * p.out_at.t + at] = (T)0.0f;
+    __syncthreads();                                      // U, the next chunk's K
+#pragma unroll
+    for (int m = 0; m < OWN; ++m) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) S[m][t][r] *= whole;
+      computed(S[m]);
+    }
+    in_this_order();
+    load_whole(next);
+    if (owner) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        Parts<3> op[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) op[t] = from_planes<3>(L + Room::faded + (16 * t + low16) * kSteps + 32 * s + 8 * quad, Room::u_plane);
+#pragma unroll
+        for (int m = 0; m < OWN; ++m) {
+          const Parts<IN> a = from_planes<IN>(L + Room::k + (16 * (at.wave * OWN + m) + low16) * kSteps + 32 * s + 8 * quad, Room::k_plane);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) multiply<3>(S[m][t], a, op[t]);
+        }
+      }
+    }
   }
   if (!p.h_last || !owner) return;
 #pragma unroll
@@ -198,30 +235,145 @@ __global__ __launch_bounds__(256) void scan_kernel(const DeltaParams p, int tile
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int row = 16 * (wave * OWN + m) + 4 * quad + r;
-        if (row < p.Dk && col[t] < p.Dv) p.h_last[head * state + (int64_t)row * p.Dv + col[t]] = S[m][t][r];
-      }
+      for (int r = 0; r < 4; ++r)
+        if (state_row[m] + r < p.Dk && at.col[t] < p.Dv) p.h_last[at.head * at.state + (int64_t)(state_row[m] + r) * p.Dv + at.col[t]] = S[m][t][r];
 }
 
-template <typename T, int DK, int NT>
+// The outputs, from what the chain leaves in LDS.  And its K: the next chunk's as it stands, this one's transposed, zero behind Dk, so that S is.
+template <typename T, int DK, int NT, bool WHOLE>
+__device__ __forceinline__ void scan_outputs(const DeltaParams& p, const ScanPlace<T, NT>& at, uint8_t* lds) {
+  using Room = ScanRoom<T, DK, NT>;
+  constexpr int IN = Kind<T>::in, OUT = Kind<T>::out, KS = DK / 32;
+  bf16* const L = (bf16*)lds;
+  T* const key_row = (T*)(L + Room::rows) + at.row * Room::key + 8 * at.quad;
+  const int low16 = at.low16, quad = at.quad, rows = at.rows;
+  const Identity id(at.lane);
+  Piece<T, 8> key[KS], query[KS];
+  Parts<OUT> products[2];
+  f32x4_t start;
+  const auto load_queries = [&](int c) {
+    const T* from = at.step(at.q, p.q_at.t, c, at.row);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) load_piece<WHOLE>(query[s], from, 32 * s + 8 * quad, p.Dk);
+    start = *reinterpret_cast<const f32x4_t*>(at.room(p, c).start + rows);
+  };
+  // whole rows at a time on the way from memory
+  constexpr int pieces = DK / 8;
+  const int key_at = 16 * at.wave + at.lane / pieces, key_col = 8 * (at.lane % pieces);
+  const auto load_keys = [&](int c) {
+#pragma unroll
+    for (int s = 0; s < KS; ++s) load_piece<WHOLE>(key[s], at.step(at.k, p.k_at.t, c, key_at + s * (64 / pieces)), key_col, p.Dk);
+  };
+  const auto keep_keys = [&] {
+#pragma unroll
+    for (int s = 0; s < KS; ++s) store_aligned((T*)(L + Room::rows) + (key_at + s * (64 / pieces)) * Room::key + key_col, key[s]);
+  };
+  if (at.chunks) {
+    load_keys(0);
+    keep_keys();
+    in_this_order();
+    load_keys(at.chunks > 1 ? 1 : 0);                     // in the loop's order: waits count what was asked for behind
+    in_this_order();
+    at.load_matrix(products, at.room(p, 0).products);
+    load_queries(0);
+  }
+  __syncthreads();                                        // the first chunk's K
+  for (int c = 0; c < at.chunks; ++c) {
+    const int64_t from = (int64_t)c * kChunk;
+    const int n = at.steps(c), next = c + 1 < at.chunks ? c + 1 : c, after = c + 2 < at.chunks ? c + 2 : next;
+    __syncthreads();                                      // S, the shares of K S
+#pragma unroll
+    for (int s = 0; s < KS; ++s) transpose_to<IN>(L + Room::k, Room::k_plane, parts_of(load_aligned<T, 8>(key_row + 32 * s)), 16 * at.wave, 32 * s, id, at.lane, p.Dk);
+    __syncthreads();                                      // right-hand sides, K transposed
+    keep_keys();
+    in_this_order();
+    load_keys(after);
+    f32x4_t o[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) o[t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const Parts<IN> a = parts_of(query[s]);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) multiply<OUT>(o[t], a, from_planes<OUT>(L + Room::s + (16 * t + low16) * Room::key + 32 * s + 8 * quad, Room::s_plane));
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) o[t][r] *= start[r];
+    __syncthreads();                                      // U, the next chunk's K
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      if (s && at.wave < 2) continue;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) multiply<OUT>(o[t], products[s], from_planes<OUT>(L + Room::u + (16 * t + low16) * kSteps + 32 * s + 8 * quad, Room::u_plane));
+    }
+    computed(o);
+    in_this_order();
+    T* to[NT][4];
+    T* const nowhere = (T*)at.room(p, c).low;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      T* const line = at.out + (from + rows + r) * p.out_at.t;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) to[t][r] = line + at.col[t];
+    }
+    if (n < kChunk || at.first + Room::columns > p.Dv) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          if (rows + r >= n) o[t][r] = 0.0f;
+          if (from + rows + r >= p.T || at.col[t] >= p.Dv) to[t][r] = nowhere;
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) store_device(to[t][r], (T)o[t][r]);
+    at.load_matrix(products, at.room(p, next).products);
+    load_queries(next);
+  }
+  // behind the last chunk's steps
+  for (int64_t t = (int64_t)at.chunks * kChunk + threadIdx.x % 256 / Room::columns; t < p.T; t += 256 / Room::columns) {
+    const int c = at.first + threadIdx.x % Room::columns;
+    if (c < p.Dv) at.out[t * p.out_at.t + c] = (T)0.0f;
+  }
+}
+
+template <typename T, int DK, int NT, bool WHOLE, bool KEEP>
+__global__ __launch_bounds__(512) void scan_kernel(const DeltaParams p, int tiles) {
+  extern __shared__ __align__(16) uint8_t lds[];
+  const ScanPlace<T, NT> at(p, tiles);
+  // both meet at the same barriers: one, then three a chunk
+  if (__builtin_amdgcn_readfirstlane(threadIdx.x / 256) == 0) scan_states<T, DK, NT, WHOLE, KEEP>(p, at, lds);
+  else scan_outputs<T, DK, NT, WHOLE>(p, at, lds);
+}
+
+template <typename T, int DK, int NT, bool WHOLE, bool KEEP>
 hipError_t scan_shaped(const DeltaParams& p, hipStream_t s) {
   const int tiles = (p.Dv + 16 * NT - 1) / (16 * NT);
-  constexpr int bytes = ScanRoom<T, DK, NT>::size * 2;
+  constexpr int bytes = ScanRoom<T, DK, NT>::bytes;
   if (bytes > 64 << 10) {
-    const hipError_t e = hipFuncSetAttribute((const void*)scan_kernel<T, DK, NT>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    const hipError_t e = hipFuncSetAttribute((const void*)scan_kernel<T, DK, NT, WHOLE, KEEP>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((scan_kernel<T, DK, NT>), dim3((unsigned)((int64_t)p.B * p.v_heads * tiles)), dim3(256), bytes, s, p, tiles);
+  hipLaunchKernelGGL((scan_kernel<T, DK, NT, WHOLE, KEEP>), dim3((unsigned)((int64_t)p.B * p.v_heads * tiles)), dim3(512), bytes, s, p, tiles);
   return hipGetLastError();
 }
 
-template <typename T, int NT>
+template <typename T, int DK, int NT, bool WHOLE, bool KEEP>
+hipError_t scan_fitting(const DeltaParams& p, hipStream_t s) {      // float32 keys of 128 features in three parts leave LDS for 16 columns
+  return scan_shaped<T, DK, (ScanRoom<T, DK, NT>::bytes <= 160 << 10 ? NT : 1), WHOLE, KEEP>(p, s);
+}
+
+template <typename T, int NT, bool KEEP>
 hipError_t scan_typed(const DeltaParams& p, hipStream_t s) {
+  const bool whole = p.Dk % 8 == 0;      // pieces of 8 and of 4
   switch (padded_key(p.Dk)) {
-    case 32: return scan_shaped<T, 32, NT>(p, s);
-    case 64: return scan_shaped<T, 64, NT>(p, s);
-    default: return scan_shaped<T, 128, NT>(p, s);
+    case 32: return whole ? scan_fitting<T, 32, NT, true, KEEP>(p, s) : scan_fitting<T, 32, NT, false, KEEP>(p, s);
+    case 64: return whole ? scan_fitting<T, 64, NT, true, KEEP>(p, s) : scan_fitting<T, 64, NT, false, KEEP>(p, s);
+    default: return whole ? scan_fitting<T, 128, NT, true, KEEP>(p, s) : scan_fitting<T, 128, NT, false, KEEP>(p, s);
   }
 }
 
@@ -236,9 +388,13 @@ hipError_t delta_scan_launch(const DeltaParams& given, uint8_t* workspace, hipSt
   p.chunk_room = workspace;
   const hipError_t e = delta_prepare_launch(p, false, s);
   if (e != hipSuccess) return e;
-  const bool narrow = delta_narrow(p.B, p.v_heads, p.Dv);
-  if (p.bf16) return narrow ? scan_typed<bf16, 1>(p, s) : scan_typed<bf16, 2>(p, s);
-  return narrow ? scan_typed<float, 1>(p, s) : scan_typed<float, 2>(p, s);
+  const auto with = [&](auto keep) {
+    constexpr bool KEEP = decltype(keep)::value;
+    const bool narrow = delta_narrow(p.B, p.v_heads, p.Dv);
+    if (p.bf16) return narrow ? scan_typed<bf16, 1, KEEP>(p, s) : scan_typed<bf16, 2, KEEP>(p, s);
+    return narrow ? scan_typed<float, 1, KEEP>(p, s) : scan_typed<float, 2, KEEP>(p, s);
+  };
+  return p.states ? with(std::true_type()) : with(std::false_type());
 }
 
 }  // namespace tac

@@ -30,7 +30,8 @@ __global__ __launch_bounds__(256) void back_scan_kernel(const DeltaParams p, int
   constexpr int IN = Kind<T>::in, KS = DK / 32, MT = DK / 16, OWN = MT > 4 ? MT / 4 : 1;
   extern __shared__ __align__(16) uint8_t lds[];
   bf16* const L = (bf16*)lds;
-  const int index = blockIdx.x, tile = index % tiles, h = index / tiles % p.v_heads, b = index / tiles / p.v_heads;
+  const HeadTile place(blockIdx.x, p.B * p.v_heads, tiles);
+  const int tile = place.tile, h = place.head % p.v_heads, b = place.head / p.v_heads;
   const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, low16 = lane & 15, quad = lane >> 4;
   const int hk = h / (p.v_heads / p.k_heads), first = tile * Room::columns;
   const int64_t length = p.lengths ? min((int64_t)max(p.lengths[b], 0), p.T) : p.T;
@@ -120,7 +121,7 @@ __global__ __launch_bounds__(256) void back_scan_kernel(const DeltaParams p, int
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       if (32 * s + 31 < 16 * wave) continue;           // rows of the transposed matrices begin at the diagonal
-      const Parts<3> a = from_planes<3>(room.products + (16 * wave + low16) * kChunk + 32 * s + 8 * quad, ChunkRoom::plane);
+      const Parts<3> a = from_planes<3>(room.products + ChunkRoom::operand(wave, s, lane), ChunkRoom::plane);
 #pragma unroll
       for (int t = 0; t < NT; ++t) multiply<3>(x[t], a, from_planes<IN>(L + Room::grad + (16 * t + low16) * kSteps + 32 * s + 8 * quad, Room::u_plane));
     }
@@ -128,8 +129,8 @@ __global__ __launch_bounds__(256) void back_scan_kernel(const DeltaParams p, int
     for (int t = 0; t < NT; ++t) quad_to_planes<3>(L + Room::x + (16 * t + low16) * kSteps + 16 * wave + 4 * quad, Room::u_plane, x[t]);
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-      transpose_to<IN>(L + Room::k, Room::k_plane, key[s], 16 * wave, 32 * s, id, lane);
-      transpose_to<IN>(L + Room::q, Room::k_plane, query[s], 16 * wave, 32 * s, id, lane);
+      transpose_to<IN>(L + Room::k, Room::k_plane, key[s], 16 * wave, 32 * s, id, lane, p.Dk);
+      transpose_to<IN>(L + Room::q, Room::k_plane, query[s], 16 * wave, 32 * s, id, lane, p.Dk);
     }
     __syncthreads();
 
@@ -139,7 +140,7 @@ __global__ __launch_bounds__(256) void back_scan_kernel(const DeltaParams p, int
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       if (32 * s + 31 < 16 * wave) continue;
-      const Parts<3> a = from_planes<3>(room.inverse + (16 * wave + low16) * kChunk + 32 * s + 8 * quad, ChunkRoom::plane);
+      const Parts<3> a = from_planes<3>(room.inverse + ChunkRoom::operand(wave, s, lane), ChunkRoom::plane);
 #pragma unroll
       for (int t = 0; t < NT; ++t) multiply<3>(R[t], a, from_planes<3>(L + Room::x + (16 * t + low16) * kSteps + 32 * s + 8 * quad, Room::u_plane));
     }
@@ -372,7 +373,7 @@ __global__ __launch_bounds__(256) void gradient_kernel(const DeltaParams p) {
       const int at = 32 * s + 8 * quad;
       Eight<T> e;
       e.load(k + (int64_t)own * p.k_at.t + at, own < n ? p.Dk - at : 0);
-      transpose_to<IN>(L + Room::k, Room::k_plane, e.parts(), 16 * wave, 32 * s, id, lane);
+      transpose_to<IN>(L + Room::k, Room::k_plane, e.parts(), 16 * wave, 32 * s, id, lane, p.Dk);
     }
     __syncthreads();
     f32x4_t dG = {0.0f, 0.0f, 0.0f, 0.0f}, leaves = dG;      // of the four steps of this lane's results: a part over the features
@@ -405,7 +406,7 @@ __global__ __launch_bounds__(256) void gradient_kernel(const DeltaParams p) {
       const int at = 32 * s + 8 * quad;
       Eight<T> e;
       e.load(q + (int64_t)own * p.q_at.t + at, own < n ? p.Dk - at : 0);
-      transpose_to<IN>(L + Room::k, Room::k_plane, e.parts(), 16 * wave, 32 * s, id, lane);
+      transpose_to<IN>(L + Room::k, Room::k_plane, e.parts(), 16 * wave, 32 * s, id, lane, p.Dk);
     }
     __syncthreads();
 #pragma unroll

@@ -137,18 +137,37 @@ struct Identity {
     }
   }
 };
-// `to`: LDS planes [PARTS][columns][kSteps]; the operand holds steps `row`.. (16 of them) and columns col.. (32)
+// `to`: LDS planes [PARTS][columns][kSteps]; the operand holds steps `row`.. (16 of them) and columns col.. (32), of which those from `cols` on are taken as zero
 template <int PARTS>
-__device__ __forceinline__ void transpose_to(bf16* to, int plane, const Parts<PARTS>& a, int row, int col, const Identity& id, int lane) {
+__device__ __forceinline__ void transpose_to(bf16* to, int plane, const Parts<PARTS>& a, int row, int col, const Identity& id, int lane, int cols) {
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
     bf16* at = to + (col + 16 * half + (lane & 15)) * kSteps + row + 4 * (lane >> 4);
 #pragma unroll
     for (int q = 0; q < PARTS; ++q) {
-      const f32x4_t t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[q], half ? id.odd.p[0] : id.even.p[0], f32x4_t{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
+      f32x4_t t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[q], half ? id.odd.p[0] : id.even.p[0], f32x4_t{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
+      if (col + 16 * half + (lane & 15) >= cols) t = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
       *reinterpret_cast<u32x2_t*>(at + q * plane) = u32x2_t{pack_bf16(t[0], t[1]), pack_bf16(t[2], t[3])};
     }
   }
+}
+
+// Everything that was asked for from memory is there.  In front of a loop whose loads stay on their way: the compiler would otherwise keep the wait for what was
+// loaded before the loop at its first use inside, where it waits for the loop's own loads in every turn.
+__device__ __forceinline__ void loads_arrive() { __builtin_amdgcn_s_waitcnt(0x0f70); }      // vmcnt(0)
+
+// keeps the loads behind it behind it, so that they can take the registers of what was used before it
+__device__ __forceinline__ void in_this_order() { __builtin_amdgcn_sched_barrier(0); }
+template <int N>
+__device__ __forceinline__ void computed(f32x4_t (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(v[i]));
+}
+
+// a store to device memory, also where the compiler cannot tell from a chosen address that it is
+template <typename T>
+__device__ __forceinline__ void store_device(T* to, T v) {
+  *(__attribute__((address_space(1))) T*)(uintptr_t)to = v;
 }
 
 __device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f); }
@@ -173,29 +192,124 @@ struct DeltaParams {
   float *back_states, *r, *shared;   // backward: gradients of the states behind every chunk, r as updates are laid out, sums over heads that share a key
 };
 
+// Which head and which tile of its columns a workgroup takes.  Consecutive workgroups go to the eight dies in turn: a head's tiles, which read the same queries, keys and matrices,
+// are eight apart, so that one die's cache holds them (a sequence of 32768 steps, 16 heads: before, the loads of one chunk took longer than the chunk before it).
+struct HeadTile {
+  int head, tile;
+  __device__ __forceinline__ HeadTile(int index, int heads, int tiles) {
+    const int group = index / (8 * tiles), at = index - group * 8 * tiles, wide = min(8, heads - 8 * group);
+    head = 8 * group + at % wide;
+    tile = at / wide;
+  }
+};
+
 __device__ __forceinline__ int steps_of(const DeltaParams& p, int b, int64_t from) {      // steps of the chunk that begins at `from`
   const int64_t n = p.lengths ? min((int64_t)max(p.lengths[b], 0), p.T) : p.T;
   return (int)max((int64_t)0, min((int64_t)kChunk, n - from));
 }
 
-// What prepare_kernel leaves of a chunk and head: planes of the inverse (three parts) and of the queries' products, then factors of the steps.
-// Backwards both matrices stand transposed, so that a row's neighbours are what is summed over.
+// What prepare_kernel leaves of a chunk and head: the inverse in three parts and the queries' products in P_PARTS, [64][64] each, then float32 factors of the steps.
+// Backwards both matrices stand transposed, so that a row's neighbours are what is summed over.  A plane is in the order in which it is read, the operand of 16 rows and 32
+// columns in one piece, a lane's eight numbers after the other's; of the operands only those that hold something are written.
 struct ChunkRoom {
+  // operand of rows 16 tile.. and columns 32 step..
+  static __device__ __forceinline__ int operand(int tile, int step, int lane) { return ((tile * 2 + step) * 64 + lane) * 8; }
   static constexpr int plane = kChunk * kChunk;
   static constexpr int64_t bytes(int p_parts) { return (int64_t)(3 + p_parts) * plane * 2 + 5 * kChunk * 4; }
-  const bf16 *inverse, *products;
-  const float *start, *rest, *beta, *high, *low;      // e^G, e^(G_end - G), b, and G in two numbers
-  __device__ ChunkRoom(const uint8_t* base, int64_t index, int p_parts) {
-    const uint8_t* at = base + index * bytes(p_parts);
-    inverse = (const bf16*)at;
+  bf16 *inverse, *products;
+  float *start, *rest, *beta, *high, *low;      // e^G, e^(G_end - G), b, and G in two numbers
+  __device__ __forceinline__ ChunkRoom(uint8_t* base, int64_t index, int p_parts) {
+    inverse = (bf16*)(base + index * bytes(p_parts));
     products = inverse + 3 * plane;
-    start = (const float*)(products + p_parts * plane);
+    start = (float*)(products + p_parts * plane);
     rest = start + kChunk;
     beta = rest + kChunk;
     high = beta + kChunk;
     low = high + kChunk;
   }
 };
+
+// A lane's pieces of one row of queries or keys, N neighbours from each of `at`, as they stand in memory.  Loads of the next chunk are on their way while this one is
+// worked on: nothing here looks at what is loaded, and nothing branches, since behind a branch the compiler waits for everything.  WHOLE: Dk is a multiple of N, a piece
+// is there or not; else element by element.  What is not there is read from where something of the row is: it stands beside a state's rows behind Dk, which are zero.
+template <typename T, int N>
+struct Piece;
+template <int N>
+struct Piece<bf16, N> {
+  uint32_t w[N / 2];
+  __device__ __forceinline__ void set(int e, bf16 x) {
+    const uint32_t v = __builtin_bit_cast(uint16_t, x);
+    w[e / 2] = e % 2 ? (w[e / 2] & 0xffffu) | v << 16 : (w[e / 2] & 0xffff0000u) | v;
+  }
+};
+template <int N>
+struct Piece<float, N> {
+  float w[N];
+  __device__ __forceinline__ void set(int e, float x) { w[e] = x; }
+};
+template <bool WHOLE, typename T, int N>
+__device__ __forceinline__ void load_piece(Piece<T, N>& v, const T* row, int at, int Dk) {
+  if constexpr (WHOLE) {
+    __builtin_memcpy(v.w, row + (at < Dk ? at : 0), N * sizeof(T));
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e) v.set(e, row[min(at + e, Dk - 1)]);
+  }
+}
+// the same in LDS, aligned
+template <typename T, int N>
+__device__ __forceinline__ void store_aligned(T* to, const Piece<T, N>& v) {
+  constexpr int words = N * sizeof(T) / 4;
+  if constexpr (words == 2) {
+    *reinterpret_cast<u32x2_t*>(to) = u32x2_t{v.w[0], v.w[1]};
+  } else {
+#pragma unroll
+    for (int i = 0; i < words; i += 4) {
+      u32x4_t w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = __builtin_bit_cast(uint32_t, v.w[i + e]);
+      reinterpret_cast<u32x4_t*>(to)[i / 4] = w;
+    }
+  }
+}
+template <typename T, int N>
+__device__ __forceinline__ Piece<T, N> load_aligned(const T* from) {
+  constexpr int words = N * sizeof(T) / 4;
+  Piece<T, N> v;
+  if constexpr (words == 2) {
+    const u32x2_t w = *reinterpret_cast<const u32x2_t*>(from);
+    v.w[0] = w[0];
+    v.w[1] = w[1];
+  } else {
+#pragma unroll
+    for (int i = 0; i < words; i += 4) {
+      const u32x4_t w = reinterpret_cast<const u32x4_t*>(from)[i / 4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t one = w[e];             // a vector's element itself is not what a bit cast takes
+        v.w[i + e] = __builtin_bit_cast(std::remove_reference_t<decltype(v.w[0])>, one);
+      }
+    }
+  }
+  return v;
+}
+// eight summed indices as an operand: one piece of eight, or two of four
+__device__ __forceinline__ Parts<1> parts_of(const Piece<bf16, 8>& v) { return {__builtin_bit_cast(bf16x8_t, v)}; }
+__device__ __forceinline__ Parts<1> parts_of(const Piece<bf16, 4>& a, const Piece<bf16, 4>& b) {
+  return {__builtin_bit_cast(bf16x8_t, u32x4_t{a.w[0], a.w[1], b.w[0], b.w[1]})};
+}
+__device__ __forceinline__ Parts<3> parts_of(const Piece<float, 8>& v) { return split<3>(v.w); }
+__device__ __forceinline__ Parts<3> parts_of(const Piece<float, 4>& a, const Piece<float, 4>& b) {
+  const float v[8] = {a.w[0], a.w[1], a.w[2], a.w[3], b.w[0], b.w[1], b.w[2], b.w[3]};
+  return split<3>(v);
+}
+template <int PARTS>
+__device__ __forceinline__ Parts<PARTS> first_parts(const Parts<3>& a) {
+  Parts<PARTS> r;
+#pragma unroll
+  for (int i = 0; i < PARTS; ++i) r.p[i] = a.p[i];
+  return r;
+}
 
 // bytes of LDS, by the features of a key (padded to 32, 64 or 128) and the kind of elements
 inline int padded_key(int Dk) { return Dk <= 32 ? 32 : Dk <= 64 ? 64 : 128; }

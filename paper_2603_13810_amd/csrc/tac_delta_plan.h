@@ -34,9 +34,9 @@ inline int64_t delta_chunks(int64_t T) { return (T + TAC_DELTA_CHUNK - 1) / TAC_
 // Columns of a state that a workgroup takes: 32, or 16 where those would leave compute units without work.
 inline bool delta_narrow(int64_t B, int64_t heads, int64_t Dv) { return Dv <= 16 || B * heads * ((Dv + 31) / 32) < 2 * kFittedUnits; }
 
-// A launch has a workgroup of 256 threads for every chunk and head, or for every 16 columns of a head: fewer than 2^32 threads.
+// A launch has a workgroup of up to 512 threads for every chunk and head, or for every 16 columns of a head: fewer than 2^32 threads.
 inline bool delta_fits(int64_t T, int64_t B, int64_t heads, int64_t Dv) {
-  const int64_t most = (1ll << 24) - 1;
+  const int64_t most = (1ll << 23) - 1;
   if (B * heads > most) return false;
   return delta_chunks(T) <= most / (B * heads) && (Dv + 15) / 16 <= most / (B * heads);
 }

@@ -26,10 +26,27 @@ __device__ __forceinline__ void scan_pairs(float& high, float& low, int lane) {
   }
 }
 
+// A matrix in LDS, or its transpose, to planes; operands that hold nothing are left out.
+template <int PARTS, bool BACK>
+__device__ __forceinline__ void store_planes(bf16* to, const float (&from)[kChunk][kPitch]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int operand = threadIdx.x / 64 + 4 * i, lane = threadIdx.x % 64, tile = operand / 2, step = operand % 2;
+    if (BACK ? step < tile / 2 : step > tile / 2) continue;
+    const int row = 16 * tile + lane % 16, col = 32 * step + 8 * (lane / 16);
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = BACK ? from[col + e][row] : from[row][col + e];
+    const Parts<PARTS> a = split<PARTS>(v);
+#pragma unroll
+    for (int part = 0; part < PARTS; ++part) *reinterpret_cast<bf16x8_t*>(to + part * ChunkRoom::plane + ChunkRoom::operand(tile, step, lane)) = a.p[part];
+  }
+}
+
 template <typename T, int DK, bool BACK>
 __global__ __launch_bounds__(256) void prepare_kernel(const DeltaParams p) {
   constexpr int IN = Kind<T>::in, OUT = BACK ? 3 : Kind<T>::out, KS = DK / 32;
-  __shared__ float A[kChunk][kPitch], P[kChunk][kPitch], inverse[kChunk][kPitch];
+  __shared__ __align__(16) float A[kChunk][kPitch], P[kChunk][kPitch];      // P's place takes the inverse
   __shared__ float diagonal[4][16][20];
   __shared__ float high[kChunk], low[kChunk], beta[kChunk];
   const int h = blockIdx.x % p.v_heads, b = blockIdx.x / p.v_heads % p.B;
@@ -66,6 +83,7 @@ __global__ __launch_bounds__(256) void prepare_kernel(const DeltaParams p) {
     own_q[s] = e.parts();
   }
   __syncthreads();
+  const ChunkRoom room(p.chunk_room, blockIdx.x, OUT);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     f32x4_t kk = {0.0f, 0.0f, 0.0f, 0.0f}, qk = kk;
@@ -84,11 +102,12 @@ __global__ __launch_bounds__(256) void prepare_kernel(const DeltaParams p) {
     for (int r = 0; r < 4; ++r) {
       const int t = 16 * wave + 4 * quad + r, c = 16 * j + low16;
       const float decay = fast_exp((high[t] - high[c]) + (low[t] - low[c]));
-      A[t][c] = c < t ? beta[t] * decay * kk[r] : 0.0f;
-      P[t][c] = c <= t ? decay * qk[r] : 0.0f;
+      if (j <= wave) A[t][c] = c < t ? beta[t] * decay * kk[r] : 0.0f;
+      if (j / 2 <= wave / 2) P[t][c] = c <= t ? decay * qk[r] : 0.0f;
     }
   }
   __syncthreads();
+  store_planes<OUT, BACK>(room.products, P);
   // a diagonal block's inverse: column low16 of x, row by row
   float x[16];
 #pragma unroll
@@ -126,34 +145,19 @@ __global__ __launch_bounds__(256) void prepare_kernel(const DeltaParams p) {
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i)
+    if (wave / 2 <= i / 2) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) inverse[16 * i + 4 * quad + r][16 * wave + low16] = block[i][r];
-  __syncthreads();
-  const ChunkRoom room(p.chunk_room, blockIdx.x, OUT);
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int piece = threadIdx.x + 256 * i;
-    const int row = BACK ? piece % 64 : piece / 8, col = BACK ? 8 * (piece / 64) : 8 * (piece % 8);
-    float v[8], w[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      v[e] = BACK ? inverse[col + e][row] : inverse[row][col + e];
-      w[e] = BACK ? P[col + e][row] : P[row][col + e];
+      for (int r = 0; r < 4; ++r) P[16 * i + 4 * quad + r][16 * wave + low16] = block[i][r];
     }
-    const Parts<3> a = split<3>(v);
-    const Parts<OUT> c = split<OUT>(w);
-#pragma unroll
-    for (int part = 0; part < 3; ++part) *reinterpret_cast<bf16x8_t*>(const_cast<bf16*>(room.inverse) + part * ChunkRoom::plane + row * kChunk + col) = a.p[part];
-#pragma unroll
-    for (int part = 0; part < OUT; ++part) *reinterpret_cast<bf16x8_t*>(const_cast<bf16*>(room.products) + part * ChunkRoom::plane + row * kChunk + col) = c.p[part];
-  }
+  __syncthreads();
+  store_planes<3, BACK>(room.inverse, P);
   if (threadIdx.x < kChunk) {
     const int t = threadIdx.x;
-    const_cast<float*>(room.start)[t] = fast_exp(high[t] + low[t]);
-    const_cast<float*>(room.rest)[t] = fast_exp((high[kChunk - 1] - high[t]) + (low[kChunk - 1] - low[t]));
-    const_cast<float*>(room.beta)[t] = beta[t];
-    const_cast<float*>(room.high)[t] = high[t];
-    const_cast<float*>(room.low)[t] = low[t];
+    room.start[t] = fast_exp(high[t] + low[t]);
+    room.rest[t] = fast_exp((high[kChunk - 1] - high[t]) + (low[kChunk - 1] - low[t]));
+    room.beta[t] = beta[t];
+    room.high[t] = high[t];
+    room.low[t] = low[t];
   }
 }
 
