@@ -14,7 +14,6 @@ namespace {
 
 // LDS of scan_kernel.  float32 [4][columns][kSums]: the waves' shares of K S; then in bfloat16 numbers S [OUT][columns][DK + 8] for the outputs, right-hand sides
 // [3][columns][kSteps], U faded [3], U [OUT], K transposed [IN][DK][kSteps]; and K as it stands, [64][DK + 8] elements.
-constexpr int kSums = kChunk + 4;
 template <typename T, int DK, int NT>
 struct ScanRoom {
   static constexpr int columns = 16 * NT, key = DK + 8;
@@ -24,52 +23,12 @@ struct ScanRoom {
   static constexpr int bytes = 2 * rows + kChunk * key * (int)sizeof(T);
 };
 
-// What a workgroup of scan_kernel works on, and where this lane stands: wave w of either four has the chunk's steps from 16 w on as rows.
-template <typename T, int NT>
-struct ScanPlace {
-  int wave, lane, low16, quad, row, rows;      // row: of operands; rows: the first of four of results
-  int first, chunks, last;                     // last: steps of the last chunk
-  int col[NT];
-  int64_t head, state;
-  const T *q, *k, *v;
-  T* out;
-  __device__ ScanPlace(const DeltaParams& p, int tiles) {
-    const HeadTile place(blockIdx.x, p.B * p.v_heads, tiles);
-    const int tile = place.tile, h = place.head % p.v_heads, b = place.head / p.v_heads, hk = h / (p.v_heads / p.k_heads);
-    wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64 % 4);
-    lane = threadIdx.x % 64;
-    low16 = lane & 15;
-    quad = lane >> 4;
-    row = 16 * wave + low16;
-    rows = 16 * wave + 4 * quad;
-    first = tile * 16 * NT;
-#pragma unroll
-    for (int t = 0; t < NT; ++t) col[t] = first + 16 * t + low16;
-    const int64_t length = p.lengths ? min((int64_t)max(p.lengths[b], 0), p.T) : p.T;
-    chunks = (int)((length + kChunk - 1) / kChunk);
-    last = (int)(length - (int64_t)(chunks - 1) * kChunk);
-    head = (int64_t)b * p.v_heads + h;
-    state = (int64_t)p.Dk * p.Dv;
-    q = (const T*)p.q + (int64_t)b * p.q_at.b + (int64_t)hk * p.q_at.head;
-    k = (const T*)p.k + (int64_t)b * p.k_at.b + (int64_t)hk * p.k_at.head;
-    v = (const T*)p.v + (int64_t)b * p.v_at.b + (int64_t)h * p.v_at.head;
-    out = (T*)p.out + (int64_t)b * p.out_at.b + (int64_t)h * p.out_at.head;
-  }
-  __device__ __forceinline__ ChunkRoom room(const DeltaParams& p, int c) const { return ChunkRoom(p.chunk_room, (int64_t)c * p.B * p.v_heads + head, Kind<T>::out); }
-  __device__ __forceinline__ int steps(int c) const { return c + 1 < chunks ? kChunk : last; }
-  // step `i` of chunk c, of a tensor whose steps are `stride` apart.  What is behind the last step is read from there: it stands beside b = 0, or is not stored.
-  template <typename E>
-  __device__ __forceinline__ E* step(E* base, int64_t stride, int c, int i) const {
-    base += (int64_t)c * kChunk * stride;
-    return base + (steps(c) == kChunk ? (int64_t)i * stride : (int64_t)min(i, last - 1) * stride);
-  }
-  // a row of the inverse or of the products; nothing stands above the diagonal
-  template <int PARTS>
-  __device__ __forceinline__ void load_matrix(Parts<PARTS> (&m)[2], const bf16* at) const {
-    m[0] = from_planes<PARTS>(at + ChunkRoom::operand(wave, 0, lane), ChunkRoom::plane);
-    m[1] = from_planes<PARTS>(at + ChunkRoom::operand(wave, wave >= 2 ? 1 : 0, lane), ChunkRoom::plane);
-  }
-};
+// a row of the inverse or of the products; nothing stands above the diagonal
+template <int PARTS, typename T, int NT>
+__device__ __forceinline__ void load_rows_of(Parts<PARTS> (&m)[2], const bf16* from, const ScanPlace<T, NT>& at) {
+  m[0] = from_planes<PARTS>(from + ChunkRoom::operand(at.wave, 0, at.lane), ChunkRoom::plane);
+  m[1] = from_planes<PARTS>(from + ChunkRoom::operand(at.wave, at.wave >= 2 ? 1 : 0, at.lane), ChunkRoom::plane);
+}
 
 // Loads of the next chunk are asked for as soon as this one's have been used, a chunk before they are waited for; memory operations come in the same number whatever
 // the sizes (behind a branch the compiler waits for all of them), so what is not to be stored goes to a place of the workspace that nobody reads.
@@ -115,7 +74,7 @@ __device__ __forceinline__ void scan_states(const DeltaParams& p, const ScanPlac
   };
   const auto load_matrix = [&](int c) {
     const ChunkRoom room = at.room(p, c);
-    at.load_matrix(inverse, room.inverse);
+    load_rows_of(inverse, room.inverse, at);
     rest = *reinterpret_cast<const f32x4_t*>(room.rest + rows);
   };
   const auto load_whole = [&](int c) { whole = at.room(p, c).start[kChunk - 1]; };
@@ -129,7 +88,7 @@ __device__ __forceinline__ void scan_states(const DeltaParams& p, const ScanPlac
   for (int c = 0; c < at.chunks; ++c) {
     const int64_t from = (int64_t)c * kChunk;
     const int next = c + 1 < at.chunks ? c + 1 : c;
-    float* const nowhere = at.room(p, c).high;            // read backwards only, from a workspace of its own
+    float* const nowhere = at.room(p, c).nowhere;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       float own[8];
@@ -274,7 +233,7 @@ __device__ __forceinline__ void scan_outputs(const DeltaParams& p, const ScanPla
     in_this_order();
     load_keys(at.chunks > 1 ? 1 : 0);                     // in the loop's order: waits count what was asked for behind
     in_this_order();
-    at.load_matrix(products, at.room(p, 0).products);
+    load_rows_of(products, at.room(p, 0).products, at);
     load_queries(0);
   }
   __syncthreads();                                        // the first chunk's K
@@ -311,7 +270,7 @@ __device__ __forceinline__ void scan_outputs(const DeltaParams& p, const ScanPla
     computed(o);
     in_this_order();
     T* to[NT][4];
-    T* const nowhere = (T*)at.room(p, c).low;
+    T* const nowhere = (T*)at.room(p, c).nowhere;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       T* const line = at.out + (from + rows + r) * p.out_at.t;
@@ -331,7 +290,7 @@ __device__ __forceinline__ void scan_outputs(const DeltaParams& p, const ScanPla
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) store_device(to[t][r], (T)o[t][r]);
-    at.load_matrix(products, at.room(p, next).products);
+    load_rows_of(products, at.room(p, next).products, at);
     load_queries(next);
   }
   // behind the last chunk's steps
@@ -344,7 +303,7 @@ __device__ __forceinline__ void scan_outputs(const DeltaParams& p, const ScanPla
 template <typename T, int DK, int NT, bool WHOLE, bool KEEP>
 __global__ __launch_bounds__(512) void scan_kernel(const DeltaParams p, int tiles) {
   extern __shared__ __align__(16) uint8_t lds[];
-  const ScanPlace<T, NT> at(p, tiles);
+  const ScanPlace<T, NT> at(p, tiles, p.v, p.v_at, p.out, p.out_at);
   // both meet at the same barriers: one, then three a chunk
   if (__builtin_amdgcn_readfirstlane(threadIdx.x / 256) == 0) scan_states<T, DK, NT, WHOLE, KEEP>(p, at, lds);
   else scan_outputs<T, DK, NT, WHOLE>(p, at, lds);

@@ -15,178 +15,182 @@ namespace tac {
 
 namespace {
 
-// LDS of back_scan_kernel in bfloat16 numbers: dS [3][columns][DK + 8], dO [IN][columns][kSteps], e^G dO [3], X [3], b e^G R [3], K and Q transposed [IN][DK][kSteps]
+// LDS of back_scan_kernel.  float32 [5][columns][kSums]: the waves' shares of K dS, and P^T dO; [columns][DK + 4]: Q^T (e^G dO); then in bfloat16 numbers X
+// [3][columns][kSteps], b e^G R [3], dO [IN], e^G dO [3], K transposed [IN][DK][kSteps]; and K as it stands, [64][DK + 8] elements.
 template <typename T, int DK, int NT>
 struct BackRoom {
-  static constexpr int columns = 16 * NT, key = DK + 8;
-  static constexpr int s_plane = columns * key, u_plane = columns * kSteps, k_plane = DK * kSteps;
-  static constexpr int s = 0, grad = s + 3 * s_plane, fading = grad + Kind<T>::in * u_plane, x = fading + 3 * u_plane, r = x + 3 * u_plane, k = r + 3 * u_plane;
-  static constexpr int q = k + Kind<T>::in * k_plane, size = q + Kind<T>::in * k_plane;
+  static constexpr int columns = 16 * NT, key = DK + 8, fed_pitch = DK + 4;
+  static constexpr int u_plane = columns * kSteps, k_plane = DK * kSteps;
+  static constexpr int fed = 5 * columns * kSums;                            // float32 numbers before it
+  static constexpr int x = 2 * (fed + columns * fed_pitch), r = x + 3 * u_plane, grad = r + 3 * u_plane, fading = grad + Kind<T>::in * u_plane;
+  static constexpr int k = fading + 3 * u_plane, rows = k + Kind<T>::in * k_plane;
+  static constexpr int bytes = 2 * rows + kChunk * key * (int)sizeof(T);
 };
 
-template <typename T, int DK, int NT>
-__global__ __launch_bounds__(256) void back_scan_kernel(const DeltaParams p, int tiles) {
+// The chain: the gradients of the states from chunk to chunk, last to first, as scan_states has the states.
+template <typename T, int DK, int NT, bool WHOLE>
+__device__ __forceinline__ void back_states(const DeltaParams& p, const ScanPlace<T, NT>& at, uint8_t* lds) {
   using Room = BackRoom<T, DK, NT>;
-  constexpr int IN = Kind<T>::in, KS = DK / 32, MT = DK / 16, OWN = MT > 4 ? MT / 4 : 1;
-  extern __shared__ __align__(16) uint8_t lds[];
+  constexpr int IN = Kind<T>::in, MT = DK / 16, OWN = MT > 4 ? 2 : 1;
+  float* const sums = (float*)lds;
   bf16* const L = (bf16*)lds;
-  const HeadTile place(blockIdx.x, p.B * p.v_heads, tiles);
-  const int tile = place.tile, h = place.head % p.v_heads, b = place.head / p.v_heads;
-  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, low16 = lane & 15, quad = lane >> 4;
-  const int hk = h / (p.v_heads / p.k_heads), first = tile * Room::columns;
-  const int64_t length = p.lengths ? min((int64_t)max(p.lengths[b], 0), p.T) : p.T;
-  const T* const q = (const T*)p.q + (int64_t)b * p.q_at.b + (int64_t)hk * p.q_at.head;
-  const T* const k = (const T*)p.k + (int64_t)b * p.k_at.b + (int64_t)hk * p.k_at.head;
-  const T* const go = (const T*)p.grad_out + (int64_t)b * p.out_at.b + (int64_t)h * p.out_at.head;
-  T* const gv = (T*)p.grad_v + (int64_t)b * p.grad_v_at.b + (int64_t)h * p.grad_v_at.head;
-  const int64_t head = (int64_t)b * p.v_heads + h, state = (int64_t)p.Dk * p.Dv;
-  const Identity id(lane);
-  const bool owner = MT >= 4 || wave < MT;
-  int col[NT];
+  const int low16 = at.low16, quad = at.quad, rows = at.rows;
+  const bool owner = MT >= 4 || at.wave < MT;
+  int state_row[OWN];
 #pragma unroll
-  for (int t = 0; t < NT; ++t) col[t] = first + 16 * t + low16;
-
-  f32x4_t S[OWN][NT];                 // dS
+  for (int m = 0; m < OWN; ++m) state_row[m] = 16 * (at.wave * OWN + m) + 4 * quad;
+  f32x4_t S[OWN][NT];                                     // dS
 #pragma unroll
   for (int m = 0; m < OWN; ++m)
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int row = 16 * (wave * OWN + m) + 4 * quad + r;
-        S[m][t][r] = p.grad_h_last && row < p.Dk && col[t] < p.Dv ? p.grad_h_last[head * state + (int64_t)row * p.Dv + col[t]] : 0.0f;
-      }
+      for (int r = 0; r < 4; ++r)
+        S[m][t][r] = p.grad_h_last && state_row[m] + r < p.Dk && at.col[t] < p.Dv ? p.grad_h_last[at.head * at.state + (int64_t)(state_row[m] + r) * p.Dv + at.col[t]] : 0.0f;
 
-  const int chunks = (int)((length + kChunk - 1) / kChunk);
-  for (int c = chunks - 1; c >= 0; --c) {
+  Parts<3> inverse[2];                                    // transposed: rows begin at the diagonal
+  f32x4_t start, rest, beta;
+  float whole;
+  const auto load_rest = [&](int c) { rest = *reinterpret_cast<const f32x4_t*>(at.room(p, c, 3).rest + rows); };
+  const auto load_matrix = [&](int c) {
+    const ChunkRoom room = at.room(p, c, 3);
+    inverse[0] = from_planes<3>(room.inverse + ChunkRoom::operand(at.wave, at.wave >= 2 ? 1 : 0, at.lane), ChunkRoom::plane);
+    inverse[1] = from_planes<3>(room.inverse + ChunkRoom::operand(at.wave, 1, at.lane), ChunkRoom::plane);
+    start = *reinterpret_cast<const f32x4_t*>(room.start + rows);
+    beta = *reinterpret_cast<const f32x4_t*>(room.beta + rows);
+  };
+  const auto load_whole = [&](int c) { whole = at.room(p, c, 3).start[kChunk - 1]; };
+  loads_arrive();
+  if (at.chunks) {
+    load_rest(at.chunks - 1);
+    load_matrix(at.chunks - 1);
+    load_whole(at.chunks - 1);
+  }
+  __syncthreads();                                        // the last chunk's K, dO
+  for (int c = at.chunks - 1; c >= 0; --c) {
     const int64_t from = (int64_t)c * kChunk;
-    const int n = (int)min((int64_t)kChunk, length - from);
-    const int64_t index_of_chunk = (int64_t)c * p.B * p.v_heads + head;
-    const ChunkRoom room(p.chunk_room, index_of_chunk, 3);
-    Parts<IN> key[KS], query[KS];
-    {
-      const int row = 16 * wave + low16;
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const int at = 32 * s + 8 * quad, left = row < n ? p.Dk - at : 0;
-        Eight<T> e;
-        e.load(k + (from + row) * p.k_at.t + at, left);
-        key[s] = e.parts();
-        e.load(q + (from + row) * p.q_at.t + at, left);
-        query[s] = e.parts();
-      }
-    }
-    const f32x4_t start = *reinterpret_cast<const f32x4_t*>(room.start + 16 * wave + 4 * quad);
-    const f32x4_t rest = *reinterpret_cast<const f32x4_t*>(room.rest + 16 * wave + 4 * quad);
-    const f32x4_t beta = *reinterpret_cast<const f32x4_t*>(room.beta + 16 * wave + 4 * quad);
-    const float whole = room.start[kChunk - 1];
+    const int n = at.steps(c), next = c ? c - 1 : 0;
+    float* const nowhere = at.room(p, c, 3).nowhere;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      f32x4_t grad, fading;
+      float own[8];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int row = 16 * wave + 4 * quad + r;
-        grad[r] = row < n && col[t] < p.Dv ? (float)go[(from + row) * p.out_at.t + col[t]] : 0.0f;
-        fading[r] = start[r] * grad[r];
+      for (int e = 0; e < 8; ++e) own[e] = e / 4 < OWN ? S[e / 4 < OWN ? e / 4 : 0][t][e % 4] : 0.0f;
+      const Parts<3> op = split<3>(own);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        f32x4_t share = {0.0f, 0.0f, 0.0f, 0.0f};
+        const T* const key = (const T*)(L + Room::rows) + (16 * i + low16) * Room::key;
+        const Piece<T, 4> a = load_aligned<T, 4>(key + (owner ? state_row[0] : 0));
+        if constexpr (OWN == 2) multiply<3>(share, parts_of(a, load_aligned<T, 4>(key + state_row[1])), op);
+        else multiply<3>(share, parts_of(a, a), op);          // the other half of S's operand is zero
+        *reinterpret_cast<f32x4_t*>(sums + (at.wave * Room::columns + 16 * t + low16) * kSums + 16 * i + 4 * quad) = share;
       }
-      const int at = (16 * t + low16) * kSteps + 16 * wave + 4 * quad;
-      quad_to_planes<IN>(L + Room::grad + at, Room::u_plane, grad);
-      quad_to_planes<3>(L + Room::fading + at, Room::u_plane, fading);
     }
-    if (owner) {
-#pragma unroll
-      for (int m = 0; m < OWN; ++m)
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          const int row = 16 * (wave * OWN + m) + 4 * quad;
-          quad_to_planes<3>(L + Room::s + (16 * t + low16) * Room::key + row, Room::s_plane, S[m][t]);
-          if (col[t] < p.Dv) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (row + r < p.Dk) p.back_states[index_of_chunk * state + (int64_t)(row + r) * p.Dv + col[t]] = S[m][t][r];
-          }
-        }
-    }
-    __syncthreads();
-
-    f32x4_t x[NT];
+    __syncthreads();                                      // shares of K dS, P^T dO
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      x[t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+      f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int s = 0; s < KS; ++s) multiply<3>(x[t], key[s], from_planes<3>(L + Room::s + (16 * t + low16) * Room::key + 32 * s + 8 * quad, Room::s_plane));
+      for (int w = 0; w < 4; ++w) x += *reinterpret_cast<const f32x4_t*>(sums + (w * Room::columns + 16 * t + low16) * kSums + rows);
+      const f32x4_t y = *reinterpret_cast<const f32x4_t*>(sums + (4 * Room::columns + 16 * t + low16) * kSums + rows);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) x[t][r] *= rest[r];
+      for (int r = 0; r < 4; ++r) x[r] = fmaf(rest[r], x[r], y[r]);
+      quad_to_planes<3>(L + Room::x + (16 * t + low16) * kSteps + rows, Room::u_plane, x);
     }
+    in_this_order();
+    load_rest(next);
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      if (32 * s + 31 < 16 * wave) continue;           // rows of the transposed matrices begin at the diagonal
-      const Parts<3> a = from_planes<3>(room.products + ChunkRoom::operand(wave, s, lane), ChunkRoom::plane);
+    for (int m = 0; m < OWN; ++m)
 #pragma unroll
-      for (int t = 0; t < NT; ++t) multiply<3>(x[t], a, from_planes<IN>(L + Room::grad + (16 * t + low16) * kSteps + 32 * s + 8 * quad, Room::u_plane));
-    }
+      for (int t = 0; t < NT; ++t) {
+        float* to = p.back_states + ((int64_t)c * p.B * p.v_heads + at.head) * at.state + (int64_t)state_row[m] * p.Dv + at.col[t];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) quad_to_planes<3>(L + Room::x + (16 * t + low16) * kSteps + 16 * wave + 4 * quad, Room::u_plane, x[t]);
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      transpose_to<IN>(L + Room::k, Room::k_plane, key[s], 16 * wave, 32 * s, id, lane, p.Dk);
-      transpose_to<IN>(L + Room::q, Room::k_plane, query[s], 16 * wave, 32 * s, id, lane, p.Dk);
-    }
-    __syncthreads();
-
-    f32x4_t R[NT];
+        for (int r = 0; r < 4; ++r) store_device(state_row[m] + r < p.Dk && at.col[t] < p.Dv ? to + r * p.Dv : nowhere, S[m][t][r]);
+      }
+    __syncthreads();                                      // X
+    f32x4_t R[NT], faded[NT], scaled[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) R[t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      if (32 * s + 31 < 16 * wave) continue;
-      const Parts<3> a = from_planes<3>(room.inverse + ChunkRoom::operand(wave, s, lane), ChunkRoom::plane);
+      if (!s && at.wave >= 2) continue;
 #pragma unroll
-      for (int t = 0; t < NT; ++t) multiply<3>(R[t], a, from_planes<3>(L + Room::x + (16 * t + low16) * kSteps + 32 * s + 8 * quad, Room::u_plane));
+      for (int t = 0; t < NT; ++t) multiply<3>(R[t], inverse[s], from_planes<3>(L + Room::x + (16 * t + low16) * kSteps + 32 * s + 8 * quad, Room::u_plane));
     }
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      f32x4_t faded;
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) faded[r] = -(beta[r] * start[r]) * R[t][r];
-      quad_to_planes<3>(L + Room::r + (16 * t + low16) * kSteps + 16 * wave + 4 * quad, Room::u_plane, faded);
-      if (col[t] < p.Dv) {
+      for (int r = 0; r < 4; ++r) {
+        scaled[t][r] = beta[r] * R[t][r];
+        faded[t][r] = -start[r] * scaled[t][r];
+      }
+    computed(scaled);
+    computed(faded);
+    in_this_order();
+    load_matrix(next);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int row = 16 * wave + 4 * quad + r;
-          if (from + row >= p.T) continue;
-          p.r[((from + row) * p.B * p.v_heads + head) * p.Dv + col[t]] = R[t][r];
-          gv[(from + row) * p.grad_v_at.t + col[t]] = (T)(row < n ? beta[r] * R[t][r] : 0.0f);
+    for (int t = 0; t < NT; ++t) quad_to_planes<3>(L + Room::r + (16 * t + low16) * kSteps + rows, Room::u_plane, faded[t]);
+    {
+      float* r_to[NT][4];
+      T* v_to[NT][4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float* const line = p.r + ((from + rows + r) * p.B * p.v_heads + at.head) * p.Dv;
+        T* const value = at.out + (from + rows + r) * p.grad_v_at.t;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          r_to[t][r] = line + at.col[t];
+          v_to[t][r] = value + at.col[t];
         }
       }
-    }
-    __syncthreads();
-
-    if (owner) {
-#pragma unroll
-      for (int m = 0; m < OWN; ++m) {
-        const int row = (16 * (wave * OWN + m) + low16) * kSteps;
+      if (n < kChunk || at.first + Room::columns > p.Dv) {
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) S[m][t][r] *= whole;
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const Parts<IN> a = from_planes<IN>(L + Room::q + row + 32 * s + 8 * quad, Room::k_plane), d = from_planes<IN>(L + Room::k + row + 32 * s + 8 * quad, Room::k_plane);
-#pragma unroll
-          for (int t = 0; t < NT; ++t) {
-            const int at = (16 * t + low16) * kSteps + 32 * s + 8 * quad;
-            multiply<3>(S[m][t], a, from_planes<3>(L + Room::fading + at, Room::u_plane));
-            multiply<3>(S[m][t], d, from_planes<3>(L + Room::r + at, Room::u_plane));
+          for (int r = 0; r < 4; ++r) {
+            if (rows + r >= n) scaled[t][r] = 0.0f;
+            if (from + rows + r >= p.T || at.col[t] >= p.Dv) {
+              r_to[t][r] = nowhere;
+              v_to[t][r] = (T*)nowhere;
+            }
           }
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          store_device(r_to[t][r], R[t][r]);
+          store_device(v_to[t][r], (T)scaled[t][r]);
+        }
+    }
+    __syncthreads();                                      // b e^G R, K transposed, Q^T (e^G dO), the next chunk's K and dO
+#pragma unroll
+    for (int m = 0; m < OWN; ++m) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const f32x4_t fed = *reinterpret_cast<const f32x4_t*>(sums + Room::fed + (16 * t + low16) * Room::fed_pitch + (owner ? state_row[m] : 0));
+#pragma unroll
+        for (int r = 0; r < 4; ++r) S[m][t][r] = owner ? fmaf(whole, S[m][t][r], fed[r]) : 0.0f;
+      }
+      computed(S[m]);
+    }
+    in_this_order();
+    load_whole(next);
+    if (owner) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        Parts<3> op[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) op[t] = from_planes<3>(L + Room::r + (16 * t + low16) * kSteps + 32 * s + 8 * quad, Room::u_plane);
+#pragma unroll
+        for (int m = 0; m < OWN; ++m) {
+          const Parts<IN> a = from_planes<IN>(L + Room::k + (16 * (at.wave * OWN + m) + low16) * kSteps + 32 * s + 8 * quad, Room::k_plane);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) multiply<3>(S[m][t], a, op[t]);
         }
       }
     }
-    __syncthreads();                                   // the next chunk's gradients take the place of these
-  }
-  for (int64_t t = (int64_t)chunks * kChunk + threadIdx.x / Room::columns; t < p.T; t += 256 / Room::columns) {
-    const int at = first + threadIdx.x % Room::columns;
-    if (at < p.Dv) gv[t * p.grad_v_at.t + at] = (T)0.0f;
   }
   if (!p.grad_h0 || !owner) return;
 #pragma unroll
@@ -194,10 +198,176 @@ __global__ __launch_bounds__(256) void back_scan_kernel(const DeltaParams p, int
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (state_row[m] + r < p.Dk && at.col[t] < p.Dv) p.grad_h0[at.head * at.state + (int64_t)(state_row[m] + r) * p.Dv + at.col[t]] = S[m][t][r];
+}
+
+// What the chain takes that does not wait for it: of this chunk Q^T (e^G dO) and K transposed, of the one in front of it K, dO and P^T dO.
+template <typename T, int DK, int NT, bool WHOLE>
+__device__ __forceinline__ void back_inputs(const DeltaParams& p, const ScanPlace<T, NT>& at, uint8_t* lds) {
+  using Room = BackRoom<T, DK, NT>;
+  constexpr int IN = Kind<T>::in, KS = DK / 32, MT = DK / 16, OWN = MT > 4 ? 2 : 1;
+  float* const sums = (float*)lds;
+  bf16* const L = (bf16*)lds;
+  const int low16 = at.low16, quad = at.quad, rows = at.rows;
+  const Identity id(at.lane);
+  const T* const key_row = (const T*)(L + Room::rows) + at.row * Room::key + 8 * quad;
+  const int own_col = 32 * (at.wave * OWN / 2);           // the 32 features that hold the wave's rows of dS
+  const bool owner = MT >= 4 || at.wave < MT;
+  Piece<T, 8> key[KS], query[4];                          // queries: all steps, the wave's 32 features
+  Parts<3> products[2];
+  T grad[NT][4];
+  f32x4_t start;
+  constexpr int pieces = DK / 8;
+  const int key_at = 16 * at.wave + at.lane / pieces, key_col = 8 * (at.lane % pieces);
+  const auto load_keys = [&](int c) {
+#pragma unroll
+    for (int s = 0; s < KS; ++s) load_piece<WHOLE>(key[s], at.step(at.k, p.k_at.t, c, key_at + s * (64 / pieces)), key_col, p.Dk);
+  };
+  const auto keep_keys = [&] {
+#pragma unroll
+    for (int s = 0; s < KS; ++s) store_aligned((T*)(L + Room::rows) + (key_at + s * (64 / pieces)) * Room::key + key_col, key[s]);
+  };
+  const auto load_queries = [&](int c) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) load_piece<WHOLE>(query[i], at.step(at.q, p.q_at.t, c, 16 * i + low16), own_col + 8 * quad, p.Dk);
+  };
+  const auto load_grads = [&](int c) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const T* from = at.step(at.v, p.out_at.t, c, rows + r);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) grad[t][r] = from[min(at.col[t], p.Dv - 1)];
+    }
+    start = *reinterpret_cast<const f32x4_t*>(at.room(p, c, 3).start + rows);
+  };
+  const auto keep_grads = [&](int c) {
+    const int n = at.steps(c);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      f32x4_t g, fading;
+#pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int row = 16 * (wave * OWN + m) + 4 * quad + r;
-        if (row < p.Dk && col[t] < p.Dv) p.grad_h0[head * state + (int64_t)row * p.Dv + col[t]] = S[m][t][r];
+        g[r] = rows + r < n ? (float)grad[t][r] : 0.0f;
+        fading[r] = start[r] * g[r];
       }
+      const int place = (16 * t + low16) * kSteps + rows;
+      quad_to_planes<IN>(L + Room::grad + place, Room::u_plane, g);
+      quad_to_planes<3>(L + Room::fading + place, Room::u_plane, fading);
+    }
+  };
+  const auto load_matrix = [&](int c) {
+    const ChunkRoom room = at.room(p, c, 3);
+    products[0] = from_planes<3>(room.products + ChunkRoom::operand(at.wave, at.wave >= 2 ? 1 : 0, at.lane), ChunkRoom::plane);
+    products[1] = from_planes<3>(room.products + ChunkRoom::operand(at.wave, 1, at.lane), ChunkRoom::plane);
+  };
+  const auto from_outputs = [&] {                         // P^T dO
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        if (!s && at.wave >= 2) continue;
+        multiply<3>(x, products[s], from_planes<IN>(L + Room::grad + (16 * t + low16) * kSteps + 32 * s + 8 * quad, Room::u_plane));
+      }
+      *reinterpret_cast<f32x4_t*>(sums + (4 * Room::columns + 16 * t + low16) * kSums + rows) = x;
+    }
+  };
+  const int top = at.chunks - 1;
+  if (at.chunks) {
+    load_keys(top);
+    load_grads(top);
+    keep_keys();
+    keep_grads(top);
+    in_this_order();
+    load_queries(top);
+    load_keys(top ? top - 1 : 0);
+    load_grads(top ? top - 1 : 0);
+    load_matrix(top);
+  }
+  __syncthreads();                                        // the last chunk's K, dO
+  if (at.chunks) {
+    from_outputs();
+    in_this_order();
+    load_matrix(top ? top - 1 : 0);
+  }
+  for (int c = top; c >= 0; --c) {
+    const int next = c ? c - 1 : 0, after = c > 1 ? c - 2 : 0;
+    __syncthreads();                                      // shares of K dS, P^T dO
+    // Q^T (e^G dO) for the wave's rows.  A transpose by the identity leaves a column's steps in fours as the summed index wants them; e^G dO is read to match
+    f32x4_t fed[OWN][NT];
+#pragma unroll
+    for (int m = 0; m < OWN; ++m)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) fed[m][t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      Parts<IN> turned[OWN];
+      const Parts<IN> a = parts_of(query[2 * s]), b = parts_of(query[2 * s + 1]);
+#pragma unroll
+      for (int m = 0; m < OWN; ++m) {
+        const Parts<1>& which = OWN == 2 ? (m ? id.odd : id.even) : at.wave % 2 ? id.odd : id.even;
+#pragma unroll
+        for (int i = 0; i < IN; ++i) {
+          const f32x4_t zero = {0.0f, 0.0f, 0.0f, 0.0f};
+          const f32x4_t x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], which.p[0], zero, 0, 0, 0);
+          const f32x4_t y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.p[i], which.p[0], zero, 0, 0, 0);
+          turned[m].p[i] = __builtin_bit_cast(bf16x8_t, u32x4_t{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])});
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        Parts<3> op;
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+          const bf16* const f = L + Room::fading + i * Room::u_plane + (16 * t + low16) * kSteps + 32 * s + 4 * quad;
+          const u32x2_t x = *reinterpret_cast<const u32x2_t*>(f), y = *reinterpret_cast<const u32x2_t*>(f + 16);
+          op.p[i] = __builtin_bit_cast(bf16x8_t, u32x4_t{x[0], x[1], y[0], y[1]});
+        }
+#pragma unroll
+        for (int m = 0; m < OWN; ++m) multiply<3>(fed[m][t], turned[m], op);
+      }
+    }
+    if (owner) {
+#pragma unroll
+      for (int m = 0; m < OWN; ++m)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const int first = 16 * (at.wave * OWN + m) + 4 * quad;
+          f32x4_t v = fed[m][t];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v[r] = first + r < p.Dk ? v[r] : 0.0f;
+          *reinterpret_cast<f32x4_t*>(sums + Room::fed + (16 * t + low16) * Room::fed_pitch + first) = v;
+        }
+    }
+    in_this_order();
+    load_queries(next);
+    __syncthreads();                                      // X
+#pragma unroll
+    for (int s = 0; s < KS; ++s) transpose_to<IN>(L + Room::k, Room::k_plane, parts_of(load_aligned<T, 8>(key_row + 32 * s)), 16 * at.wave, 32 * s, id, at.lane, p.Dk);
+    keep_keys();
+    keep_grads(next);
+    in_this_order();
+    load_keys(after);
+    load_grads(after);
+    __syncthreads();                                      // b e^G R, K transposed, Q^T (e^G dO), the next chunk's K and dO
+    from_outputs();
+    in_this_order();
+    load_matrix(after);
+  }
+  // behind the last chunk's steps
+  for (int64_t t = (int64_t)at.chunks * kChunk + threadIdx.x % 256 / Room::columns; t < p.T; t += 256 / Room::columns) {
+    const int c = at.first + threadIdx.x % Room::columns;
+    if (c < p.Dv) at.out[t * p.grad_v_at.t + c] = (T)0.0f;
+  }
+}
+
+template <typename T, int DK, int NT, bool WHOLE>
+__global__ __launch_bounds__(512) void back_scan_kernel(const DeltaParams p, int tiles) {
+  extern __shared__ __align__(16) uint8_t lds[];
+  const ScanPlace<T, NT> at(p, tiles, p.grad_out, p.out_at, p.grad_v, p.grad_v_at);
+  if (__builtin_amdgcn_readfirstlane(threadIdx.x / 256) == 0) back_states<T, DK, NT, WHOLE>(p, at, lds);
+  else back_inputs<T, DK, NT, WHOLE>(p, at, lds);
 }
 
 // LDS of gradient_kernel in bytes.  While values' features are summed over, 32 at a time: S and dS [OUT][DK][40], U [OUT][64][40]; then K or Q transposed [IN][DK][kSteps],
@@ -485,23 +655,25 @@ hipError_t with_lds(K kernel, int bytes) {
   return bytes > 64 << 10 ? hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) : hipSuccess;
 }
 
-template <typename T, int DK, int NT>
+template <typename T, int DK, int NT, bool WHOLE>
 hipError_t back_scan_shaped(const DeltaParams& p, hipStream_t s) {
-  const int tiles = (p.Dv + 16 * NT - 1) / (16 * NT);
-  constexpr int bytes = BackRoom<T, DK, NT>::size * 2;
-  const hipError_t e = with_lds(back_scan_kernel<T, DK, NT>, bytes);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((back_scan_kernel<T, DK, NT>), dim3((unsigned)((int64_t)p.B * p.v_heads * tiles)), dim3(256), bytes, s, p, tiles);
-  return hipGetLastError();
+  if constexpr (NT > 1 && BackRoom<T, DK, NT>::bytes > 160 << 10) {      // float32 keys in three parts leave LDS for 16 columns
+    return back_scan_shaped<T, DK, 1, WHOLE>(p, s);
+  } else {
+    const int tiles = (p.Dv + 16 * NT - 1) / (16 * NT);
+    constexpr int bytes = BackRoom<T, DK, NT>::bytes;
+    const hipError_t e = with_lds(back_scan_kernel<T, DK, NT, WHOLE>, bytes);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((back_scan_kernel<T, DK, NT, WHOLE>), dim3((unsigned)((int64_t)p.B * p.v_heads * tiles)), dim3(512), bytes, s, p, tiles);
+    return hipGetLastError();
+  }
 }
 
 template <typename T, int DK>
 hipError_t backward_shaped(const DeltaParams& p, hipStream_t s) {
-  // float32 keys of 128 features in three parts leave LDS for 16 columns
-  const bool narrow = delta_narrow(p.B, p.v_heads, p.Dv) || BackRoom<T, DK, 2>::size * 2 > 160 << 10;
-  hipError_t e;
-  if constexpr (BackRoom<T, DK, 2>::size * 2 <= 160 << 10) e = narrow ? back_scan_shaped<T, DK, 1>(p, s) : back_scan_shaped<T, DK, 2>(p, s);
-  else e = back_scan_shaped<T, DK, 1>(p, s);
+  const bool whole = p.Dk % 8 == 0, narrow = delta_narrow(p.B, p.v_heads, p.Dv);
+  hipError_t e = narrow ? (whole ? back_scan_shaped<T, DK, 1, true>(p, s) : back_scan_shaped<T, DK, 1, false>(p, s))
+                        : (whole ? back_scan_shaped<T, DK, 2, true>(p, s) : back_scan_shaped<T, DK, 2, false>(p, s));
   if (e != hipSuccess) return e;
   constexpr int bytes = GradientRoom<T, DK>::size * 2;
   e = with_lds(gradient_kernel<T, DK>, bytes);

@@ -215,9 +215,10 @@ struct ChunkRoom {
   // operand of rows 16 tile.. and columns 32 step..
   static __device__ __forceinline__ int operand(int tile, int step, int lane) { return ((tile * 2 + step) * 64 + lane) * 8; }
   static constexpr int plane = kChunk * kChunk;
-  static constexpr int64_t bytes(int p_parts) { return (int64_t)(3 + p_parts) * plane * 2 + 5 * kChunk * 4; }
+  static constexpr int64_t bytes(int p_parts) { return (int64_t)(3 + p_parts) * plane * 2 + 6 * kChunk * 4; }
   bf16 *inverse, *products;
   float *start, *rest, *beta, *high, *low;      // e^G, e^(G_end - G), b, and G in two numbers
+  float* nowhere;                               // takes what is not to be stored
   __device__ __forceinline__ ChunkRoom(uint8_t* base, int64_t index, int p_parts) {
     inverse = (bf16*)(base + index * bytes(p_parts));
     products = inverse + 3 * plane;
@@ -226,6 +227,7 @@ struct ChunkRoom {
     beta = rest + kChunk;
     high = beta + kChunk;
     low = high + kChunk;
+    nowhere = low + kChunk;
   }
 };
 
@@ -310,6 +312,50 @@ __device__ __forceinline__ Parts<PARTS> first_parts(const Parts<3>& a) {
   for (int i = 0; i < PARTS; ++i) r.p[i] = a.p[i];
   return r;
 }
+
+constexpr int kSums = kChunk + 4;             // pitch of LDS rows of a chunk's steps in float32
+
+// What a workgroup of a walk over the chunks works on, and where this lane stands: of its eight waves, wave w of either four has the chunk's steps from 16 w on as rows.
+template <typename T, int NT>
+struct ScanPlace {
+  int wave, lane, low16, quad, row, rows;      // row: of operands; rows: the first of four of results
+  int first, chunks, last;                     // last: steps of the last chunk
+  int col[NT];
+  int64_t head, state;
+  const T *q, *k, *v;
+  T* out;
+  // v, out: what is read and written in the layout of values
+  __device__ ScanPlace(const DeltaParams& p, int tiles, const void* v_base, const tac_delta_strides_t& v_at, void* out_base, const tac_delta_strides_t& out_at) {
+    const HeadTile place(blockIdx.x, p.B * p.v_heads, tiles);
+    const int tile = place.tile, h = place.head % p.v_heads, b = place.head / p.v_heads, hk = h / (p.v_heads / p.k_heads);
+    wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64 % 4);
+    lane = threadIdx.x % 64;
+    low16 = lane & 15;
+    quad = lane >> 4;
+    row = 16 * wave + low16;
+    rows = 16 * wave + 4 * quad;
+    first = tile * 16 * NT;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) col[t] = first + 16 * t + low16;
+    const int64_t length = p.lengths ? min((int64_t)max(p.lengths[b], 0), p.T) : p.T;
+    chunks = (int)((length + kChunk - 1) / kChunk);
+    last = (int)(length - (int64_t)(chunks - 1) * kChunk);
+    head = (int64_t)b * p.v_heads + h;
+    state = (int64_t)p.Dk * p.Dv;
+    q = (const T*)p.q + (int64_t)b * p.q_at.b + (int64_t)hk * p.q_at.head;
+    k = (const T*)p.k + (int64_t)b * p.k_at.b + (int64_t)hk * p.k_at.head;
+    v = (const T*)v_base + (int64_t)b * v_at.b + (int64_t)h * v_at.head;
+    out = (T*)out_base + (int64_t)b * out_at.b + (int64_t)h * out_at.head;
+  }
+  __device__ __forceinline__ ChunkRoom room(const DeltaParams& p, int c, int p_parts = Kind<T>::out) const { return ChunkRoom(p.chunk_room, (int64_t)c * p.B * p.v_heads + head, p_parts); }
+  __device__ __forceinline__ int steps(int c) const { return c + 1 < chunks ? kChunk : last; }
+  // step `i` of chunk c, of a tensor whose steps are `stride` apart.  What is behind the last step is read from there: it stands beside b = 0, or is not stored.
+  template <typename E>
+  __device__ __forceinline__ E* step(E* base, int64_t stride, int c, int i) const {
+    base += (int64_t)c * kChunk * stride;
+    return base + (steps(c) == kChunk ? (int64_t)i * stride : (int64_t)min(i, last - 1) * stride);
+  }
+};
 
 // bytes of LDS, by the features of a key (padded to 32, 64 or 128) and the kind of elements
 inline int padded_key(int Dk) { return Dk <= 32 ? 32 : Dk <= 64 ? 64 : 128; }
