@@ -370,18 +370,19 @@ __global__ __launch_bounds__(512) void back_scan_kernel(const DeltaParams p, int
   else back_inputs<T, DK, NT, WHOLE>(p, at, lds);
 }
 
-// LDS of gradient_kernel in bytes.  While values' features are summed over, 32 at a time: S and dS [OUT][DK][40], U [OUT][64][40]; then K or Q transposed [IN][DK][kSteps],
-// Z and its transpose, Y or its transpose [OUT][64][kSteps] each.
+// LDS of gradient_kernel in bfloat16 numbers.  While values' features are summed over, 32 at a time: S and dS [OUT][DK][40], U and R [OUT][64][40], dO [IN][64][40]; then K or Q
+// transposed [IN][DK][kSteps], Z and its transpose, Y or its transpose [OUT][64][kSteps] each; at last the gradients, [2][64][DK + 8] elements.
 template <typename T, int DK>
 struct GradientRoom {
-  static constexpr int IN = Kind<T>::in, OUT = Kind<T>::out, pitch = 40;
+  static constexpr int IN = Kind<T>::in, OUT = Kind<T>::out, pitch = 40, out_pitch = DK + 8;
   static constexpr int s_plane = DK * pitch, u_plane = kChunk * pitch, k_plane = DK * kSteps, y_plane = kChunk * kSteps;
-  static constexpr int s = 0, back = s + OUT * s_plane, u = back + OUT * s_plane, first_size = u + OUT * u_plane;
+  static constexpr int s = 0, back = s + OUT * s_plane, u = back + OUT * s_plane, r = u + OUT * u_plane, g = r + OUT * u_plane, first_size = g + IN * u_plane;
   static constexpr int k = 0, z = k + IN * k_plane, z_turned = z + OUT * y_plane, y = z_turned + OUT * y_plane, second_size = y + OUT * y_plane;
-  static constexpr int size = first_size > second_size ? first_size : second_size;
+  static constexpr int third_size = 2 * kChunk * out_pitch * (int)sizeof(T) / 2;
+  static constexpr int most = first_size > second_size ? first_size : second_size, bytes = 2 * (most > third_size ? most : third_size);
 };
 
-// rows 4 quad .. of column `col` of a 16 x 16 result, to planes [rows][kSteps]: as it stands, or transposed (a column's rows are neighbours)
+// rows 4 quad .. of column `col` of a 16 x 16 result, to planes [rows][kSteps] as it stands
 template <int PARTS>
 __device__ __forceinline__ void result_to_planes(bf16* to, int plane, const f32x4_t& v, int row, int col) {
   u32x2_t q[PARTS];
@@ -408,16 +409,22 @@ __device__ __forceinline__ f32x4_t steps_from_planes(const bf16* at, int plane) 
   return v;
 }
 
-template <typename T, int DK>
-__global__ __launch_bounds__(256) void gradient_kernel(const DeltaParams p) {
+__device__ __forceinline__ float value_of(const Piece<bf16, 4>& v, int e) { return bits_float(e % 2 ? v.w[e / 2] & 0xffff0000u : v.w[e / 2] << 16); }
+__device__ __forceinline__ float value_of(const Piece<float, 4>& v, int e) { return v.w[e]; }
+
+// One chunk of a head of queries and keys, the heads of values that share it one after the other.  Eight waves: wave w of either four has the steps from 16 w on as rows and half of a
+// key's features as columns, the first four form Y, the others Z.  All that is summed over values comes through LDS, whole lines at a time and a step ahead.
+// WHOLE: Dk and Dv are multiples of 8.
+template <typename T, int DK, bool WHOLE>
+__global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
   using Room = GradientRoom<T, DK>;
-  constexpr int IN = Kind<T>::in, OUT = Kind<T>::out, KS = DK / 32, NT = DK / 16;
+  constexpr int IN = Kind<T>::in, OUT = Kind<T>::out, NT = DK / 32, KS = NT > 1 ? NT / 2 : 1;      // tiles and pieces of this half of the features
   extern __shared__ __align__(16) uint8_t lds[];
-  __shared__ float high[kChunk], low[kChunk], change[kChunk], both[4];
+  __shared__ float high[kChunk], low[kChunk], change[2][kChunk], both[8];
   bf16* const L = (bf16*)lds;
   const int hk = blockIdx.x % p.k_heads, b = blockIdx.x / p.k_heads % p.B;
   const int64_t chunk = blockIdx.x / p.k_heads / p.B, from = chunk * kChunk;
-  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, low16 = lane & 15, quad = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64 % 4), half = __builtin_amdgcn_readfirstlane(threadIdx.x / 256);
   const int group = p.v_heads / p.k_heads;
   const int n = steps_of(p, b, from), here = (int)min((int64_t)kChunk, p.T - from);
   T* const gq = (T*)p.grad_q + from * p.grad_q_at.t + (int64_t)b * p.grad_q_at.b + (int64_t)hk * p.grad_q_at.head;
@@ -425,94 +432,161 @@ __global__ __launch_bounds__(256) void gradient_kernel(const DeltaParams p) {
   T* const gg = (T*)p.grad_gate + from * p.grad_gate_at.t + (int64_t)b * p.grad_gate_at.b;
   T* const gw = (T*)p.grad_write + from * p.grad_write_at.t + (int64_t)b * p.grad_write_at.b;
   if (n == 0) {
-    for (int i = threadIdx.x; i < here * p.Dk; i += 256) {
+    const int tid = threadIdx.x;
+    for (int i = tid; i < here * p.Dk; i += 512) {
       gq[(int64_t)(i / p.Dk) * p.grad_q_at.t + i % p.Dk] = (T)0.0f;
       gk[(int64_t)(i / p.Dk) * p.grad_k_at.t + i % p.Dk] = (T)0.0f;
     }
-    for (int i = threadIdx.x; i < here * group; i += 256) {
+    for (int i = tid; i < here * group; i += 512) {
       gg[(int64_t)(i / group) * p.grad_gate_at.t + hk * group + i % group] = (T)0.0f;
       gw[(int64_t)(i / group) * p.grad_write_at.t + hk * group + i % group] = (T)0.0f;
     }
     return;
   }
-  const T* const q = (const T*)p.q + from * p.q_at.t + (int64_t)b * p.q_at.b + (int64_t)hk * p.q_at.head;
-  const T* const k = (const T*)p.k + from * p.k_at.t + (int64_t)b * p.k_at.b + (int64_t)hk * p.k_at.head;
-  float* const shared = p.shared + (int64_t)blockIdx.x * 2 * kChunk * DK;       // sums of this head's queries and keys over the values' heads before
-  const int own = 16 * wave + low16;                 // the step whose rows this lane has as an operand
-  const Identity id(lane);
+  // the features of this half: tiles of 16, and pieces of 32 that hold them
+  const int tile0 = half * NT, piece0 = tile0 / 2;
+  Piece<T, 8> key[KS], query[KS];
+  const auto load_rows = [&] {
+    const int lane = fresh(threadIdx.x) % 64, row = 16 * wave + lane % 16, quad = lane / 16;
+    const T* const k = (const T*)p.k + (from + min(row, n - 1)) * p.k_at.t + (int64_t)b * p.k_at.b + (int64_t)hk * p.k_at.head;
+    const T* const q = (const T*)p.q + (from + min(row, n - 1)) * p.q_at.t + (int64_t)b * p.q_at.b + (int64_t)hk * p.q_at.head;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      load_piece<WHOLE>(key[s], k, 32 * (piece0 + s) + 8 * quad, p.Dk);
+      load_piece<WHOLE>(query[s], q, 32 * (piece0 + s) + 8 * quad, p.Dk);
+    }
+  };
+  const auto turn = [&](const Piece<T, 8>(&x)[KS], int lane) {      // this half's features transposed
+    const Identity id(lane);
+    const int low16 = lane & 15, rows = 16 * wave + 4 * (lane >> 4);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const Parts<IN> a = parts_of(x[s]);
+#pragma unroll
+      for (int odd = 0; odd < 2; ++odd) {
+        if (NT == 1 && odd != half) continue;
+        const int col = 32 * (piece0 + s) + 16 * odd + low16;
+#pragma unroll
+        for (int i = 0; i < IN; ++i) {
+          f32x4_t t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], odd ? id.odd.p[0] : id.even.p[0], f32x4_t{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
+          if (col >= p.Dk) t = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+          *reinterpret_cast<u32x2_t*>(L + Room::k + i * Room::k_plane + col * kSteps + rows) = u32x2_t{pack_bf16(t[0], t[1]), pack_bf16(t[2], t[3])};
+        }
+      }
+    }
+  };
+  f32x4_t* const shared = (f32x4_t*)p.shared + (int64_t)blockIdx.x * (2 * NT * 512);      // [2 NT][threads]: a thread's sums over the values' heads before
+
+  // What a thread brings of S and dS (eight of a row), U, R and dO (four of a row): two steps of 32 values are on their way, of the next head too.
+  struct Brought {
+    Piece<float, 8> s, d;
+    Piece<float, 4> u, r;
+    Piece<T, 4> g;
+  } brought[2];
+  const int steps = (p.Dv + 31) / 32, even_steps = (steps + 1) / 2 * 2;
+  const auto bring = [&](Brought& x, int h, int step) {
+    const int tid = fresh(threadIdx.x), s_row = tid / 4, s_col = 8 * (tid % 4), u_row = tid / 8, u_col = 4 * (tid % 8);
+    const int64_t head = (int64_t)b * p.v_heads + h;
+    const int64_t state = (chunk * p.B * p.v_heads + head) * (int64_t)p.Dk * p.Dv + (int64_t)min(s_row, p.Dk - 1) * p.Dv;
+    const int64_t update = ((from + min(u_row, n - 1)) * p.B * p.v_heads + head) * p.Dv;
+    const T* const go = (const T*)p.grad_out + (from + min(u_row, n - 1)) * p.out_at.t + (int64_t)b * p.out_at.b + (int64_t)h * p.out_at.head;
+    load_piece<WHOLE>(x.s, p.states + state, 32 * step + s_col, p.Dv);
+    load_piece<WHOLE>(x.d, p.back_states + state, 32 * step + s_col, p.Dv);
+    load_piece<WHOLE>(x.u, p.updates + update, 32 * step + u_col, p.Dv);
+    load_piece<WHOLE>(x.r, p.r + update, 32 * step + u_col, p.Dv);
+    load_piece<WHOLE>(x.g, go, 32 * step + u_col, p.Dv);
+  };
+  bring(brought[0], hk * group, 0);
+  bring(brought[1], hk * group, 1);
 
   for (int member = 0; member < group; ++member) {
     const int h = hk * group + member;
-    const int64_t head = (int64_t)b * p.v_heads + h, index_of_chunk = chunk * p.B * p.v_heads + head;
-    const ChunkRoom room(p.chunk_room, index_of_chunk, 3);
-    const float* const S = p.states + index_of_chunk * (int64_t)p.Dk * p.Dv;
-    const float* const back = p.back_states + index_of_chunk * (int64_t)p.Dk * p.Dv;
-    const T* const go = (const T*)p.grad_out + (from + own) * p.out_at.t + (int64_t)b * p.out_at.b + (int64_t)h * p.out_at.head;
-    const float* const U = p.updates + (from * p.B * p.v_heads + head) * (int64_t)p.Dv;
-    const float* const R = p.r + (from * p.B * p.v_heads + head) * (int64_t)p.Dv;
-    const int64_t step = (int64_t)p.B * p.v_heads * p.Dv;
-    __syncthreads();                                 // the member before has been done with LDS
-    if (threadIdx.x < kChunk) {
-      high[threadIdx.x] = room.high[threadIdx.x];
-      low[threadIdx.x] = room.low[threadIdx.x];
+    const ChunkRoom room(p.chunk_room, chunk * p.B * p.v_heads + (int64_t)b * p.v_heads + h, 3);
+    const int tid = fresh(threadIdx.x), lane = tid % 64, low16 = lane & 15, quad = lane >> 4, row = 16 * wave + low16, rows = 16 * wave + 4 * quad;
+    const int s_row = tid / 4, s_col = 8 * (tid % 4), u_row = tid / 8, u_col = 4 * (tid % 8);
+    const f32x4_t start = *reinterpret_cast<const f32x4_t*>(room.start + rows);
+    const f32x4_t rest = *reinterpret_cast<const f32x4_t*>(room.rest + rows);
+    const f32x4_t beta = *reinterpret_cast<const f32x4_t*>(room.beta + rows);
+    const float whole = room.start[kChunk - 1];
+    const T gate = ((const T*)p.gate)[(from + min(kChunk - 1 - lane, n - 1)) * p.gate_at.t + (int64_t)b * p.gate_at.b + h];
+    const T write = ((const T*)p.write)[(from + min(u_row, n - 1)) * p.write_at.t + (int64_t)b * p.write_at.b + h];
+    if (tid < kChunk) {
+      high[tid] = room.high[tid];
+      low[tid] = room.low[tid];
     }
-    f32x4_t y[4], z[4], dq[NT], reads[NT], writes[NT];
+    load_rows();
+    f32x4_t w[4], dq[NT], reads[NT], writes[NT];      // w: Y or Z
 #pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = z[i] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int i = 0; i < 4; ++i) w[i] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < NT; ++i) dq[i] = reads[i] = writes[i] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    float written = 0.0f, kept = 0.0f;               // R . U of the own step (a part), <S, dS> (this thread's part)
+    float written = 0.0f, kept = 0.0f;               // R . U of step u_row, <S, dS>: this thread's parts
 
-    for (int v = 0; v < p.Dv; v += 32) {
-      const int at = v + 8 * quad;
-      __syncthreads();                               // the features before have been read
+    for (int pair = 0; pair < even_steps; pair += 2) {
 #pragma unroll
-      for (int i = 0; i < DK * 4 / 256 + (DK * 4 % 256 != 0); ++i) {
-        const int piece = threadIdx.x + 256 * i, row = piece / 4, c = 8 * (piece % 4);
-        if (row >= DK) break;
-        Eight<float> s, d;
-        s.load(S + (int64_t)row * p.Dv + v + c, row < p.Dk ? p.Dv - v - c : 0);
-        d.load(back + (int64_t)row * p.Dv + v + c, row < p.Dk ? p.Dv - v - c : 0);
-        const Parts<OUT> a = split<OUT>(s.v), e = split<OUT>(d.v);
+      for (int k = 0; k < 2; ++k) {
+        const int step = pair + k, v = 32 * step;
+        const bool there_is = step < steps;            // for everybody
+        if (there_is) {
+          __syncthreads();                             // the features before have been read
+          Brought& x = brought[k];
+          float s[8], d[8];
 #pragma unroll
-        for (int m = 0; m < 8; ++m) kept = fmaf(s.v[m], d.v[m], kept);
+          for (int e = 0; e < 8; ++e) {
+            const bool there = v + s_col + e < p.Dv;
+            s[e] = there ? x.s.w[e] : 0.0f;
+            d[e] = there ? x.d.w[e] : 0.0f;
+            kept = fmaf(s[e], s_row < p.Dk ? d[e] : 0.0f, kept);
+          }
+          if (s_row < DK) {
+            const Parts<OUT> a = split<OUT>(s), c = split<OUT>(d);
 #pragma unroll
-        for (int m = 0; m < OUT; ++m) {
-          *reinterpret_cast<bf16x8_t*>(L + Room::s + m * Room::s_plane + row * Room::pitch + c) = a.p[m];
-          *reinterpret_cast<bf16x8_t*>(L + Room::back + m * Room::s_plane + row * Room::pitch + c) = e.p[m];
+            for (int i = 0; i < OUT; ++i) {
+              *reinterpret_cast<bf16x8_t*>(L + Room::s + i * Room::s_plane + s_row * Room::pitch + s_col) = a.p[i];
+              *reinterpret_cast<bf16x8_t*>(L + Room::back + i * Room::s_plane + s_row * Room::pitch + s_col) = c.p[i];
+            }
+          }
+          f32x4_t u, r, g;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const bool there = u_row < n && v + u_col + e < p.Dv;
+            u[e] = there ? x.u.w[e] : 0.0f;
+            r[e] = there ? x.r.w[e] : 0.0f;
+            g[e] = there ? value_of(x.g, e) : 0.0f;
+            written = fmaf(u[e], r[e], written);
+          }
+          const int place = u_row * Room::pitch + u_col;
+          quad_to_planes<OUT>(L + Room::u + place, Room::u_plane, u);
+          quad_to_planes<OUT>(L + Room::r + place, Room::u_plane, r);
+          quad_to_planes<IN>(L + Room::g + place, Room::u_plane, g);
         }
-      }
-      Eight<float> u, r;
-      u.load(U + own * step + at, own < n ? p.Dv - at : 0);
-      r.load(R + own * step + at, own < n ? p.Dv - at : 0);
+        in_this_order();
+        bring(brought[k], step + 2 < even_steps || member + 1 == group ? h : h + 1, step + 2 < even_steps ? step + 2 : k);
+        if (there_is) {
+          __syncthreads();
+          const int place = row * Room::pitch + 8 * quad;
+          const Parts<IN> own_g = from_planes<IN>(L + Room::g + place, Room::u_plane);
+          const Parts<OUT> own_r = from_planes<OUT>(L + Room::r + place, Room::u_plane), own_u = from_planes<OUT>(L + Room::u + place, Room::u_plane);
 #pragma unroll
-      for (int m = 0; m < 8; ++m) written = fmaf(u.v[m], r.v[m], written);
-      const Parts<OUT> own_u = split<OUT>(u.v), own_r = split<OUT>(r.v);
+          for (int i = 0; i < 4; ++i) {
+            if (i > wave) continue;
+            const Parts<OUT> o = from_planes<OUT>(L + Room::u + (16 * i + low16) * Room::pitch + 8 * quad, Room::u_plane);
+            if (half) multiply<OUT>(w[i], own_r, o);
+            else multiply<OUT>(w[i], own_g, o);
+          }
 #pragma unroll
-      for (int m = 0; m < OUT; ++m) *reinterpret_cast<bf16x8_t*>(L + Room::u + m * Room::u_plane + own * Room::pitch + 8 * quad) = own_u.p[m];
-      Eight<T> g;
-      g.load(go + at, own < n ? p.Dv - at : 0);
-      const Parts<IN> own_g = g.parts();
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (i > wave) continue;
-        const Parts<OUT> o = from_planes<OUT>(L + Room::u + (16 * i + low16) * Room::pitch + 8 * quad, Room::u_plane);
-        multiply<OUT>(y[i], own_g, o);
-        multiply<OUT>(z[i], own_r, o);
-      }
-#pragma unroll
-      for (int i = 0; i < NT; ++i) {
-        const Parts<OUT> s = from_planes<OUT>(L + Room::s + (16 * i + low16) * Room::pitch + 8 * quad, Room::s_plane);
-        multiply<OUT>(dq[i], own_g, s);
-        multiply<OUT>(reads[i], own_r, s);
-        multiply<OUT>(writes[i], own_u, from_planes<OUT>(L + Room::back + (16 * i + low16) * Room::pitch + 8 * quad, Room::s_plane));
+          for (int i = 0; i < NT; ++i) {
+            const int feature = (16 * (tile0 + i) + low16) * Room::pitch + 8 * quad;
+            const Parts<OUT> s = from_planes<OUT>(L + Room::s + feature, Room::s_plane);
+            multiply<OUT>(dq[i], own_g, s);
+            multiply<OUT>(reads[i], own_r, s);
+            multiply<OUT>(writes[i], own_u, from_planes<OUT>(L + Room::back + feature, Room::s_plane));
+            in_this_order();
+          }
+        }
       }
     }
 
-    const f32x4_t start = *reinterpret_cast<const f32x4_t*>(room.start + 16 * wave + 4 * quad);
-    const f32x4_t rest = *reinterpret_cast<const f32x4_t*>(room.rest + 16 * wave + 4 * quad);
-    const f32x4_t beta = *reinterpret_cast<const f32x4_t*>(room.beta + 16 * wave + 4 * quad);
 #pragma unroll
     for (int i = 0; i < NT; ++i)
 #pragma unroll
@@ -525,96 +599,86 @@ __global__ __launch_bounds__(256) void gradient_kernel(const DeltaParams p) {
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int t = 16 * wave + 4 * quad + r, j = 16 * i + low16;
+        const int t = rows + r, j = 16 * i + low16;
         const float decay = fast_exp((high[t] - high[j]) + (low[t] - low[j]));
-        y[i][r] = j <= t ? decay * y[i][r] : 0.0f;
-        z[i][r] = j < t ? -beta[r] * decay * z[i][r] : 0.0f;
+        w[i][r] = half ? (j < t ? -beta[r] * decay * w[i][r] : 0.0f) : (j <= t ? decay * w[i][r] : 0.0f);
       }
-    __syncthreads();                                 // S, dS and U have been read: K, Z and Y take their place
+    __syncthreads();                                 // S, dS, U, R and dO have been read: K, Z and Y take their place
+    turn(key, lane);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int t = 16 * wave + 4 * quad, j = 16 * i + low16;
-      result_to_planes<OUT>(L + Room::z, Room::y_plane, z[i], t, j);
-      result_to_planes<OUT>(L + Room::y, Room::y_plane, y[i], t, j);
-      quad_to_planes<OUT>(L + Room::z_turned + j * kSteps + t, Room::y_plane, z[i]);
-    }
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      const int at = 32 * s + 8 * quad;
-      Eight<T> e;
-      e.load(k + (int64_t)own * p.k_at.t + at, own < n ? p.Dk - at : 0);
-      transpose_to<IN>(L + Room::k, Room::k_plane, e.parts(), 16 * wave, 32 * s, id, lane, p.Dk);
+      const int j = 16 * i + low16;
+      result_to_planes<OUT>(L + (half ? Room::z : Room::y), Room::y_plane, w[i], rows, j);
+      if (half) quad_to_planes<OUT>(L + Room::z_turned + j * kSteps + rows, Room::y_plane, w[i]);
     }
     __syncthreads();
-    f32x4_t dG = {0.0f, 0.0f, 0.0f, 0.0f}, leaves = dG;      // of the four steps of this lane's results: a part over the features
+    f32x4_t dG = {0.0f, 0.0f, 0.0f, 0.0f}, leaves = dG, kept_key[NT];      // of the four steps of this lane's results: a part over the features
 #pragma unroll
-    for (int i = 0; i < NT; ++i) leaves += steps_from_planes<IN>(L + Room::k + (16 * i + low16) * kSteps + 16 * wave + 4 * quad, Room::k_plane) * writes[i];
+    for (int i = 0; i < NT; ++i) {
+      kept_key[i] = steps_from_planes<IN>(L + Room::k + (16 * (tile0 + i) + low16) * kSteps + rows, Room::k_plane);
+      leaves += kept_key[i] * writes[i];
+    }
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       const int at = 32 * s + 8 * quad;
-      const Parts<OUT> a = from_planes<OUT>(L + Room::y + own * kSteps + at, Room::y_plane), c = from_planes<OUT>(L + Room::z + own * kSteps + at, Room::y_plane),
-                       d = from_planes<OUT>(L + Room::z_turned + own * kSteps + at, Room::y_plane);
+      const Parts<OUT> a = from_planes<OUT>(L + Room::y + row * kSteps + at, Room::y_plane), c = from_planes<OUT>(L + Room::z + row * kSteps + at, Room::y_plane),
+                       d = from_planes<OUT>(L + Room::z_turned + row * kSteps + at, Room::y_plane);
 #pragma unroll
       for (int i = 0; i < NT; ++i) {
-        const Parts<IN> o = from_planes<IN>(L + Room::k + (16 * i + low16) * kSteps + at, Room::k_plane);
+        const Parts<IN> o = from_planes<IN>(L + Room::k + (16 * (tile0 + i) + low16) * kSteps + at, Room::k_plane);
         multiply<OUT>(dq[i], a, o);
         multiply<OUT>(reads[i], c, o);
         multiply<OUT>(writes[i], d, o);
       }
     }
+#pragma unroll
+    for (int i = 0; i < NT; ++i) dG += kept_key[i] * reads[i];
     __syncthreads();                                 // K and Y have been read: Q and Y transposed take their place
+    turn(query, lane);
+    if (!half) {
 #pragma unroll
-    for (int i = 0; i < NT; ++i) dG += steps_from_planes<IN>(L + Room::k + (16 * i + low16) * kSteps + 16 * wave + 4 * quad, Room::k_plane) * reads[i];
-    f32x4_t key[NT];                                 // the writing keys' products wait for the queries'
-#pragma unroll
-    for (int i = 0; i < NT; ++i) key[i] = steps_from_planes<IN>(L + Room::k + (16 * i + low16) * kSteps + 16 * wave + 4 * quad, Room::k_plane);
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) quad_to_planes<OUT>(L + Room::y + (16 * i + low16) * kSteps + 16 * wave + 4 * quad, Room::y_plane, y[i]);
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      const int at = 32 * s + 8 * quad;
-      Eight<T> e;
-      e.load(q + (int64_t)own * p.q_at.t + at, own < n ? p.Dk - at : 0);
-      transpose_to<IN>(L + Room::k, Room::k_plane, e.parts(), 16 * wave, 32 * s, id, lane, p.Dk);
+      for (int i = 0; i < 4; ++i) quad_to_planes<OUT>(L + Room::y + (16 * i + low16) * kSteps + rows, Room::y_plane, w[i]);
     }
     __syncthreads();
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       const int at = 32 * s + 8 * quad;
-      const Parts<OUT> a = from_planes<OUT>(L + Room::y + own * kSteps + at, Room::y_plane);
+      const Parts<OUT> a = from_planes<OUT>(L + Room::y + row * kSteps + at, Room::y_plane);
 #pragma unroll
-      for (int i = 0; i < NT; ++i) multiply<OUT>(writes[i], a, from_planes<IN>(L + Room::k + (16 * i + low16) * kSteps + at, Room::k_plane));
+      for (int i = 0; i < NT; ++i) multiply<OUT>(writes[i], a, from_planes<IN>(L + Room::k + (16 * (tile0 + i) + low16) * kSteps + at, Room::k_plane));
     }
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-      dG += steps_from_planes<IN>(L + Room::k + (16 * i + low16) * kSteps + 16 * wave + 4 * quad, Room::k_plane) * dq[i];
-      dG -= key[i] * writes[i];
+      dG += steps_from_planes<IN>(L + Room::k + (16 * (tile0 + i) + low16) * kSteps + rows, Room::k_plane) * dq[i];
+      dG -= kept_key[i] * writes[i];
     }
-    // sums over the features: 16 lanes; over the own step's values: four lanes 16 apart; over everything
+    // sums over this half's features: 16 lanes; over a step's values: 8 threads; over everything
     kept = sum_over_lanes<64>(kept);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       dG[r] = sum_over_lanes<16>(dG[r]);
       leaves[r] = sum_over_lanes<16>(leaves[r]);
     }
-    float out = sum_over_lanes<64>(low16 == 0 ? (leaves[0] + leaves[1]) + (leaves[2] + leaves[3]) : 0.0f);
-    written = over_rows(written, [](float a, float c) { return a + c; });
+    const float out = sum_over_lanes<64>(low16 == 0 ? (leaves[0] + leaves[1]) + (leaves[2] + leaves[3]) : 0.0f);
+    written = sum_over_lanes<8>(written);
     if (low16 == 0) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) change[16 * wave + 4 * quad + r] = dG[r];
+      for (int r = 0; r < 4; ++r) change[half][rows + r] = dG[r];
     }
-    if (lane == 0) both[wave] = fmaf(room.start[kChunk - 1], kept, out);
-    if (quad == 0 && own < here) {
+    if (lane == 0) both[tid / 64] = fmaf(whole, kept, out);
+    if (tid % 8 == 0 && u_row < here) {
       float d = 0.0f;                                // 1 - b by itself: from a rounded b near 1 nothing would be left of it
-      if (own < n) d = sigmoid(-(float)((const T*)p.write)[(from + own) * p.write_at.t + (int64_t)b * p.write_at.b + h]) * written;
-      gw[(int64_t)own * p.grad_write_at.t + h] = (T)d;
+      if (u_row < n) d = sigmoid(-(float)write) * written;
+      gw[(int64_t)u_row * p.grad_write_at.t + h] = (T)d;
     }
     __syncthreads();
-    if (wave == 0) {
+    if (tid < 64) {
       // the sum from every step on, in 64 bits: its terms are far larger than what is left of them
-      double total = (double)change[kChunk - 1 - lane];
-      if (lane == 0) total += ((double)both[0] + both[1]) + ((double)both[2] + both[3]);
+      double total = (double)change[0][kChunk - 1 - lane] + (double)change[1][kChunk - 1 - lane];
+      if (lane == 0) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) total += (double)both[i];
+      }
 #pragma unroll
       for (int by = 1; by < 64; by *= 2) {
         const double before = __shfl_up(total, by);
@@ -623,30 +687,49 @@ __global__ __launch_bounds__(256) void gradient_kernel(const DeltaParams p) {
       const int t = kChunk - 1 - lane;
       if (t < here) {
         float d = 0.0f;
-        if (t < n) d = sigmoid(-(float)((const T*)p.gate)[(from + t) * p.gate_at.t + (int64_t)b * p.gate_at.b + h]) * (float)total;
+        if (t < n) d = sigmoid(-(float)gate) * (float)total;
         gg[(int64_t)t * p.grad_gate_at.t + h] = (T)d;
       }
     }
+    const bool last = member + 1 == group;
 #pragma unroll
-    for (int i = 0; i < NT; ++i)
+    for (int i = 0; i < NT; ++i) {
+      f32x4_t a = dq[i], d = reads[i] + writes[i];
+      f32x4_t* const kept_q = shared + 2 * i * 512;
+      f32x4_t* const kept_k = kept_q + 512;
+      if (member) {
+        a += kept_q[tid];
+        d += kept_k[tid];
+      }
+      if (!last) {
+        kept_q[tid] = a;
+        kept_k[tid] = d;
+      } else {                                       // every wave has read Q and Y
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int t = 16 * wave + 4 * quad + r, c = 16 * i + low16;
-        float a = dq[i][r], d = reads[i][r] + writes[i][r];
-        float* const kept_q = shared + t * DK + c;
-        float* const kept_k = kept_q + kChunk * DK;
-        if (member) {                                // the same lane's sums
-          a += *kept_q;
-          d += *kept_k;
-        }
-        if (member + 1 < group) {
-          *kept_q = a;
-          *kept_k = d;
-        } else if (t < here && c < p.Dk) {
-          gq[(int64_t)t * p.grad_q_at.t + c] = (T)(t < n ? a : 0.0f);
-          gk[(int64_t)t * p.grad_k_at.t + c] = (T)(t < n ? d : 0.0f);
+        for (int r = 0; r < 4; ++r) {
+          T* const to = (T*)lds + (rows + r) * Room::out_pitch + 16 * (tile0 + i) + low16;
+          to[0] = (T)a[r];
+          to[kChunk * Room::out_pitch] = (T)d[r];
         }
       }
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 2 * kChunk * (DK / 8); i += 512) {
+    const int which = i / (kChunk * (DK / 8)), t = i / (DK / 8) % kChunk, c = 8 * (i % (DK / 8)), left = p.Dk - c;
+    if (t >= here || left <= 0) continue;
+    Piece<T, 8> v = load_aligned<T, 8>((const T*)lds + (which * kChunk + t) * Room::out_pitch + c);
+    if (t >= n) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v.set(e, (T)0.0f);
+    }
+    T* const to = which ? gk + (int64_t)t * p.grad_k_at.t + c : gq + (int64_t)t * p.grad_q_at.t + c;
+    if (left >= 8) {
+      __builtin_memcpy(to, v.w, 8 * sizeof(T));
+    } else {
+      const T* const at = (const T*)lds + (which * kChunk + t) * Room::out_pitch + c;
+      for (int e = 0; e < left; ++e) to[e] = t < n ? at[e] : (T)0.0f;
+    }
   }
 }
 
@@ -675,10 +758,17 @@ hipError_t backward_shaped(const DeltaParams& p, hipStream_t s) {
   hipError_t e = narrow ? (whole ? back_scan_shaped<T, DK, 1, true>(p, s) : back_scan_shaped<T, DK, 1, false>(p, s))
                         : (whole ? back_scan_shaped<T, DK, 2, true>(p, s) : back_scan_shaped<T, DK, 2, false>(p, s));
   if (e != hipSuccess) return e;
-  constexpr int bytes = GradientRoom<T, DK>::size * 2;
-  e = with_lds(gradient_kernel<T, DK>, bytes);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((gradient_kernel<T, DK>), dim3((unsigned)((int64_t)p.chunks * p.B * p.k_heads)), dim3(256), bytes, s, p);
+  constexpr int bytes = GradientRoom<T, DK>::bytes;
+  const dim3 grid((unsigned)((int64_t)p.chunks * p.B * p.k_heads));
+  if (whole && p.Dv % 8 == 0) {
+    e = with_lds(gradient_kernel<T, DK, true>, bytes);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((gradient_kernel<T, DK, true>), grid, dim3(512), bytes, s, p);
+  } else {
+    e = with_lds(gradient_kernel<T, DK, false>, bytes);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((gradient_kernel<T, DK, false>), grid, dim3(512), bytes, s, p);
+  }
   return hipGetLastError();
 }
 

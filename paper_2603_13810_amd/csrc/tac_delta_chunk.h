@@ -164,6 +164,12 @@ __device__ __forceinline__ void computed(f32x4_t (&v)[N]) {
   for (int i = 0; i < N; ++i) asm volatile("" : "+v"(v[i]));
 }
 
+// The same number, of which the compiler does not know that it is: what is computed from it is computed here, not kept in registers around a loop.
+__device__ __forceinline__ int fresh(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // a store to device memory, also where the compiler cannot tell from a chosen address that it is
 template <typename T>
 __device__ __forceinline__ void store_device(T* to, T v) {
