@@ -46,7 +46,7 @@ tac::HeadNormParams head_params(const tac_head_norm_desc_t* d) {
   p.interleaved = d->interleaved != 0;
   p.bf16 = d->dtype == TAC_BF16;
   p.eps = d->eps;
-  p.log2_base = d->axes ? std::log2(d->base) : 0.0;
+  for (int a = 0; a < d->axes; ++a) p.log2_step[a] = std::log2(d->base) / d->pairs[a];
   return p;
 }
 

@@ -409,9 +409,6 @@ __device__ __forceinline__ f32x4_t steps_from_planes(const bf16* at, int plane) 
   return v;
 }
 
-__device__ __forceinline__ float value_of(const Piece<bf16, 4>& v, int e) { return bits_float(e % 2 ? v.w[e / 2] & 0xffff0000u : v.w[e / 2] << 16); }
-__device__ __forceinline__ float value_of(const Piece<float, 4>& v, int e) { return v.w[e]; }
-
 // One chunk of a head of queries and keys, the heads of values that share it one after the other.  Eight waves: wave w of either four has the steps from 16 w on as rows and half of a
 // key's features as columns, the first four form Y, the others Z.  All that is summed over values comes through LDS, whole lines at a time and a step ahead.
 // WHOLE: Dk and Dv are multiples of 8.

@@ -240,21 +240,6 @@ struct ChunkRoom {
 // A lane's pieces of one row of queries or keys, N neighbours from each of `at`, as they stand in memory.  Loads of the next chunk are on their way while this one is
 // worked on: nothing here looks at what is loaded, and nothing branches, since behind a branch the compiler waits for everything.  WHOLE: Dk is a multiple of N, a piece
 // is there or not; else element by element.  What is not there is read from where something of the row is: it stands beside a state's rows behind Dk, which are zero.
-template <typename T, int N>
-struct Piece;
-template <int N>
-struct Piece<bf16, N> {
-  uint32_t w[N / 2];
-  __device__ __forceinline__ void set(int e, bf16 x) {
-    const uint32_t v = __builtin_bit_cast(uint16_t, x);
-    w[e / 2] = e % 2 ? (w[e / 2] & 0xffffu) | v << 16 : (w[e / 2] & 0xffff0000u) | v;
-  }
-};
-template <int N>
-struct Piece<float, N> {
-  float w[N];
-  __device__ __forceinline__ void set(int e, float x) { w[e] = x; }
-};
 template <bool WHOLE, typename T, int N>
 __device__ __forceinline__ void load_piece(Piece<T, N>& v, const T* row, int at, int Dk) {
   if constexpr (WHOLE) {

@@ -27,6 +27,31 @@ __device__ __forceinline__ float sum_over_lanes(float v) {
   return v;
 }
 
+// N elements as they stand in memory
+template <typename T, int N>
+struct Piece;
+template <int N>
+struct Piece<bf16, N> {
+  uint32_t w[N / 2];
+  __device__ __forceinline__ void set(int e, bf16 x) {
+    const uint32_t v = __builtin_bit_cast(uint16_t, x);
+    w[e / 2] = e % 2 ? (w[e / 2] & 0xffffu) | v << 16 : (w[e / 2] & 0xffff0000u) | v;
+  }
+};
+template <int N>
+struct Piece<float, N> {
+  float w[N];
+  __device__ __forceinline__ void set(int e, float x) { w[e] = x; }
+};
+template <int N>
+__device__ __forceinline__ float value_of(const Piece<bf16, N>& v, int e) {
+  return bits_float(e % 2 ? v.w[e / 2] & 0xffff0000u : v.w[e / 2] << 16);
+}
+template <int N>
+__device__ __forceinline__ float value_of(const Piece<float, N>& v, int e) {
+  return v.w[e];
+}
+
 // 1 / (1 + exp(-x)); exp overflows to infinity, whose reciprocal is 0
 __device__ __forceinline__ float sigmoid(float x) { return 1.0f / (1.0f + expf(-x)); }
 
@@ -46,7 +71,7 @@ struct HeadNormParams {
   int D, axes, pairs[TAC_ROTATION_AXES], rotated;      // rotated: pairs in all
   int interleaved, bf16, slices;
   float eps;
-  double log2_base;
+  double log2_step[TAC_ROTATION_AXES];      // log2(base) / pairs
 };
 size_t head_norm_workspace(int64_t rows, int heads, int D);
 hipError_t head_norm_launch(const HeadNormParams& p, hipStream_t s);

@@ -32,22 +32,26 @@ struct Lane {
 
   __device__ Lane(const HeadNormParams& p, int lane) {
     count = min(max(p.D / 2 - kPairs * lane, 0), kPairs);
+    double part[kPairs];             // of the axis's pairs, those before this one
 #pragma unroll
     for (int j = 0; j < kPairs; ++j) {
       const int pair = kPairs * lane + j;
 #pragma unroll
       for (int second = 0; second < 2; ++second) at[MODE == ROW ? 2 * j + second : j + kPairs * second] = j < count ? feature_of(p, pair, second) : 0;
       axis[j] = -1;
-      turns[j] = 0.0;
+      part[j] = 0.0;
       int begin = 0;
-      for (int a = 0; a < p.axes; ++a) {
-        if (pair >= begin && pair < begin + p.pairs[a]) {
+#pragma unroll
+      for (int a = 0; a < TAC_ROTATION_AXES; ++a) {
+        if (a < p.axes && pair >= begin && pair < begin + p.pairs[a]) {
           axis[j] = a;
-          turns[j] = exp2(-(double)(pair - begin) / (double)p.pairs[a] * p.log2_base) * 0.15915494309189533577;      // 1 / (2 pi)
+          part[j] = (double)(pair - begin) * p.log2_step[a];
         }
         begin += p.pairs[a];
       }
     }
+#pragma unroll
+    for (int j = 0; j < kPairs; ++j) turns[j] = exp2(-part[j]) * 0.15915494309189533577;      // 1 / (2 pi); four at once, not one in each branch
   }
   __device__ __forceinline__ int first(int j) const { return MODE == ROW ? 2 * j : j; }
   __device__ __forceinline__ int second(int j) const { return MODE == ROW ? 2 * j + 1 : j + kPairs; }
@@ -63,38 +67,38 @@ struct Lane {
       }
     }
   }
+  // without branches: a lane behind the last pair reads the head's first ones, and has zeros in their place
   template <typename T>
-  __device__ __forceinline__ void load(const T* x, float (&v)[2 * kPairs]) const {
+  __device__ __forceinline__ void load(const T* x, Piece<T, 8>& v) const {
     if constexpr (MODE == ROW) {
-      if (count) load_floats<T, 8, true>(x + at[0], 8, v);
+      __builtin_memcpy(v.w, __builtin_assume_aligned(x + at[0], 16), 8 * sizeof(T));
     } else if constexpr (MODE == QUADS) {
-      if (count) {
-        float a[4], b[4];
-        load_floats<T, 4, true>(x + at[0], 4, a);
-        load_floats<T, 4, true>(x + at[4], 4, b);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = a[e], v[e + 4] = b[e];
-      }
+      __builtin_memcpy(v.w, __builtin_assume_aligned(x + at[0], 4 * sizeof(T)), 4 * sizeof(T));
+      __builtin_memcpy(&v.w[sizeof(v.w) / sizeof(v.w[0]) / 2], __builtin_assume_aligned(x + at[4], 4 * sizeof(T)), 4 * sizeof(T));
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (e % kPairs < count) v[e] = (float)x[at[e]];
+      for (int e = 0; e < 8; ++e) v.set(e, x[at[e]]);
     }
   }
   template <typename T>
+  __device__ __forceinline__ void values(const Piece<T, 8>& x, float (&v)[2 * kPairs]) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = count > (MODE == ROW ? e / 2 : e % kPairs) ? value_of(x, e) : 0.0f;
+  }
+  template <bool PAST, typename T>
   __device__ __forceinline__ void store(T* y, const float (&v)[2 * kPairs]) const {
-    if constexpr (MODE == ROW) {
-      if (count) store_floats<T, 8, true>(y + at[0], 8, v);
-    } else if constexpr (MODE == QUADS) {
-      if (count) {
-        const float a[4] = {v[0], v[1], v[2], v[3]}, b[4] = {v[4], v[5], v[6], v[7]};
-        store_floats<T, 4, true>(y + at[0], 4, a);
-        store_floats<T, 4, true>(y + at[4], 4, b);
-      }
-    } else {
+    if constexpr (MODE == EACH) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
         if (e % kPairs < count) y[at[e]] = (T)v[e];
+    } else if (count) {
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        T* const to = MODE == ROW ? y + at[0] + 4 * half : y + at[4 * half];
+        const float* const w = v + 4 * half;
+        if constexpr (sizeof(T) == 4) store_past<PAST>(reinterpret_cast<f32x4_t*>(to), f32x4_t{w[0], w[1], w[2], w[3]});
+        else store_past<PAST>(reinterpret_cast<u32x2_t*>(to), u32x2_t{pack_bf16(w[0], w[1]), pack_bf16(w[2], w[3])});
+      }
     }
   }
   __device__ __forceinline__ void gains(const float* gain, float (&v)[2 * kPairs]) const {
@@ -107,126 +111,165 @@ struct Lane {
 template <int MODE>
 __device__ __forceinline__ constexpr int in_order(int e) { return MODE == ROW ? 2 * (e % kPairs) + e / kPairs : e; }
 
-__device__ __forceinline__ void zero(float (&v)[2 * kPairs]) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+// Where a lane group is: slices of rows one after the other, of each the heads some at once.  The next ones are read while these are worked on.
+template <int LANES, int AT_ONCE>
+struct Walk {
+  uint32_t unit, row;
+  int slice, begin;
+  __device__ __forceinline__ Walk() : unit(blockIdx.x * (256 / LANES) + threadIdx.x / LANES) {}
+  __device__ __forceinline__ void enter(const HeadNormParams& p) {
+    row = unit / (uint32_t)p.slices;
+    slice = (int)(unit - row * (uint32_t)p.slices);
+    begin = slice;
+  }
+  __device__ __forceinline__ bool more(const HeadNormParams& p) const { return unit < (uint32_t)p.rows * (uint32_t)p.slices; }
+  __device__ __forceinline__ int head(const HeadNormParams& p, int i) const { return begin + i * p.slices; }
+  __device__ __forceinline__ void next(const HeadNormParams& p, int heads) {
+    begin += AT_ONCE * p.slices;
+    if (begin < heads) return;
+    unit += gridDim.x * (256 / LANES);
+    enter(p);
+  }
+};
+
+// where head h of a row stands, of queries and keys; F: which of the tensors
+enum { X, GRAD_OUT, OUT };
+template <int F, typename T>
+__device__ __forceinline__ T* head_at(const HeadNormParams& p, uint32_t row, int h) {
+  const bool key = h >= p.q.heads;
+  const auto& s = F == X ? (key ? p.k.x_stride : p.q.x_stride) : F == GRAD_OUT ? (key ? p.k.grad_out_stride : p.q.grad_out_stride) : key ? p.k.out_stride : p.q.out_stride;
+  const void* base = F == X ? (key ? p.k.x : p.q.x) : F == GRAD_OUT ? (key ? p.k.grad_out : p.q.grad_out) : key ? p.k.out : p.q.out;
+  return (T*)base + (int64_t)row * s.row + (int64_t)(key ? h - p.q.heads : h) * s.head;
 }
 
-template <typename T, int LANES, int MODE>
+template <typename T, int LANES, int MODE, bool PAST>
 __global__ __launch_bounds__(256) void head_norm_kernel(const HeadNormParams p) {
   const Lane<MODE> lane(p, threadIdx.x % LANES);
   float gain[2][8];
   lane.gains(p.q.gain, gain[0]);
   lane.gains(p.k.gain, gain[1]);
   const int heads = p.q.heads + p.k.heads;
-  const uint32_t units = (uint32_t)p.rows * (uint32_t)p.slices, step = gridDim.x * (256 / LANES);
-  for (uint32_t unit = blockIdx.x * (256 / LANES) + threadIdx.x / LANES; unit < units; unit += step) {
-    const uint32_t row = unit / (uint32_t)p.slices;
-    const int slice = (int)(unit - row * (uint32_t)p.slices);
-    float c[kPairs], s[kPairs];
-    for (int begin = slice; begin < heads; begin += kAtOnce * p.slices) {
-      float v[kAtOnce][8];
+  Walk<LANES, kAtOnce> here;
+  if (!here.more(p)) return;
+  Piece<T, 8> x[kAtOnce];
+  const auto read = [&](const Walk<LANES, kAtOnce>& w) {
 #pragma unroll
-      for (int i = 0; i < kAtOnce; ++i) {
-        const int h = begin + i * p.slices;
-        zero(v[i]);
-        if (h < p.q.heads) lane.load((const T*)p.q.x + (int64_t)row * p.q.x_stride.row + (int64_t)h * p.q.x_stride.head, v[i]);
-        else if (h < heads) lane.load((const T*)p.k.x + (int64_t)row * p.k.x_stride.row + (int64_t)(h - p.q.heads) * p.k.x_stride.head, v[i]);
+    for (int i = 0; i < kAtOnce; ++i) lane.load(head_at<X, const T>(p, w.row, min(w.head(p, i), heads - 1)), x[i]);
+  };
+  here.enter(p);
+  read(here);
+  float c[kPairs], s[kPairs];
+  while (true) {
+    float v[kAtOnce][8];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) lane.values(x[i], v[i]);
+    if (here.begin == here.slice) lane.angles(p, here.row, c, s);
+    Walk<LANES, kAtOnce> ahead = here;
+    ahead.next(p, heads);
+    const bool more = ahead.more(p);
+    if (more) read(ahead);
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const int h = here.head(p, i);
+      if (h >= heads) break;
+      float squares = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) squares = fmaf(v[i][in_order<MODE>(e)], v[i][in_order<MODE>(e)], squares);
+      const float rstd = p.eps > 0.0f ? 1.0f / sqrtf(sum_over_lanes<LANES>(squares) / (float)p.D + p.eps) : 1.0f;
+      const bool key = h >= p.q.heads;
+      float y[8];
+#pragma unroll
+      for (int j = 0; j < kPairs; ++j) {
+        const int f = lane.first(j), g = lane.second(j);
+        const float a = v[i][f] * rstd * (key ? gain[1][f] : gain[0][f]), b = v[i][g] * rstd * (key ? gain[1][g] : gain[0][g]);
+        y[f] = lane.axis[j] >= 0 ? fmaf(a, c[j], -(b * s[j])) : a;       // a NaN beside a feature that is not turned stays where it is
+        y[g] = lane.axis[j] >= 0 ? fmaf(b, c[j], a * s[j]) : b;
       }
-      if (begin == slice) lane.angles(p, row, c, s);
-#pragma unroll
-      for (int i = 0; i < kAtOnce; ++i) {
-        const int h = begin + i * p.slices;
-        if (h >= heads) break;
-        float squares = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) squares = fmaf(v[i][in_order<MODE>(e)], v[i][in_order<MODE>(e)], squares);
-        const float rstd = p.eps > 0.0f ? 1.0f / sqrtf(sum_over_lanes<LANES>(squares) / (float)p.D + p.eps) : 1.0f;
-        const bool key = h >= p.q.heads;
-        float y[8];
-#pragma unroll
-        for (int j = 0; j < kPairs; ++j) {
-          const int f = lane.first(j), g = lane.second(j);
-          const float a = v[i][f] * rstd * (key ? gain[1][f] : gain[0][f]), b = v[i][g] * rstd * (key ? gain[1][g] : gain[0][g]);
-          y[f] = lane.axis[j] >= 0 ? fmaf(a, c[j], -(b * s[j])) : a;       // a NaN beside a feature that is not turned stays where it is
-          y[g] = lane.axis[j] >= 0 ? fmaf(b, c[j], a * s[j]) : b;
-        }
-        if (key) lane.store((T*)p.k.out + (int64_t)row * p.k.out_stride.row + (int64_t)(h - p.q.heads) * p.k.out_stride.head, y);
-        else lane.store((T*)p.q.out + (int64_t)row * p.q.out_stride.row + (int64_t)h * p.q.out_stride.head, y);
-      }
+      lane.template store<PAST>(head_at<OUT, T>(p, here.row, h), y);
     }
+    if (!more) return;
+    here = ahead;
   }
 }
 
 // The gains' gradients stay in a lane's registers over all heads that it takes, are added up over the workgroup in LDS and leave as a row of the
 // workspace [workgroup][queries, keys][8 LANES]; head_gain_kernel adds those up in their order.
-template <typename T, int LANES, int MODE>
+template <typename T, int LANES, int MODE, bool PAST>
 __global__ __launch_bounds__(256) void head_norm_backward_kernel(const HeadNormParams p) {
+  constexpr int AT_ONCE = kAtOnce / 2;
   __shared__ float room[256 * 8];
   const Lane<MODE> lane(p, threadIdx.x % LANES);
   float gain[2][8], sums[2][8];
   lane.gains(p.q.gain, gain[0]);
   lane.gains(p.k.gain, gain[1]);
-  zero(sums[0]);
-  zero(sums[1]);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sums[0][e] = sums[1][e] = 0.0f;
   const int heads = p.q.heads + p.k.heads;
-  const uint32_t units = (uint32_t)p.rows * (uint32_t)p.slices, step = gridDim.x * (256 / LANES);
-  for (uint32_t unit = blockIdx.x * (256 / LANES) + threadIdx.x / LANES; unit < units; unit += step) {
-    const uint32_t row = unit / (uint32_t)p.slices;
-    const int slice = (int)(unit - row * (uint32_t)p.slices);
-    float c[kPairs], s[kPairs];
-    for (int begin = slice; begin < heads; begin += kAtOnce / 2 * p.slices) {
-      float v[kAtOnce / 2][8], d[kAtOnce / 2][8];
+  Walk<LANES, AT_ONCE> here;
+  Piece<T, 8> x[AT_ONCE], dy[AT_ONCE];
+  const auto read = [&](const Walk<LANES, AT_ONCE>& w) {
 #pragma unroll
-      for (int i = 0; i < kAtOnce / 2; ++i) {
-        const int h = begin + i * p.slices;
-        zero(v[i]);
-        zero(d[i]);
-        if (h >= heads) continue;
-        const HeadTensor& t = h < p.q.heads ? p.q : p.k;
-        const int at = h < p.q.heads ? h : h - p.q.heads;
-        lane.load((const T*)t.x + (int64_t)row * t.x_stride.row + (int64_t)at * t.x_stride.head, v[i]);
-        lane.load((const T*)t.grad_out + (int64_t)row * t.grad_out_stride.row + (int64_t)at * t.grad_out_stride.head, d[i]);
-      }
-      if (begin == slice) lane.angles(p, row, c, s);
-#pragma unroll
-      for (int i = 0; i < kAtOnce / 2; ++i) {
-        const int h = begin + i * p.slices;
-        if (h >= heads) break;
-        const bool key = h >= p.q.heads;
-        float rstd = 1.0f;
-        if (p.eps > 0.0f) {
-          float squares = 0.0f;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) squares = fmaf(v[i][in_order<MODE>(e)], v[i][in_order<MODE>(e)], squares);
-          rstd = 1.0f / sqrtf(sum_over_lanes<LANES>(squares) / (float)p.D + p.eps);
-        }
-        float w[8], dot = 0.0f;
-#pragma unroll
-        for (int j = 0; j < kPairs; ++j) {
-          const int f = lane.first(j), g = lane.second(j);
-          w[f] = lane.axis[j] >= 0 ? fmaf(d[i][f], c[j], d[i][g] * s[j]) : d[i][f];
-          w[g] = lane.axis[j] >= 0 ? fmaf(d[i][g], c[j], -(d[i][f] * s[j])) : d[i][g];
-        }
-#pragma unroll
-        for (int m = 0; m < 8; ++m) {
-          const int e = in_order<MODE>(m);
-          v[i][e] *= rstd;
-          const float one = w[e] * v[i][e];
-          if (key) sums[1][e] += one;
-          else sums[0][e] += one;
-          w[e] *= key ? gain[1][e] : gain[0][e];
-          dot = fmaf(w[e], v[i][e], dot);
-        }
-        if (p.eps > 0.0f) {
-          const float mean = sum_over_lanes<LANES>(dot) / (float)p.D;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) w[e] = rstd * (w[e] - v[i][e] * mean);
-        }
-        if (key) lane.store((T*)p.k.out + (int64_t)row * p.k.out_stride.row + (int64_t)(h - p.q.heads) * p.k.out_stride.head, w);
-        else lane.store((T*)p.q.out + (int64_t)row * p.q.out_stride.row + (int64_t)h * p.q.out_stride.head, w);
-      }
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const int h = min(w.head(p, i), heads - 1);
+      lane.load(head_at<X, const T>(p, w.row, h), x[i]);
+      lane.load(head_at<GRAD_OUT, const T>(p, w.row, h), dy[i]);
     }
+  };
+  bool more = here.more(p);
+  if (more) {
+    here.enter(p);
+    read(here);
+  }
+  float c[kPairs], s[kPairs];
+  while (more) {
+    float v[AT_ONCE][8], d[AT_ONCE][8];
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      lane.values(x[i], v[i]);
+      lane.values(dy[i], d[i]);
+    }
+    if (here.begin == here.slice) lane.angles(p, here.row, c, s);
+    Walk<LANES, AT_ONCE> ahead = here;
+    ahead.next(p, heads);
+    more = ahead.more(p);
+    if (more) read(ahead);
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const int h = here.head(p, i);
+      if (h >= heads) break;
+      const bool key = h >= p.q.heads;
+      float rstd = 1.0f;
+      if (p.eps > 0.0f) {
+        float squares = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) squares = fmaf(v[i][in_order<MODE>(e)], v[i][in_order<MODE>(e)], squares);
+        rstd = 1.0f / sqrtf(sum_over_lanes<LANES>(squares) / (float)p.D + p.eps);
+      }
+      float w[8], dot = 0.0f;
+#pragma unroll
+      for (int j = 0; j < kPairs; ++j) {
+        const int f = lane.first(j), g = lane.second(j);
+        w[f] = lane.axis[j] >= 0 ? fmaf(d[i][f], c[j], d[i][g] * s[j]) : d[i][f];
+        w[g] = lane.axis[j] >= 0 ? fmaf(d[i][g], c[j], -(d[i][f] * s[j])) : d[i][g];
+      }
+#pragma unroll
+      for (int m = 0; m < 8; ++m) {
+        const int e = in_order<MODE>(m);
+        v[i][e] *= rstd;
+        const float one = w[e] * v[i][e];
+        if (key) sums[1][e] += one;
+        else sums[0][e] += one;
+        w[e] *= key ? gain[1][e] : gain[0][e];
+        dot = fmaf(w[e], v[i][e], dot);
+      }
+      if (p.eps > 0.0f) {
+        const float mean = sum_over_lanes<LANES>(dot) / (float)p.D;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = rstd * (w[e] - v[i][e] * mean);
+      }
+      lane.template store<PAST>(head_at<OUT, T>(p, here.row, h), w);
+    }
+    here = ahead;
   }
   if (!p.partial) return;
 #pragma unroll
@@ -305,10 +348,13 @@ hipError_t head_norm_launch(const HeadNormParams& given, hipStream_t s) {
   const int lanes = head_lanes(p.D);
   p.slices = head_slices(p.rows, p.q.heads + p.k.heads, lanes);
   const unsigned groups = (unsigned)head_groups(p.rows, p.slices, lanes, kHeadGroups);
+  const bool past = streamed(p.rows * (p.q.heads + p.k.heads) * p.D * (p.bf16 ? 2 : 4));
   return by_shape(p, [&](auto l, auto m) {
     constexpr int L = decltype(l)::value, M = decltype(m)::value;
-    if (p.bf16) hipLaunchKernelGGL((head_norm_kernel<bf16, L, M>), dim3(groups), dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((head_norm_kernel<float, L, M>), dim3(groups), dim3(256), 0, s, p);
+    if (p.bf16 && past) hipLaunchKernelGGL((head_norm_kernel<bf16, L, M, true>), dim3(groups), dim3(256), 0, s, p);
+    else if (p.bf16) hipLaunchKernelGGL((head_norm_kernel<bf16, L, M, false>), dim3(groups), dim3(256), 0, s, p);
+    else if (past) hipLaunchKernelGGL((head_norm_kernel<float, L, M, true>), dim3(groups), dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((head_norm_kernel<float, L, M, false>), dim3(groups), dim3(256), 0, s, p);
     return hipGetLastError();
   });
 }
@@ -324,10 +370,13 @@ hipError_t head_norm_backward_launch(const HeadNormParams& given, hipStream_t s)
   p.slices = head_slices(p.rows, p.q.heads + p.k.heads, lanes);
   const unsigned groups = (unsigned)head_groups(p.rows, p.slices, lanes, kHeadBackwardGroups);
   if (!p.grad_gain_q && !p.grad_gain_k) p.partial = nullptr;
+  const bool past = streamed(p.rows * (p.q.heads + p.k.heads) * p.D * (p.bf16 ? 2 : 4));
   return by_shape(p, [&](auto l, auto m) {
     constexpr int L = decltype(l)::value, M = decltype(m)::value;
-    if (p.bf16) hipLaunchKernelGGL((head_norm_backward_kernel<bf16, L, M>), dim3(groups), dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((head_norm_backward_kernel<float, L, M>), dim3(groups), dim3(256), 0, s, p);
+    if (p.bf16 && past) hipLaunchKernelGGL((head_norm_backward_kernel<bf16, L, M, true>), dim3(groups), dim3(256), 0, s, p);
+    else if (p.bf16) hipLaunchKernelGGL((head_norm_backward_kernel<bf16, L, M, false>), dim3(groups), dim3(256), 0, s, p);
+    else if (past) hipLaunchKernelGGL((head_norm_backward_kernel<float, L, M, true>), dim3(groups), dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((head_norm_backward_kernel<float, L, M, false>), dim3(groups), dim3(256), 0, s, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !p.partial) return e;
     hipLaunchKernelGGL((head_gain_kernel<M>), dim3(L / 2, p.k.heads ? 2 : 1), dim3(256), 0, s, p, (int)groups, L);
