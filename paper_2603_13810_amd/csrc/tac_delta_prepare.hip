@@ -28,7 +28,7 @@ __device__ __forceinline__ void scan_pairs(float& high, float& low, int lane) {
 
 // A matrix in LDS, or its transpose, to planes; operands that hold nothing are left out.
 template <int PARTS, bool BACK>
-__device__ __forceinline__ void store_planes(bf16* to, const float (&from)[kChunk][kPitch]) {
+__device__ __forceinline__ void store_planes(bf16* to, const float (*from)[kPitch]) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int operand = threadIdx.x / 64 + 4 * i, lane = threadIdx.x % 64, tile = operand / 2, step = operand % 2;
@@ -43,10 +43,20 @@ __device__ __forceinline__ void store_planes(bf16* to, const float (&from)[kChun
   }
 }
 
-template <typename T, int DK, bool BACK>
+// K and Q as they stand, [2][64][DK + 8] elements, give their place to A and P, and P its to the inverse.
+template <typename T, int DK>
+struct PrepareRoom {
+  static constexpr int pitch = DK + 8, inputs = 2 * kChunk * pitch * (int)sizeof(T), matrices = 2 * kChunk * kPitch * 4;
+  static constexpr int bytes = inputs > matrices ? inputs : matrices;
+};
+
+template <typename T, int DK, bool BACK, bool WHOLE>
 __global__ __launch_bounds__(256) void prepare_kernel(const DeltaParams p) {
+  using Room = PrepareRoom<T, DK>;
   constexpr int IN = Kind<T>::in, OUT = BACK ? 3 : Kind<T>::out, KS = DK / 32;
-  __shared__ __align__(16) float A[kChunk][kPitch], P[kChunk][kPitch];      // P's place takes the inverse
+  __shared__ __align__(16) uint8_t lds[Room::bytes];
+  float(*const A)[kPitch] = (float(*)[kPitch])lds;
+  float(*const P)[kPitch] = A + kChunk;
   __shared__ float diagonal[4][16][20];
   __shared__ float high[kChunk], low[kChunk], beta[kChunk];
   const int h = blockIdx.x % p.v_heads, b = blockIdx.x / p.v_heads % p.B;
@@ -72,38 +82,53 @@ __global__ __launch_bounds__(256) void prepare_kernel(const DeltaParams p) {
     low[lane] = lo;
     beta[lane] = w;
   }
-  Parts<IN> own_k[KS], own_q[KS];
+  // whole rows from memory; what is behind the last step is zero
+  constexpr int pieces = DK / 8;
+  T* const rows_of_k = (T*)lds;
+  T* const rows_of_q = rows_of_k + kChunk * Room::pitch;
 #pragma unroll
-  for (int s = 0; s < KS; ++s) {
-    const int row = 16 * wave + low16, col = 32 * s + 8 * quad, left = row < n ? p.Dk - col : 0;
-    Eight<T> e;
-    e.load(k + (int64_t)row * p.k_at.t + col, left);
-    own_k[s] = e.parts();
-    e.load(q + (int64_t)row * p.q_at.t + col, left);
-    own_q[s] = e.parts();
+  for (int i = 0; i < kChunk * pieces / 256; ++i) {
+    const int piece = threadIdx.x + 256 * i, row = piece / pieces, col = 8 * (piece % pieces), left = row < n ? p.Dk - col : 0;
+    Piece<T, 8> a, c;
+    load_piece<WHOLE>(a, k + (int64_t)min(row, n - 1) * p.k_at.t, col, p.Dk);
+    load_piece<WHOLE>(c, q + (int64_t)min(row, n - 1) * p.q_at.t, col, p.Dk);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (e >= left) {
+        a.set(e, (T)0.0f);
+        c.set(e, (T)0.0f);
+      }
+    }
+    store_aligned(rows_of_k + row * Room::pitch + col, a);
+    store_aligned(rows_of_q + row * Room::pitch + col, c);
   }
   __syncthreads();
   const ChunkRoom room(p.chunk_room, blockIdx.x, OUT);
+  f32x4_t kk[4], qk[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) kk[j] = qk[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    const int at = (16 * wave + low16) * Room::pitch + 32 * s + 8 * quad;
+    const Parts<IN> own_k = parts_of(load_aligned<T, 8>(rows_of_k + at)), own_q = parts_of(load_aligned<T, 8>(rows_of_q + at));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (j > wave) continue;
+      const Parts<IN> other = parts_of(load_aligned<T, 8>(rows_of_k + (16 * j + low16) * Room::pitch + 32 * s + 8 * quad));
+      multiply<IN>(kk[j], own_k, other);
+      multiply<IN>(qk[j], own_q, other);
+    }
+  }
+  __syncthreads();                                    // K and Q have been read
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    f32x4_t kk = {0.0f, 0.0f, 0.0f, 0.0f}, qk = kk;
-    if (j <= wave) {
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const int row = 16 * j + low16, col = 32 * s + 8 * quad;
-        Eight<T> e;
-        e.load(k + (int64_t)row * p.k_at.t + col, row < n ? p.Dk - col : 0);
-        const Parts<IN> other = e.parts();
-        multiply<IN>(kk, own_k[s], other);
-        multiply<IN>(qk, own_q[s], other);
-      }
-    }
+    if (j / 2 > wave / 2) continue;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int t = 16 * wave + 4 * quad + r, c = 16 * j + low16;
       const float decay = fast_exp((high[t] - high[c]) + (low[t] - low[c]));
-      if (j <= wave) A[t][c] = c < t ? beta[t] * decay * kk[r] : 0.0f;
-      if (j / 2 <= wave / 2) P[t][c] = c <= t ? decay * qk[r] : 0.0f;
+      A[t][c] = c < t ? beta[t] * decay * kk[j][r] : 0.0f;
+      P[t][c] = c <= t ? decay * qk[j][r] : 0.0f;
     }
   }
   __syncthreads();
@@ -164,12 +189,16 @@ __global__ __launch_bounds__(256) void prepare_kernel(const DeltaParams p) {
 template <typename T, bool BACK>
 hipError_t prepare_typed(const DeltaParams& p, hipStream_t s) {
   const dim3 grid((unsigned)((int64_t)p.chunks * p.B * p.v_heads));
-  switch (padded_key(p.Dk)) {
-    case 32: hipLaunchKernelGGL((prepare_kernel<T, 32, BACK>), grid, dim3(256), 0, s, p); break;
-    case 64: hipLaunchKernelGGL((prepare_kernel<T, 64, BACK>), grid, dim3(256), 0, s, p); break;
-    default: hipLaunchKernelGGL((prepare_kernel<T, 128, BACK>), grid, dim3(256), 0, s, p);
-  }
-  return hipGetLastError();
+  const auto with = [&](auto whole) {
+    constexpr bool WHOLE = decltype(whole)::value;
+    switch (padded_key(p.Dk)) {
+      case 32: hipLaunchKernelGGL((prepare_kernel<T, 32, BACK, WHOLE>), grid, dim3(256), 0, s, p); break;
+      case 64: hipLaunchKernelGGL((prepare_kernel<T, 64, BACK, WHOLE>), grid, dim3(256), 0, s, p); break;
+      default: hipLaunchKernelGGL((prepare_kernel<T, 128, BACK, WHOLE>), grid, dim3(256), 0, s, p);
+    }
+    return hipGetLastError();
+  };
+  return p.Dk % 8 == 0 ? with(std::true_type()) : with(std::false_type());
 }
 
 }  // namespace
