@@ -593,13 +593,16 @@ __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
         writes[i][r] *= rest[r];
       }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i) {
+      if (i > wave) continue;                        // above the diagonal: zeros
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int t = rows + r, j = 16 * i + low16;
         const float decay = fast_exp((high[t] - high[j]) + (low[t] - low[j]));
-        w[i][r] = half ? (j < t ? -beta[r] * decay * w[i][r] : 0.0f) : (j <= t ? decay * w[i][r] : 0.0f);
+        w[i][r] *= half ? -beta[r] * decay : decay;
+        if (half ? j >= t : j > t) w[i][r] = 0.0f;
       }
+    }
     __syncthreads();                                 // S, dS, U, R and dO have been read: K, Z and Y take their place
     turn(key, lane);
 #pragma unroll
@@ -618,14 +621,21 @@ __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       const int at = 32 * s + 8 * quad;
-      const Parts<OUT> a = from_planes<OUT>(L + Room::y + row * kSteps + at, Room::y_plane), c = from_planes<OUT>(L + Room::z + row * kSteps + at, Room::y_plane),
-                       d = from_planes<OUT>(L + Room::z_turned + row * kSteps + at, Room::y_plane);
+      const bool lower = 2 * s <= wave, upper = 2 * s + 1 >= wave;      // whether these 32 columns of Y and Z, and of Z transposed, hold something
+      Parts<OUT> a, c, d;
+      if (lower) {
+        a = from_planes<OUT>(L + Room::y + row * kSteps + at, Room::y_plane);
+        c = from_planes<OUT>(L + Room::z + row * kSteps + at, Room::y_plane);
+      }
+      if (upper) d = from_planes<OUT>(L + Room::z_turned + row * kSteps + at, Room::y_plane);
 #pragma unroll
       for (int i = 0; i < NT; ++i) {
         const Parts<IN> o = from_planes<IN>(L + Room::k + (16 * (tile0 + i) + low16) * kSteps + at, Room::k_plane);
-        multiply<OUT>(dq[i], a, o);
-        multiply<OUT>(reads[i], c, o);
-        multiply<OUT>(writes[i], d, o);
+        if (lower) {
+          multiply<OUT>(dq[i], a, o);
+          multiply<OUT>(reads[i], c, o);
+        }
+        if (upper) multiply<OUT>(writes[i], d, o);
       }
     }
 #pragma unroll
@@ -639,6 +649,7 @@ __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
     __syncthreads();
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
+      if (2 * s + 1 < wave) continue;
       const int at = 32 * s + 8 * quad;
       const Parts<OUT> a = from_planes<OUT>(L + Room::y + row * kSteps + at, Room::y_plane);
 #pragma unroll

@@ -120,15 +120,34 @@ __global__ __launch_bounds__(256) void prepare_kernel(const DeltaParams p) {
     }
   }
   __syncthreads();                                    // K and Q have been read
+  // e^(G_t - G_c) of blocks below the diagonal is two factors, to the step in front of the block's rows and from there on, neither above 1
+  float since[4], with_beta[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int t = 16 * wave + 4 * quad + r, from_step = max(16 * wave - 1, 0);
+    since[r] = fast_exp((high[t] - high[from_step]) + (low[t] - low[from_step]));
+    with_beta[r] = since[r] * beta[t];
+  }
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     if (j / 2 > wave / 2) continue;
+    const int c = 16 * j + low16;
+    if (j < wave) {
+      const float until = fast_exp((high[16 * wave - 1] - high[c]) + (low[16 * wave - 1] - low[c]));
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int t = 16 * wave + 4 * quad + r, c = 16 * j + low16;
-      const float decay = fast_exp((high[t] - high[c]) + (low[t] - low[c]));
-      A[t][c] = c < t ? beta[t] * decay * kk[j][r] : 0.0f;
-      P[t][c] = c <= t ? decay * qk[j][r] : 0.0f;
+      for (int r = 0; r < 4; ++r) {
+        const int t = 16 * wave + 4 * quad + r;
+        A[t][c] = with_beta[r] * until * kk[j][r];
+        P[t][c] = since[r] * until * qk[j][r];
+      }
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int t = 16 * wave + 4 * quad + r;
+        const float decay = fast_exp((high[t] - high[c]) + (low[t] - low[c]));
+        A[t][c] = c < t ? beta[t] * decay * kk[j][r] : 0.0f;
+        P[t][c] = c <= t ? decay * qk[j][r] : 0.0f;
+      }
     }
   }
   __syncthreads();
