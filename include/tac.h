@@ -596,14 +596,15 @@ typedef struct tac_delta_desc {
  *   gate, write  DEVICE, read-only, [T][B][v_heads]
  *   lengths      DEVICE, read-only, int32 [B], taken as 0 .. T where outside; NULL: all T
  *   h0           DEVICE, read-only, float32 [B][v_heads][Dk][Dv], or NULL: zeros
- *   out          DEVICE, written, [T][B][v_heads][Dv]; no output may lie on an input, but for h_last on h0
+ *   out          DEVICE, written, [T][B][v_heads][Dv]; no output may lie on an input, but for h_last on h0 (where one begins at an input's address the call is refused)
  *   h_last       DEVICE, written, float32 [B][v_heads][Dk][Dv], or NULL; may be h0
  *   states       DEVICE, written, float32 [ceil(T / TAC_DELTA_CHUNK)][B][v_heads][Dk][Dv]: the state before every chunk of steps, and
  *   updates      DEVICE, written, float32 [T][B][v_heads][Dv]: u, which are all that the backward pass keeps; both or both NULL.  Of chunks that lie
  *                behind a sequence's length nothing is written
  *   workspace    DEVICE, scratch, tac_delta_scan_workspace_bytes(desc) bytes, 16-byte aligned
  * The same bits from call to call.
- * Errors: TAC_ERR_NULL, TAC_ERR_BAD_SHAPE, TAC_ERR_UNSUPPORTED (more features than the limits), TAC_ERR_BAD_PARAM, TAC_ERR_ALIGN, TAC_ERR_HIP. */
+ * Errors: TAC_ERR_NULL, TAC_ERR_BAD_SHAPE (also 2^23 or more chunks of heads, or pieces of 16 columns of heads' states), TAC_ERR_UNSUPPORTED (more features than the limits),
+ * TAC_ERR_BAD_PARAM, TAC_ERR_ALIGN, TAC_ERR_HIP. */
 size_t tac_delta_scan_workspace_bytes(const tac_delta_desc_t* desc);
 int tac_delta_scan(const tac_delta_desc_t* desc, const void* query, const void* key, const void* value, const void* gate, const void* write,
                    const int32_t* lengths, const float* h0, void* out, float* h_last, float* states, float* updates, void* workspace, void* stream);
@@ -617,7 +618,7 @@ int tac_delta_scan(const tac_delta_desc_t* desc, const void* query, const void* 
  *   states, updates  DEVICE, read-only, as tac_delta_scan wrote them
  *   grad_out         DEVICE, read-only, strides `out`
  *   grad_h_last      DEVICE, read-only, float32 [B][v_heads][Dk][Dv], or NULL: zeros
- *   grad_query, grad_key, grad_value, grad_gate, grad_write   DEVICE, written
+ *   grad_query, grad_key, grad_value, grad_gate, grad_write   DEVICE, written; none may lie on an input
  *   grad_h0          DEVICE, written, float32 [B][v_heads][Dk][Dv], or NULL; may be grad_h_last
  *   workspace        DEVICE, scratch, tac_delta_scan_backward_workspace_bytes(desc) bytes, 16-byte aligned */
 size_t tac_delta_scan_backward_workspace_bytes(const tac_delta_desc_t* desc);
@@ -631,7 +632,7 @@ int tac_delta_scan_backward(const tac_delta_desc_t* desc, const void* query, con
  *   pool   DEVICE, updated, float32 [n_slots][v_heads][Dk][Dv]
  *   slots  DEVICE, read-only, int32 [B], each slot at most once; a slot outside 0 .. n_slots - 1 stands for no sequence: its rows of out are
  *          zero and no state changes.  NULL: sequence b has slot b (n_slots >= B)
- *   out    DEVICE, written, [B][v_heads][Dv] */
+ *   out    DEVICE, written, [B][v_heads][Dv]; not on an input */
 int tac_delta_step(const tac_delta_desc_t* desc, const void* query, const void* key, const void* value, const void* gate, const void* write,
                    float* pool, int64_t n_slots, const int32_t* slots, void* out, void* stream);
 
