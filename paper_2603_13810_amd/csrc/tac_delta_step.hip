@@ -12,9 +12,10 @@ namespace {
 constexpr int kTile = 32;            // columns of a workgroup
 constexpr int kRows = TAC_DELTA_MAX_KEY / 32;
 
-template <bool VEC>
+template <bool VEC, bool PAST>
 __device__ __forceinline__ f32x4_t load_four(const float* p, int n) {
-  if constexpr (VEC) return *reinterpret_cast<const f32x4_t*>(p);
+  if constexpr (VEC && PAST) return __builtin_nontemporal_load(reinterpret_cast<const f32x4_t*>(p));
+  else if constexpr (VEC) return *reinterpret_cast<const f32x4_t*>(p);
   f32x4_t v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
   for (int e = 0; e < 4; ++e)
@@ -22,7 +23,7 @@ __device__ __forceinline__ f32x4_t load_four(const float* p, int n) {
   return v;
 }
 
-template <typename T, bool VEC>
+template <typename T, bool VEC, bool PAST>
 __global__ __launch_bounds__(256) void delta_step_kernel(const DeltaStepParams p) {
   __shared__ float room[4][8][9];                      // per wave and lane of a row: four sums with the key, four with the query, k . q
   const int tiles = (p.Dv + kTile - 1) / kTile;
@@ -47,7 +48,7 @@ __global__ __launch_bounds__(256) void delta_step_kernel(const DeltaStepParams p
     s[i] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     kr[i] = qr[i] = 0.0f;
     if (r < p.Dk) {
-      if (left > 0) s[i] = load_four<VEC>(S + (int64_t)r * p.Dv + col, left);
+      if (left > 0) s[i] = load_four<VEC, PAST>(S + (int64_t)r * p.Dv + col, left);
       kr[i] = (float)k[r];
       qr[i] = (float)q[r];
     }
@@ -94,7 +95,7 @@ __global__ __launch_bounds__(256) void delta_step_kernel(const DeltaStepParams p
       for (int e = 0; e < 4; ++e) s[i][e] = fmaf(kr[i], u[e], s[i][e]);
       float* to = S + (int64_t)r * p.Dv + col;
       if constexpr (VEC) {
-        *reinterpret_cast<f32x4_t*>(to) = s[i];
+        store_past<PAST>(reinterpret_cast<f32x4_t*>(to), s[i]);
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -114,10 +115,16 @@ __global__ __launch_bounds__(256) void delta_step_kernel(const DeltaStepParams p
 hipError_t delta_step_launch(const DeltaStepParams& p, hipStream_t s) {
   const dim3 grid((unsigned)((int64_t)p.B * p.v_heads * ((p.Dv + kTile - 1) / kTile)));
   const bool vec = p.Dv % 4 == 0 && ((uintptr_t)p.pool & 15) == 0;
-  if (p.bf16 && vec) hipLaunchKernelGGL((delta_step_kernel<bf16, true>), grid, dim3(256), 0, s, p);
-  else if (p.bf16) hipLaunchKernelGGL((delta_step_kernel<bf16, false>), grid, dim3(256), 0, s, p);
-  else if (vec) hipLaunchKernelGGL((delta_step_kernel<float, true>), grid, dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((delta_step_kernel<float, false>), grid, dim3(256), 0, s, p);
+  // states that would not stay in the last-level cache go past it both ways: 128 sequences of 16 heads x 128 x 128, pools in turn, 65.6 -> 57.6 us
+  const bool past = vec && streamed((int64_t)p.B * p.v_heads * p.Dk * p.Dv * 4);
+  const auto with = [&](auto type) {
+    using T = decltype(type);
+    if (past) hipLaunchKernelGGL((delta_step_kernel<T, true, true>), grid, dim3(256), 0, s, p);
+    else if (vec) hipLaunchKernelGGL((delta_step_kernel<T, true, false>), grid, dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((delta_step_kernel<T, false, false>), grid, dim3(256), 0, s, p);
+  };
+  if (p.bf16) with(bf16());
+  else with(float());
   return hipGetLastError();
 }
 

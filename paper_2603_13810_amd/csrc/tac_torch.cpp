@@ -13,8 +13,6 @@
 
 #include <pybind11/pybind11.h>
 
-#include <vector>
-
 #include "tac.h"
 
 namespace {
@@ -598,16 +596,16 @@ struct Delta {
       if (t.size(i) > INT32_MAX) refuse("%s is too large", name);
     return t;
   }
-  std::vector<int64_t> lead() const { return step ? std::vector<int64_t>{(int64_t)d.B} : std::vector<int64_t>{d.T, (int64_t)d.B}; }
-  std::vector<int64_t> shape(std::initializer_list<int64_t> rest) const {
-    std::vector<int64_t> s = lead();
-    s.insert(s.end(), rest);
-    return s;
-  }
-  std::vector<int64_t> keys() const { return shape({d.k_heads, d.Dk}); }
-  std::vector<int64_t> values() const { return shape({d.v_heads, d.Dv}); }
-  std::vector<int64_t> gates() const { return shape({d.v_heads}); }
-  std::vector<int64_t> state() const { return {d.B, d.v_heads, d.Dk, d.Dv}; }
+  // a shape without an allocation
+  struct Shape {
+    int64_t n[5];
+    size_t count;
+    operator at::IntArrayRef() const { return at::IntArrayRef(n, count); }
+  };
+  Shape keys() const { return step ? Shape{{d.B, d.k_heads, d.Dk}, 3} : Shape{{d.T, d.B, d.k_heads, d.Dk}, 4}; }
+  Shape values() const { return step ? Shape{{d.B, d.v_heads, d.Dv}, 3} : Shape{{d.T, d.B, d.v_heads, d.Dv}, 4}; }
+  Shape gates() const { return step ? Shape{{d.B, d.v_heads}, 2} : Shape{{d.T, d.B, d.v_heads}, 3}; }
+  Shape state() const { return Shape{{d.B, d.v_heads, d.Dk, d.Dv}, 4}; }
   tac_delta_strides_t strides(const Tensor& t) const {
     return step ? tac_delta_strides_t{0, t.stride(0), t.stride(1)} : tac_delta_strides_t{t.stride(0), t.stride(1), t.stride(2)};
   }
@@ -685,7 +683,7 @@ PyObject* delta_scan_backward(PyObject*, PyObject* const* a, Py_ssize_t count) {
   const int32_t* lengths = (const int32_t*)c.whole(maybe(a[8], "lengths"), "lengths", ScalarType::Int, {d.B});
   const float* last = (const float*)c.whole(maybe(a[9], "grad_h_last"), "grad_h_last", ScalarType::Float, x.state());
   const char* const names[5] = {"grad_query", "grad_key", "grad_value", "grad_gate", "grad_write"};
-  const std::vector<int64_t> shapes[5] = {x.keys(), x.keys(), x.values(), x.gates(), x.gates()};
+  const Delta::Shape shapes[5] = {x.keys(), x.keys(), x.values(), x.gates(), x.gates()};
   tac_delta_strides_t* const strides[5] = {&x.d.grad_query, &x.d.grad_key, &x.d.grad_value, &x.d.grad_gate, &x.d.grad_write};
   Tensor grads[5];
   void* at[5];
