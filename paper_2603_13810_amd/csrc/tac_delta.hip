@@ -37,7 +37,7 @@ __device__ __forceinline__ void load_rows_of(Parts<PARTS> (&m)[2], const bf16* f
 // registers: the summed index may come in any order, so the result's layout is taken as it is, and K is read to match; the waves' shares of K S are
 // added up through LDS, which moves a third of what S in parts would.  Of the chunk's K the wave reads every step, from LDS: a compute unit takes 64 bytes a cycle from the
 // caches, and every load that is not asked for twice counts.
-template <typename T, int DK, int NT, bool WHOLE, bool KEEP>
+template <typename T, int DK, int NT, int MODE, bool KEEP>
 __device__ __forceinline__ void scan_states(const DeltaParams& p, const ScanPlace<T, NT>& at, uint8_t* lds) {
   using Room = ScanRoom<T, DK, NT>;
   constexpr int IN = Kind<T>::in, OUT = Kind<T>::out, MT = DK / 16, OWN = MT > 4 ? 2 : 1;
@@ -199,7 +199,7 @@ __device__ __forceinline__ void scan_states(const DeltaParams& p, const ScanPlac
 }
 
 // The outputs, from what the chain leaves in LDS.  And its K: the next chunk's as it stands, this one's transposed, zero behind Dk, so that S is.
-template <typename T, int DK, int NT, bool WHOLE>
+template <typename T, int DK, int NT, int MODE>
 __device__ __forceinline__ void scan_outputs(const DeltaParams& p, const ScanPlace<T, NT>& at, uint8_t* lds) {
   using Room = ScanRoom<T, DK, NT>;
   constexpr int IN = Kind<T>::in, OUT = Kind<T>::out, KS = DK / 32;
@@ -213,7 +213,7 @@ __device__ __forceinline__ void scan_outputs(const DeltaParams& p, const ScanPla
   const auto load_queries = [&](int c) {
     const T* from = at.step(at.q, p.q_at.t, c, at.row);
 #pragma unroll
-    for (int s = 0; s < KS; ++s) load_piece<WHOLE>(query[s], from, 32 * s + 8 * quad, p.Dk);
+    for (int s = 0; s < KS; ++s) load_piece<MODE>(query[s], from, 32 * s + 8 * quad, p.Dk);
     start = *reinterpret_cast<const f32x4_t*>(at.room(p, c).start + rows);
   };
   // whole rows at a time on the way from memory
@@ -221,11 +221,11 @@ __device__ __forceinline__ void scan_outputs(const DeltaParams& p, const ScanPla
   const int key_at = 16 * at.wave + at.lane / pieces, key_col = 8 * (at.lane % pieces);
   const auto load_keys = [&](int c) {
 #pragma unroll
-    for (int s = 0; s < KS; ++s) load_piece<WHOLE>(key[s], at.step(at.k, p.k_at.t, c, key_at + s * (64 / pieces)), key_col, p.Dk);
+    for (int s = 0; s < KS; ++s) load_piece<MODE>(key[s], at.step(at.k, p.k_at.t, c, key_at + s * (64 / pieces)), key_col, p.Dk);
   };
   const auto keep_keys = [&] {
 #pragma unroll
-    for (int s = 0; s < KS; ++s) store_aligned((T*)(L + Room::rows) + (key_at + s * (64 / pieces)) * Room::key + key_col, key[s]);
+    for (int s = 0; s < KS; ++s) store_aligned((T*)(L + Room::rows) + (key_at + s * (64 / pieces)) * Room::key + key_col, arranged<MODE>(key[s], key_col, p.Dk));
   };
   if (at.chunks) {
     load_keys(0);
@@ -252,7 +252,7 @@ __device__ __forceinline__ void scan_outputs(const DeltaParams& p, const ScanPla
     for (int t = 0; t < NT; ++t) o[t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-      const Parts<IN> a = parts_of(query[s]);
+      const Parts<IN> a = parts_of(arranged<MODE>(query[s], 32 * s + 8 * quad, p.Dk));
 #pragma unroll
       for (int t = 0; t < NT; ++t) multiply<OUT>(o[t], a, from_planes<OUT>(L + Room::s + (16 * t + low16) * Room::key + 32 * s + 8 * quad, Room::s_plane));
     }
@@ -300,40 +300,42 @@ __device__ __forceinline__ void scan_outputs(const DeltaParams& p, const ScanPla
   }
 }
 
-template <typename T, int DK, int NT, bool WHOLE, bool KEEP>
+template <typename T, int DK, int NT, int MODE, bool KEEP>
 __global__ __launch_bounds__(512) void scan_kernel(const DeltaParams p, int tiles) {
   extern __shared__ __align__(16) uint8_t lds[];
   const ScanPlace<T, NT> at(p, tiles, p.v, p.v_at, p.out, p.out_at);
   // both meet at the same barriers: one, then three a chunk
-  if (__builtin_amdgcn_readfirstlane(threadIdx.x / 256) == 0) scan_states<T, DK, NT, WHOLE, KEEP>(p, at, lds);
-  else scan_outputs<T, DK, NT, WHOLE>(p, at, lds);
+  if (__builtin_amdgcn_readfirstlane(threadIdx.x / 256) == 0) scan_states<T, DK, NT, MODE, KEEP>(p, at, lds);
+  else scan_outputs<T, DK, NT, MODE>(p, at, lds);
 }
 
-template <typename T, int DK, int NT, bool WHOLE, bool KEEP>
+template <typename T, int DK, int NT, int MODE, bool KEEP>
 hipError_t scan_shaped(const DeltaParams& p, hipStream_t s) {
   const int tiles = (p.Dv + 16 * NT - 1) / (16 * NT);
   constexpr int bytes = ScanRoom<T, DK, NT>::bytes;
   if (bytes > 64 << 10) {
-    const hipError_t e = hipFuncSetAttribute((const void*)scan_kernel<T, DK, NT, WHOLE, KEEP>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    const hipError_t e = hipFuncSetAttribute((const void*)scan_kernel<T, DK, NT, MODE, KEEP>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((scan_kernel<T, DK, NT, WHOLE, KEEP>), dim3((unsigned)((int64_t)p.B * p.v_heads * tiles)), dim3(512), bytes, s, p, tiles);
+  hipLaunchKernelGGL((scan_kernel<T, DK, NT, MODE, KEEP>), dim3((unsigned)((int64_t)p.B * p.v_heads * tiles)), dim3(512), bytes, s, p, tiles);
   return hipGetLastError();
 }
 
-template <typename T, int DK, int NT, bool WHOLE, bool KEEP>
+template <typename T, int DK, int NT, int MODE, bool KEEP>
 hipError_t scan_fitting(const DeltaParams& p, hipStream_t s) {      // float32 keys of 128 features in three parts leave LDS for 16 columns
-  return scan_shaped<T, DK, (ScanRoom<T, DK, NT>::bytes <= 160 << 10 ? NT : 1), WHOLE, KEEP>(p, s);
+  return scan_shaped<T, DK, (ScanRoom<T, DK, NT>::bytes <= 160 << 10 ? NT : 1), MODE, KEEP>(p, s);
 }
 
 template <typename T, int NT, bool KEEP>
 hipError_t scan_typed(const DeltaParams& p, hipStream_t s) {
-  const bool whole = p.Dk % 8 == 0;      // pieces of 8 and of 4
-  switch (padded_key(p.Dk)) {
-    case 32: return whole ? scan_fitting<T, 32, NT, true, KEEP>(p, s) : scan_fitting<T, 32, NT, false, KEEP>(p, s);
-    case 64: return whole ? scan_fitting<T, 64, NT, true, KEEP>(p, s) : scan_fitting<T, 64, NT, false, KEEP>(p, s);
-    default: return whole ? scan_fitting<T, 128, NT, true, KEEP>(p, s) : scan_fitting<T, 128, NT, false, KEEP>(p, s);
-  }
+  return by_mode(piece_mode(p.Dk, 8), [&](auto mode) {
+    constexpr int MODE = decltype(mode)::value;
+    switch (padded_key(p.Dk)) {
+      case 32: return scan_fitting<T, 32, NT, MODE, KEEP>(p, s);
+      case 64: return scan_fitting<T, 64, NT, MODE, KEEP>(p, s);
+      default: return scan_fitting<T, 128, NT, MODE, KEEP>(p, s);
+    }
+  });
 }
 
 }  // namespace

@@ -28,7 +28,7 @@ struct BackRoom {
 };
 
 // The chain: the gradients of the states from chunk to chunk, last to first, as scan_states has the states.
-template <typename T, int DK, int NT, bool WHOLE>
+template <typename T, int DK, int NT, int MODE>
 __device__ __forceinline__ void back_states(const DeltaParams& p, const ScanPlace<T, NT>& at, uint8_t* lds) {
   using Room = BackRoom<T, DK, NT>;
   constexpr int IN = Kind<T>::in, MT = DK / 16, OWN = MT > 4 ? 2 : 1;
@@ -203,7 +203,7 @@ __device__ __forceinline__ void back_states(const DeltaParams& p, const ScanPlac
 }
 
 // What the chain takes that does not wait for it: of this chunk Q^T (e^G dO) and K transposed, of the one in front of it K, dO and P^T dO.
-template <typename T, int DK, int NT, bool WHOLE>
+template <typename T, int DK, int NT, int MODE>
 __device__ __forceinline__ void back_inputs(const DeltaParams& p, const ScanPlace<T, NT>& at, uint8_t* lds) {
   using Room = BackRoom<T, DK, NT>;
   constexpr int IN = Kind<T>::in, KS = DK / 32, MT = DK / 16, OWN = MT > 4 ? 2 : 1;
@@ -222,15 +222,15 @@ __device__ __forceinline__ void back_inputs(const DeltaParams& p, const ScanPlac
   const int key_at = 16 * at.wave + at.lane / pieces, key_col = 8 * (at.lane % pieces);
   const auto load_keys = [&](int c) {
 #pragma unroll
-    for (int s = 0; s < KS; ++s) load_piece<WHOLE>(key[s], at.step(at.k, p.k_at.t, c, key_at + s * (64 / pieces)), key_col, p.Dk);
+    for (int s = 0; s < KS; ++s) load_piece<MODE>(key[s], at.step(at.k, p.k_at.t, c, key_at + s * (64 / pieces)), key_col, p.Dk);
   };
   const auto keep_keys = [&] {
 #pragma unroll
-    for (int s = 0; s < KS; ++s) store_aligned((T*)(L + Room::rows) + (key_at + s * (64 / pieces)) * Room::key + key_col, key[s]);
+    for (int s = 0; s < KS; ++s) store_aligned((T*)(L + Room::rows) + (key_at + s * (64 / pieces)) * Room::key + key_col, arranged<MODE>(key[s], key_col, p.Dk));
   };
   const auto load_queries = [&](int c) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) load_piece<WHOLE>(query[i], at.step(at.q, p.q_at.t, c, 16 * i + low16), own_col + 8 * quad, p.Dk);
+    for (int i = 0; i < 4; ++i) load_piece<MODE>(query[i], at.step(at.q, p.q_at.t, c, 16 * i + low16), own_col + 8 * quad, p.Dk);
   };
   const auto load_grads = [&](int c) {
 #pragma unroll
@@ -303,10 +303,11 @@ __device__ __forceinline__ void back_inputs(const DeltaParams& p, const ScanPlac
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       Parts<IN> turned[OWN];
-      const Parts<IN> a = parts_of(query[2 * s]), b = parts_of(query[2 * s + 1]);
+      const Parts<IN> a = parts_of(arranged<MODE>(query[2 * s], own_col + 8 * quad, p.Dk)), b = parts_of(arranged<MODE>(query[2 * s + 1], own_col + 8 * quad, p.Dk));
 #pragma unroll
       for (int m = 0; m < OWN; ++m) {
-        const Parts<1>& which = OWN == 2 ? (m ? id.odd : id.even) : at.wave % 2 ? id.odd : id.even;
+        Parts<1> which = m ? id.odd : id.even;
+        if (OWN == 1) which = id.of(at.wave % 2);
 #pragma unroll
         for (int i = 0; i < IN; ++i) {
           const f32x4_t zero = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -362,12 +363,12 @@ __device__ __forceinline__ void back_inputs(const DeltaParams& p, const ScanPlac
   }
 }
 
-template <typename T, int DK, int NT, bool WHOLE>
+template <typename T, int DK, int NT, int MODE>
 __global__ __launch_bounds__(512) void back_scan_kernel(const DeltaParams p, int tiles) {
   extern __shared__ __align__(16) uint8_t lds[];
   const ScanPlace<T, NT> at(p, tiles, p.grad_out, p.out_at, p.grad_v, p.grad_v_at);
-  if (__builtin_amdgcn_readfirstlane(threadIdx.x / 256) == 0) back_states<T, DK, NT, WHOLE>(p, at, lds);
-  else back_inputs<T, DK, NT, WHOLE>(p, at, lds);
+  if (__builtin_amdgcn_readfirstlane(threadIdx.x / 256) == 0) back_states<T, DK, NT, MODE>(p, at, lds);
+  else back_inputs<T, DK, NT, MODE>(p, at, lds);
 }
 
 // LDS of gradient_kernel in bfloat16 numbers.  While values' features are summed over, 32 at a time: S and dS [OUT][DK][40], U and R [OUT][64][40], dO [IN][64][40]; then K or Q
@@ -411,8 +412,8 @@ __device__ __forceinline__ f32x4_t steps_from_planes(const bf16* at, int plane) 
 
 // One chunk of a head of queries and keys, the heads of values that share it one after the other.  Eight waves: wave w of either four has the steps from 16 w on as rows and half of a
 // key's features as columns, the first four form Y, the others Z.  All that is summed over values comes through LDS, whole lines at a time and a step ahead.
-// WHOLE: Dk and Dv are multiples of 8.
-template <typename T, int DK, bool WHOLE>
+// MODE: of pieces of 8 of a key and of 4 of a value.
+template <typename T, int DK, int MODE>
 __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
   using Room = GradientRoom<T, DK>;
   constexpr int IN = Kind<T>::in, OUT = Kind<T>::out, NT = DK / 32, KS = NT > 1 ? NT / 2 : 1;      // tiles and pieces of this half of the features
@@ -449,8 +450,8 @@ __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
     const T* const q = (const T*)p.q + (from + min(row, n - 1)) * p.q_at.t + (int64_t)b * p.q_at.b + (int64_t)hk * p.q_at.head;
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-      load_piece<WHOLE>(key[s], k, 32 * (piece0 + s) + 8 * quad, p.Dk);
-      load_piece<WHOLE>(query[s], q, 32 * (piece0 + s) + 8 * quad, p.Dk);
+      load_piece<MODE>(key[s], k, 32 * (piece0 + s) + 8 * quad, p.Dk);
+      load_piece<MODE>(query[s], q, 32 * (piece0 + s) + 8 * quad, p.Dk);
     }
   };
   const auto turn = [&](const Piece<T, 8>(&x)[KS], int lane) {      // this half's features transposed
@@ -458,7 +459,7 @@ __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
     const int low16 = lane & 15, rows = 16 * wave + 4 * (lane >> 4);
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-      const Parts<IN> a = parts_of(x[s]);
+      const Parts<IN> a = parts_of(arranged<MODE>(x[s], 32 * (piece0 + s) + 8 * (lane >> 4), p.Dk));
 #pragma unroll
       for (int odd = 0; odd < 2; ++odd) {
         if (NT == 1 && odd != half) continue;
@@ -476,8 +477,7 @@ __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
 
   // What a thread brings of S and dS (eight of a row), U, R and dO (four of a row): two steps of 32 values are on their way, of the next head too.
   struct Brought {
-    Piece<float, 8> s, d;
-    Piece<float, 4> u, r;
+    Piece<float, 4> s[2], d[2], u, r;
     Piece<T, 4> g;
   } brought[2];
   const int steps = (p.Dv + 31) / 32, even_steps = (steps + 1) / 2 * 2;
@@ -487,11 +487,14 @@ __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
     const int64_t state = (chunk * p.B * p.v_heads + head) * (int64_t)p.Dk * p.Dv + (int64_t)min(s_row, p.Dk - 1) * p.Dv;
     const int64_t update = ((from + min(u_row, n - 1)) * p.B * p.v_heads + head) * p.Dv;
     const T* const go = (const T*)p.grad_out + (from + min(u_row, n - 1)) * p.out_at.t + (int64_t)b * p.out_at.b + (int64_t)h * p.out_at.head;
-    load_piece<WHOLE>(x.s, p.states + state, 32 * step + s_col, p.Dv);
-    load_piece<WHOLE>(x.d, p.back_states + state, 32 * step + s_col, p.Dv);
-    load_piece<WHOLE>(x.u, p.updates + update, 32 * step + u_col, p.Dv);
-    load_piece<WHOLE>(x.r, p.r + update, 32 * step + u_col, p.Dv);
-    load_piece<WHOLE>(x.g, go, 32 * step + u_col, p.Dv);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      load_piece<MODE>(x.s[i], p.states + state, 32 * step + s_col + 4 * i, p.Dv);
+      load_piece<MODE>(x.d[i], p.back_states + state, 32 * step + s_col + 4 * i, p.Dv);
+    }
+    load_piece<MODE>(x.u, p.updates + update, 32 * step + u_col, p.Dv);
+    load_piece<MODE>(x.r, p.r + update, 32 * step + u_col, p.Dv);
+    load_piece<MODE>(x.g, go, 32 * step + u_col, p.Dv);
   };
   bring(brought[0], hk * group, 0);
   bring(brought[1], hk * group, 1);
@@ -528,11 +531,17 @@ __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
           __syncthreads();                             // the features before have been read
           Brought& x = brought[k];
           float s[8], d[8];
+          Piece<float, 4> ps[2], pd[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            ps[i] = arranged<MODE>(x.s[i], v + s_col + 4 * i, p.Dv);
+            pd[i] = arranged<MODE>(x.d[i], v + s_col + 4 * i, p.Dv);
+          }
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             const bool there = v + s_col + e < p.Dv;
-            s[e] = there ? x.s.w[e] : 0.0f;
-            d[e] = there ? x.d.w[e] : 0.0f;
+            s[e] = there ? ps[e / 4].w[e % 4] : 0.0f;
+            d[e] = there ? pd[e / 4].w[e % 4] : 0.0f;
             kept = fmaf(s[e], s_row < p.Dk ? d[e] : 0.0f, kept);
           }
           if (s_row < DK) {
@@ -544,12 +553,14 @@ __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
             }
           }
           f32x4_t u, r, g;
+          const Piece<float, 4> pu = arranged<MODE>(x.u, v + u_col, p.Dv), pr = arranged<MODE>(x.r, v + u_col, p.Dv);
+          const Piece<T, 4> pg = arranged<MODE>(x.g, v + u_col, p.Dv);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const bool there = u_row < n && v + u_col + e < p.Dv;
-            u[e] = there ? x.u.w[e] : 0.0f;
-            r[e] = there ? x.r.w[e] : 0.0f;
-            g[e] = there ? value_of(x.g, e) : 0.0f;
+            u[e] = there ? pu.w[e] : 0.0f;
+            r[e] = there ? pr.w[e] : 0.0f;
+            g[e] = there ? value_of(pg, e) : 0.0f;
             written = fmaf(u[e], r[e], written);
           }
           const int place = u_row * Room::pitch + u_col;
@@ -746,38 +757,38 @@ hipError_t with_lds(K kernel, int bytes) {
   return bytes > 64 << 10 ? hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) : hipSuccess;
 }
 
-template <typename T, int DK, int NT, bool WHOLE>
+template <typename T, int DK, int NT, int MODE>
 hipError_t back_scan_shaped(const DeltaParams& p, hipStream_t s) {
   if constexpr (NT > 1 && BackRoom<T, DK, NT>::bytes > 160 << 10) {      // float32 keys in three parts leave LDS for 16 columns
-    return back_scan_shaped<T, DK, 1, WHOLE>(p, s);
+    return back_scan_shaped<T, DK, 1, MODE>(p, s);
   } else {
     const int tiles = (p.Dv + 16 * NT - 1) / (16 * NT);
     constexpr int bytes = BackRoom<T, DK, NT>::bytes;
-    const hipError_t e = with_lds(back_scan_kernel<T, DK, NT, WHOLE>, bytes);
+    const hipError_t e = with_lds(back_scan_kernel<T, DK, NT, MODE>, bytes);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((back_scan_kernel<T, DK, NT, WHOLE>), dim3((unsigned)((int64_t)p.B * p.v_heads * tiles)), dim3(512), bytes, s, p, tiles);
+    hipLaunchKernelGGL((back_scan_kernel<T, DK, NT, MODE>), dim3((unsigned)((int64_t)p.B * p.v_heads * tiles)), dim3(512), bytes, s, p, tiles);
     return hipGetLastError();
   }
 }
 
 template <typename T, int DK>
 hipError_t backward_shaped(const DeltaParams& p, hipStream_t s) {
-  const bool whole = p.Dk % 8 == 0, narrow = delta_narrow(p.B, p.v_heads, p.Dv);
-  hipError_t e = narrow ? (whole ? back_scan_shaped<T, DK, 1, true>(p, s) : back_scan_shaped<T, DK, 1, false>(p, s))
-                        : (whole ? back_scan_shaped<T, DK, 2, true>(p, s) : back_scan_shaped<T, DK, 2, false>(p, s));
+  const bool narrow = delta_narrow(p.B, p.v_heads, p.Dv);
+  const int key = piece_mode(p.Dk, 8), value = piece_mode(p.Dv, 4);
+  const hipError_t e = by_mode(key, [&](auto mode) {
+    constexpr int MODE = decltype(mode)::value;
+    return narrow ? back_scan_shaped<T, DK, 1, MODE>(p, s) : back_scan_shaped<T, DK, 2, MODE>(p, s);
+  });
   if (e != hipSuccess) return e;
-  constexpr int bytes = GradientRoom<T, DK>::bytes;
-  const dim3 grid((unsigned)((int64_t)p.chunks * p.B * p.k_heads));
-  if (whole && p.Dv % 8 == 0) {
-    e = with_lds(gradient_kernel<T, DK, true>, bytes);
+  // whole pieces of a row that is long enough may be read as shifted ones, by nothing
+  const int both = key == EACH || value == EACH ? EACH : key == WHOLE && value == WHOLE ? WHOLE : p.Dk >= 8 && p.Dv >= 4 ? SHIFTED : EACH;
+  return by_mode(both, [&](auto mode) {
+    constexpr int MODE = decltype(mode)::value, bytes = GradientRoom<T, DK>::bytes;
+    const hipError_t e = with_lds(gradient_kernel<T, DK, MODE>, bytes);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((gradient_kernel<T, DK, true>), grid, dim3(512), bytes, s, p);
-  } else {
-    e = with_lds(gradient_kernel<T, DK, false>, bytes);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((gradient_kernel<T, DK, false>), grid, dim3(512), bytes, s, p);
-  }
-  return hipGetLastError();
+    hipLaunchKernelGGL((gradient_kernel<T, DK, MODE>), dim3((unsigned)((int64_t)p.chunks * p.B * p.k_heads)), dim3(512), bytes, s, p);
+    return hipGetLastError();
+  });
 }
 
 template <typename T>

@@ -128,6 +128,13 @@ __device__ __forceinline__ void quad_to_planes(bf16* at, int plane, const f32x4_
 // The transpose of a 16 x 32 operand by products with the identity: exact, every sum has one term.  to[column][step], 4 steps a store.
 struct Identity {
   Parts<1> even, odd;
+  __device__ __forceinline__ Parts<1> of(int second) const {      // by value: a reference to one of the two would put both into memory
+    const u32x4_t a = __builtin_bit_cast(u32x4_t, even.p[0]), b = __builtin_bit_cast(u32x4_t, odd.p[0]);
+    u32x4_t r;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] = second ? b[e] : a[e];
+    return {__builtin_bit_cast(bf16x8_t, r)};
+  }
   __device__ Identity(int lane) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -237,18 +244,52 @@ struct ChunkRoom {
   }
 };
 
-// A lane's pieces of one row of queries or keys, N neighbours from each of `at`, as they stand in memory.  Loads of the next chunk are on their way while this one is
-// worked on: nothing here looks at what is loaded, and nothing branches, since behind a branch the compiler waits for everything.  WHOLE: Dk is a multiple of N, a piece
-// is there or not; else element by element.  What is not there is read from where something of the row is: it stands beside a state's rows behind Dk, which are zero.
-template <bool WHOLE, typename T, int N>
-__device__ __forceinline__ void load_piece(Piece<T, N>& v, const T* row, int at, int Dk) {
-  if constexpr (WHOLE) {
-    __builtin_memcpy(v.w, row + (at < Dk ? at : 0), N * sizeof(T));
+// A piece of a row of n elements, N neighbours from `at` on, as it stands in memory.  Loads of the next chunk are on their way while this one is worked on: nothing here looks
+// at what is loaded, and nothing branches, since behind a branch the compiler waits for everything.
+//   WHOLE    n is a multiple of N: a piece is there or not
+//   SHIFTED  n is at least N: the last piece is read so that it ends with the row, and arranged() moves its elements to their places
+//   EACH     element by element
+// Of what is not there something of the row is read instead, which is no zero.
+enum { EACH = 0, SHIFTED = 1, WHOLE = 2 };
+inline int piece_mode(int n, int N) { return n % N == 0 ? WHOLE : n > N ? SHIFTED : EACH; }
+
+// f(mode) with it as a constant
+template <typename F>
+hipError_t by_mode(int mode, F f) {
+  using std::integral_constant;
+  return mode == WHOLE ? f(integral_constant<int, WHOLE>()) : mode == SHIFTED ? f(integral_constant<int, SHIFTED>()) : f(integral_constant<int, EACH>());
+}
+
+template <int MODE, typename T, int N>
+__device__ __forceinline__ void load_piece(Piece<T, N>& v, const T* row, int at, int n) {
+  if constexpr (MODE == WHOLE) {
+    __builtin_memcpy(v.w, row + (at < n ? at : 0), N * sizeof(T));
+  } else if constexpr (MODE == SHIFTED) {
+    __builtin_memcpy(v.w, row + min(at, n - N), N * sizeof(T));
   } else {
 #pragma unroll
-    for (int e = 0; e < N; ++e) v.set(e, row[min(at + e, Dk - 1)]);
+    for (int e = 0; e < N; ++e) v.set(e, row[min(at + e, n - 1)]);
   }
 }
+template <int MODE, typename T, int N>
+__device__ __forceinline__ Piece<T, N> arranged(const Piece<T, N>& v, int at, int n) {
+  if constexpr (MODE != SHIFTED) return v;
+  const int by = at - min(at, n - N);                 // elements; N and more: nothing of the piece is there
+  constexpr int words = N * sizeof(T) / 4, per = 4 / sizeof(T);
+  Piece<T, N> r = v;
+  if constexpr (per == 2) {
+#pragma unroll
+    for (int i = 0; i < words; ++i) r.w[i] = __builtin_amdgcn_alignbit(i + 1 < words ? v.w[i + 1] : 0u, v.w[i], (by & 1) * 16);
+  }
+#pragma unroll
+  for (int step = 1; step < words; step *= 2) {
+    const bool on = (by / per) & step;
+#pragma unroll
+    for (int i = 0; i < words; ++i) r.w[i] = on ? (i + step < words ? r.w[i + step] : std::remove_reference_t<decltype(r.w[0])>()) : r.w[i];
+  }
+  return r;
+}
+
 // the same in LDS, aligned
 template <typename T, int N>
 __device__ __forceinline__ void store_aligned(T* to, const Piece<T, N>& v) {

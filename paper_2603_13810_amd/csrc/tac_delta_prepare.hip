@@ -50,7 +50,7 @@ struct PrepareRoom {
   static constexpr int bytes = inputs > matrices ? inputs : matrices;
 };
 
-template <typename T, int DK, bool BACK, bool WHOLE>
+template <typename T, int DK, bool BACK, int MODE>
 __global__ __launch_bounds__(256) void prepare_kernel(const DeltaParams p) {
   using Room = PrepareRoom<T, DK>;
   constexpr int IN = Kind<T>::in, OUT = BACK ? 3 : Kind<T>::out, KS = DK / 32;
@@ -90,8 +90,10 @@ __global__ __launch_bounds__(256) void prepare_kernel(const DeltaParams p) {
   for (int i = 0; i < kChunk * pieces / 256; ++i) {
     const int piece = threadIdx.x + 256 * i, row = piece / pieces, col = 8 * (piece % pieces), left = row < n ? p.Dk - col : 0;
     Piece<T, 8> a, c;
-    load_piece<WHOLE>(a, k + (int64_t)min(row, n - 1) * p.k_at.t, col, p.Dk);
-    load_piece<WHOLE>(c, q + (int64_t)min(row, n - 1) * p.q_at.t, col, p.Dk);
+    load_piece<MODE>(a, k + (int64_t)min(row, n - 1) * p.k_at.t, col, p.Dk);
+    load_piece<MODE>(c, q + (int64_t)min(row, n - 1) * p.q_at.t, col, p.Dk);
+    a = arranged<MODE>(a, col, p.Dk);
+    c = arranged<MODE>(c, col, p.Dk);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       if (e >= left) {
@@ -208,16 +210,16 @@ __global__ __launch_bounds__(256) void prepare_kernel(const DeltaParams p) {
 template <typename T, bool BACK>
 hipError_t prepare_typed(const DeltaParams& p, hipStream_t s) {
   const dim3 grid((unsigned)((int64_t)p.chunks * p.B * p.v_heads));
-  const auto with = [&](auto whole) {
-    constexpr bool WHOLE = decltype(whole)::value;
+  const auto with = [&](auto mode) {
+    constexpr int MODE = decltype(mode)::value;
     switch (padded_key(p.Dk)) {
-      case 32: hipLaunchKernelGGL((prepare_kernel<T, 32, BACK, WHOLE>), grid, dim3(256), 0, s, p); break;
-      case 64: hipLaunchKernelGGL((prepare_kernel<T, 64, BACK, WHOLE>), grid, dim3(256), 0, s, p); break;
-      default: hipLaunchKernelGGL((prepare_kernel<T, 128, BACK, WHOLE>), grid, dim3(256), 0, s, p);
+      case 32: hipLaunchKernelGGL((prepare_kernel<T, 32, BACK, MODE>), grid, dim3(256), 0, s, p); break;
+      case 64: hipLaunchKernelGGL((prepare_kernel<T, 64, BACK, MODE>), grid, dim3(256), 0, s, p); break;
+      default: hipLaunchKernelGGL((prepare_kernel<T, 128, BACK, MODE>), grid, dim3(256), 0, s, p);
     }
     return hipGetLastError();
   };
-  return p.Dk % 8 == 0 ? with(std::true_type()) : with(std::false_type());
+  return by_mode(piece_mode(p.Dk, 8), with);
 }
 
 }  // namespace
