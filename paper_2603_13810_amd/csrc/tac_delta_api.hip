@@ -112,6 +112,10 @@ bool on_each_other(std::initializer_list<const void*> written, std::initializer_
   }
   return false;
 }
+// in place, but not head by head
+bool moved(const tac_head_norm_desc_t* d, int heads, const void* from, const tac_head_strides_t& a, const void* to, const tac_head_strides_t& b) {
+  return from == to && ((d->rows > 1 && a.row != b.row) || (heads > 1 && a.head != b.head));
+}
 
 }  // namespace
 
@@ -129,6 +133,8 @@ int tac_head_norm(const tac_head_norm_desc_t* d, const void* query, const void* 
   if (any_misaligned({query, out_query}, el) || (d->key_heads && any_misaligned({key, out_key}, el)) || any_misaligned({gain_query, gain_key}, 4) ||
       (d->axes && misaligned(positions, 4)))
     return TAC_ERR_ALIGN;
+  if (moved(d, d->query_heads, query, d->query, out_query, d->out_query)) return TAC_ERR_BAD_PARAM;
+  if (d->key_heads && (moved(d, d->key_heads, key, d->key, out_key, d->out_key) || on_each_other({out_query}, {key, out_key}) || out_key == query)) return TAC_ERR_BAD_PARAM;
   tac::HeadNormParams p = head_params(d);
   p.q = {query, nullptr, out_query, gain_query, d->query, {}, d->out_query, d->query_heads};
   p.k = {key, nullptr, out_key, gain_key, d->key, {}, d->out_key, d->key_heads};
@@ -137,7 +143,11 @@ int tac_head_norm(const tac_head_norm_desc_t* d, const void* query, const void* 
 }
 
 size_t tac_head_norm_workspace_bytes(const tac_head_norm_desc_t* d) {
-  return check_heads(d) ? 0 : tac::head_norm_workspace(d->rows, d->query_heads + d->key_heads, d->D);
+  if (check_heads(d)) return 0;
+  tac::HeadNormParams p = head_params(d);
+  p.q.heads = d->query_heads;
+  p.k.heads = d->key_heads;
+  return tac::head_norm_workspace(p);
 }
 
 int tac_head_norm_backward(const tac_head_norm_desc_t* d, const void* query, const void* key, const float* gain_query, const float* gain_key,
@@ -155,6 +165,10 @@ int tac_head_norm_backward(const tac_head_norm_desc_t* d, const void* query, con
   if (any_misaligned({query, grad_out_query, grad_query}, el) || (d->key_heads && any_misaligned({key, grad_out_key, grad_key}, el)) ||
       any_misaligned({gain_query, gain_key, grad_gain_query, grad_gain_key}, 4) || (d->axes && misaligned(positions, 4)) || misaligned(workspace, 16))
     return TAC_ERR_ALIGN;
+  if (moved(d, d->query_heads, grad_out_query, d->out_query, grad_query, d->grad_query) || grad_query == query) return TAC_ERR_BAD_PARAM;
+  if (d->key_heads && (moved(d, d->key_heads, grad_out_key, d->out_key, grad_key, d->grad_key) || on_each_other({grad_query}, {key, grad_out_key, grad_key}) ||
+                       on_each_other({grad_key}, {query, key, grad_out_query})))
+    return TAC_ERR_BAD_PARAM;
   tac::HeadNormParams p = head_params(d);
   p.q = {query, grad_out_query, grad_query, gain_query, d->query, d->out_query, d->grad_query, d->query_heads};
   p.k = {key, grad_out_key, grad_key, gain_key, d->key, d->out_key, d->grad_key, d->key_heads};

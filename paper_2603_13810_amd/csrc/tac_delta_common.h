@@ -69,11 +69,11 @@ struct HeadNormParams {
   float *partial, *grad_gain_q, *grad_gain_k;
   int64_t rows;
   int D, axes, pairs[TAC_ROTATION_AXES], rotated;      // rotated: pairs in all
-  int interleaved, bf16, slices;
+  int interleaved, bf16, slices, apart;
   float eps;
   double log2_step[TAC_ROTATION_AXES];      // log2(base) / pairs
 };
-size_t head_norm_workspace(int64_t rows, int heads, int D);
+size_t head_norm_workspace(const HeadNormParams& p);
 hipError_t head_norm_launch(const HeadNormParams& p, hipStream_t s);
 hipError_t head_norm_backward_launch(const HeadNormParams& p, hipStream_t s);
 

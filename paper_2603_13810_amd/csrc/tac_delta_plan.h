@@ -6,8 +6,16 @@ namespace tac {
 
 // ---- head norm -----------------------------------------------------------------------------------
 
-// lanes that share a head: each holds four pairs of features
-inline int head_lanes(int D) { return D <= 64 ? 8 : D <= 128 ? 16 : D <= 256 ? 32 : 64; }
+// Lanes that share a head.  Each holds up to four pairs of features: rotated ones from the first lane on and the others from a lane of their own on, so that a lane's first and its second
+// features are neighbours each; only where that takes more than 64 lanes does a lane hold some of both.
+struct HeadLanes {
+  int lanes, apart;                  // apart: rotated pairs and others on lanes of their own
+};
+inline HeadLanes head_lanes(int D, int rotated) {
+  const auto room = [](int n) { return n <= 8 ? 8 : n <= 16 ? 16 : n <= 32 ? 32 : 64; };
+  const int apart = (rotated + 3) / 4 + (D / 2 - rotated + 3) / 4;
+  return apart <= 64 ? HeadLanes{room(apart), 1} : HeadLanes{64, 0};
+}
 
 // Slices of a row's heads: the lanes of a slice take every `slices`-th head and turn them all by the angles that they have formed once.  As few slices as
 // give every compute unit four workgroups of 256 lanes.

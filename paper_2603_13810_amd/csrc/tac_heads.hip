@@ -20,30 +20,44 @@ __device__ __forceinline__ int feature_of(const HeadNormParams& p, int pair, int
   return pair < p.rotated ? pair + second * p.rotated : 2 * p.rotated + (pair - p.rotated) + second * rest;
 }
 
-// How a lane's eight features are read: EACH by itself; QUADS: the first and the second features of its pairs are four neighbours each, aligned; ROW: all eight are neighbours.
-enum { EACH = 0, QUADS = 1, ROW = 2 };
+// The first pair of a lane, and how many it has.
+__device__ __forceinline__ int pairs_of(const HeadNormParams& p, int lane, int& count) {
+  const int begin = p.apart ? (p.rotated + kPairs - 1) / kPairs : 0;      // lanes before the others' first
+  const bool rotated = !p.apart || lane < begin;
+  const int pair = rotated ? kPairs * lane : p.rotated + kPairs * (lane - begin), end = p.apart && rotated ? p.rotated : p.D / 2;
+  count = min(max(end - pair, 0), kPairs);
+  return pair;
+}
+
+// How a lane's eight features are read and written, in pieces at any address:
+//   QUADS  the first and the second ones of its pairs are four neighbours each, all there or none     LOOSE_QUADS  some lanes have fewer than four pairs
+//   ROW    all eight are neighbours, all there or none (interleaved)                                   LOOSE_ROW    the last lane has fewer
+//   EACH   feature by feature: heads too short for a piece, and those of both kinds of pairs on a lane
+// A loose piece is read so that it lies within the head, its features moved to their places; of a lane with fewer pairs each feature is written by itself.
+enum { EACH, QUADS, ROW, LOOSE_QUADS, LOOSE_ROW };
 
 template <int MODE>
 struct Lane {
-  int at[2 * kPairs];                // features: the pairs' first ones, then their second ones (ROW: in their order)
+  static constexpr bool row = MODE == ROW || MODE == LOOSE_ROW, loose = MODE == LOOSE_QUADS || MODE == LOOSE_ROW;
+  int at[2 * kPairs];                // features: the pairs' first ones, then their second ones (row: in their order); what is not there: 0
   int count;                         // pairs that there are
   double turns[kPairs];              // per unit of position
   int axis[kPairs];                  // -1: not rotated
 
   __device__ Lane(const HeadNormParams& p, int lane) {
-    count = min(max(p.D / 2 - kPairs * lane, 0), kPairs);
+    const int first_pair = pairs_of(p, lane, count);
     double part[kPairs];             // of the axis's pairs, those before this one
 #pragma unroll
     for (int j = 0; j < kPairs; ++j) {
-      const int pair = kPairs * lane + j;
+      const int pair = first_pair + j;
 #pragma unroll
-      for (int second = 0; second < 2; ++second) at[MODE == ROW ? 2 * j + second : j + kPairs * second] = j < count ? feature_of(p, pair, second) : 0;
+      for (int second = 0; second < 2; ++second) at[row ? 2 * j + second : j + kPairs * second] = j < count ? feature_of(p, pair, second) : 0;
       axis[j] = -1;
       part[j] = 0.0;
       int begin = 0;
 #pragma unroll
       for (int a = 0; a < TAC_ROTATION_AXES; ++a) {
-        if (a < p.axes && pair >= begin && pair < begin + p.pairs[a]) {
+        if (a < p.axes && j < count && pair >= begin && pair < begin + p.pairs[a]) {
           axis[j] = a;
           part[j] = (double)(pair - begin) * p.log2_step[a];
         }
@@ -53,8 +67,8 @@ struct Lane {
 #pragma unroll
     for (int j = 0; j < kPairs; ++j) turns[j] = exp2(-part[j]) * 0.15915494309189533577;      // 1 / (2 pi); four at once, not one in each branch
   }
-  __device__ __forceinline__ int first(int j) const { return MODE == ROW ? 2 * j : j; }
-  __device__ __forceinline__ int second(int j) const { return MODE == ROW ? 2 * j + 1 : j + kPairs; }
+  __device__ __forceinline__ int first(int j) const { return row ? 2 * j : j; }
+  __device__ __forceinline__ int second(int j) const { return row ? 2 * j + 1 : j + kPairs; }
 
   __device__ __forceinline__ void angles(const HeadNormParams& p, int64_t row, float (&c)[kPairs], float (&s)[kPairs]) const {
 #pragma unroll
@@ -69,47 +83,69 @@ struct Lane {
   }
   // without branches: a lane behind the last pair reads the head's first ones, and has zeros in their place
   template <typename T>
-  __device__ __forceinline__ void load(const T* x, Piece<T, 8>& v) const {
-    if constexpr (MODE == ROW) {
-      __builtin_memcpy(v.w, __builtin_assume_aligned(x + at[0], 16), 8 * sizeof(T));
-    } else if constexpr (MODE == QUADS) {
-      __builtin_memcpy(v.w, __builtin_assume_aligned(x + at[0], 4 * sizeof(T)), 4 * sizeof(T));
-      __builtin_memcpy(&v.w[sizeof(v.w) / sizeof(v.w[0]) / 2], __builtin_assume_aligned(x + at[4], 4 * sizeof(T)), 4 * sizeof(T));
+  __device__ __forceinline__ void load(const T* x, Piece<T, 8>& v, int D) const {
+    if constexpr (row) {
+      __builtin_memcpy(v.w, x + (loose ? min(at[0], D - 8) : at[0]), 8 * sizeof(T));
+    } else if constexpr (MODE != EACH) {
+      __builtin_memcpy(v.w, x + (loose ? min(at[0], D - 4) : at[0]), 4 * sizeof(T));
+      __builtin_memcpy(&v.w[sizeof(v.w) / sizeof(v.w[0]) / 2], x + (loose ? min(at[4], D - 4) : at[4]), 4 * sizeof(T));
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v.set(e, x[at[e]]);
     }
   }
   template <typename T>
-  __device__ __forceinline__ void values(const Piece<T, 8>& x, float (&v)[2 * kPairs]) const {
+  __device__ __forceinline__ void values(const Piece<T, 8>& x, float (&v)[2 * kPairs], int D) const {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = count > (MODE == ROW ? e / 2 : e % kPairs) ? value_of(x, e) : 0.0f;
+    for (int e = 0; e < 8; ++e) v[e] = value_of(x, e);
+    if constexpr (loose) {
+      // towards the front by what the piece was read too early: 0 .. 3 of four, 0 .. 7 of eight features
+      constexpr int N = row ? 8 : 4;
+#pragma unroll
+      for (int q = 0; q < 8; q += N) {
+        const int by = at[q] - min(at[q], D - N);
+#pragma unroll
+        for (int step = 1; step < N; step *= 2) {
+#pragma unroll
+          for (int e = 0; e < N; ++e) v[q + e] = by & step ? (e + step < N ? v[q + e + step] : 0.0f) : v[q + e];
+        }
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = count > (row ? e / 2 : e % kPairs) ? v[e] : 0.0f;
   }
   template <bool PAST, typename T>
   __device__ __forceinline__ void store(T* y, const float (&v)[2 * kPairs]) const {
-    if constexpr (MODE == EACH) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (e % kPairs < count) y[at[e]] = (T)v[e];
-    } else if (count) {
+    if (MODE != EACH && count == kPairs) {
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        T* const to = MODE == ROW ? y + at[0] + 4 * half : y + at[4 * half];
+        T* const to = row ? y + at[0] + 4 * half : y + at[4 * half];
         const float* const w = v + 4 * half;
-        if constexpr (sizeof(T) == 4) store_past<PAST>(reinterpret_cast<f32x4_t*>(to), f32x4_t{w[0], w[1], w[2], w[3]});
-        else store_past<PAST>(reinterpret_cast<u32x2_t*>(to), u32x2_t{pack_bf16(w[0], w[1]), pack_bf16(w[2], w[3])});
+        if constexpr (sizeof(T) == 4) {
+          const f32x4_t x = {w[0], w[1], w[2], w[3]};
+          if constexpr (PAST) __builtin_nontemporal_store(x, reinterpret_cast<f32x4_t*>(to));
+          else __builtin_memcpy(to, &x, 16);
+        } else {
+          const u32x2_t x = {pack_bf16(w[0], w[1]), pack_bf16(w[2], w[3])};
+          if constexpr (PAST) __builtin_nontemporal_store(x, reinterpret_cast<u32x2_t*>(to));
+          else __builtin_memcpy(to, &x, 8);
+        }
       }
+    } else if (MODE == EACH || loose) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (count > (row ? e / 2 : e % kPairs)) y[at[e]] = (T)v[e];
     }
   }
   __device__ __forceinline__ void gains(const float* gain, float (&v)[2 * kPairs]) const {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = gain && count > (MODE == ROW ? e / 2 : e % kPairs) ? gain[at[e]] : 1.0f;
+    for (int e = 0; e < 8; ++e) v[e] = gain && count > (row ? e / 2 : e % kPairs) ? gain[at[e]] : 1.0f;
   }
 };
 
 // whatever the order that they are read in, features are summed in this one: results do not depend on addresses
 template <int MODE>
-__device__ __forceinline__ constexpr int in_order(int e) { return MODE == ROW ? 2 * (e % kPairs) + e / kPairs : e; }
+__device__ __forceinline__ constexpr int in_order(int e) { return Lane<MODE>::row ? 2 * (e % kPairs) + e / kPairs : e; }
 
 // Where a lane group is: slices of rows one after the other, of each the heads some at once.  The next ones are read while these are worked on.
 template <int LANES, int AT_ONCE>
@@ -154,7 +190,7 @@ __global__ __launch_bounds__(256) void head_norm_kernel(const HeadNormParams p) 
   Piece<T, 8> x[kAtOnce];
   const auto read = [&](const Walk<LANES, kAtOnce>& w) {
 #pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) lane.load(head_at<X, const T>(p, w.row, min(w.head(p, i), heads - 1)), x[i]);
+    for (int i = 0; i < kAtOnce; ++i) lane.load(head_at<X, const T>(p, w.row, min(w.head(p, i), heads - 1)), x[i], p.D);
   };
   here.enter(p);
   read(here);
@@ -162,7 +198,7 @@ __global__ __launch_bounds__(256) void head_norm_kernel(const HeadNormParams p) 
   while (true) {
     float v[kAtOnce][8];
 #pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) lane.values(x[i], v[i]);
+    for (int i = 0; i < kAtOnce; ++i) lane.values(x[i], v[i], p.D);
     if (here.begin == here.slice) lane.angles(p, here.row, c, s);
     Walk<LANES, kAtOnce> ahead = here;
     ahead.next(p, heads);
@@ -211,8 +247,8 @@ __global__ __launch_bounds__(256) void head_norm_backward_kernel(const HeadNormP
 #pragma unroll
     for (int i = 0; i < AT_ONCE; ++i) {
       const int h = min(w.head(p, i), heads - 1);
-      lane.load(head_at<X, const T>(p, w.row, h), x[i]);
-      lane.load(head_at<GRAD_OUT, const T>(p, w.row, h), dy[i]);
+      lane.load(head_at<X, const T>(p, w.row, h), x[i], p.D);
+      lane.load(head_at<GRAD_OUT, const T>(p, w.row, h), dy[i], p.D);
     }
   };
   bool more = here.more(p);
@@ -225,8 +261,8 @@ __global__ __launch_bounds__(256) void head_norm_backward_kernel(const HeadNormP
     float v[AT_ONCE][8], d[AT_ONCE][8];
 #pragma unroll
     for (int i = 0; i < AT_ONCE; ++i) {
-      lane.values(x[i], v[i]);
-      lane.values(dy[i], d[i]);
+      lane.values(x[i], v[i], p.D);
+      lane.values(dy[i], d[i], p.D);
     }
     if (here.begin == here.slice) lane.angles(p, here.row, c, s);
     Walk<LANES, AT_ONCE> ahead = here;
@@ -301,39 +337,52 @@ __global__ __launch_bounds__(256) void head_gain_kernel(const HeadNormParams p, 
   if (slice) return;
 #pragma unroll
   for (int s = 1; s < 16; ++s) total += room[s][threadIdx.x % 16];
-  const int e = slot / lanes, pair = kPairs * (slot % lanes) + (MODE == ROW ? e / 2 : e % kPairs), second = MODE == ROW ? e % 2 : e / kPairs;
+  constexpr bool row = Lane<MODE>::row;
+  int count;
+  const int e = slot / lanes, j = row ? e / 2 : e % kPairs, pair = pairs_of(p, slot % lanes, count) + j, second = row ? e % 2 : e / kPairs;
   float* to = t ? p.grad_gain_k : p.grad_gain_q;
-  if (to && pair < p.D / 2) to[feature_of(p, pair, second)] = total;
+  if (to && j < count) to[feature_of(p, pair, second)] = total;
 }
 
-bool quads_aligned(const void* at, const tac_head_strides_t& s, size_t piece, size_t el) {
+bool pieces_aligned(const void* at, const tac_head_strides_t& s, size_t piece, size_t el) {
   return !at || (((uintptr_t)at | (uintptr_t)(s.row * (int64_t)el) | (uintptr_t)(s.head * (int64_t)el)) & (piece - 1)) == 0;
 }
 
 int mode_of(const HeadNormParams& p) {
-  const size_t el = p.bf16 ? 2 : 4, piece = p.interleaved ? 16 : 4 * el;
-  bool aligned = true;
-  for (const HeadTensor* t : {&p.q, &p.k}) {
-    if (!t->heads) continue;
-    aligned &= quads_aligned(t->x, t->x_stride, piece, el) && quads_aligned(t->grad_out, t->grad_out_stride, piece, el) && quads_aligned(t->out, t->out_stride, piece, el);
-  }
-  if (!aligned) return EACH;
-  if (p.interleaved) return p.D % 8 == 0 ? ROW : EACH;
-  return p.rotated % kPairs == 0 && (p.D / 2 - p.rotated) % kPairs == 0 ? QUADS : EACH;
+  if (p.interleaved) return p.D % 8 == 0 ? ROW : p.D > 8 ? LOOSE_ROW : EACH;
+  if (!p.apart || p.D < 4) return EACH;
+  return p.rotated % kPairs == 0 && (p.D / 2 - p.rotated) % kPairs == 0 ? QUADS : LOOSE_QUADS;
 }
 
-// f(lanes, mode) with both as constants
+// lanes, slices and the way past the caches: large results whose pieces start where stores of their size may
+void lay_out(HeadNormParams& p, int& lanes, bool& past) {
+  const HeadLanes l = head_lanes(p.D, p.interleaved ? p.D / 2 : p.rotated);
+  const size_t el = p.bf16 ? 2 : 4;
+  lanes = l.lanes;
+  p.apart = l.apart && !p.interleaved;
+  p.slices = head_slices(p.rows, p.q.heads + p.k.heads, lanes);
+  past = streamed(p.rows * (p.q.heads + p.k.heads) * p.D * (int64_t)el) && pieces_aligned(p.q.out, p.q.out_stride, 4 * el, el) &&
+         (!p.k.heads || pieces_aligned(p.k.out, p.k.out_stride, 4 * el, el));
+  const int mode = mode_of(p);
+  past &= mode == QUADS || mode == ROW;
+}
+
+// f(lanes, mode, past) with all as constants
 template <typename F>
-hipError_t by_shape(const HeadNormParams& p, F f) {
+hipError_t by_shape(const HeadNormParams& p, int lanes, bool past, F f) {
   using std::integral_constant;
-  const auto with = [&](auto lanes) {
+  const auto with = [&](auto l) {
+    const std::false_type here;
+    const std::true_type beyond;
     switch (mode_of(p)) {
-      case QUADS: return f(lanes, integral_constant<int, QUADS>());
-      case ROW: return f(lanes, integral_constant<int, ROW>());
-      default: return f(lanes, integral_constant<int, EACH>());
+      case QUADS: return past ? f(l, integral_constant<int, QUADS>(), beyond) : f(l, integral_constant<int, QUADS>(), here);
+      case ROW: return past ? f(l, integral_constant<int, ROW>(), beyond) : f(l, integral_constant<int, ROW>(), here);
+      case LOOSE_QUADS: return f(l, integral_constant<int, LOOSE_QUADS>(), here);
+      case LOOSE_ROW: return f(l, integral_constant<int, LOOSE_ROW>(), here);
+      default: return f(l, integral_constant<int, EACH>(), here);
     }
   };
-  switch (head_lanes(p.D)) {
+  switch (lanes) {
     case 8: return with(integral_constant<int, 8>());
     case 16: return with(integral_constant<int, 16>());
     case 32: return with(integral_constant<int, 32>());
@@ -345,38 +394,39 @@ hipError_t by_shape(const HeadNormParams& p, F f) {
 
 hipError_t head_norm_launch(const HeadNormParams& given, hipStream_t s) {
   HeadNormParams p = given;
-  const int lanes = head_lanes(p.D);
-  p.slices = head_slices(p.rows, p.q.heads + p.k.heads, lanes);
+  int lanes;
+  bool past;
+  lay_out(p, lanes, past);
   const unsigned groups = (unsigned)head_groups(p.rows, p.slices, lanes, kHeadGroups);
-  const bool past = streamed(p.rows * (p.q.heads + p.k.heads) * p.D * (p.bf16 ? 2 : 4));
-  return by_shape(p, [&](auto l, auto m) {
+  return by_shape(p, lanes, past, [&](auto l, auto m, auto beyond) {
     constexpr int L = decltype(l)::value, M = decltype(m)::value;
-    if (p.bf16 && past) hipLaunchKernelGGL((head_norm_kernel<bf16, L, M, true>), dim3(groups), dim3(256), 0, s, p);
-    else if (p.bf16) hipLaunchKernelGGL((head_norm_kernel<bf16, L, M, false>), dim3(groups), dim3(256), 0, s, p);
-    else if (past) hipLaunchKernelGGL((head_norm_kernel<float, L, M, true>), dim3(groups), dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((head_norm_kernel<float, L, M, false>), dim3(groups), dim3(256), 0, s, p);
+    constexpr bool PAST = decltype(beyond)::value;
+    if (p.bf16) hipLaunchKernelGGL((head_norm_kernel<bf16, L, M, PAST>), dim3(groups), dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((head_norm_kernel<float, L, M, PAST>), dim3(groups), dim3(256), 0, s, p);
     return hipGetLastError();
   });
 }
 
-size_t head_norm_workspace(int64_t rows, int heads, int D) {
-  const int lanes = head_lanes(D);
-  return (size_t)head_groups(rows, head_slices(rows, heads, lanes), lanes, kHeadBackwardGroups) * 2 * 8 * (size_t)lanes * sizeof(float);
+size_t head_norm_workspace(const HeadNormParams& given) {
+  HeadNormParams p = given;
+  int lanes;
+  bool past;
+  lay_out(p, lanes, past);
+  return (size_t)head_groups(p.rows, p.slices, lanes, kHeadBackwardGroups) * 2 * 8 * (size_t)lanes * sizeof(float);
 }
 
 hipError_t head_norm_backward_launch(const HeadNormParams& given, hipStream_t s) {
   HeadNormParams p = given;
-  const int lanes = head_lanes(p.D);
-  p.slices = head_slices(p.rows, p.q.heads + p.k.heads, lanes);
+  int lanes;
+  bool past;
+  lay_out(p, lanes, past);
   const unsigned groups = (unsigned)head_groups(p.rows, p.slices, lanes, kHeadBackwardGroups);
   if (!p.grad_gain_q && !p.grad_gain_k) p.partial = nullptr;
-  const bool past = streamed(p.rows * (p.q.heads + p.k.heads) * p.D * (p.bf16 ? 2 : 4));
-  return by_shape(p, [&](auto l, auto m) {
+  return by_shape(p, lanes, past, [&](auto l, auto m, auto beyond) {
     constexpr int L = decltype(l)::value, M = decltype(m)::value;
-    if (p.bf16 && past) hipLaunchKernelGGL((head_norm_backward_kernel<bf16, L, M, true>), dim3(groups), dim3(256), 0, s, p);
-    else if (p.bf16) hipLaunchKernelGGL((head_norm_backward_kernel<bf16, L, M, false>), dim3(groups), dim3(256), 0, s, p);
-    else if (past) hipLaunchKernelGGL((head_norm_backward_kernel<float, L, M, true>), dim3(groups), dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((head_norm_backward_kernel<float, L, M, false>), dim3(groups), dim3(256), 0, s, p);
+    constexpr bool PAST = decltype(beyond)::value;
+    if (p.bf16) hipLaunchKernelGGL((head_norm_backward_kernel<bf16, L, M, PAST>), dim3(groups), dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((head_norm_backward_kernel<float, L, M, PAST>), dim3(groups), dim3(256), 0, s, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !p.partial) return e;
     hipLaunchKernelGGL((head_gain_kernel<M>), dim3(L / 2, p.k.heads ? 2 : 1), dim3(256), 0, s, p, (int)groups, L);

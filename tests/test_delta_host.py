@@ -89,6 +89,22 @@ def test_head_norm_backward_refuses(kw, status):
     assert head_norm_backward(**kw) == getattr(api, "TAC_ERR_" + status)
 
 
+def test_head_norm_refuses_outputs_on_other_tensors():
+    a = [P + 4096 * i for i in range(8)]
+    f = dict(query=a[0], key=a[1], out_query=a[2], out_key=a[3])
+    for kw in (dict(out_query=a[1]), dict(out_key=a[0]), dict(out_key=a[2])):
+        assert head_norm(**{**f, **kw}) == api.TAC_ERR_BAD_PARAM
+    b = dict(query=a[0], key=a[1], grad_out_query=a[2], grad_out_key=a[3], grad_query_at=a[4], grad_key_at=a[5])
+    for kw in (dict(grad_query_at=a[0]), dict(grad_query_at=a[1]), dict(grad_query_at=a[3]), dict(grad_key_at=a[0]), dict(grad_key_at=a[1]), dict(grad_key_at=a[2]), dict(grad_key_at=a[4])):
+        assert head_norm_backward(**{**b, **kw}) == api.TAC_ERR_BAD_PARAM
+    call = lambda d, q, k, oq, ok: api.lib().tac_head_norm(ctypes.byref(d), q, k, P, P, P, oq, ok, None)
+    assert call(heads_desc(out_query=(128, 16)), a[0], a[1], a[0], a[3]) == api.TAC_ERR_BAD_PARAM          # in place with other strides
+    assert call(heads_desc(out_key=(16, 80)), a[0], a[1], a[2], a[1]) == api.TAC_ERR_BAD_PARAM
+    back = lambda d, gq, gk: api.lib().tac_head_norm_backward(ctypes.byref(d), a[0], a[1], P, P, P, a[2], a[3], gq, gk, P, P, P, None)
+    assert back(heads_desc(grad_query=(128, 16)), a[2], a[5]) == api.TAC_ERR_BAD_PARAM
+    assert back(heads_desc(grad_key=(16, 80)), a[4], a[3]) == api.TAC_ERR_BAD_PARAM
+
+
 def test_what_is_ignored_may_be_anything():
     """No keys, no rotation, no gain's gradient: their pointers and sizes do not count.  Refused by the features alone, so that nothing is launched."""
     bad = dict(D=15)

@@ -24,10 +24,16 @@ def shim(tmp_path_factory):
     return L
 
 
-@pytest.mark.parametrize("D", list(range(2, api.TAC_HEAD_MAX_FEATURES + 1, 2)))
+@pytest.mark.parametrize("D", [2, 4, 6, 16, 62, 64, 66, 126, 128, 130, 250, 256, 258, 508, 510, 512])
 def test_a_heads_lanes_hold_its_pairs(shim, D):
-    lanes = shim.head_lanes_of(D)
-    assert lanes in (8, 16, 32, 64) and 4 * lanes >= D // 2
+    for rotated in range(D // 2 + 1):
+        lanes, apart = shim.head_lanes_of(D, rotated), shim.head_apart_of(D, rotated)
+        assert lanes in (8, 16, 32, 64)
+        if apart:                                    # pairs of both kinds on lanes of their own
+            assert -(-rotated // 4) + -(-(D // 2 - rotated) // 4) <= lanes
+        else:
+            assert 4 * lanes >= D // 2
+        assert apart or D > 500
 
 
 def test_slices_and_groups_of_heads(shim):

@@ -115,6 +115,28 @@ def test_without_norm_rotation_gain_or_keys(dtype):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("D,sections", [(4, (1,)), (8, (3,)), (10, (5,)), (18, (2, 3)), (70, (9,)), (254, (31, 1, 70)), (512, (254, 1))])
+def test_heads_that_are_no_whole_pieces(D, sections, interleaved, dtype):
+    """Odd numbers of pairs, rows at any address with NaN between them: the same values as from whole rows, and nothing beside the results is written."""
+    rows, hq, hk = 9, 3, 1
+    q, k, gq, gk, dq, dk = make(rows, hq, hk, D, dtype, 20 + D)
+    how = dict(eps=EPS, positions=positions_of(rows, len(sections), 200), sections=sections, interleaved=interleaved)
+    plain, _ = check(q, k, gq, gk, how, sections)
+    back = api.tac_head_norm_backward(q.contiguous(), k.contiguous(), gq, gk, dq, dk, **how)
+    pad = lambda t, by=3: torch.nn.functional.pad(t, (1, by), value=float("nan"))
+    inner = lambda t: t[..., 1:1 + D]
+    room = {n: torch.full((rows, h, D + 4), 7.0, dtype=dtype, device=DEV) for n, h in (("q", hq), ("k", hk))}
+    got = api.tac_head_norm(inner(pad(q)), inner(pad(k)), gq, gk, out_query=inner(room["q"]), out_key=inner(room["k"]), **how)
+    for n in got:
+        assert torch.equal(got[n], plain[n])
+        assert (room[n][..., 0] == 7).all() and (room[n][..., 1 + D:] == 7).all()
+    again = api.tac_head_norm_backward(inner(pad(q)), inner(pad(k)), gq, gk, inner(pad(dq)), inner(pad(dk)), grad_query=inner(room["q"]), grad_key=inner(room["k"]), **how)
+    assert all(torch.equal(again[n], back[n]) for n in back)
+    assert all((t[..., 0] == 7).all() and (t[..., 1 + D:] == 7).all() for t in room.values())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("interleaved", [False, True])
 def test_strides_addresses_and_in_place(interleaved, dtype):
     rows, hq, hk, D = 21, 3, 2, 64
     q, k, gq, gk, dq, dk = make(rows, hq, hk, D, dtype, 10)
