@@ -94,7 +94,7 @@ __device__ __forceinline__ void scan_states(const DeltaParams& p, const ScanPlac
       float own[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) own[e] = e / 4 < OWN ? S[e / 4 < OWN ? e / 4 : 0][t][e % 4] : 0.0f;
-      const Parts<3> op = split<3>(own);
+      const Parts<3> op = split<3, false>(own);
       if (owner) {
 #pragma unroll
         for (int m = 0; m < OWN; ++m)

@@ -372,46 +372,30 @@ __global__ __launch_bounds__(512) void back_scan_kernel(const DeltaParams p, int
 }
 
 // LDS of gradient_kernel in bfloat16 numbers.  While values' features are summed over, 32 at a time: S and dS [OUT][DK][40], U and R [OUT][64][40], dO [IN][64][40]; then K or Q
-// transposed [IN][DK][kSteps], Z and its transpose, Y or its transpose [OUT][64][kSteps] each; at last the gradients, [2][64][DK + 8] elements.
+// [IN][64][turned_pitch], Z and Y transposed [OUT][64][kSteps] each; at last the gradients, [2][64][DK + 8] elements.
 template <typename T, int DK>
 struct GradientRoom {
   static constexpr int IN = Kind<T>::in, OUT = Kind<T>::out, pitch = 40, out_pitch = DK + 8;
-  static constexpr int s_plane = DK * pitch, u_plane = kChunk * pitch, k_plane = DK * kSteps, y_plane = kChunk * kSteps;
+  static constexpr int s_plane = DK * pitch, u_plane = kChunk * pitch, k_pitch = turned_pitch(DK), k_plane = kChunk * k_pitch, y_plane = kChunk * kSteps;
   static constexpr int s = 0, back = s + OUT * s_plane, u = back + OUT * s_plane, r = u + OUT * u_plane, g = r + OUT * u_plane, first_size = g + IN * u_plane;
-  static constexpr int k = 0, z = k + IN * k_plane, z_turned = z + OUT * y_plane, y = z_turned + OUT * y_plane, second_size = y + OUT * y_plane;
+  static constexpr int k = 0, z = k + IN * k_plane, y = z + OUT * y_plane, second_size = y + OUT * y_plane;
   static constexpr int third_size = 2 * kChunk * out_pitch * (int)sizeof(T) / 2;
   static constexpr int most = first_size > second_size ? first_size : second_size, bytes = 2 * (most > third_size ? most : third_size);
 };
 
-// rows 4 quad .. of column `col` of a 16 x 16 result, to planes [rows][kSteps] as it stands
+// four steps of a feature, from what stands as rows
 template <int PARTS>
-__device__ __forceinline__ void result_to_planes(bf16* to, int plane, const f32x4_t& v, int row, int col) {
-  u32x2_t q[PARTS];
-  split_quad<PARTS>(v, q);
-#pragma unroll
-  for (int i = 0; i < PARTS; ++i) {
-    uint16_t* at = (uint16_t*)(to + i * plane) + row * kSteps + col;
-    at[0] = (uint16_t)q[i][0];
-    at[kSteps] = (uint16_t)(q[i][0] >> 16);
-    at[2 * kSteps] = (uint16_t)q[i][1];
-    at[3 * kSteps] = (uint16_t)(q[i][1] >> 16);
-  }
-}
-
-// four steps of one feature from planes [features][kSteps], whole numbers again
-template <int PARTS>
-__device__ __forceinline__ f32x4_t steps_from_planes(const bf16* at, int plane) {
+__device__ __forceinline__ f32x4_t steps_of_rows(const bf16* rows, int plane, int pitch, int step, int col, int lane) {
+  u32x2_t w[PARTS];
+  turned_quad(w, rows, plane, pitch, step, col, lane);
   f32x4_t v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-  for (int i = PARTS - 1; i >= 0; --i) {
-    const u32x2_t w = *reinterpret_cast<const u32x2_t*>(at + i * plane);
-    v += f32x4_t{bits_float(w[0] << 16), bits_float(w[0] & 0xffff0000u), bits_float(w[1] << 16), bits_float(w[1] & 0xffff0000u)};
-  }
+  for (int i = PARTS - 1; i >= 0; --i) v += f32x4_t{bits_float(w[i][0] << 16), bits_float(w[i][0] & 0xffff0000u), bits_float(w[i][1] << 16), bits_float(w[i][1] & 0xffff0000u)};
   return v;
 }
 
 // One chunk of a head of queries and keys, the heads of values that share it one after the other.  Eight waves: wave w of either four has the steps from 16 w on as rows and half of a
-// key's features as columns, the first four form Y, the others Z.  All that is summed over values comes through LDS, whole lines at a time and a step ahead.
+// key's features as columns, the first four form Y, the others Z.  All that is summed over values comes through LDS, whole lines at a time and two steps ahead.
 // MODE: of pieces of 8 of a key and of 4 of a value.
 template <typename T, int DK, int MODE>
 __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
@@ -420,10 +404,10 @@ __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
   extern __shared__ __align__(16) uint8_t lds[];
   __shared__ float high[kChunk], low[kChunk], change[2][kChunk], both[8];
   bf16* const L = (bf16*)lds;
-  const int hk = blockIdx.x % p.k_heads, b = blockIdx.x / p.k_heads % p.B;
-  const int64_t chunk = blockIdx.x / p.k_heads / p.B, from = chunk * kChunk;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64 % 4), half = __builtin_amdgcn_readfirstlane(threadIdx.x / 256);
   const int group = p.v_heads / p.k_heads;
+  const int hk = blockIdx.x % p.k_heads, b = blockIdx.x / p.k_heads % p.B;
+  const int64_t chunk = blockIdx.x / p.k_heads / p.B, from = chunk * kChunk;
   const int n = steps_of(p, b, from), here = (int)min((int64_t)kChunk, p.T - from);
   T* const gq = (T*)p.grad_q + from * p.grad_q_at.t + (int64_t)b * p.grad_q_at.b + (int64_t)hk * p.grad_q_at.head;
   T* const gk = (T*)p.grad_k + from * p.grad_k_at.t + (int64_t)b * p.grad_k_at.b + (int64_t)hk * p.grad_k_at.head;
@@ -454,26 +438,17 @@ __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
       load_piece<MODE>(query[s], q, 32 * (piece0 + s) + 8 * quad, p.Dk);
     }
   };
-  const auto turn = [&](const Piece<T, 8>(&x)[KS], int lane) {      // this half's features transposed
-    const Identity id(lane);
-    const int low16 = lane & 15, rows = 16 * wave + 4 * (lane >> 4);
+  const auto keep = [&](const Piece<T, 8>(&x)[KS], int lane) {      // this half's features
+    const int row = 16 * wave + lane % 16;
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-      const Parts<IN> a = parts_of(arranged<MODE>(x[s], 32 * (piece0 + s) + 8 * (lane >> 4), p.Dk));
+      const int col = 32 * (piece0 + s) + 8 * (lane / 16);
+      if (NT == 1 && lane / 32 != half) continue;
+      const Parts<IN> a = parts_of(zero_ended<MODE>(x[s], col, p.Dk));
 #pragma unroll
-      for (int odd = 0; odd < 2; ++odd) {
-        if (NT == 1 && odd != half) continue;
-        const int col = 32 * (piece0 + s) + 16 * odd + low16;
-#pragma unroll
-        for (int i = 0; i < IN; ++i) {
-          f32x4_t t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], odd ? id.odd.p[0] : id.even.p[0], f32x4_t{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
-          if (col >= p.Dk) t = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-          *reinterpret_cast<u32x2_t*>(L + Room::k + i * Room::k_plane + col * kSteps + rows) = u32x2_t{pack_bf16(t[0], t[1]), pack_bf16(t[2], t[3])};
-        }
-      }
+      for (int i = 0; i < IN; ++i) *reinterpret_cast<bf16x8_t*>(L + Room::k + i * Room::k_plane + row * Room::k_pitch + col) = a.p[i];
     }
   };
-  f32x4_t* const shared = (f32x4_t*)p.shared + (int64_t)blockIdx.x * (2 * NT * 512);      // [2 NT][threads]: a thread's sums over the values' heads before
 
   // What a thread brings of S and dS (eight of a row), U, R and dO (four of a row): two steps of 32 values are on their way, of the next head too.
   struct Brought {
@@ -481,12 +456,15 @@ __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
     Piece<T, 4> g;
   } brought[2];
   const int steps = (p.Dv + 31) / 32, even_steps = (steps + 1) / 2 * 2;
+  // where its rows are in the chunk's head: products of 64 bits once for many pieces
+  const int state_row = min((int)threadIdx.x / 4, p.Dk - 1) * p.Dv;
+  const int64_t own_row = min((int)threadIdx.x / 8, n - 1), update_row = own_row * p.B * p.v_heads * p.Dv, grad_row = own_row * p.out_at.t;
   const auto bring = [&](Brought& x, int h, int step) {
-    const int tid = fresh(threadIdx.x), s_row = tid / 4, s_col = 8 * (tid % 4), u_row = tid / 8, u_col = 4 * (tid % 8);
+    const int tid = fresh(threadIdx.x), s_col = 8 * (tid % 4), u_col = 4 * (tid % 8);
     const int64_t head = (int64_t)b * p.v_heads + h;
-    const int64_t state = (chunk * p.B * p.v_heads + head) * (int64_t)p.Dk * p.Dv + (int64_t)min(s_row, p.Dk - 1) * p.Dv;
-    const int64_t update = ((from + min(u_row, n - 1)) * p.B * p.v_heads + head) * p.Dv;
-    const T* const go = (const T*)p.grad_out + (from + min(u_row, n - 1)) * p.out_at.t + (int64_t)b * p.out_at.b + (int64_t)h * p.out_at.head;
+    const int64_t state = (chunk * p.B * p.v_heads + head) * (int64_t)p.Dk * p.Dv + state_row;
+    const int64_t update = (from * p.B * p.v_heads + head) * p.Dv + update_row;
+    const T* const go = (const T*)p.grad_out + (from * p.out_at.t + (int64_t)b * p.out_at.b + (int64_t)h * p.out_at.head) + grad_row;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       load_piece<MODE>(x.s[i], p.states + state, 32 * step + s_col + 4 * i, p.Dv);
@@ -498,6 +476,7 @@ __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
   };
   bring(brought[0], hk * group, 0);
   bring(brought[1], hk * group, 1);
+  f32x4_t* const shared = (f32x4_t*)p.shared + (int64_t)blockIdx.x * (2 * NT * 512);      // [2 NT][threads]: a thread's sums over the values' heads before
 
   for (int member = 0; member < group; ++member) {
     const int h = hk * group + member;
@@ -510,10 +489,7 @@ __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
     const float whole = room.start[kChunk - 1];
     const T gate = ((const T*)p.gate)[(from + min(kChunk - 1 - lane, n - 1)) * p.gate_at.t + (int64_t)b * p.gate_at.b + h];
     const T write = ((const T*)p.write)[(from + min(u_row, n - 1)) * p.write_at.t + (int64_t)b * p.write_at.b + h];
-    if (tid < kChunk) {
-      high[tid] = room.high[tid];
-      low[tid] = room.low[tid];
-    }
+    const float own_high = room.high[tid % kChunk], own_low = room.low[tid % kChunk];      // used behind the products: to wait for them here is to wait for what was brought
     load_rows();
     f32x4_t w[4], dq[NT], reads[NT], writes[NT];      // w: Y or Z
 #pragma unroll
@@ -522,7 +498,8 @@ __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
     for (int i = 0; i < NT; ++i) dq[i] = reads[i] = writes[i] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     float written = 0.0f, kept = 0.0f;               // R . U of step u_row, <S, dS>: this thread's parts
 
-    for (int pair = 0; pair < even_steps; pair += 2) {
+    int pair = 0;
+    do {                                               // at least once, and known to be: otherwise what is loaded around it would be waited for together
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         const int step = pair + k, v = 32 * step;
@@ -539,10 +516,18 @@ __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
           }
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const bool there = v + s_col + e < p.Dv;
-            s[e] = there ? ps[e / 4].w[e % 4] : 0.0f;
-            d[e] = there ? pd[e / 4].w[e % 4] : 0.0f;
-            kept = fmaf(s[e], s_row < p.Dk ? d[e] : 0.0f, kept);
+            s[e] = ps[e / 4].w[e % 4];               // behind the last value stand numbers of the row, beside zeros of U, R and dO
+            d[e] = pd[e / 4].w[e % 4];
+          }
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float one = s[4 * i + e] * d[4 * i + e];
+              sum += MODE == WHOLE || v + s_col + 4 * i + e < p.Dv ? one : 0.0f;
+            }
+            kept += MODE != WHOLE || v + s_col + 4 * i < p.Dv ? sum : 0.0f;
           }
           if (s_row < DK) {
             const Parts<OUT> a = split<OUT>(s), c = split<OUT>(d);
@@ -593,8 +578,13 @@ __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
           }
         }
       }
+      pair += 2;
+    } while (pair < even_steps);
+    if (tid < kChunk) {
+      high[tid] = own_high;
+      low[tid] = own_low;
     }
-
+    __syncthreads();                                 // S, dS, U, R and dO have been read: K, Z and Y take their place
 #pragma unroll
     for (int i = 0; i < NT; ++i)
 #pragma unroll
@@ -614,19 +604,17 @@ __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
         if (half ? j >= t : j > t) w[i][r] = 0.0f;
       }
     }
-    __syncthreads();                                 // S, dS, U, R and dO have been read: K, Z and Y take their place
-    turn(key, lane);
+    keep(key, lane);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int j = 16 * i + low16;
-      result_to_planes<OUT>(L + (half ? Room::z : Room::y), Room::y_plane, w[i], rows, j);
-      if (half) quad_to_planes<OUT>(L + Room::z_turned + j * kSteps + rows, Room::y_plane, w[i]);
+      quad_to_planes<OUT>(L + (half ? Room::z : Room::y) + j * kSteps + rows, Room::y_plane, w[i]);
     }
     __syncthreads();
     f32x4_t dG = {0.0f, 0.0f, 0.0f, 0.0f}, leaves = dG, kept_key[NT];      // of the four steps of this lane's results: a part over the features
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-      kept_key[i] = steps_from_planes<IN>(L + Room::k + (16 * (tile0 + i) + low16) * kSteps + rows, Room::k_plane);
+      kept_key[i] = steps_of_rows<IN>(L + Room::k, Room::k_plane, Room::k_pitch, rows, 16 * (tile0 + i), lane);
       leaves += kept_key[i] * writes[i];
     }
 #pragma unroll
@@ -635,13 +623,13 @@ __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
       const bool lower = 2 * s <= wave, upper = 2 * s + 1 >= wave;      // whether these 32 columns of Y and Z, and of Z transposed, hold something
       Parts<OUT> a, c, d;
       if (lower) {
-        a = from_planes<OUT>(L + Room::y + row * kSteps + at, Room::y_plane);
-        c = from_planes<OUT>(L + Room::z + row * kSteps + at, Room::y_plane);
+        a = turned<OUT>(L + Room::y, Room::y_plane, kSteps, 32 * s, 16 * wave, lane);
+        c = turned<OUT>(L + Room::z, Room::y_plane, kSteps, 32 * s, 16 * wave, lane);
       }
-      if (upper) d = from_planes<OUT>(L + Room::z_turned + row * kSteps + at, Room::y_plane);
+      if (upper) d = from_planes<OUT>(L + Room::z + row * kSteps + at, Room::y_plane);
 #pragma unroll
       for (int i = 0; i < NT; ++i) {
-        const Parts<IN> o = from_planes<IN>(L + Room::k + (16 * (tile0 + i) + low16) * kSteps + at, Room::k_plane);
+        const Parts<IN> o = turned<IN>(L + Room::k, Room::k_plane, Room::k_pitch, 32 * s, 16 * (tile0 + i), lane);
         if (lower) {
           multiply<OUT>(dq[i], a, o);
           multiply<OUT>(reads[i], c, o);
@@ -651,12 +639,8 @@ __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
     }
 #pragma unroll
     for (int i = 0; i < NT; ++i) dG += kept_key[i] * reads[i];
-    __syncthreads();                                 // K and Y have been read: Q and Y transposed take their place
-    turn(query, lane);
-    if (!half) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) quad_to_planes<OUT>(L + Room::y + (16 * i + low16) * kSteps + rows, Room::y_plane, w[i]);
-    }
+    __syncthreads();                                 // K has been read: Q takes its place
+    keep(query, lane);
     __syncthreads();
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
@@ -664,15 +648,15 @@ __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
       const int at = 32 * s + 8 * quad;
       const Parts<OUT> a = from_planes<OUT>(L + Room::y + row * kSteps + at, Room::y_plane);
 #pragma unroll
-      for (int i = 0; i < NT; ++i) multiply<OUT>(writes[i], a, from_planes<IN>(L + Room::k + (16 * (tile0 + i) + low16) * kSteps + at, Room::k_plane));
+      for (int i = 0; i < NT; ++i) multiply<OUT>(writes[i], a, turned<IN>(L + Room::k, Room::k_plane, Room::k_pitch, 32 * s, 16 * (tile0 + i), lane));
     }
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-      dG += steps_from_planes<IN>(L + Room::k + (16 * (tile0 + i) + low16) * kSteps + rows, Room::k_plane) * dq[i];
+      dG += steps_of_rows<IN>(L + Room::k, Room::k_plane, Room::k_pitch, rows, 16 * (tile0 + i), lane) * dq[i];
       dG -= kept_key[i] * writes[i];
     }
     // sums over this half's features: 16 lanes; over a step's values: 8 threads; over everything
-    kept = sum_over_lanes<64>(kept);
+    kept = sum_over_lanes<64>(s_row < p.Dk ? kept : 0.0f);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       dG[r] = sum_over_lanes<16>(dG[r]);
@@ -712,25 +696,33 @@ __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
     }
     const bool last = member + 1 == group;
 #pragma unroll
-    for (int i = 0; i < NT; ++i) {
-      f32x4_t a = dq[i], d = reads[i] + writes[i];
-      f32x4_t* const kept_q = shared + 2 * i * 512;
-      f32x4_t* const kept_k = kept_q + 512;
-      if (member) {
-        a += kept_q[tid];
-        d += kept_k[tid];
+    for (int i = 0; i < NT; ++i) reads[i] += writes[i];
+    if (member) {
+      f32x4_t before[2 * NT];                        // all on their way together
+#pragma unroll
+      for (int i = 0; i < 2 * NT; ++i) before[i] = shared[i * 512 + tid];
+      in_this_order();
+#pragma unroll
+      for (int i = 0; i < NT; ++i) {
+        dq[i] += before[2 * i];
+        reads[i] += before[2 * i + 1];
       }
-      if (!last) {
-        kept_q[tid] = a;
-        kept_k[tid] = d;
-      } else {                                       // every wave has read Q and Y
+    }
+    if (!last) {
+#pragma unroll
+      for (int i = 0; i < NT; ++i) {
+        shared[2 * i * 512 + tid] = dq[i];
+        shared[(2 * i + 1) * 512 + tid] = reads[i];
+      }
+    } else {                                         // every wave has read Q and Y
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           T* const to = (T*)lds + (rows + r) * Room::out_pitch + 16 * (tile0 + i) + low16;
-          to[0] = (T)a[r];
-          to[kChunk * Room::out_pitch] = (T)d[r];
+          to[0] = (T)dq[i][r];
+          to[kChunk * Room::out_pitch] = (T)reads[i][r];
         }
-      }
     }
   }
   __syncthreads();

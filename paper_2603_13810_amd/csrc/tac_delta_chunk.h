@@ -17,7 +17,8 @@ struct Parts {
   bf16x8_t p[PARTS];
 };
 
-template <int PARTS>
+// PAIRS: two numbers an instruction, a fifth fewer of them; one by one each waits for less, for the chain of states (32768 steps: 991 us, in pairs 1014)
+template <int PARTS, bool PAIRS = true>
 __device__ __forceinline__ Parts<PARTS> split(const float (&v)[8]) {
   Parts<PARTS> r;
   float rest[8];
@@ -25,10 +26,24 @@ __device__ __forceinline__ Parts<PARTS> split(const float (&v)[8]) {
   for (int e = 0; e < 8; ++e) rest[e] = v[e];
 #pragma unroll
   for (int q = 0; q < PARTS; ++q) {
+    if constexpr (PAIRS) {
+      u32x4_t w;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      r.p[q][e] = (bf16)rest[e];
-      if (q + 1 < PARTS) rest[e] -= (float)r.p[q][e];
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t two = pack_bf16(rest[2 * e], rest[2 * e + 1]);
+        w[e] = two;
+        if (q + 1 < PARTS) {
+          rest[2 * e] -= bits_float(two << 16);
+          rest[2 * e + 1] -= bits_float(two & 0xffff0000u);
+        }
+      }
+      r.p[q] = __builtin_bit_cast(bf16x8_t, w);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        r.p[q][e] = (bf16)rest[e];
+        if (q + 1 < PARTS) rest[e] -= (float)r.p[q][e];
+      }
     }
   }
   return r;
@@ -74,39 +89,6 @@ struct Kind<bf16> {
 template <>
 struct Kind<float> {
   static constexpr int in = 3, out = 3;
-};
-
-// Eight neighbours of a tensor's row as they stand in memory, and their parts.  `n` of them are there (none: zeros).
-template <typename T>
-struct Eight;
-template <>
-struct Eight<bf16> {
-  u32x4_t v;
-  __device__ __forceinline__ void load(const bf16* p, int n) {
-    if (n >= 8) {
-      __builtin_memcpy(&v, p, 16);
-      return;
-    }
-    v = u32x4_t{0, 0, 0, 0};
-    const uint16_t* at = (const uint16_t*)p;
-#pragma unroll
-    for (int e = 0; e < 7; ++e)
-      if (e < n) v[e / 2] |= (uint32_t)at[e] << 16 * (e % 2);
-  }
-  __device__ __forceinline__ Parts<1> parts() const { return {__builtin_bit_cast(bf16x8_t, v)}; }
-};
-template <>
-struct Eight<float> {
-  float v[8];
-  __device__ __forceinline__ void load(const float* p, int n) {
-    if (n >= 8) {
-      __builtin_memcpy(v, p, 32);
-      return;
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = e < n ? p[e] : 0.0f;
-  }
-  __device__ __forceinline__ Parts<3> parts() const { return split<3>(v); }
 };
 
 // operand from LDS: rows of `pitch` bfloat16, one plane per part
@@ -157,6 +139,28 @@ __device__ __forceinline__ void transpose_to(bf16* to, int plane, const Parts<PA
       *reinterpret_cast<u32x2_t*>(at + q * plane) = u32x2_t{pack_bf16(t[0], t[1]), pack_bf16(t[2], t[3])};
     }
   }
+}
+
+// What stands in LDS as rows of steps (planes of bfloat16 parts), read turned.  Of the 16 lanes that read together each brings four neighbours of a row, four lanes a row, and gets four
+// rows of its own column: here steps from `step` on of column `col` + lane % 16.
+constexpr int turned_pitch(int features) { return features + (features == 64 ? 8 : 24); }      // of 32, 64, 128: four rows' 32 bytes meet on no bank
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+template <int PARTS>
+__device__ __forceinline__ void turned_quad(u32x2_t (&to)[PARTS], const bf16* rows, int plane, int pitch, int step, int col, int lane) {
+  const bf16* const at = rows + (step + (lane & 15) / 4) * pitch + col + 4 * (lane & 3);
+#pragma unroll
+  for (int i = 0; i < PARTS; ++i) to[i] = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(at + i * plane)));
+}
+// as an operand: rows are the columns from `col` on, summed indices the steps from `step` on
+template <int PARTS>
+__device__ __forceinline__ Parts<PARTS> turned(const bf16* rows, int plane, int pitch, int step, int col, int lane) {
+  u32x2_t a[PARTS], b[PARTS];
+  turned_quad(a, rows, plane, pitch, step + 8 * (lane >> 4), col, lane);
+  turned_quad(b, rows, plane, pitch, step + 8 * (lane >> 4) + 4, col, lane);
+  Parts<PARTS> r;
+#pragma unroll
+  for (int i = 0; i < PARTS; ++i) r.p[i] = __builtin_bit_cast(bf16x8_t, u32x4_t{a[i][0], a[i][1], b[i][0], b[i][1]});
+  return r;
 }
 
 // Everything that was asked for from memory is there.  In front of a loop whose loads stay on their way: the compiler would otherwise keep the wait for what was
@@ -217,7 +221,8 @@ struct HeadTile {
 };
 
 __device__ __forceinline__ int steps_of(const DeltaParams& p, int b, int64_t from) {      // steps of the chunk that begins at `from`
-  const int64_t n = p.lengths ? min((int64_t)max(p.lengths[b], 0), p.T) : p.T;
+  // by a scalar load: to wait for a vector one is to wait for all that were asked for before it
+  const int64_t n = p.lengths ? min((int64_t)max(*(const __attribute__((address_space(4))) int32_t*)(uintptr_t)(p.lengths + b), 0), p.T) : p.T;
   return (int)max((int64_t)0, min((int64_t)kChunk, n - from));
 }
 
@@ -274,7 +279,7 @@ __device__ __forceinline__ void load_piece(Piece<T, N>& v, const T* row, int at,
 template <int MODE, typename T, int N>
 __device__ __forceinline__ Piece<T, N> arranged(const Piece<T, N>& v, int at, int n) {
   if constexpr (MODE != SHIFTED) return v;
-  const int by = at - min(at, n - N);                 // elements; N and more: nothing of the piece is there
+  const int by = at - min(at, n - N);                 // elements; N and more: nothing of the piece is there, and what is returned is of the row
   constexpr int words = N * sizeof(T) / 4, per = 4 / sizeof(T);
   Piece<T, N> r = v;
   if constexpr (per == 2) {
@@ -286,6 +291,21 @@ __device__ __forceinline__ Piece<T, N> arranged(const Piece<T, N>& v, int at, in
     const bool on = (by / per) & step;
 #pragma unroll
     for (int i = 0; i < words; ++i) r.w[i] = on ? (i + step < words ? r.w[i + step] : std::remove_reference_t<decltype(r.w[0])>()) : r.w[i];
+  }
+  return r;
+}
+
+// zeros behind the row's end
+template <int MODE, typename T, int N>
+__device__ __forceinline__ Piece<T, N> zero_ended(const Piece<T, N>& v, int at, int n) {
+  Piece<T, N> r = arranged<MODE>(v, at, n);
+  if constexpr (MODE != EACH) {
+#pragma unroll
+    for (int i = 0; i < (int)(N * sizeof(T) / 4); ++i) r.w[i] = at < n ? r.w[i] : std::remove_reference_t<decltype(r.w[0])>();
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (at + e >= n) r.set(e, (T)0.0f);
   }
   return r;
 }
@@ -337,14 +357,6 @@ __device__ __forceinline__ Parts<3> parts_of(const Piece<float, 4>& a, const Pie
   const float v[8] = {a.w[0], a.w[1], a.w[2], a.w[3], b.w[0], b.w[1], b.w[2], b.w[3]};
   return split<3>(v);
 }
-template <int PARTS>
-__device__ __forceinline__ Parts<PARTS> first_parts(const Parts<3>& a) {
-  Parts<PARTS> r;
-#pragma unroll
-  for (int i = 0; i < PARTS; ++i) r.p[i] = a.p[i];
-  return r;
-}
-
 constexpr int kSums = kChunk + 4;             // pitch of LDS rows of a chunk's steps in float32
 
 // What a workgroup of a walk over the chunks works on, and where this lane stands: of its eight waves, wave w of either four has the chunk's steps from 16 w on as rows.
