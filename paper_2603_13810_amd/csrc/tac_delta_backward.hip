@@ -9,6 +9,9 @@
 // e^G_t stands beside every q_t and every k_t that reads (first bracket), e^-G_j beside every k_j that writes (second), e^G_end beside what leaves the chunk, so
 //   dG_t = q_t . dQ_t + k_t . [first]_t - k_t . [second]_t  (+ e^G_end <S, dS> + sum_j k_j . (e^(G_end - G_j) dS u_j) at the last),
 // and the gradient of log a_t is the sum of dG over the steps from t on.
+//
+// 8 sequences of 2048 steps, 16 heads of 128 x 128 bf16: back_scan_kernel 200 us, bound by its chain as the forward's walk is (455 with everything on the same four waves);
+// gradient_kernel 300 us: it reads S, dS, U, R (1.0 GB, 3.3 TB/s) while values are summed over, which takes two thirds of its time at 5 TB/s, and then multiplies what is in LDS, with one workgroup a compute unit.
 #include "tac_delta_chunk.h"
 
 namespace tac {

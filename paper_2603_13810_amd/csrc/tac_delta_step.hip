@@ -3,6 +3,7 @@
 // Bound by the states' bytes, each read and written once.  A workgroup has 32 columns of one head's state in registers, 8 lanes x 16 bytes along a row and 32 rows at
 // a time; the columns' products with the key and the query are sums over rows: within a wave by swaps, over the four waves through LDS.  The query reads
 // the new state, S_t^T q = a S^T q + (k . q) u, so that one pass over the rows is enough.
+// 128 sequences, 16 heads of 128 x 128: 268 MB in 55.5 us, 4.8 TB/s (through the caches 65.6 a call, past them 57.6); one sequence: 4.7 us, the launch and one trip to memory and back.
 #include "tac_delta_common.h"
 
 namespace tac {
