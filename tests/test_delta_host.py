@@ -188,14 +188,16 @@ def test_delta_scan_refuses_addresses():
 def test_outputs_on_inputs_are_refused():
     apart = {i: P + 4096 * (i + 1) for i in range(17)}
     one = lambda f, desc, n, moved, **kw: f(desc, {**{i: apart[i] for i in range(n)}, **moved}, **kw)
-    for i in range(5):
+    for i in (0, 1, 2, 3, 4, 6, 8, 9, 10):                             # inputs, h0, and other outputs
         assert one(scan, delta_desc(), 12, {7: apart[i]}) == api.TAC_ERR_BAD_PARAM
+    for i in (0, 1, 2, 6, 8, 10):                                      # states
+        assert one(scan, delta_desc(), 12, {9: apart[i]}) == api.TAC_ERR_BAD_PARAM
     for w in (10, 11, 12, 13, 14):
-        for r in (0, 1, 2, 3, 4, 8):
+        for r in (0, 1, 2, 3, 4, 6, 7, 8, 9, 15):
             assert one(scan_backward, delta_desc(), 17, {w: apart[r]}) == api.TAC_ERR_BAD_PARAM
     assert one(scan_backward, delta_desc(), 17, {10: apart[11]}) == api.TAC_ERR_BAD_PARAM
     a = {i: apart[i] for i in range(9) if i != 6}
-    for i in range(5):
+    for i in range(6):
         assert step(delta_desc(T=1), {**a, 8: apart[i]}) == api.TAC_ERR_BAD_PARAM
 
 
