@@ -3,8 +3,8 @@
 //
 // G is kept in two numbers: a chunk that fades by e^-100 in all may hold neighbours that hardly fade, and one float32 number would have lost their difference.
 // A chunk and head is a workgroup of four waves: products of keys and queries, then the inverse, whose steps follow one another; K and Q come as whole rows through LDS (read as operands they took
-// a third longer).  With 128 features bf16 it reads 32 KB and writes 31: 8192 chunks of heads 108 us, 4.8 TB/s of which the caches hold a quarter; 4096 with three parts of both, for the
-// gradients, 51; 512 of 32 features fp32 11.4, where loads, gates, products and substitution wait for each other.
+// a third longer).  With 128 features bf16 it reads 32 KB and writes 31: 8192 chunks of heads 102 us, 5.1 TB/s of which the caches hold a quarter; 4096 with three parts of both, for the
+// gradients, 49; 512 of 32 features fp32 11.2, where loads, gates, products and substitution wait for each other.
 // The inverse is formed by blocks of 16: the diagonal ones by substitution, one column a lane, those below from them on the float32 matrix cores.  A product
 // of powers of A would be shorter, but its terms grow with the number of like keys where the inverse does not.
 #include "tac_delta_chunk.h"
@@ -71,6 +71,18 @@ __global__ __launch_bounds__(256) void prepare_kernel(const DeltaParams p) {
   const T* q = (const T*)p.q + from * p.q_at.t + (int64_t)b * p.q_at.b + (int64_t)hk * p.q_at.head;
   const T* k = (const T*)p.k + from * p.k_at.t + (int64_t)b * p.k_at.b + (int64_t)hk * p.k_at.head;
 
+  // whole rows from memory, on their way while the first wave has the gates; what is behind the last step is zero
+  constexpr int pieces = DK / 8, each = kChunk * pieces / 256;
+  T* const rows_of_k = (T*)lds;
+  T* const rows_of_q = rows_of_k + kChunk * Room::pitch;
+  Piece<T, 8> a[each], c[each];
+#pragma unroll
+  for (int i = 0; i < each; ++i) {
+    const int piece = threadIdx.x + 256 * i, row = piece / pieces, col = 8 * (piece % pieces);
+    load_piece<MODE>(a[i], k + (int64_t)min(row, n - 1) * p.k_at.t, col, p.Dk);
+    load_piece<MODE>(c[i], q + (int64_t)min(row, n - 1) * p.q_at.t, col, p.Dk);
+  }
+  in_this_order();
   if (wave == 0) {
     float hi = 0.0f, lo = 0.0f, w = 0.0f;
     if (lane < n) {
@@ -85,27 +97,20 @@ __global__ __launch_bounds__(256) void prepare_kernel(const DeltaParams p) {
     low[lane] = lo;
     beta[lane] = w;
   }
-  // whole rows from memory; what is behind the last step is zero
-  constexpr int pieces = DK / 8;
-  T* const rows_of_k = (T*)lds;
-  T* const rows_of_q = rows_of_k + kChunk * Room::pitch;
 #pragma unroll
-  for (int i = 0; i < kChunk * pieces / 256; ++i) {
+  for (int i = 0; i < each; ++i) {
     const int piece = threadIdx.x + 256 * i, row = piece / pieces, col = 8 * (piece % pieces), left = row < n ? p.Dk - col : 0;
-    Piece<T, 8> a, c;
-    load_piece<MODE>(a, k + (int64_t)min(row, n - 1) * p.k_at.t, col, p.Dk);
-    load_piece<MODE>(c, q + (int64_t)min(row, n - 1) * p.q_at.t, col, p.Dk);
-    a = arranged<MODE>(a, col, p.Dk);
-    c = arranged<MODE>(c, col, p.Dk);
+    a[i] = arranged<MODE>(a[i], col, p.Dk);
+    c[i] = arranged<MODE>(c[i], col, p.Dk);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       if (e >= left) {
-        a.set(e, (T)0.0f);
-        c.set(e, (T)0.0f);
+        a[i].set(e, (T)0.0f);
+        c[i].set(e, (T)0.0f);
       }
     }
-    store_aligned(rows_of_k + row * Room::pitch + col, a);
-    store_aligned(rows_of_q + row * Room::pitch + col, c);
+    store_aligned(rows_of_k + row * Room::pitch + col, a[i]);
+    store_aligned(rows_of_q + row * Room::pitch + col, c[i]);
   }
   __syncthreads();
   const ChunkRoom room(p.chunk_room, blockIdx.x, OUT);
