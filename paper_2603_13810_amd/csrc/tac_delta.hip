@@ -16,22 +16,30 @@ namespace {
 
 // Eight waves: four take the states from chunk to chunk, and four form the outputs from what those leave in LDS.
 
-// LDS of scan_kernel.  float32 [4][columns][kSums]: the waves' shares of K S; then in bfloat16 numbers S [OUT][columns][DK + 8] for the outputs, right-hand sides
-// [3][columns][kSteps], U faded [3], U [OUT], K transposed [IN][DK][kSteps]; and K as it stands, [64][DK + 8] elements.
+// LDS of scan_kernel.  float32: the waves' shares of K S; then in bfloat16 numbers, each in three parts, S [columns][DK + 8] and U [columns][kSteps] for the outputs, right-hand sides
+// [columns][kSteps], U faded, K transposed [IN][DK][kSteps]; and K as it stands, [64][DK + 8] elements.
+// With 16 columns and bfloat16 keys of 128 features that is half of a compute unit's 160 KB, so that two workgroups are there at once (6 sequences of 2048, 16 heads of 128 x 128: 203 us,
+// one at a time 237): a wave keeps the share that it needs itself, and the shares' rows are not padded, their quads change places instead.
 template <typename T, int DK, int NT>
 struct ScanRoom {
   static constexpr int columns = 16 * NT, key = DK + 8;
+  static constexpr bool tight = NT == 1;      // with 32 columns one workgroup fits, and the selection costs more (16 sequences of 2048: 484 us, 514)
   static constexpr int s_plane = columns * key, u_plane = columns * kSteps, k_plane = DK * kSteps;
-  static constexpr int s = 4 * columns * kSums * 2, rhs = s + Kind<T>::out * s_plane, faded = rhs + 3 * u_plane, u = faded + 3 * u_plane, k = u + Kind<T>::out * u_plane;
+  static constexpr int s = (tight ? 3 * columns * kChunk : 4 * columns * kSums) * 2, u = s + 3 * s_plane, rhs = u + 3 * u_plane, faded = rhs + 3 * u_plane, k = faded + 3 * u_plane;
   static constexpr int rows = k + Kind<T>::in * k_plane;
   static constexpr int bytes = 2 * rows + kChunk * key * (int)sizeof(T);
+  // where wave `of`'s share for the steps from `step` on (four of them, wave `to`'s) of a column stands
+  static __device__ __forceinline__ int share(int of, int to, int t, int low16, int step) {
+    if constexpr (tight) return ((of < to ? of : of - 1) * 16 + low16) * kChunk + (step ^ (4 * low16));
+    else return (of * columns + 16 * t + low16) * kSums + step;
+  }
 };
 
-// a row of the inverse or of the products; nothing stands above the diagonal
-template <int PARTS, typename T, int NT>
-__device__ __forceinline__ void load_rows_of(Parts<PARTS> (&m)[2], const bf16* from, const ScanPlace<T, NT>& at) {
-  m[0] = from_planes<PARTS>(from + ChunkRoom::operand(at.wave, 0, at.lane), ChunkRoom::plane);
-  m[1] = from_planes<PARTS>(from + ChunkRoom::operand(at.wave, at.wave >= 2 ? 1 : 0, at.lane), ChunkRoom::plane);
+// a row of the inverse; nothing stands above the diagonal
+template <typename T, int NT>
+__device__ __forceinline__ void load_rows_of(Parts<3> (&m)[2], const bf16* from, const ScanPlace<T, NT>& at) {
+  m[0] = from_planes<3>(from + ChunkRoom::operand(at.wave, 0, at.lane), ChunkRoom::plane);
+  m[1] = from_planes<3>(from + ChunkRoom::operand(at.wave, at.wave >= 2 ? 1 : 0, at.lane), ChunkRoom::plane);
 }
 
 // Loads of the next chunk are asked for as soon as this one's have been used, a chunk before they are waited for; memory operations come in the same number whatever
@@ -44,7 +52,7 @@ __device__ __forceinline__ void load_rows_of(Parts<PARTS> (&m)[2], const bf16* f
 template <typename T, int DK, int NT, int MODE, bool KEEP>
 __device__ __forceinline__ void scan_states(const DeltaParams& p, const ScanPlace<T, NT>& at, uint8_t* lds) {
   using Room = ScanRoom<T, DK, NT>;
-  constexpr int IN = Kind<T>::in, OUT = Kind<T>::out, MT = DK / 16, OWN = MT > 4 ? 2 : 1;
+  constexpr int IN = Kind<T>::in, MT = DK / 16, OWN = MT > 4 ? 2 : 1;
   float* const sums = (float*)lds;
   bf16* const L = (bf16*)lds;
   const int low16 = at.low16, quad = at.quad, rows = at.rows;
@@ -93,6 +101,7 @@ __device__ __forceinline__ void scan_states(const DeltaParams& p, const ScanPlac
     const int64_t from = (int64_t)c * kChunk;
     const int next = c + 1 < at.chunks ? c + 1 : c;
     float* const nowhere = at.room(p, c).nowhere;
+    f32x4_t mine[NT];                                     // the share of K S for this wave's steps
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       float own[8];
@@ -103,7 +112,7 @@ __device__ __forceinline__ void scan_states(const DeltaParams& p, const ScanPlac
 #pragma unroll
         for (int m = 0; m < OWN; ++m)
 #pragma unroll
-          for (int i = 0; i < OUT; ++i) {
+          for (int i = 0; i < 3; ++i) {
             const u32x4_t w = __builtin_bit_cast(u32x4_t, op.p[i]);
             *reinterpret_cast<u32x2_t*>(L + Room::s + i * Room::s_plane + (16 * t + low16) * Room::key + state_row[m]) = u32x2_t{w[2 * m], w[2 * m + 1]};
           }
@@ -123,7 +132,8 @@ __device__ __forceinline__ void scan_states(const DeltaParams& p, const ScanPlac
         const Piece<T, 4> a = load_aligned<T, 4>(from + (owner ? state_row[0] : 0));
         if constexpr (OWN == 2) multiply<3>(share, parts_of(a, load_aligned<T, 4>(from + state_row[1])), op);
         else multiply<3>(share, parts_of(a, a), op);          // the other half of S's operand is zero
-        *reinterpret_cast<f32x4_t*>(sums + (at.wave * Room::columns + 16 * t + low16) * kSums + 16 * i + 4 * quad) = share;
+        if (Room::tight && i == at.wave) mine[t] = share;
+        else *reinterpret_cast<f32x4_t*>(sums + Room::share(at.wave, i, t, low16, 16 * i + 4 * quad)) = share;
       }
     }
     __syncthreads();                                      // S, the shares of K S
@@ -131,7 +141,7 @@ __device__ __forceinline__ void scan_states(const DeltaParams& p, const ScanPlac
     for (int t = 0; t < NT; ++t) {
       f32x4_t ks = {0.0f, 0.0f, 0.0f, 0.0f}, rhs;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) ks += *reinterpret_cast<const f32x4_t*>(sums + (w * Room::columns + 16 * t + low16) * kSums + rows);
+      for (int w = 0; w < 4; ++w) ks += Room::tight && w == at.wave ? mine[t] : *reinterpret_cast<const f32x4_t*>(sums + Room::share(w, at.wave, t, low16, rows));
 #pragma unroll
       for (int r = 0; r < 4; ++r) rhs[r] = beta[r] * fmaf(-start[r], ks[r], (float)value[t][r]);
       quad_to_planes<3>(L + Room::rhs + (16 * t + low16) * kSteps + rows, Room::u_plane, rhs);
@@ -159,7 +169,7 @@ __device__ __forceinline__ void scan_states(const DeltaParams& p, const ScanPlac
     for (int t = 0; t < NT; ++t) {
       const int place = (16 * t + low16) * kSteps + rows;
       quad_to_planes<3>(L + Room::faded + place, Room::u_plane, faded[t]);
-      quad_to_planes<OUT>(L + Room::u + place, Room::u_plane, u[t]);
+      quad_to_planes<3>(L + Room::u + place, Room::u_plane, u[t]);
       if constexpr (KEEP) {
         float* to = p.updates + ((from + rows) * p.B * p.v_heads + at.head) * p.Dv + at.col[t];
 #pragma unroll
@@ -206,19 +216,26 @@ __device__ __forceinline__ void scan_states(const DeltaParams& p, const ScanPlac
 template <typename T, int DK, int NT, int MODE>
 __device__ __forceinline__ void scan_outputs(const DeltaParams& p, const ScanPlace<T, NT>& at, uint8_t* lds) {
   using Room = ScanRoom<T, DK, NT>;
-  constexpr int IN = Kind<T>::in, OUT = Kind<T>::out, KS = DK / 32;
+  constexpr int IN = Kind<T>::in, KS = DK / 32;
   bf16* const L = (bf16*)lds;
   T* const key_row = (T*)(L + Room::rows) + at.row * Room::key + 8 * at.quad;
   const int low16 = at.low16, quad = at.quad, rows = at.rows;
   const Identity id(at.lane);
   Piece<T, 8> key[KS], query[KS];
-  Parts<OUT> products[2];
+  f32x4_t products[2][2];                                 // float32 numbers
   f32x4_t start;
   const auto load_queries = [&](int c) {
     const T* from = at.step(at.q, p.q_at.t, c, at.row);
 #pragma unroll
     for (int s = 0; s < KS; ++s) load_piece<MODE>(query[s], from, 32 * s + 8 * quad, p.Dk);
     start = *reinterpret_cast<const f32x4_t*>(at.room(p, c).start + rows);
+  };
+  const auto load_products = [&](int c) {
+    const float* const from = at.room(p, c).products32();
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) products[s][i] = reinterpret_cast<const f32x4_t*>(from + ChunkRoom::operand(at.wave, at.wave >= 2 ? s : 0, at.lane))[i];
   };
   // whole rows at a time on the way from memory
   constexpr int pieces = DK / 8;
@@ -237,7 +254,7 @@ __device__ __forceinline__ void scan_outputs(const DeltaParams& p, const ScanPla
     in_this_order();
     load_keys(at.chunks > 1 ? 1 : 0);                     // in the loop's order: waits count what was asked for behind
     in_this_order();
-    load_rows_of(products, at.room(p, 0).products, at);
+    load_products(0);
     load_queries(0);
   }
   __syncthreads();                                        // the first chunk's K
@@ -258,7 +275,7 @@ __device__ __forceinline__ void scan_outputs(const DeltaParams& p, const ScanPla
     for (int s = 0; s < KS; ++s) {
       const Parts<IN> a = parts_of(arranged<MODE>(query[s], 32 * s + 8 * quad, p.Dk));
 #pragma unroll
-      for (int t = 0; t < NT; ++t) multiply<OUT>(o[t], a, from_planes<OUT>(L + Room::s + (16 * t + low16) * Room::key + 32 * s + 8 * quad, Room::s_plane));
+      for (int t = 0; t < NT; ++t) multiply<3>(o[t], a, from_planes<3>(L + Room::s + (16 * t + low16) * Room::key + 32 * s + 8 * quad, Room::s_plane));
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t)
@@ -268,8 +285,9 @@ __device__ __forceinline__ void scan_outputs(const DeltaParams& p, const ScanPla
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       if (s && at.wave < 2) continue;
+      const Parts<3> a = parts_of(products[s][0], products[s][1]);
 #pragma unroll
-      for (int t = 0; t < NT; ++t) multiply<OUT>(o[t], products[s], from_planes<OUT>(L + Room::u + (16 * t + low16) * kSteps + 32 * s + 8 * quad, Room::u_plane));
+      for (int t = 0; t < NT; ++t) multiply<3>(o[t], a, from_planes<3>(L + Room::u + (16 * t + low16) * kSteps + 32 * s + 8 * quad, Room::u_plane));
     }
     computed(o);
     in_this_order();
@@ -294,7 +312,7 @@ __device__ __forceinline__ void scan_outputs(const DeltaParams& p, const ScanPla
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) store_device(to[t][r], (T)o[t][r]);
-    load_rows_of(products, at.room(p, next).products, at);
+    load_products(next);
     load_queries(next);
   }
   // behind the last chunk's steps
@@ -345,7 +363,7 @@ hipError_t scan_typed(const DeltaParams& p, hipStream_t s) {
 }  // namespace
 
 size_t delta_workspace(const DeltaParams& p) {
-  return (size_t)p.chunks * p.B * p.v_heads * (size_t)ChunkRoom::bytes(p.bf16 ? Kind<bf16>::out : Kind<float>::out);
+  return (size_t)p.chunks * p.B * p.v_heads * (size_t)ChunkRoom::bytes(ChunkRoom::kForward);
 }
 
 hipError_t delta_scan_launch(const DeltaParams& given, uint8_t* workspace, hipStream_t s) {

@@ -79,7 +79,7 @@ __device__ __forceinline__ void multiply(f32x4_t& acc, const Parts<PA>& a, const
   }
 }
 
-// How element types enter: a bfloat16 tensor's numbers are one part, and results that go to it are formed from two; float32 three and three.
+// How element types enter: a bfloat16 tensor's numbers are one part, and gradients that go to it are formed from two; float32 three and three.
 template <typename T>
 struct Kind;
 template <>
@@ -226,21 +226,24 @@ __device__ __forceinline__ int steps_of(const DeltaParams& p, int b, int64_t fro
   return (int)max((int64_t)0, min((int64_t)kChunk, n - from));
 }
 
-// What prepare_kernel leaves of a chunk and head: the inverse in three parts and the queries' products in P_PARTS, [64][64] each, then float32 factors of the steps.
+// What prepare_kernel leaves of a chunk and head: the inverse in three parts, [64][64] each; the queries' products, forwards as float32 numbers, a third less than three parts (which spare one
+// long sequence 4 % and cost a batch of them 2 %), backwards in three parts; float32 factors of the steps.
 // Backwards both matrices stand transposed, so that a row's neighbours are what is summed over.  A plane is in the order in which it is read, the operand of 16 rows and 32
 // columns in one piece, a lane's eight numbers after the other's; of the operands only those that hold something are written.
 struct ChunkRoom {
   // operand of rows 16 tile.. and columns 32 step..
   static __device__ __forceinline__ int operand(int tile, int step, int lane) { return ((tile * 2 + step) * 64 + lane) * 8; }
   static constexpr int plane = kChunk * kChunk;
-  static constexpr int64_t bytes(int p_parts) { return (int64_t)(3 + p_parts) * plane * 2 + 6 * kChunk * 4; }
-  bf16 *inverse, *products;
+  static constexpr int kForward = 2, kBackward = 3;      // what the products take, in planes of 16 bits
+  static constexpr int64_t bytes(int p_planes) { return (int64_t)(3 + p_planes) * plane * 2 + 6 * kChunk * 4; }
+  bf16 *inverse, *products;                     // forwards the products are float32 numbers: products32()
   float *start, *rest, *beta, *high, *low;      // e^G, e^(G_end - G), b, and G in two numbers
   float* nowhere;                               // takes what is not to be stored
-  __device__ __forceinline__ ChunkRoom(uint8_t* base, int64_t index, int p_parts) {
-    inverse = (bf16*)(base + index * bytes(p_parts));
+  __device__ __forceinline__ float* products32() const { return (float*)products; }
+  __device__ __forceinline__ ChunkRoom(uint8_t* base, int64_t index, int p_planes) {
+    inverse = (bf16*)(base + index * bytes(p_planes));
     products = inverse + 3 * plane;
-    start = (float*)(products + p_parts * plane);
+    start = (float*)(products + p_planes * plane);
     rest = start + kChunk;
     beta = rest + kChunk;
     high = beta + kChunk;
@@ -357,6 +360,10 @@ __device__ __forceinline__ Parts<3> parts_of(const Piece<float, 4>& a, const Pie
   const float v[8] = {a.w[0], a.w[1], a.w[2], a.w[3], b.w[0], b.w[1], b.w[2], b.w[3]};
   return split<3>(v);
 }
+__device__ __forceinline__ Parts<3> parts_of(const f32x4_t& a, const f32x4_t& b) {
+  const float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+  return split<3>(v);
+}
 constexpr int kSums = kChunk + 4;             // pitch of LDS rows of a chunk's steps in float32
 
 // What a workgroup of a walk over the chunks works on, and where this lane stands: of its eight waves, wave w of either four has the chunk's steps from 16 w on as rows.
@@ -391,7 +398,7 @@ struct ScanPlace {
     v = (const T*)v_base + (int64_t)b * v_at.b + (int64_t)h * v_at.head;
     out = (T*)out_base + (int64_t)b * out_at.b + (int64_t)h * out_at.head;
   }
-  __device__ __forceinline__ ChunkRoom room(const DeltaParams& p, int c, int p_parts = Kind<T>::out) const { return ChunkRoom(p.chunk_room, (int64_t)c * p.B * p.v_heads + head, p_parts); }
+  __device__ __forceinline__ ChunkRoom room(const DeltaParams& p, int c, int p_planes = ChunkRoom::kForward) const { return ChunkRoom(p.chunk_room, (int64_t)c * p.B * p.v_heads + head, p_planes); }
   __device__ __forceinline__ int steps(int c) const { return c + 1 < chunks ? kChunk : last; }
   // step `i` of chunk c, of a tensor whose steps are `stride` apart.  What is behind the last step is read from there: it stands beside b = 0, or is not stored.
   template <typename E>

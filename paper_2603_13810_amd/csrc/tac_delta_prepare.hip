@@ -46,6 +46,18 @@ __device__ __forceinline__ void store_planes(bf16* to, const float (*from)[kPitc
   }
 }
 
+// A matrix in LDS as it is, in the same order.
+__device__ __forceinline__ void store_numbers(float* to, const float (*from)[kPitch]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int operand = threadIdx.x / 64 + 4 * i, lane = threadIdx.x % 64, tile = operand / 2, step = operand % 2;
+    if (step > tile / 2) continue;
+    const float* const row = &from[16 * tile + lane % 16][32 * step + 8 * (lane / 16)];
+#pragma unroll
+    for (int e = 0; e < 8; e += 4) *reinterpret_cast<f32x4_t*>(to + ChunkRoom::operand(tile, step, lane) + e) = *reinterpret_cast<const f32x4_t*>(row + e);
+  }
+}
+
 // K and Q as they stand, [2][64][DK + 8] elements, give their place to A and P, and P its to the inverse.
 template <typename T, int DK>
 struct PrepareRoom {
@@ -56,7 +68,7 @@ struct PrepareRoom {
 template <typename T, int DK, bool BACK, int MODE>
 __global__ __launch_bounds__(256) void prepare_kernel(const DeltaParams p) {
   using Room = PrepareRoom<T, DK>;
-  constexpr int IN = Kind<T>::in, OUT = BACK ? 3 : Kind<T>::out, KS = DK / 32;
+  constexpr int IN = Kind<T>::in, KS = DK / 32;
   __shared__ __align__(16) uint8_t lds[Room::bytes];
   float(*const A)[kPitch] = (float(*)[kPitch])lds;
   float(*const P)[kPitch] = A + kChunk;
@@ -113,7 +125,7 @@ __global__ __launch_bounds__(256) void prepare_kernel(const DeltaParams p) {
     store_aligned(rows_of_q + row * Room::pitch + col, c[i]);
   }
   __syncthreads();
-  const ChunkRoom room(p.chunk_room, blockIdx.x, OUT);
+  const ChunkRoom room(p.chunk_room, blockIdx.x, BACK ? ChunkRoom::kBackward : ChunkRoom::kForward);
   f32x4_t kk[4], qk[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) kk[j] = qk[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
@@ -161,7 +173,8 @@ __global__ __launch_bounds__(256) void prepare_kernel(const DeltaParams p) {
     }
   }
   __syncthreads();
-  store_planes<OUT, BACK>(room.products, P);
+  if constexpr (BACK) store_planes<3, true>(room.products, P);
+  else store_numbers(room.products32(), P);
   // a diagonal block's inverse: column low16 of x, row by row
   float x[16];
 #pragma unroll
