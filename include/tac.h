@@ -572,8 +572,8 @@ int tac_head_norm_backward(const tac_head_norm_desc_t* desc, const void* query, 
  * consecutive heads of values share a head of queries and keys.  Sequences may have different lengths: out is zero from a sequence's length on, what
  * stands behind it is read into no result, and its last state is that of its last step (h0 where the length is 0).
  * Steps are taken TAC_DELTA_CHUNK at a time: what the chunk's steps write solves a triangular system, everything else is products on the
- * matrix cores.  float32 numbers enter these as three bfloat16 parts whose sum they are, sums are float32: states, results of float32
- * tensors and bfloat16 outputs before their rounding are as exact as float32 products.  Gradients that go to bfloat16 tensors come from two parts (2^-16).
+ * matrix cores.  float32 numbers enter these as three bfloat16 parts whose sum they are, sums are float32: states, and results of either type
+ * before their rounding, are as exact as float32 products.
  * An input of a sequence's head that is not finite makes that head's results of the chunk it stands in and of those behind it (backwards:
  * before it) unspecified, NaN for the most part; other heads, sequences and chunks are not touched. */
 #define TAC_DELTA_CHUNK 64

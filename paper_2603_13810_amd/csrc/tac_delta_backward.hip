@@ -374,14 +374,14 @@ __global__ __launch_bounds__(512) void back_scan_kernel(const DeltaParams p, int
   else back_inputs<T, DK, NT, MODE>(p, at, lds);
 }
 
-// LDS of gradient_kernel in bfloat16 numbers.  While values' features are summed over, 32 at a time: S and dS [OUT][DK][40], U and R [OUT][64][40], dO [IN][64][40]; then K or Q
-// [IN][64][turned_pitch], Z and Y transposed [OUT][64][kSteps] each; at last the gradients, [2][64][DK + 8] elements.
+// LDS of gradient_kernel in bfloat16 numbers.  While values' features are summed over, 32 at a time: S and dS [3][DK][40], U and R [3][64][40], dO [IN][64][40]; then K or Q
+// [IN][64][turned_pitch], Z and Y transposed [3][64][kSteps] each; at last the gradients, [2][64][DK + 8] elements.
 template <typename T, int DK>
 struct GradientRoom {
-  static constexpr int IN = Kind<T>::in, OUT = Kind<T>::out, pitch = 40, out_pitch = DK + 8;
+  static constexpr int IN = Kind<T>::in, pitch = 40, out_pitch = DK + 8;
   static constexpr int s_plane = DK * pitch, u_plane = kChunk * pitch, k_pitch = turned_pitch(DK), k_plane = kChunk * k_pitch, y_plane = kChunk * kSteps;
-  static constexpr int s = 0, back = s + OUT * s_plane, u = back + OUT * s_plane, r = u + OUT * u_plane, g = r + OUT * u_plane, first_size = g + IN * u_plane;
-  static constexpr int k = 0, z = k + IN * k_plane, y = z + OUT * y_plane, second_size = y + OUT * y_plane;
+  static constexpr int s = 0, back = s + 3 * s_plane, u = back + 3 * s_plane, r = u + 3 * u_plane, g = r + 3 * u_plane, first_size = g + IN * u_plane;
+  static constexpr int k = 0, z = k + IN * k_plane, y = z + 3 * y_plane, second_size = y + 3 * y_plane;
   static constexpr int third_size = 2 * kChunk * out_pitch * (int)sizeof(T) / 2;
   static constexpr int most = first_size > second_size ? first_size : second_size, bytes = 2 * (most > third_size ? most : third_size);
 };
@@ -403,7 +403,7 @@ __device__ __forceinline__ f32x4_t steps_of_rows(const bf16* rows, int plane, in
 template <typename T, int DK, int MODE>
 __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
   using Room = GradientRoom<T, DK>;
-  constexpr int IN = Kind<T>::in, OUT = Kind<T>::out, NT = DK / 32, KS = NT > 1 ? NT / 2 : 1;      // tiles and pieces of this half of the features
+  constexpr int IN = Kind<T>::in, NT = DK / 32, KS = NT > 1 ? NT / 2 : 1;      // tiles and pieces of this half of the features
   extern __shared__ __align__(16) uint8_t lds[];
   __shared__ float high[kChunk], low[kChunk], change[2][kChunk], both[8];
   bf16* const L = (bf16*)lds;
@@ -533,9 +533,9 @@ __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
             kept += MODE != WHOLE || v + s_col + 4 * i < p.Dv ? sum : 0.0f;
           }
           if (s_row < DK) {
-            const Parts<OUT> a = split<OUT>(s), c = split<OUT>(d);
+            const Parts<3> a = split<3>(s), c = split<3>(d);
 #pragma unroll
-            for (int i = 0; i < OUT; ++i) {
+            for (int i = 0; i < 3; ++i) {
               *reinterpret_cast<bf16x8_t*>(L + Room::s + i * Room::s_plane + s_row * Room::pitch + s_col) = a.p[i];
               *reinterpret_cast<bf16x8_t*>(L + Room::back + i * Room::s_plane + s_row * Room::pitch + s_col) = c.p[i];
             }
@@ -552,8 +552,8 @@ __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
             written = fmaf(u[e], r[e], written);
           }
           const int place = u_row * Room::pitch + u_col;
-          quad_to_planes<OUT>(L + Room::u + place, Room::u_plane, u);
-          quad_to_planes<OUT>(L + Room::r + place, Room::u_plane, r);
+          quad_to_planes<3>(L + Room::u + place, Room::u_plane, u);
+          quad_to_planes<3>(L + Room::r + place, Room::u_plane, r);
           quad_to_planes<IN>(L + Room::g + place, Room::u_plane, g);
         }
         in_this_order();
@@ -562,21 +562,21 @@ __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
           __syncthreads();
           const int place = row * Room::pitch + 8 * quad;
           const Parts<IN> own_g = from_planes<IN>(L + Room::g + place, Room::u_plane);
-          const Parts<OUT> own_r = from_planes<OUT>(L + Room::r + place, Room::u_plane), own_u = from_planes<OUT>(L + Room::u + place, Room::u_plane);
+          const Parts<3> own_r = from_planes<3>(L + Room::r + place, Room::u_plane), own_u = from_planes<3>(L + Room::u + place, Room::u_plane);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             if (i > wave) continue;
-            const Parts<OUT> o = from_planes<OUT>(L + Room::u + (16 * i + low16) * Room::pitch + 8 * quad, Room::u_plane);
-            if (half) multiply<OUT>(w[i], own_r, o);
-            else multiply<OUT>(w[i], own_g, o);
+            const Parts<3> o = from_planes<3>(L + Room::u + (16 * i + low16) * Room::pitch + 8 * quad, Room::u_plane);
+            if (half) multiply<3>(w[i], own_r, o);
+            else multiply<3>(w[i], own_g, o);
           }
 #pragma unroll
           for (int i = 0; i < NT; ++i) {
             const int feature = (16 * (tile0 + i) + low16) * Room::pitch + 8 * quad;
-            const Parts<OUT> s = from_planes<OUT>(L + Room::s + feature, Room::s_plane);
-            multiply<OUT>(dq[i], own_g, s);
-            multiply<OUT>(reads[i], own_r, s);
-            multiply<OUT>(writes[i], own_u, from_planes<OUT>(L + Room::back + feature, Room::s_plane));
+            const Parts<3> s = from_planes<3>(L + Room::s + feature, Room::s_plane);
+            multiply<3>(dq[i], own_g, s);
+            multiply<3>(reads[i], own_r, s);
+            multiply<3>(writes[i], own_u, from_planes<3>(L + Room::back + feature, Room::s_plane));
             in_this_order();
           }
         }
@@ -611,7 +611,7 @@ __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int j = 16 * i + low16;
-      quad_to_planes<OUT>(L + (half ? Room::z : Room::y) + j * kSteps + rows, Room::y_plane, w[i]);
+      quad_to_planes<3>(L + (half ? Room::z : Room::y) + j * kSteps + rows, Room::y_plane, w[i]);
     }
     __syncthreads();
     f32x4_t dG = {0.0f, 0.0f, 0.0f, 0.0f}, leaves = dG, kept_key[NT];      // of the four steps of this lane's results: a part over the features
@@ -624,20 +624,20 @@ __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
     for (int s = 0; s < 2; ++s) {
       const int at = 32 * s + 8 * quad;
       const bool lower = 2 * s <= wave, upper = 2 * s + 1 >= wave;      // whether these 32 columns of Y and Z, and of Z transposed, hold something
-      Parts<OUT> a, c, d;
+      Parts<3> a, c, d;
       if (lower) {
-        a = turned<OUT>(L + Room::y, Room::y_plane, kSteps, 32 * s, 16 * wave, lane);
-        c = turned<OUT>(L + Room::z, Room::y_plane, kSteps, 32 * s, 16 * wave, lane);
+        a = turned<3>(L + Room::y, Room::y_plane, kSteps, 32 * s, 16 * wave, lane);
+        c = turned<3>(L + Room::z, Room::y_plane, kSteps, 32 * s, 16 * wave, lane);
       }
-      if (upper) d = from_planes<OUT>(L + Room::z + row * kSteps + at, Room::y_plane);
+      if (upper) d = from_planes<3>(L + Room::z + row * kSteps + at, Room::y_plane);
 #pragma unroll
       for (int i = 0; i < NT; ++i) {
         const Parts<IN> o = turned<IN>(L + Room::k, Room::k_plane, Room::k_pitch, 32 * s, 16 * (tile0 + i), lane);
         if (lower) {
-          multiply<OUT>(dq[i], a, o);
-          multiply<OUT>(reads[i], c, o);
+          multiply<3>(dq[i], a, o);
+          multiply<3>(reads[i], c, o);
         }
-        if (upper) multiply<OUT>(writes[i], d, o);
+        if (upper) multiply<3>(writes[i], d, o);
       }
     }
 #pragma unroll
@@ -649,9 +649,9 @@ __global__ __launch_bounds__(512) void gradient_kernel(const DeltaParams p) {
     for (int s = 0; s < 2; ++s) {
       if (2 * s + 1 < wave) continue;
       const int at = 32 * s + 8 * quad;
-      const Parts<OUT> a = from_planes<OUT>(L + Room::y + row * kSteps + at, Room::y_plane);
+      const Parts<3> a = from_planes<3>(L + Room::y + row * kSteps + at, Room::y_plane);
 #pragma unroll
-      for (int i = 0; i < NT; ++i) multiply<OUT>(writes[i], a, turned<IN>(L + Room::k, Room::k_plane, Room::k_pitch, 32 * s, 16 * (tile0 + i), lane));
+      for (int i = 0; i < NT; ++i) multiply<3>(writes[i], a, turned<IN>(L + Room::k, Room::k_plane, Room::k_pitch, 32 * s, 16 * (tile0 + i), lane));
     }
 #pragma unroll
     for (int i = 0; i < NT; ++i) {

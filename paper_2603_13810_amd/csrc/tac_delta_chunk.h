@@ -11,7 +11,7 @@ constexpr int kSteps = kChunk + 8;            // pitch of LDS rows of a chunk's 
 
 // ---- numbers as sums of bfloat16 parts -----------------------------------------------------------
 // A float32 number is the sum of three bfloat16 numbers (3 x 8 digits); the product of two such sums without what is below 2^-24 of it is six products, of a
-// bfloat16 number with one three.  Two parts have 16 digits.
+// bfloat16 number with one three.
 template <int PARTS>
 struct Parts {
   bf16x8_t p[PARTS];
@@ -79,16 +79,16 @@ __device__ __forceinline__ void multiply(f32x4_t& acc, const Parts<PA>& a, const
   }
 }
 
-// How element types enter: a bfloat16 tensor's numbers are one part, and gradients that go to it are formed from two; float32 three and three.
+// In how many parts numbers enter that come from tensors of a type.  What is formed from them has three, also on its way to bfloat16 results: those are often what is left of far larger terms.
 template <typename T>
 struct Kind;
 template <>
 struct Kind<bf16> {
-  static constexpr int in = 1, out = 2;
+  static constexpr int in = 1;
 };
 template <>
 struct Kind<float> {
-  static constexpr int in = 3, out = 3;
+  static constexpr int in = 3;
 };
 
 // operand from LDS: rows of `pitch` bfloat16, one plane per part

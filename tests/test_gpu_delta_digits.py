@@ -117,3 +117,160 @@ def test_outputs_are_roundings_of_float32(T, B, hk, hv, dk, dv):
     got = api.tac_delta_scan(*[x[n] for n in NAMES], h0=h0)
     out, S, _ = O.delta(*[O.as64(x[n]) for n in NAMES], h0=O.as64(h0))
     between("out", got["out"], out, plain_bound(out))
+
+
+# ---- gradients -----------------------------------------------------------------------------------
+
+GRADS = ("grad_query", "grad_key", "grad_value", "grad_gate", "grad_write", "grad_h0")
+
+
+def backward(x, h0, grad_out=None, grad_last=None):
+    x = {n: t.to(torch.bfloat16).to(DEV) for n, t in x.items()}
+    args = [x[n] for n in NAMES]
+    got = api.tac_delta_scan(*args, h0=h0.to(DEV), want_kept=True)
+    grad_out = torch.zeros_like(x["value"]) if grad_out is None else grad_out.to(torch.bfloat16).to(DEV)
+    return got, api.tac_delta_scan_backward(*args, got["states"], got["updates"], grad_out, grad_h_last=None if grad_last is None else grad_last.to(DEV))
+
+
+def by_head(B, hk, hv, dk):
+    """1 and -1 in turn, one for all heads of values that share a head of keys, and one for every feature of a key; how many share one."""
+    heads, features = torch.ones(B, hk, 1), torch.ones(dk)
+    heads[:, 1::2] = -1
+    features[1::2] = -1
+    return heads, heads.repeat_interleave(hv // hk, 1), features, hv // hk
+
+
+@pytest.mark.parametrize("t0", PLACES)
+@pytest.mark.parametrize("shape", SHAPES)
+def test_query_gradients_from_states(shape, t0):
+    """grad_query = S grad_out, of two columns that are nearly the same."""
+    B, hk, hv, dk, dv = shape
+    key_heads, heads, features, share = by_head(B, hk, hv, dk)
+    x, h0, go = still(*shape), torch.zeros(B, hv, dk, dv), torch.zeros(70, B, hv, dv)
+    h0[..., 0], h0[..., dv - 1] = BASE + heads * features * FINE, BASE
+    go[t0, ..., 0], go[t0, ..., dv - 1] = 0.5, -0.5
+    _, got = backward(x, h0, go)
+    close(got["grad_query"][t0], share * key_heads * features * FINE / 2, 1.01 * share)
+
+
+@pytest.mark.parametrize("t0", PLACES)
+@pytest.mark.parametrize("shape", SHAPES)
+def test_key_gradients_from_the_states_gradients(shape, t0):
+    """A step that writes 1 and -1 into two columns of a state whose gradients are nearly the same."""
+    B, hk, hv, dk, dv = shape
+    key_heads, heads, features, share = by_head(B, hk, hv, dk)
+    x, last = still(*shape), torch.zeros(B, hv, dk, dv)
+    last[..., 0], last[..., dv - 1] = BASE + heads * features * FINE, BASE
+    x["value"][t0, ..., 0], x["value"][t0, ..., dv - 1] = 1, -1
+    x["write"][t0] = INF
+    _, got = backward(x, torch.zeros_like(last), grad_last=last)
+    close(got["grad_key"][t0], share * key_heads * features * FINE, 2.01 * share)
+
+
+@pytest.mark.parametrize("t0", PLACES)
+@pytest.mark.parametrize("shape", SHAPES)
+def test_key_gradients_from_what_a_step_writes(shape, t0):
+    """A step halves a row and writes BASE + fine and BASE, into columns whose gradients are 1 and -1."""
+    B, hk, hv, dk, dv = shape
+    key_heads, heads, features, share = by_head(B, hk, hv, dk)
+    x, h0, last = still(*shape), torch.zeros(B, hv, dk, dv), torch.zeros(B, hv, dk, dv)
+    h0[:, :, 1, 0], h0[:, :, 1, dv - 1] = -2 * (BASE + heads[..., 0] * FINE), -2 * BASE
+    last[..., 0], last[..., dv - 1] = features, -features
+    last[:, :, 1] = 0
+    x["key"][t0, ..., 1] = 1
+    x["write"][t0] = 0
+    kept, got = backward(x, h0, grad_last=last)
+    want = share * key_heads * features * FINE
+    want[..., 1] = 0
+    close(kept["updates"][t0, ..., 0], BASE + heads[..., 0] * FINE, 0)
+    close(got["grad_key"][t0], want, 2.01 * share)
+
+
+@pytest.mark.parametrize("digits", ["gradients", "states"])
+@pytest.mark.parametrize("t0", PLACES)
+@pytest.mark.parametrize("shape", SHAPES)
+def test_key_gradients_from_what_a_step_reads(shape, t0, digits):
+    """-b S r, where r = dS^T key is BASE + fine and BASE and a row of S is 1 and -1, or the other way around."""
+    B, hk, hv, dk, dv = shape
+    key_heads, heads, features, share = by_head(B, hk, hv, dk)
+    x, h0, last = still(*shape), torch.zeros(B, hv, dk, dv), torch.zeros(B, hv, dk, dv)
+    if digits == "gradients":
+        last[:, :, 1, 0], last[:, :, 1, dv - 1] = BASE + heads[..., 0] * FINE, BASE
+        h0[..., 0], h0[..., dv - 1] = features, -features
+    else:
+        last[:, :, 1, 0], last[:, :, 1, dv - 1] = 1, -1
+        h0[..., 0], h0[..., dv - 1] = BASE + heads * features * FINE, BASE
+    h0[:, :, 1] = 0
+    x["key"][t0, ..., 1] = 1
+    x["write"][t0] = 0
+    _, got = backward(x, h0, grad_last=last)
+    want = -share * key_heads * features * FINE / 2
+    want[..., 1] = 0
+    close(got["grad_key"][t0], want, 1.01 * share)
+
+
+def two_writers(shape, t0):
+    """Two steps that write BASE + fine and -BASE into feature 2, whose keys have it in common."""
+    B, hk, hv, dk, dv = shape
+    key_heads, heads, _, share = by_head(B, hk, hv, dk)
+    x, h0, fine = still(*shape), torch.zeros(B, hv, dk, dv), heads * FINE
+    h0[:, :, 0], h0[:, :, 1] = -2 * (BASE + fine), BASE - fine
+    x["key"][t0, ..., 0], x["key"][t0, ..., 2] = 1, 1
+    x["key"][t0 + 1, ..., 1], x["key"][t0 + 1, ..., 2] = 1, 1
+    x["write"][t0:t0 + 2] = 0
+    return x, h0, share * key_heads[..., 0] * FINE, share
+
+
+@pytest.mark.parametrize("t0", PLACES)
+@pytest.mark.parametrize("shape", SHAPES)
+def test_query_gradients_from_products_of_gradients_and_updates(shape, t0):
+    B, hk, hv, dk, dv = shape
+    x, h0, fine, share = two_writers(shape, t0)
+    go = torch.zeros(70, B, hv, dv)
+    go[t0 + 1, ..., 3] = 1
+    kept, got = backward(x, h0, go)
+    assert (kept["updates"][t0 + 1] == -BASE).all()
+    close(got["grad_query"][t0 + 1, ..., 2], fine, 2.01 * share)
+
+
+@pytest.mark.parametrize("t0", PLACES)
+@pytest.mark.parametrize("shape", SHAPES)
+def test_key_gradients_from_products_of_gradients_and_updates(shape, t0):
+    """A third step reads what the two wrote, -S r / 2."""
+    B, hk, hv, dk, dv = shape
+    x, h0, fine, share = two_writers(shape, t0)
+    x["key"][t0 + 2, ..., 3] = 1
+    x["write"][t0 + 2] = 0
+    last = torch.zeros(B, hv, dk, dv)
+    last[:, :, 3, 3] = 1
+    _, got = backward(x, h0, grad_last=last)
+    close(got["grad_key"][t0 + 2, ..., 2], -fine / 2, 1.01 * share)
+
+
+@pytest.mark.parametrize("t0", PLACES)
+@pytest.mark.parametrize("shape", SHAPES)
+def test_key_gradients_from_later_queries(shape, t0):
+    """A step writes BASE + fine and BASE into two columns; two queries read them, with opposite signs."""
+    B, hk, hv, dk, dv = shape
+    key_heads, heads, _, share = by_head(B, hk, hv, dk)
+    x, h0, go = still(*shape), torch.zeros(B, hv, dk, dv), torch.zeros(70, B, hv, dv)
+    h0[:, :, 0, 0], h0[:, :, 0, dv - 1] = -2 * (BASE + heads[..., 0] * FINE), -2 * BASE
+    x["key"][t0, ..., 0] = 1
+    x["write"][t0] = 0
+    x["query"][t0 + 1, ..., 2], x["query"][t0 + 2, ..., 2] = 1, -1
+    go[t0 + 1, ..., 0], go[t0 + 2, ..., dv - 1] = 1, 1
+    _, got = backward(x, h0, go)
+    close(got["grad_key"][t0, ..., 2], share * key_heads[..., 0] * FINE, 2.01 * share)
+
+
+@pytest.mark.parametrize("T,B,hk,hv,dk,dv", [(130, 2, 2, 4, 64, 64), (260, 1, 2, 2, 128, 128), (100, 3, 1, 2, 33, 70)])
+def test_gradients_are_roundings_of_float32(T, B, hk, hv, dk, dv):
+    x, h0 = O.delta_inputs(T, B, hk, hv, dk, dv, torch.bfloat16, 50 + dk)
+    g = torch.Generator().manual_seed(dk)
+    go, last = torch.randn(T, B, hv, dv, generator=g), torch.randn(B, hv, dk, dv, generator=g)
+    _, got = backward(x, h0, go, last)
+    args = [O.as64(x[n]) for n in NAMES]
+    kept = O.delta(*args, h0=O.as64(h0))[2]
+    want, sizes = O.delta_backward(*args, kept, O.as64(go.to(torch.bfloat16)), grad_last=O.as64(last))
+    for name, w in zip(GRADS[:5], want):
+        between(name, got[name], w, NORM * sizes if name == "grad_gate" else plain_bound(w))
