@@ -596,7 +596,7 @@ typedef struct tac_delta_desc {
  *   gate, write  DEVICE, read-only, [T][B][v_heads]
  *   lengths      DEVICE, read-only, int32 [B], taken as 0 .. T where outside; NULL: all T
  *   h0           DEVICE, read-only, float32 [B][v_heads][Dk][Dv], or NULL: zeros
- *   out          DEVICE, written, [T][B][v_heads][Dv]; no output may lie on an input, but for h_last on h0 (where one begins at an input's address the call is refused)
+ *   out          DEVICE, written, [T][B][v_heads][Dv]; no output may lie on an input or on another, but for h_last on h0 (where one, or the workspace, begins at another's address the call is refused)
  *   h_last       DEVICE, written, float32 [B][v_heads][Dk][Dv], or NULL; may be h0
  *   states       DEVICE, written, float32 [ceil(T / TAC_DELTA_CHUNK)][B][v_heads][Dk][Dv]: the state before every chunk of steps, and
  *   updates      DEVICE, written, float32 [T][B][v_heads][Dv]: u, which are all that the backward pass keeps; both or both NULL.  Of chunks that lie

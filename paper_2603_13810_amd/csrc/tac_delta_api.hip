@@ -102,9 +102,10 @@ bool any_misaligned(std::initializer_list<const void*> list, size_t to) {
   return false;
 }
 
-// Outputs that begin where an input or another output does.  (Tensors that overlap in other ways are the caller's to keep apart: slices of the same rows lie between each other.)
+// Outputs that begin where an input or another output does; what is not there (NULL) is on nothing.  (Tensors that overlap in other ways are the caller's to keep apart: slices of the same rows lie between each other.)
 bool on_each_other(std::initializer_list<const void*> written, std::initializer_list<const void*> read) {
   for (auto w = written.begin(); w != written.end(); ++w) {
+    if (!*w) continue;
     for (const void* r : read)
       if (*w == r) return true;
     for (auto other = written.begin(); other != w; ++other)
@@ -191,7 +192,7 @@ int tac_delta_scan(const tac_delta_desc_t* d, const void* query, const void* key
   if (any_misaligned({query, key, value, gate, write, out}, bytes_of(d->dtype)) || any_misaligned({lengths, h0, h_last, states, updates}, 4) ||
       misaligned(workspace, 16))
     return TAC_ERR_ALIGN;
-  if (on_each_other({out}, {query, key, value, gate, write, h0, h_last}) || (states && on_each_other({out, states, updates}, {query, key, value, h0, h_last}))) return TAC_ERR_BAD_PARAM;
+  if (on_each_other({out, h_last, states, updates, workspace}, {query, key, value, gate, write, lengths}) || on_each_other({out, states, updates, workspace}, {h0})) return TAC_ERR_BAD_PARAM;
   tac::DeltaParams p = delta_params(d);
   p.q = query;
   p.k = key;
