@@ -618,8 +618,8 @@ int tac_delta_scan(const tac_delta_desc_t* desc, const void* query, const void* 
  *   states, updates  DEVICE, read-only, as tac_delta_scan wrote them
  *   grad_out         DEVICE, read-only, strides `out`
  *   grad_h_last      DEVICE, read-only, float32 [B][v_heads][Dk][Dv], or NULL: zeros
- *   grad_query, grad_key, grad_value, grad_gate, grad_write   DEVICE, written; none may lie on an input
- *   grad_h0          DEVICE, written, float32 [B][v_heads][Dk][Dv], or NULL; may be grad_h_last
+ *   grad_query, grad_key, grad_value, grad_gate, grad_write   DEVICE, written; none may lie on an input or on another output (refused as above)
+ *   grad_h0          DEVICE, written, float32 [B][v_heads][Dk][Dv], or NULL; may be grad_h_last, but on no other
  *   workspace        DEVICE, scratch, tac_delta_scan_backward_workspace_bytes(desc) bytes, 16-byte aligned */
 size_t tac_delta_scan_backward_workspace_bytes(const tac_delta_desc_t* desc);
 int tac_delta_scan_backward(const tac_delta_desc_t* desc, const void* query, const void* key, const void* value, const void* gate, const void* write,

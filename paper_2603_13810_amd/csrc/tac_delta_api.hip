@@ -223,7 +223,9 @@ int tac_delta_scan_backward(const tac_delta_desc_t* d, const void* query, const 
   if (any_misaligned({query, key, value, gate, write, grad_out, grad_query, grad_key, grad_value, grad_gate, grad_write}, bytes_of(d->dtype)) ||
       any_misaligned({lengths, states, updates, grad_h_last, grad_h0}, 4) || misaligned(workspace, 16))
     return TAC_ERR_ALIGN;
-  if (on_each_other({grad_query, grad_key, grad_value, grad_gate, grad_write}, {query, key, value, gate, write, grad_out, states, updates, grad_h_last, grad_h0})) return TAC_ERR_BAD_PARAM;
+  if (on_each_other({grad_query, grad_key, grad_value, grad_gate, grad_write, grad_h0, workspace}, {query, key, value, gate, write, lengths, states, updates, grad_out}) ||
+      on_each_other({grad_query, grad_key, grad_value, grad_gate, grad_write, workspace}, {grad_h_last}))
+    return TAC_ERR_BAD_PARAM;
   tac::DeltaParams p = delta_params(d);
   p.q = query;
   p.k = key;

@@ -2,7 +2,7 @@
 import pytest
 
 from paper_2603_13810_amd import api
-from test_delta_host import P, delta_desc, scan
+from test_delta_host import P, delta_desc, scan, scan_backward
 
 APART = [P + 4096 * (i + 1) for i in range(24)]
 
@@ -26,3 +26,16 @@ def test_delta_scan(written):
     for other in SCAN[:6]:
         if written in ("out", "h_last", "workspace"):
             assert scan(delta_desc(), {**at(12, **{"_%d" % w: APART[SCAN.index(other)]}), 9: None, 10: None}) == api.TAC_ERR_BAD_PARAM, other
+
+
+BACK = ("query", "key", "value", "gate", "write", "lengths", "states", "updates", "grad_out", "grad_h_last", "grad_query", "grad_key", "grad_value", "grad_gate", "grad_write", "grad_h0",
+        "workspace")
+
+
+@pytest.mark.parametrize("written", BACK[10:])
+def test_delta_scan_backward(written):
+    w = BACK.index(written)
+    for other in BACK:
+        if other == written or {written, other} == {"grad_h0", "grad_h_last"}:
+            continue
+        assert scan_backward(delta_desc(), at(17, **{"_%d" % w: APART[BACK.index(other)]})) == api.TAC_ERR_BAD_PARAM, other
