@@ -556,7 +556,7 @@ int tac_head_norm(const tac_head_norm_desc_t* desc, const void* query, const voi
  *   query, key                        DEVICE, read-only: what the forward pass read
  *   grad_out_query, grad_out_key      DEVICE, read-only, strides out_query, out_key
  *   grad_query, grad_key              DEVICE, written; may be grad_out_query and grad_out_key (with their strides)
- *   grad_gain_query, grad_gain_key    DEVICE, written, float32 [D], or NULL
+ *   grad_gain_query, grad_gain_key    DEVICE, written, float32 [D], or NULL.  Neither, nor the workspace, may begin at another tensor (refused)
  *   workspace                         DEVICE, scratch, tac_head_norm_workspace_bytes(desc) bytes, 16-byte aligned; may be NULL where neither gain's gradient is asked for
  * Sums are formed in an order that depends on the sizes alone: the same bits from call to call. */
 size_t tac_head_norm_workspace_bytes(const tac_head_norm_desc_t* desc);

@@ -166,9 +166,14 @@ int tac_head_norm_backward(const tac_head_norm_desc_t* d, const void* query, con
   if (any_misaligned({query, grad_out_query, grad_query}, el) || (d->key_heads && any_misaligned({key, grad_out_key, grad_key}, el)) ||
       any_misaligned({gain_query, gain_key, grad_gain_query, grad_gain_key}, 4) || (d->axes && misaligned(positions, 4)) || misaligned(workspace, 16))
     return TAC_ERR_ALIGN;
-  if (moved(d, d->query_heads, grad_out_query, d->out_query, grad_query, d->grad_query) || grad_query == query) return TAC_ERR_BAD_PARAM;
-  if (d->key_heads && (moved(d, d->key_heads, grad_out_key, d->out_key, grad_key, d->grad_key) || on_each_other({grad_query}, {key, grad_out_key, grad_key}) ||
-                       on_each_other({grad_key}, {query, key, grad_out_query})))
+  // what is ignored may be anywhere
+  const bool keys = d->key_heads != 0, sums = grad_gain_query || grad_gain_key;
+  const void *k = keys ? key : nullptr, *go_k = keys ? grad_out_key : nullptr, *g_k = keys ? grad_key : nullptr;
+  if (moved(d, d->query_heads, grad_out_query, d->out_query, grad_query, d->grad_query) || (keys && moved(d, d->key_heads, grad_out_key, d->out_key, grad_key, d->grad_key)) ||
+      on_each_other({grad_query}, {query, k, go_k, g_k}) || on_each_other({g_k}, {query, k, grad_out_query}))
+    return TAC_ERR_BAD_PARAM;
+  if (on_each_other({grad_gain_query, grad_gain_key, sums ? workspace : nullptr},
+                    {query, k, gain_query, keys ? gain_key : nullptr, d->axes ? positions : nullptr, grad_out_query, go_k, grad_query, g_k}))
     return TAC_ERR_BAD_PARAM;
   tac::HeadNormParams p = head_params(d);
   p.q = {query, grad_out_query, grad_query, gain_query, d->query, d->out_query, d->grad_query, d->query_heads};

@@ -2,7 +2,7 @@
 import pytest
 
 from paper_2603_13810_amd import api
-from test_delta_host import P, delta_desc, scan, scan_backward
+from test_delta_host import P, delta_desc, head_norm_backward, scan, scan_backward
 
 APART = [P + 4096 * (i + 1) for i in range(24)]
 
@@ -39,3 +39,14 @@ def test_delta_scan_backward(written):
         if other == written or {written, other} == {"grad_h0", "grad_h_last"}:
             continue
         assert scan_backward(delta_desc(), at(17, **{"_%d" % w: APART[BACK.index(other)]})) == api.TAC_ERR_BAD_PARAM, other
+
+
+HEADS_BACK = ("query", "key", "gain_query", "gain_key", "positions", "grad_out_query", "grad_out_key", "grad_query_at", "grad_key_at", "grad_gain_query", "grad_gain_key", "workspace")
+
+
+@pytest.mark.parametrize("written", HEADS_BACK[9:])
+def test_gradients_of_gains(written):
+    apart = dict(zip(HEADS_BACK, APART))
+    for other in HEADS_BACK:
+        if other != written:
+            assert head_norm_backward(**{**apart, written: apart[other]}) == api.TAC_ERR_BAD_PARAM, other
