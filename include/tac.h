@@ -546,7 +546,7 @@ typedef struct tac_head_norm_desc {
 /*   query, key            DEVICE, read-only, [rows][heads][D]
  *   gain_query, gain_key  DEVICE, read-only, float32 [D], or NULL: ones
  *   positions             DEVICE, read-only, int32 [rows][axes] (ignored without a rotation)
- *   out_query, out_key    DEVICE, written; may be query and key (with their strides).  An output that begins at another input, or with other strides, is refused
+ *   out_query, out_key    DEVICE, written; may be query and key (with their strides).  An output that begins at another input or output, or with other strides, is refused
  * Errors: TAC_ERR_NULL, TAC_ERR_BAD_SHAPE, TAC_ERR_UNSUPPORTED (more than TAC_HEAD_MAX_FEATURES features), TAC_ERR_BAD_PARAM, TAC_ERR_ALIGN, TAC_ERR_HIP. */
 int tac_head_norm(const tac_head_norm_desc_t* desc, const void* query, const void* key, const float* gain_query, const float* gain_key,
                   const int32_t* positions, void* out_query, void* out_key, void* stream);
@@ -555,7 +555,7 @@ int tac_head_norm(const tac_head_norm_desc_t* desc, const void* query, const voi
  *   grad_x = rstd (w - n' mean(w n')),  grad_gain = sum over rows and heads of g n'      (without a norm: w, and sum of g x)
  *   query, key                        DEVICE, read-only: what the forward pass read
  *   grad_out_query, grad_out_key      DEVICE, read-only, strides out_query, out_key
- *   grad_query, grad_key              DEVICE, written; may be grad_out_query and grad_out_key (with their strides)
+ *   grad_query, grad_key              DEVICE, written; may be grad_out_query and grad_out_key (with their strides), but no other tensor (refused)
  *   grad_gain_query, grad_gain_key    DEVICE, written, float32 [D], or NULL.  Neither, nor the workspace, may begin at another tensor (refused)
  *   workspace                         DEVICE, scratch, tac_head_norm_workspace_bytes(desc) bytes, 16-byte aligned; may be NULL where neither gain's gradient is asked for
  * Sums are formed in an order that depends on the sizes alone: the same bits from call to call. */

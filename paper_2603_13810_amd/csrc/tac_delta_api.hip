@@ -134,8 +134,12 @@ int tac_head_norm(const tac_head_norm_desc_t* d, const void* query, const void* 
   if (any_misaligned({query, out_query}, el) || (d->key_heads && any_misaligned({key, out_key}, el)) || any_misaligned({gain_query, gain_key}, 4) ||
       (d->axes && misaligned(positions, 4)))
     return TAC_ERR_ALIGN;
-  if (moved(d, d->query_heads, query, d->query, out_query, d->out_query)) return TAC_ERR_BAD_PARAM;
-  if (d->key_heads && (moved(d, d->key_heads, key, d->key, out_key, d->out_key) || on_each_other({out_query}, {key, out_key}) || out_key == query)) return TAC_ERR_BAD_PARAM;
+  // what is ignored may be anywhere
+  const bool keys = d->key_heads != 0;
+  const void *k = keys ? key : nullptr, *o_k = keys ? out_key : nullptr, *gain_k = keys ? gain_key : nullptr, *at = d->axes ? positions : nullptr;
+  if (moved(d, d->query_heads, query, d->query, out_query, d->out_query) || (keys && moved(d, d->key_heads, key, d->key, out_key, d->out_key)) ||
+      on_each_other({out_query}, {k, o_k, gain_query, gain_k, at}) || on_each_other({o_k}, {query, gain_query, gain_k, at}))
+    return TAC_ERR_BAD_PARAM;
   tac::HeadNormParams p = head_params(d);
   p.q = {query, nullptr, out_query, gain_query, d->query, {}, d->out_query, d->query_heads};
   p.k = {key, nullptr, out_key, gain_key, d->key, {}, d->out_key, d->key_heads};
@@ -168,12 +172,11 @@ int tac_head_norm_backward(const tac_head_norm_desc_t* d, const void* query, con
     return TAC_ERR_ALIGN;
   // what is ignored may be anywhere
   const bool keys = d->key_heads != 0, sums = grad_gain_query || grad_gain_key;
-  const void *k = keys ? key : nullptr, *go_k = keys ? grad_out_key : nullptr, *g_k = keys ? grad_key : nullptr;
+  const void *k = keys ? key : nullptr, *go_k = keys ? grad_out_key : nullptr, *g_k = keys ? grad_key : nullptr, *gain_k = keys ? gain_key : nullptr,
+             *at = d->axes ? positions : nullptr;
   if (moved(d, d->query_heads, grad_out_query, d->out_query, grad_query, d->grad_query) || (keys && moved(d, d->key_heads, grad_out_key, d->out_key, grad_key, d->grad_key)) ||
-      on_each_other({grad_query}, {query, k, go_k, g_k}) || on_each_other({g_k}, {query, k, grad_out_query}))
-    return TAC_ERR_BAD_PARAM;
-  if (on_each_other({grad_gain_query, grad_gain_key, sums ? workspace : nullptr},
-                    {query, k, gain_query, keys ? gain_key : nullptr, d->axes ? positions : nullptr, grad_out_query, go_k, grad_query, g_k}))
+      on_each_other({grad_query}, {query, k, go_k, g_k, gain_query, gain_k, at}) || on_each_other({g_k}, {query, k, grad_out_query, gain_query, gain_k, at}) ||
+      on_each_other({grad_gain_query, grad_gain_key, sums ? workspace : nullptr}, {query, k, gain_query, gain_k, at, grad_out_query, go_k, grad_query, g_k}))
     return TAC_ERR_BAD_PARAM;
   tac::HeadNormParams p = head_params(d);
   p.q = {query, grad_out_query, grad_query, gain_query, d->query, d->out_query, d->grad_query, d->query_heads};

@@ -2,7 +2,7 @@
 import pytest
 
 from paper_2603_13810_amd import api
-from test_delta_host import P, delta_desc, head_norm_backward, scan, scan_backward
+from test_delta_host import P, delta_desc, head_norm, head_norm_backward, scan, scan_backward
 
 APART = [P + 4096 * (i + 1) for i in range(24)]
 
@@ -49,4 +49,23 @@ def test_gradients_of_gains(written):
     apart = dict(zip(HEADS_BACK, APART))
     for other in HEADS_BACK:
         if other != written:
+            assert head_norm_backward(**{**apart, written: apart[other]}) == api.TAC_ERR_BAD_PARAM, other
+
+
+HEADS = ("query", "key", "gain_query", "gain_key", "positions", "out_query", "out_key")
+
+
+@pytest.mark.parametrize("written", ["out_query", "out_key"])
+def test_head_norm(written):
+    apart = dict(zip(HEADS, APART))
+    for other in HEADS:
+        if other not in (written, written[4:]):                            # heads in place
+            assert head_norm(**{**apart, written: apart[other]}) == api.TAC_ERR_BAD_PARAM, other
+
+
+@pytest.mark.parametrize("written", ["grad_query_at", "grad_key_at"])
+def test_head_norm_backward(written):
+    apart = dict(zip(HEADS_BACK, APART))
+    for other in HEADS_BACK:
+        if other not in (written, "grad_out_" + written[5:-3]):
             assert head_norm_backward(**{**apart, written: apart[other]}) == api.TAC_ERR_BAD_PARAM, other
