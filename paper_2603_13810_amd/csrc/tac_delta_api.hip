@@ -127,18 +127,15 @@ int tac_head_norm(const tac_head_norm_desc_t* d, const void* query, const void* 
   const int rc = check_heads(d);
   if (rc) return rc;
   if (!query || !out_query || (d->key_heads && (!key || !out_key)) || (d->axes && !positions)) return TAC_ERR_NULL;
+  if (!d->key_heads) key = out_key = nullptr, gain_key = nullptr;      // what is ignored may be anywhere, and no kernel reads it
+  if (!d->axes) positions = nullptr;
   if (bad_heads(d, d->query_heads, d->query) || bad_heads(d, d->query_heads, d->out_query) || bad_heads(d, d->key_heads, d->key) ||
       bad_heads(d, d->key_heads, d->out_key))
     return TAC_ERR_BAD_SHAPE;
   const size_t el = bytes_of(d->dtype);
-  if (any_misaligned({query, out_query}, el) || (d->key_heads && any_misaligned({key, out_key}, el)) || any_misaligned({gain_query, gain_key}, 4) ||
-      (d->axes && misaligned(positions, 4)))
-    return TAC_ERR_ALIGN;
-  // what is ignored may be anywhere
-  const bool keys = d->key_heads != 0;
-  const void *k = keys ? key : nullptr, *o_k = keys ? out_key : nullptr, *gain_k = keys ? gain_key : nullptr, *at = d->axes ? positions : nullptr;
-  if (moved(d, d->query_heads, query, d->query, out_query, d->out_query) || (keys && moved(d, d->key_heads, key, d->key, out_key, d->out_key)) ||
-      on_each_other({out_query}, {k, o_k, gain_query, gain_k, at}) || on_each_other({o_k}, {query, gain_query, gain_k, at}))
+  if (any_misaligned({query, key, out_query, out_key}, el) || any_misaligned({gain_query, gain_key, positions}, 4)) return TAC_ERR_ALIGN;
+  if (moved(d, d->query_heads, query, d->query, out_query, d->out_query) || (key && moved(d, d->key_heads, key, d->key, out_key, d->out_key)) ||
+      on_each_other({out_query}, {key, out_key, gain_query, gain_key, positions}) || on_each_other({out_key}, {query, gain_query, gain_key, positions}))
     return TAC_ERR_BAD_PARAM;
   tac::HeadNormParams p = head_params(d);
   p.q = {query, nullptr, out_query, gain_query, d->query, {}, d->out_query, d->query_heads};
@@ -161,22 +158,21 @@ int tac_head_norm_backward(const tac_head_norm_desc_t* d, const void* query, con
   const int rc = check_heads(d);
   if (rc) return rc;
   if (!query || !grad_out_query || !grad_query || (d->key_heads && (!key || !grad_out_key || !grad_key)) || (d->axes && !positions)) return TAC_ERR_NULL;
-  if (!d->key_heads) grad_gain_key = nullptr;
-  if ((grad_gain_query || grad_gain_key) && !workspace) return TAC_ERR_NULL;
+  if (!d->key_heads) key = grad_out_key = grad_key = nullptr, gain_key = grad_gain_key = nullptr;      // what is ignored may be anywhere, and no kernel reads it
+  if (!d->axes) positions = nullptr;
+  if (!grad_gain_query && !grad_gain_key) workspace = nullptr;
+  else if (!workspace) return TAC_ERR_NULL;
   if (bad_heads(d, d->query_heads, d->query) || bad_heads(d, d->query_heads, d->out_query) || bad_heads(d, d->query_heads, d->grad_query) ||
       bad_heads(d, d->key_heads, d->key) || bad_heads(d, d->key_heads, d->out_key) || bad_heads(d, d->key_heads, d->grad_key))
     return TAC_ERR_BAD_SHAPE;
   const size_t el = bytes_of(d->dtype);
-  if (any_misaligned({query, grad_out_query, grad_query}, el) || (d->key_heads && any_misaligned({key, grad_out_key, grad_key}, el)) ||
-      any_misaligned({gain_query, gain_key, grad_gain_query, grad_gain_key}, 4) || (d->axes && misaligned(positions, 4)) || misaligned(workspace, 16))
+  if (any_misaligned({query, key, grad_out_query, grad_out_key, grad_query, grad_key}, el) ||
+      any_misaligned({gain_query, gain_key, grad_gain_query, grad_gain_key, positions}, 4) || misaligned(workspace, 16))
     return TAC_ERR_ALIGN;
-  // what is ignored may be anywhere
-  const bool keys = d->key_heads != 0, sums = grad_gain_query || grad_gain_key;
-  const void *k = keys ? key : nullptr, *go_k = keys ? grad_out_key : nullptr, *g_k = keys ? grad_key : nullptr, *gain_k = keys ? gain_key : nullptr,
-             *at = d->axes ? positions : nullptr;
-  if (moved(d, d->query_heads, grad_out_query, d->out_query, grad_query, d->grad_query) || (keys && moved(d, d->key_heads, grad_out_key, d->out_key, grad_key, d->grad_key)) ||
-      on_each_other({grad_query}, {query, k, go_k, g_k, gain_query, gain_k, at}) || on_each_other({g_k}, {query, k, grad_out_query, gain_query, gain_k, at}) ||
-      on_each_other({grad_gain_query, grad_gain_key, sums ? workspace : nullptr}, {query, k, gain_query, gain_k, at, grad_out_query, go_k, grad_query, g_k}))
+  if (moved(d, d->query_heads, grad_out_query, d->out_query, grad_query, d->grad_query) || (key && moved(d, d->key_heads, grad_out_key, d->out_key, grad_key, d->grad_key)) ||
+      on_each_other({grad_query}, {query, key, grad_out_key, grad_key, gain_query, gain_key, positions}) ||
+      on_each_other({grad_key}, {query, key, grad_out_query, gain_query, gain_key, positions}) ||
+      on_each_other({grad_gain_query, grad_gain_key, workspace}, {query, key, gain_query, gain_key, positions, grad_out_query, grad_out_key, grad_query, grad_key}))
     return TAC_ERR_BAD_PARAM;
   tac::HeadNormParams p = head_params(d);
   p.q = {query, grad_out_query, grad_query, gain_query, d->query, d->out_query, d->grad_query, d->query_heads};
