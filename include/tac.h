@@ -632,7 +632,7 @@ int tac_delta_scan_backward(const tac_delta_desc_t* desc, const void* query, con
  *   pool   DEVICE, updated, float32 [n_slots][v_heads][Dk][Dv]
  *   slots  DEVICE, read-only, int32 [B], each slot at most once; a slot outside 0 .. n_slots - 1 stands for no sequence: its rows of out are
  *          zero and no state changes.  NULL: sequence b has slot b (n_slots >= B)
- *   out    DEVICE, written, [B][v_heads][Dv]; not on an input */
+ *   out    DEVICE, written, [B][v_heads][Dv].  Neither out nor pool on an input or on each other (where one begins at another's address the call is refused) */
 int tac_delta_step(const tac_delta_desc_t* desc, const void* query, const void* key, const void* value, const void* gate, const void* write,
                    float* pool, int64_t n_slots, const int32_t* slots, void* out, void* stream);
 

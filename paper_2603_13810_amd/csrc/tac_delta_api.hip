@@ -257,7 +257,7 @@ int tac_delta_step(const tac_delta_desc_t* d, const void* query, const void* key
   if (!query || !key || !value || !gate || !write || !pool || !out) return TAC_ERR_NULL;
   if (d->T != 1 || n_slots < 1 || n_slots > kMost || (!slots && n_slots < d->B) || bad_inputs(d)) return TAC_ERR_BAD_SHAPE;
   if (any_misaligned({query, key, value, gate, write, out}, bytes_of(d->dtype)) || any_misaligned({pool, slots}, 4)) return TAC_ERR_ALIGN;
-  if (on_each_other({out}, {query, key, value, gate, write, pool})) return TAC_ERR_BAD_PARAM;
+  if (on_each_other({out, pool}, {query, key, value, gate, write, slots})) return TAC_ERR_BAD_PARAM;
   const tac::DeltaStepParams p = {query, key, value, gate, write, pool, slots, out, n_slots, d->query, d->key, d->value, d->gate, d->write, d->out,
                                   d->B, d->k_heads, d->v_heads, d->Dk, d->Dv, d->dtype == TAC_BF16};
   return finish(tac::delta_step_launch(p, (hipStream_t)stream), "tac_delta_step");

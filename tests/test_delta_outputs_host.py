@@ -4,7 +4,7 @@ import ctypes
 import pytest
 
 from paper_2603_13810_amd import api
-from test_delta_host import P, delta_desc, head_norm, head_norm_backward, heads_desc, scan, scan_backward
+from test_delta_host import P, delta_desc, head_norm, head_norm_backward, heads_desc, scan, scan_backward, step
 
 APART = [P + 4096 * (i + 1) for i in range(24)]
 
@@ -41,6 +41,18 @@ def test_delta_scan_backward(written):
         if other == written or {written, other} == {"grad_h0", "grad_h_last"}:
             continue
         assert scan_backward(delta_desc(), at(17, **{"_%d" % w: APART[BACK.index(other)]})) == api.TAC_ERR_BAD_PARAM, other
+
+
+STEP = ("query", "key", "value", "gate", "write", "pool", None, "slots", "out")
+
+
+@pytest.mark.parametrize("written", ["pool", "out"])
+def test_delta_step(written):
+    w = STEP.index(written)
+    apart = {i: APART[i] for i, n in enumerate(STEP) if n}
+    for i, other in enumerate(STEP):
+        if other not in (None, written):
+            assert step(delta_desc(T=1), {**apart, w: APART[i]}) == api.TAC_ERR_BAD_PARAM, other
 
 
 HEADS_BACK = ("query", "key", "gain_query", "gain_key", "positions", "grad_out_query", "grad_out_key", "grad_query_at", "grad_key_at", "grad_gain_query", "grad_gain_key", "workspace")
