@@ -524,8 +524,9 @@ int tac_gated_step(const tac_scan_desc_t* desc, const void* gate, const void* va
  *   n = x / sqrt(mean over the head of x^2 + eps) * gain,   then pairs of features are turned:
  *   (y0, y1) = (n0 cos t - n1 sin t, n1 cos t + n0 sin t),   t = position[axis] * base^(-i / pairs[axis])
  * for the i-th of an axis's pairs; the axes' pairs follow each other.  With P pairs in all the first 2 P features of a head are turned, pair p
- * being features (p, P + p), or (2 p, 2 p + 1) with `interleaved`; the others stay as the norm has them.  Angles are formed in 64 bits,
- * so that far positions have the angles of near ones' precision; the rest is float32, each result rounded once. */
+ * being features (p, P + p), or (2 p, 2 p + 1) with `interleaved`; the others stay as the norm has them.  Angles are formed in 64 bits
+ * and brought to the nearest turn there: with a base of 1 or more they are off by less than |position| 2^-51, which is less than float32's own rounding
+ * of the turn for positions up to 2^27, and 1e-6 at 2^31.  The rest is float32, each result rounded once. */
 #define TAC_ROTATION_AXES 4
 #define TAC_HEAD_MAX_FEATURES 512
 typedef struct tac_head_strides { int64_t row, head; } tac_head_strides_t;      /* elements from row to row and from head to head, >= D where more than one */
