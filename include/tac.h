@@ -548,6 +548,7 @@ typedef struct tac_head_norm_desc {
  *   gain_query, gain_key  DEVICE, read-only, float32 [D], or NULL: ones
  *   positions             DEVICE, read-only, int32 [rows][axes] (ignored without a rotation)
  *   out_query, out_key    DEVICE, written; may be query and key (with their strides).  An output that begins at another input or output, or with other strides, is refused
+ * The squares of a head are summed in float32: magnitudes beyond 2^59 may overflow (the head's results are then zero).
  * Errors: TAC_ERR_NULL, TAC_ERR_BAD_SHAPE, TAC_ERR_UNSUPPORTED (more than TAC_HEAD_MAX_FEATURES features), TAC_ERR_BAD_PARAM, TAC_ERR_ALIGN, TAC_ERR_HIP. */
 int tac_head_norm(const tac_head_norm_desc_t* desc, const void* query, const void* key, const float* gain_query, const float* gain_key,
                   const int32_t* positions, void* out_query, void* out_key, void* stream);

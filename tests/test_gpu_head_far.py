@@ -75,3 +75,16 @@ def test_without_keys_through_the_c_interface():
     assert api.lib().tac_head_norm_backward(ctypes.byref(d), p(q), p(q), p(gain), p(grad), None, p(dq), p(dq), p(grad), p(q), p(sums), p(sums), p(work), stream) == 0
     torch.cuda.synchronize()
     assert torch.equal(out, want) and torch.equal(grad, back["grad_q"]) and torch.equal(sums, back["grad_gain_q"])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("D", [16, 512])
+def test_large_magnitudes(D, dtype):
+    """A head's squares are summed in float32: up to 2^59 they have room, whatever the head's size; where they have not, the results are zero."""
+    x = torch.full((2, 1, D), 2.0 ** 59, device=DEV, dtype=dtype)
+    x[..., ::2] *= -1
+    x[1] *= 2.0 ** 6
+    got = api.tac_head_norm(x, eps=1e-6)["q"].float()
+    # 8 terms in a lane and 6 joinings, half of it in the root; a root and a division (2 each), a product; the result's own rounding
+    assert ((got[0] - torch.sign(x[0].float())).abs() <= (7 + 4 + 1) * O.U + O.HALF[dtype]).all()
+    assert (got[1] == 0).all()
