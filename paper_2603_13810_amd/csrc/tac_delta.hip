@@ -5,9 +5,9 @@
 //   U = (I + A)^-1 b (V - e^G K S),   O = e^G Q S + P U,   S <- e^G_end S + K^T (e^(G_end - G) U).
 // S, the right-hand sides and U go from one product's result to the next one's operand through LDS as bfloat16 parts; S itself stays in registers in float32.
 //
-// Bound by the chain: a chunk waits for the state that the one before leaves, and what is in between (parts of S, K S over LDS, the right-hand sides, the inverse, U over LDS, K^T U) is some 4000
-// cycles, of which the matrix cores work 300.  32768 steps, 16 heads of 128 x 128 bf16: 860 us for 512 chunks, 1.7 us each, on 128 workgroups; 8 sequences of 2048 steps with what training
-// keeps: 192 us.  What shortened it: outputs on waves of their own, S as an operand from registers, loads a chunk ahead, whole lines, a head's tiles on one die (3020 us at first).
+// Bound by the chain: a chunk waits for the state that the one before leaves, and what is in between (parts of S, K S over LDS, the right-hand sides, the inverse, U over LDS, K^T U) is some 4500
+// cycles, of which the matrix cores work 300.  32768 steps, 16 heads of 128 x 128 bf16: 953 us for 512 chunks, 1.9 us each, on 128 workgroups (865 where the outputs' products had 16
+// digits); 8 sequences of 2048 steps with what training keeps: 188 us.  What shortened it: outputs on waves of their own, S as an operand from registers, loads a chunk ahead, whole lines, a head's tiles on one die (3020 us at first).
 #include "tac_delta_chunk.h"
 
 namespace tac {

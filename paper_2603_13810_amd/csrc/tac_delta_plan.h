@@ -41,8 +41,8 @@ constexpr int64_t kHeadBackwardGroups = 3 * kFittedUnits;      // as many as are
 inline int64_t delta_chunks(int64_t T) { return (T + TAC_DELTA_CHUNK - 1) / TAC_DELTA_CHUNK; }
 
 // Columns of a state that a workgroup takes: 32, or 16 where 32 would make fewer than two workgroups a compute unit.  With 16 a chunk's matrices are read twice as often, with 32 its products
-// take longer: one sequence of 32768 steps, 16 heads of 128 x 128: 16 columns 993 us, 32 columns 1437; 5 prompts of 777, 6 heads of 96 x 80: 49 and 60; forward and backward of 8
-// sequences of 2048, 16 heads of 128 x 128: 845 and 781, of 128 sequences of 25, 4 heads of 32 x 32 fp32: 97 and 93.
+// take longer: one sequence of 32768 steps, 16 heads of 128 x 128: 16 columns 1061 us, 32 columns 1500; 5 prompts of 777, 6 heads of 96 x 80: 43 and 55; forward and backward of 8
+// sequences of 2048, 16 heads of 128 x 128: 1246 and 1046, of 128 sequences of 25, 4 heads of 32 x 32 fp32: 92 and 82.
 inline bool delta_narrow(int64_t B, int64_t heads, int64_t Dv) { return Dv <= 16 || B * heads * ((Dv + 31) / 32) < 2 * kFittedUnits; }
 
 // A launch has a workgroup of up to 512 threads for every chunk and head, or for every 16 columns of a head: fewer than 2^32 threads.

@@ -4,7 +4,7 @@
 // G is kept in two numbers: a chunk that fades by e^-100 in all may hold neighbours that hardly fade, and one float32 number would have lost their difference.
 // A chunk and head is a workgroup of four waves: products of keys and queries, then the inverse, whose steps follow one another; K and Q come as whole rows through LDS (read as operands they took
 // a third longer).  With 128 features bf16 it reads 32 KB and writes 31: 8192 chunks of heads 102 us, 5.1 TB/s of which the caches hold a quarter; 4096 with three parts of both, for the
-// gradients, 49; 512 of 32 features fp32 11.2, where loads, gates, products and substitution wait for each other.
+// gradients, 49; 512 of 32 features fp32 11.6, where loads, gates, products and substitution wait for each other.
 // The inverse is formed by blocks of 16: the diagonal ones by substitution, one column a lane, those below from them on the float32 matrix cores.  A product
 // of powers of A would be shorter, but its terms grow with the number of like keys where the inverse does not.
 #include "tac_delta_chunk.h"
